@@ -56,6 +56,44 @@ def build_all(verbose: bool = False):
     return build(verbose), build(verbose, out=LIB_FMA, extra=FMA_FLAGS)
 
 
+# a learner's operators (include/ps_learner.h): a library of its own, since its sums
+# may be contracted (they are compared within rounding, not bit for bit). One object
+# per source, compiled side by side.
+LEARNER_LIB = os.path.join(HERE, "libgadeilearner.so")
+LEARNER_SOURCES = [os.path.join(CSRC, s) for s in (
+    "pl_api.cpp", "pl_rows.hip", "pl_embed_grad.hip", "pl_quantize.hip", "pl_matmul.hip")]
+LEARNER_FLAGS = [f for f in FLAGS if not f.startswith("-ffp-contract=") and f != "-shared"]
+
+
+def build_learner(verbose: bool = False) -> str:
+    import tempfile
+    with tempfile.TemporaryDirectory() as tmp:
+        objects = [os.path.join(tmp, os.path.basename(s) + ".o") for s in LEARNER_SOURCES]
+        running = []
+        for src, obj in zip(LEARNER_SOURCES, objects):
+            cmd = [HIPCC, *LEARNER_FLAGS, "-c", src, "-o", obj]
+            if verbose:
+                print(" ".join(cmd), flush=True)
+            running.append((src, subprocess.Popen(cmd, stdout=subprocess.PIPE,
+                                                  stderr=subprocess.STDOUT, text=True)))
+        failed = []
+        for src, p in running:
+            text = p.communicate()[0]
+            if p.returncode != 0:
+                sys.stderr.write(text)
+                failed.append(os.path.basename(src))
+        if failed:
+            raise RuntimeError("hipcc failed compiling " + ", ".join(failed))
+        out = LEARNER_LIB + ".tmp"
+        r = subprocess.run([HIPCC, "--offload-arch=gfx950", "-shared", *objects, "-o", out],
+                           capture_output=True, text=True)
+        if r.returncode != 0:
+            sys.stderr.write(r.stdout + r.stderr)
+            raise RuntimeError("hipcc failed linking " + os.path.basename(LEARNER_LIB))
+        os.replace(out, LEARNER_LIB)
+    return LEARNER_LIB
+
+
 # the Python binding's per-step calls (host only; needs torch's headers)
 BINDING_SRC = os.path.join(CSRC, "ps_binding.cpp")
 BINDING = os.path.join(HERE, "_binding.so")
@@ -106,4 +144,4 @@ def build_c_smoke(verbose: bool = False) -> str:
 
 
 if __name__ == "__main__":
-    print(build_all(verbose=True), build_binding(verbose=True))
+    print(build_all(verbose=True), build_learner(verbose=True), build_binding(verbose=True))

@@ -1,0 +1,111 @@
+// Streams over the rows of a matrix: embedding lookup and dropout.
+//
+// Mathematics: out[r, c] = keep(r, c) * factor * x[src(r), c], src(r) = r or ids[r].
+// Bound by memory: every element is read once and written once. A thread takes eight
+// consecutive columns (one evaluation of the generator gives their eight 16-bit
+// numbers) of kUnroll rows, whose loads are issued together.
+#include "pl_device.h"
+
+namespace gadei::learner {
+namespace {
+
+constexpr int kBlock = 256;
+constexpr int kUnroll = 4;
+
+// The block's threads cover 2^lx groups of eight columns times 256 / 2^lx rows.
+template <int IDT, int X, int OUT, bool DROP>
+__global__ __launch_bounds__(kBlock) void rows_kernel(RowsArgs a, int lx, uint32_t tiles_x) {
+    const uint32_t tile_y = blockIdx.x / tiles_x, tile_x = blockIdx.x % tiles_x;
+    const uint32_t group = (tile_x << lx) + (threadIdx.x & ((1u << lx) - 1));
+    const uint32_t ny = kBlock >> lx;
+    const uint64_t first = static_cast<uint64_t>(tile_y) * ny * kUnroll + (threadIdx.x >> lx);
+    const uint64_t col = 8ull * group;
+    if (col >= a.cols) return;
+    const int count = a.cols - col < 8 ? static_cast<int>(a.cols - col) : 8;
+
+    int64_t src[kUnroll];   // row of x; -1: zeros; -2: past the last row
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+        const uint64_t r = first + u * ny;
+        src[u] = -2;
+        if (r < a.rows) {
+            if constexpr (IDT == kNoIds) {
+                src[u] = static_cast<int64_t>(r);
+            } else {
+                int64_t id;
+                if constexpr (IDT == PL_I32) id = static_cast<const int32_t *>(a.ids)[r];
+                else id = static_cast<const int64_t *>(a.ids)[r];
+                src[u] = static_cast<uint64_t>(id) < a.vocab ? id : -1;
+            }
+        }
+    }
+    float x[kUnroll][8];
+    if (count == 8) {
+        Bits8<X> bits[kUnroll] = {};
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u)
+            if (src[u] >= 0) bits[u] = load8<X>(a.x, src[u] * a.x_ld + static_cast<int64_t>(col));
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) widen8<X>(x[u], bits[u]);
+    } else {
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u)
+            load_some<X>(x[u], a.x, src[u] * a.x_ld + static_cast<int64_t>(col),
+                         src[u] >= 0 ? count : 0);
+    }
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+        if (src[u] == -2) continue;
+        const uint64_t r = first + u * ny;
+        if constexpr (DROP) {
+            drop8(x[u], a.factor, group, static_cast<uint32_t>(r), a.drop);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[u][e] *= a.factor;
+        }
+        if (src[u] == -1) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[u][e] = 0.0f;   // not factor * 0: the factor may be NaN
+        }
+        const int64_t at = static_cast<int64_t>(r) * a.out_ld + static_cast<int64_t>(col);
+        if (count == 8) store8<OUT>(a.out, at, x[u]);
+        else store_some<OUT>(a.out, at, x[u], count);
+    }
+}
+
+template <int IDT, int X, int OUT>
+hipError_t launch(const RowsArgs &a, hipStream_t s) {
+    const uint64_t groups = (a.cols + 7) / 8;
+    int lx = 0;
+    while (lx < 8 && (1ull << lx) < groups) ++lx;
+    const uint64_t tiles_x = (groups + (1ull << lx) - 1) >> lx;
+    const uint64_t rows = static_cast<uint64_t>(kBlock >> lx) * kUnroll;
+    const uint64_t blocks = tiles_x * ((a.rows + rows - 1) / rows);
+    if (blocks > 0xffffffffull / kBlock) return hipErrorInvalidConfiguration;
+    if (a.drop.drop != 0)
+        rows_kernel<IDT, X, OUT, true><<<static_cast<uint32_t>(blocks), kBlock, 0, s>>>(
+            a, lx, static_cast<uint32_t>(tiles_x));
+    else
+        rows_kernel<IDT, X, OUT, false><<<static_cast<uint32_t>(blocks), kBlock, 0, s>>>(
+            a, lx, static_cast<uint32_t>(tiles_x));
+    return hipGetLastError();
+}
+
+template <int IDT>
+hipError_t launch_typed(const RowsArgs &a, int x, int out, hipStream_t s) {
+    if (x == PS_F32)
+        return out == PS_F32 ? launch<IDT, PS_F32, PS_F32>(a, s) : launch<IDT, PS_F32, PS_BF16>(a, s);
+    return out == PS_F32 ? launch<IDT, PS_BF16, PS_F32>(a, s) : launch<IDT, PS_BF16, PS_BF16>(a, s);
+}
+
+}  // namespace
+
+hipError_t launch_rows(const RowsArgs &a, int id_type, int x, int out, hipStream_t s) {
+    if (id_type == PL_I32) return launch_typed<PL_I32>(a, x, out, s);
+    if (id_type == PL_I64) return launch_typed<PL_I64>(a, x, out, s);
+    // dropout keeps its input's type
+    return x == PS_F32 ? launch<kNoIds, PS_F32, PS_F32>(a, s)
+                       : launch<kNoIds, PS_BF16, PS_BF16>(a, s);
+}
+
+}  // namespace gadei::learner

@@ -1,0 +1,443 @@
+"""A learner's operators on the GPU against their definitions in 64 bits.
+
+Tolerances. u = 2^-24 is fp32's unit roundoff, 2^-8 bf16's; an output in bf16 is
+rounded once more than one in fp32.
+  lookups, dropout  the factor (scale and 1 / kept) is rounded to fp32 once and
+                    multiplied once: 2 u relative, 3 u allowed
+  table gradients   a sum of c terms, each rounded at every addition, and the same
+                    factor: (c + 3) u of the sum of the terms' magnitudes; what is
+                    accumulated to adds one more rounding of the result
+  8-bit values      equal: scaling by powers of two is exact
+  products          equal where all partial sums are whole numbers below 2^24 times one power of
+                    two; else every instruction adds 128 exact products to the running sum,
+                    with at most 4 units of 2^-23 of the sum of magnitudes each
+"""
+import numpy as np
+import pytest
+
+from paper_1611_06213_amd import ps
+from tests import learner_ref as ref
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+B16 = 2.0 ** -8
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.fail("GPU tests need a GPU")
+    return torch
+
+
+@pytest.fixture(scope="module")
+def learner(torch):
+    from paper_1611_06213_amd import learner
+    learner.load_library()
+    return learner
+
+
+DT = {"f32": "float32", "bf16": "bfloat16", "i32": "int32", "i64": "int64"}
+
+
+def dt(torch, name):
+    return getattr(torch, DT[name])
+
+
+def gen(torch, seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def randn(torch, g, *shape, dtype=None, std=1.0):
+    return (torch.randn(shape, generator=g, device="cuda") * std).to(dtype or torch.float32)
+
+
+def placed(torch, rows, cols, dtype, offset, gap, fill=float("nan")):
+    """A rows x cols view `offset` elements into a buffer, rows `gap` elements apart, and the buffer."""
+    ld = cols + gap
+    buf = torch.full((offset + rows * ld + 64,), fill, dtype=dtype, device="cuda")
+    return torch.as_strided(buf, (rows, cols), (ld, 1), offset), buf
+
+
+def within(got, want, tol):
+    got = ref.f64(got).reshape(want.shape)
+    bad = ~(np.abs(got - want) <= tol + 1e-44)
+    bad &= ~(np.isnan(got) & np.isnan(want))
+    bad &= ~(got == want)   # infinities
+    assert not bad.any(), (np.argwhere(bad)[:4], got[bad][:4], want[bad][:4])
+
+
+def out_tol(name):
+    return B16 if name == "bf16" else 0.0
+
+
+# ----------------------------------------------------------------- embedding
+
+@pytest.mark.parametrize("tokens,vocab,dim", [(1, 1, 1), (1, 50, 100), (5, 7, 3), (64, 300, 8),
+                                              (333, 1000, 100), (1025, 40, 257), (70, 9, 2051)])
+@pytest.mark.parametrize("p", [None, 0.3])
+@pytest.mark.parametrize("x,out,ids", [("f32", "f32", "i64"), ("bf16", "bf16", "i32"),
+                                       ("f32", "bf16", "i32"), ("bf16", "f32", "i64")])
+def test_embedding(torch, learner, tokens, vocab, dim, p, x, out, ids):
+    g = gen(torch, tokens + dim)
+    table, _ = placed(torch, vocab, dim, dt(torch, x), 3, 5)
+    table.copy_(randn(torch, g, vocab, dim))
+    idx = torch.randint(-1, vocab + 1, (tokens,), generator=g, device="cuda").to(dt(torch, ids))
+    drop = None if p is None else learner.Dropout(p, 77, 1 << 40)
+    dst, buf = placed(torch, tokens, dim, dt(torch, out), 1, 3, 7.0)
+    got = learner.embedding(idx, table, 1.5, drop, out=dst)
+    assert got is dst
+    want = ref.embedding(idx, table, 1.5, drop)
+    within(dst, want, np.abs(want) * (3 * U + out_tol(out)))
+    torch.as_strided(buf, dst.shape, dst.stride(), 1).fill_(7.0)   # and nothing around it
+    assert bool((buf == 7.0).all())
+
+
+def test_embedding_shapes_and_padding(torch, learner):
+    table = torch.tensor([[float("nan"), 1.0], [float("inf"), 2.0]], device="cuda")
+    ids = torch.tensor([[1, -1], [2, 0]], device="cuda")
+    y = learner.embedding(ids, table)
+    assert y.shape == (2, 2, 2)
+    assert y[0, 0].tolist() == [float("inf"), 2.0] and bool((y[0, 1] == 0).all())
+    assert bool((y[1, 0] == 0).all()) and bool(y[1, 1, 0].isnan())
+    # padding is zeros whatever the scale; what is dropped is 0, not NaN
+    assert bool((learner.embedding(ids, table, float("nan"))[0, 1] == 0).all())
+    assert bool((learner.embedding(ids, table, 1.0, learner.Dropout(1.0, 5)) == 0).all())
+    assert learner.embedding(ids[:0], table).shape == (0, 2, 2)
+    none = learner.embedding(ids, table[:0])
+    assert none.shape == (2, 2, 2) and bool((none == 0).all())
+    assert learner.embedding(ids, table[:, :0]).shape == (2, 2, 0)
+
+
+# ------------------------------------------------------------ its gradient
+
+CASES = [(0, 5, 4), (1, 1, 1), (3, 70, 10), (64, 300, 8), (65, 1, 100), (1000, 3, 33),
+         (5000, 700, 24), (4097, 100_000, 5), (300, 2, 2051), (9000, 270_000, 3)]
+
+
+@pytest.mark.parametrize("tokens,vocab,dim", CASES)
+@pytest.mark.parametrize("p", [None, 0.3])
+@pytest.mark.parametrize("x,out,ids", [("f32", "f32", "i64"), ("bf16", "f32", "i32"),
+                                       ("bf16", "bf16", "i64"), ("f32", "bf16", "i32")])
+def test_embedding_grad(torch, learner, tokens, vocab, dim, p, x, out, ids):
+    g = gen(torch, tokens + dim)
+    grad, _ = placed(torch, tokens, dim, dt(torch, x), 5, 3)
+    grad.copy_(randn(torch, g, tokens, dim))
+    # some ids far more frequent than others, some no token
+    idx = (torch.rand(tokens, generator=g, device="cuda") ** 3 * (vocab + 2)).long() - 1
+    idx = idx.to(dt(torch, ids))
+    drop = None if p is None else learner.Dropout(p, 3, 4)
+    dst, buf = placed(torch, vocab, dim, dt(torch, out), 3, 1, 7.0)
+    learner.embedding_grad(idx, grad, vocab, 0.75, drop, out=dst)
+    want, size, count = ref.embedding_grad(idx, grad, vocab, 0.75, drop)
+    tol = (count[:, None] + 3) * U * size
+    within(dst, want, tol + (np.abs(want) + tol) * out_tol(out))
+    again = learner.embedding_grad(idx, grad, vocab, 0.75, drop, dtype=dt(torch, out))
+    assert torch.equal(again, dst)   # the same bits
+    torch.as_strided(buf, dst.shape, dst.stride(), 3).fill_(7.0)
+    assert bool((buf == 7.0).all())
+
+
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+def test_embedding_grad_accumulates(torch, learner, out):
+    g = gen(torch, 1)
+    tokens, vocab, dim = 700, 90, 21
+    ids = (torch.rand(tokens, generator=g, device="cuda") ** 4 * vocab).long()
+    ids[ids == 5] = 6
+    grad = randn(torch, g, tokens, dim)
+    old = randn(torch, g, vocab, dim, dtype=dt(torch, out))
+    old[5] = float("nan")   # a row without tokens is not touched
+    got = learner.embedding_grad(ids, grad, vocab, 2.0, out=old.clone(), accumulate=True)
+    want, size, count = ref.embedding_grad(ids, grad, vocab, 2.0)
+    want = want + ref.f64(old)
+    tol = (count[:, None] + 3) * U * size + np.abs(want) * U
+    within(got, want, tol + (np.abs(want) + tol) * out_tol(out))
+
+
+def test_one_token_everywhere(torch, learner):
+    """Every token the same id: the longest sum there is, and all other rows zeros."""
+    tokens, vocab, dim = 20_011, 300, 40
+    grad = randn(torch, gen(torch, 2), tokens, dim)
+    ids = torch.full((tokens,), 299, device="cuda", dtype=torch.int32)
+    got = learner.embedding_grad(ids, grad, vocab)
+    want, size, count = ref.embedding_grad(ids, grad, vocab, 1.0)
+    within(got, want, (count[:, None] + 3) * U * size)
+
+
+def test_embedding_grad_against_differences(torch, learner):
+    """The lookup is linear in its table: <grad, f(table + h) - f(table)> = <gradient, h>, with
+    whole numbers and p = 1/2 (a factor of two) without any rounding."""
+    g = gen(torch, 3)
+    tokens, vocab, dim = 400, 37, 19
+    ids = torch.randint(-1, vocab, (tokens,), generator=g, device="cuda")
+    ints = lambda *s: torch.randint(-9, 10, s, generator=g, device="cuda").float()
+    table, grad = ints(vocab, dim), ints(tokens, dim)
+    drop = learner.Dropout(0.5, 11, 12)
+    gradient = learner.embedding_grad(ids, grad, vocab, 3.0, drop)
+    for _ in range(5):
+        h = ints(vocab, dim)
+        moved = (learner.embedding(ids, table + h, 3.0, drop)
+                 - learner.embedding(ids, table, 3.0, drop))
+        assert (moved.double() * grad.double()).sum() == (gradient.double() * h.double()).sum()
+
+
+# ------------------------------------------------------------------- dropout
+
+@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 7), (3, 8), (1, 100_003), (129, 65), (1000, 24),
+                                       (7, 4099)])
+@pytest.mark.parametrize("p", [0.0, 0.1, 0.5, 0.97, 1.0])
+@pytest.mark.parametrize("x", ["f32", "bf16"])
+def test_dropout(torch, learner, rows, cols, p, x):
+    g = gen(torch, rows)
+    src, _ = placed(torch, rows, cols, dt(torch, x), 1, 9)
+    src.copy_(randn(torch, g, rows, cols))
+    drop = learner.Dropout(p, (1 << 63) + 5, 1 << 33)
+    want = ref.drop(ref.f64(src), drop)
+    tol = np.abs(want) * (3 * U + out_tol(x))
+    within(learner.dropout(src, drop), want, tol)
+    dst, buf = placed(torch, rows, cols, dt(torch, x), 3, 1, 7.0)
+    learner.dropout(src, drop, out=dst)
+    within(dst, want, tol)
+    torch.as_strided(buf, dst.shape, dst.stride(), 3).fill_(7.0)
+    assert bool((buf == 7.0).all())
+    learner.dropout(src, drop, out=src)   # in place
+    within(src, want, tol)
+
+
+def test_dropout_shapes_and_rates(torch, learner):
+    x = torch.ones(50, 40, 512, device="cuda")
+    y = learner.dropout(x, learner.Dropout(0.25, 1))
+    assert y.shape == x.shape
+    kept = float((y != 0).float().mean())
+    # a binomial of 1,024,000 draws: 6 standard deviations are 0.0026
+    assert abs(kept - 0.75) < 0.0026
+    assert torch.equal(y.unique(), torch.tensor([0.0, 1 / 0.75], device="cuda"))
+    other = learner.dropout(x, learner.Dropout(0.25, 1, 1))
+    both = float(((y != 0) & (other != 0)).float().mean())
+    assert abs(both - 0.5625) < 0.003
+    assert learner.dropout(x[:0], learner.Dropout(0.25, 1)).shape == (0, 40, 512)
+    # what is dropped is 0 even where it is not finite
+    bad = learner.dropout(torch.full((4, 4096), float("nan"), device="cuda"), learner.Dropout(0.5, 3))
+    assert 0.4 < float((bad == 0).float().mean()) < 0.6
+
+
+# -------------------------------------------------------- 8-bit floating point
+
+@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 128), (3, 129), (130, 100), (257, 700), (128, 512),
+                                       (33, 1400)])
+@pytest.mark.parametrize("square", [False, True])
+@pytest.mark.parametrize("x", ["f32", "bf16"])
+def test_quantize(torch, learner, rows, cols, square, x):
+    g = gen(torch, rows * cols)
+    src, _ = placed(torch, rows, cols, dt(torch, x), 3, 7)
+    # magnitudes over many powers of two; exact powers, zeros and block maxima on the edge
+    src.copy_(randn(torch, g, rows, cols) * torch.exp2(
+        torch.randint(-20, 21, (rows, cols), generator=g, device="cuda").float()))
+    src[rows // 2] = 0
+    src[0, 0] = 448 * 2.0 ** 30
+    src[rows - 1, cols - 1] = 450 * 2.0 ** 25
+    q = learner.quantize_fp8(src, square)
+    want, e = ref.quantize(src, square)
+    assert np.array_equal(q.exponents().cpu().numpy(), e)
+    v = q.values.float().cpu().numpy()
+    assert np.array_equal(v[:, :cols], want.astype(np.float32))
+    assert not v[:, cols:].any()
+    t = learner.quantize_fp8(src, square, transpose=True)
+    want_t, e_t = ref.quantize(src.t(), square)
+    assert np.array_equal(t.exponents().cpu().numpy(), e_t)
+    assert np.array_equal(t.values.float().cpu().numpy()[:, :rows], want_t.astype(np.float32))
+    assert not t.values.float().cpu().numpy()[:, rows:].any()
+    both = learner.quantize_fp8_both(src, square)
+    for a, b in zip(both, (q, t)):
+        assert torch.equal(a.values.view(torch.uint8), b.values.view(torch.uint8))
+        assert torch.equal(a.exponents(), b.exponents())
+    if square:
+        assert torch.equal(q.dequantize(), t.dequantize().t())
+
+
+def test_quantize_edges(torch, learner):
+    """Largest and smallest numbers, and what is not finite, in one block each."""
+    x = torch.zeros(6, 128, device="cuda")
+    x[0, :3] = torch.tensor([3.4028234e38, 1.0, -3.0e38])
+    x[1, :2] = torch.tensor([2.0 ** -149, 2.0 ** -126])
+    x[2, :4] = torch.tensor([float("nan"), float("inf"), float("-inf"), 448.0])
+    x[3, :2] = torch.tensor([float("inf"), 0.0])
+    x[4, :3] = torch.tensor([448.0, 2.0 ** -9, 2.0 ** -10])   # e4m3's ends; a tie to 0
+    x[5, :2] = torch.tensor([448.0000305, 464.0])
+    q = learner.quantize_fp8(x)
+    want, e = ref.quantize(x)
+    assert np.array_equal(q.exponents().cpu().numpy(), e)
+    got = q.values.float().cpu().numpy()
+    assert np.array_equal(got, want.astype(np.float32), equal_nan=True)
+    assert np.isnan(got[2, :3]).all() and np.isnan(got[3, 0]) and got[2, 3] == 448
+
+
+def integers(torch, g, rows, cols):
+    """Small whole numbers: exact in e4m3."""
+    return torch.randint(-8, 9, (rows, cols), generator=g, device="cuda").float()
+
+
+SIZES = [(1, 1, 1), (1, 16, 128), (1, 1000, 4096), (2, 33, 700), (16, 130, 1024), (17, 64, 129),
+         (33, 100, 513), (64, 257, 3000), (65, 129, 128), (100, 1000, 900), (128, 128, 2048),
+         (129, 300, 640), (257, 255, 1280), (300, 520, 8200), (4100, 4099, 257)]
+
+
+@pytest.mark.parametrize("m,n,k", SIZES)
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+def test_matmul_exact(torch, learner, m, n, k, out):
+    """Whole numbers, with blocks scaled by powers of two against each other in a and b: every
+    product and partial sum is exact in fp32, so the result is one rounding."""
+    g = gen(torch, m + n + k)
+    a, b = integers(torch, g, m, k), integers(torch, g, n, k)
+    up = torch.exp2(torch.randint(-9, 10, (-(-k // 128),), generator=g, device="cuda").float())
+    up = up.repeat_interleave(128)[:k]
+    qa, qb = learner.quantize_fp8(a * up), learner.quantize_fp8(b / up)
+    assert torch.equal(qa.dequantize(), a * up) and torch.equal(qb.dequantize(), b / up)
+    want = (a.double() @ b.double().t()).to(dt(torch, out))
+    dst, buf = placed(torch, m, n, dt(torch, out), 1, 3, 7.0)
+    got = learner.matmul_fp8(qa, qb, out=dst)
+    assert torch.equal(got, want)
+    torch.as_strided(buf, dst.shape, dst.stride(), 1).fill_(7.0)
+    assert bool((buf == 7.0).all())
+    bias = torch.randint(-50, 50, (n,), generator=g, device="cuda").float()
+    y = learner.matmul_fp8(qa, qb, bias=bias, relu=True, dtype=dt(torch, out))
+    assert torch.equal(y, (a.double() @ b.double().t() + bias).clamp(min=0).to(dt(torch, out)))
+    y = learner.matmul_fp8(qa, qb, bias=bias.bfloat16(), dtype=dt(torch, out))
+    assert torch.equal(y, (a.double() @ b.double().t() + bias).to(dt(torch, out)))
+    old = torch.randint(-50, 50, (m, n), generator=g, device="cuda").to(dt(torch, out))
+    y = learner.matmul_fp8(qa, qb, out=old.clone(), accumulate=True)
+    assert torch.equal(y, (a.double() @ b.double().t() + old).to(dt(torch, out)))
+
+
+@pytest.mark.parametrize("m,n,k", [(1, 512, 9216), (48, 200, 1000), (200, 300, 4096), (1030, 1030, 900)])
+def test_matmul_rounding(torch, learner, m, n, k):
+    g = gen(torch, k)
+    a, b = randn(torch, g, m, k), randn(torch, g, n, k, std=0.05)
+    qa, qb = learner.quantize_fp8(a), learner.quantize_fp8(b, square=True)
+    va, vb = ref.values(a), ref.values(b, True)
+    got = learner.matmul_fp8(qa, qb, dtype=torch.float32)
+    tol = 4 * (k / 128 + 16) * 2.0 ** -23 * (np.abs(va) @ np.abs(vb).T)
+    within(got, va @ vb.T, tol)
+    assert torch.equal(got, learner.matmul_fp8(qa, qb, dtype=torch.float32))
+    assert torch.equal(got, learner.linear_fp8(a, qb, dtype=torch.float32))
+    within(learner.linear_fp8(a, qb), va @ vb.T, tol + (np.abs(va @ vb.T) + tol) * B16)
+
+
+def test_matmul_not_finite(torch, learner):
+    """A NaN or infinity makes its row (of a) or column (of b) NaN, and no other; relu keeps it."""
+    for m in (3, 200):
+        a, b = torch.ones(m, 300, device="cuda"), torch.ones(70, 300, device="cuda")
+        a[1, 299], b[5, 0] = float("inf"), float("nan")
+        y = learner.linear_fp8(a, learner.quantize_fp8(b), relu=True, dtype=torch.float32)
+        want = torch.full((m, 70), 300.0, device="cuda")
+        want[1], want[:, 5] = float("nan"), float("nan")
+        assert torch.equal(y.isnan(), want.isnan()) and torch.equal(y.nan_to_num(), want.nan_to_num())
+
+
+def test_matmul_empty(torch, learner):
+    q = lambda r, c: learner.quantize_fp8(torch.ones(r, c, device="cuda"))
+    assert learner.matmul_fp8(q(0, 5), q(4, 5)).shape == (0, 4)
+    assert learner.matmul_fp8(q(3, 5), q(0, 5)).shape == (3, 0)
+    bias = torch.arange(4.0, device="cuda")
+    assert torch.equal(learner.matmul_fp8(q(3, 0), q(4, 0), bias=bias, dtype=torch.float32),
+                       bias.expand(3, 4))
+
+
+@pytest.mark.parametrize("m,n,k", [(1, 3, 5), (57, 1000, 900), (200, 130, 300), (513, 260, 129)])
+@pytest.mark.parametrize("x", ["f32", "bf16"])
+def test_linear_grad(torch, learner, m, n, k, x):
+    """Both gradients against the formula's, and against differences: with whole numbers nothing
+    is rounded by the 8-bit form, so <grad, (x + h) w^T - x w^T> = <gradient, h> exactly."""
+    g = gen(torch, m)
+    w, a, grad = (integers(torch, g, r, c).to(dt(torch, x)) for r, c in ((n, k), (m, k), (m, n)))
+    w_q, w_t = learner.quantize_fp8_both(w, square=True)
+    dx, dw = learner.linear_fp8_grad(a, grad, w_t, dtype=torch.float32)
+    assert torch.equal(dx, (grad.double() @ w.double()).float())
+    assert torch.equal(dw, (grad.double().t() @ a.double()).float())
+    h = torch.randint(-1, 2, (m, k), generator=g, device="cuda").to(a.dtype)
+    y = lambda v: learner.linear_fp8(v, w_q, dtype=torch.float32).double()
+    # a + h and w + v are below 10: still exact in e4m3 up to 16
+    assert ((y(a + h) - y(a)) * grad.double()).sum() == (dx.double() * h.double()).sum()
+    v = torch.randint(-1, 2, (n, k), generator=g, device="cuda").to(w.dtype)
+    moved = learner.linear_fp8(a, learner.quantize_fp8(w + v, square=True), dtype=torch.float32)
+    assert ((moved.double() - y(a)) * grad.double()).sum() == (dw.double() * v.double()).sum()
+    row = torch.full((n * k + 3,), 2.0, device="cuda")
+    into = row[3:].view(n, k)
+    learner.linear_fp8_grad(a, grad, w_t, weight_out=into, accumulate=True)
+    assert torch.equal(into, dw + 2.0) and bool((row[:3] == 2.0).all())
+
+
+def test_linear_grad_rounding(torch, learner):
+    g = gen(torch, 9)
+    m, n, k = 300, 200, 500
+    a, grad, w = randn(torch, g, m, k), randn(torch, g, m, n, std=1e-3), randn(torch, g, n, k)
+    dx, dw = learner.linear_fp8_grad(a, grad, learner.quantize_fp8(w, square=True, transpose=True),
+                                     dtype=torch.float32)
+    vw = ref.values(w, True)
+    for got, x, y in ((dx, ref.values(grad), vw.T), (dw, ref.values(grad.t()), ref.values(a.t()))):
+        within(got, x @ y.T, 4 * 20 * 2.0 ** -23 * (np.abs(x) @ np.abs(y).T))
+
+
+# ------------------------------------------------ streams, graphs, refusals
+
+def test_on_a_stream_and_in_a_graph(torch, learner):
+    """The whole set captured once; every replay, with other inputs and eager work between,
+    equals the eager calls."""
+    g = gen(torch, 4)
+    stream = torch.cuda.Stream()
+    ids = torch.zeros(300, dtype=torch.int64, device="cuda")
+    table, w = randn(torch, g, 500, 200), randn(torch, g, 90, 200, std=0.1)
+    drop = learner.Dropout(0.2, 1, 2)
+
+    def step():
+        wq, wt = learner.quantize_fp8_both(w, square=True)
+        x = learner.embedding(ids, table, 2.0, drop)
+        y = learner.dropout(learner.linear_fp8(x, wq, relu=True, dtype=torch.float32), drop)
+        dx, dw = learner.linear_fp8_grad(x, y, wt, dtype=torch.float32)
+        return y, dw, learner.embedding_grad(ids, dx, 500, 2.0, drop)
+
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        step()
+        graph = torch.cuda.CUDAGraph()
+        stream.synchronize()
+        with torch.cuda.graph(graph, stream=stream):
+            outs = step()
+    for i in range(4):
+        ids.copy_(torch.randint(0, 500, (300,), generator=g, device="cuda"))
+        table.mul_(1.25)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for got, want in zip(outs, step()):
+            assert torch.equal(got, want), i
+
+
+def test_refusals_on_the_device(torch, learner):
+    x = torch.ones(8, 8, device="cuda")
+    with pytest.raises(ps.PSError, match="overlaps"):
+        learner.dropout(x[:7], learner.Dropout(0.5, 1), out=x[1:])
+    with pytest.raises(ps.PSError, match="probability"):
+        learner.dropout(x, learner.Dropout(1.5, 1))
+    with pytest.raises(ValueError, match="apart"):
+        learner.dropout(x.t(), learner.Dropout(0.5, 1))
+    with pytest.raises(ps.PSError, match="row stride"):
+        learner.dropout(x[:1].expand(8, 8), learner.Dropout(0.5, 1))
+    with pytest.raises(TypeError, match="float32 or bfloat16"):
+        learner.dropout(x.half(), learner.Dropout(0.5, 1))
+    with pytest.raises(TypeError, match="int32 or int64"):
+        learner.embedding(x, x)
+    with pytest.raises(ValueError, match="64-bit"):
+        learner.dropout(x, learner.Dropout(0.5, -1))
+    with pytest.raises(ValueError, match="columns"):
+        learner.matmul_fp8(learner.quantize_fp8(x), learner.quantize_fp8(x[:, :4].contiguous()))
+    with pytest.raises(ps.PSError, match="accumulate"):
+        learner.matmul_fp8(learner.quantize_fp8(x), learner.quantize_fp8(x), relu=True,
+                           out=torch.ones(8, 8, device="cuda"), accumulate=True)
+    with pytest.raises(ValueError, match="grad of shape"):
+        learner.embedding_grad(torch.zeros(3, 2, dtype=torch.int64, device="cuda"),
+                               torch.ones(2, 3, 4, device="cuda"), 5)
+

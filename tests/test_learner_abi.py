@@ -1,0 +1,198 @@
+"""The learner's operators on a machine without a GPU: the library loads, exports what
+include/ps_learner.h declares, and refuses what the host can see to be wrong before any
+device work; its kernels' code keeps to the rules that the others' keeps to."""
+import ctypes
+import os
+import re
+import subprocess
+
+import pytest
+import torch
+
+from paper_1611_06213_amd import build as B
+from paper_1611_06213_amd import learner, ps
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+P = 1 << 20   # an address: nothing here reaches a kernel
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(learner.LIB_PATH):
+        pytest.fail("libgadeilearner.so is not built (run __graft_entry__.build())")
+    return learner.load_library()
+
+
+def test_every_declared_symbol_is_exported(lib):
+    text = open(os.path.join(ROOT, "include", "ps_learner.h")).read()
+    text = re.sub(r"/\*.*?\*/", "", text, flags=re.S)
+    names = set(re.findall(r"\b(pl_[a-z0-9_]+)\s*\(", text))
+    assert names == set(learner._SIGS) and len(names) >= 10
+    for n in names:
+        assert hasattr(lib, n), n
+    for name in ("PL_I32", "PL_I64"):
+        assert int(re.search(rf"\b{name}\s*=\s*(\d+)", text).group(1)) == getattr(learner, name)
+
+
+def test_header_is_c(tmp_path):
+    src = tmp_path / "t.c"
+    src.write_text('#include "ps_learner.h"\n'
+                   "int main(void) { pl_drop d = {0.5f, 1, 2}; pl_fp8 q = {0, 0};"
+                   " return d.p > 1 || q.values != 0; }\n")
+    r = subprocess.run(["gcc", "-std=c99", "-Wall", "-Wextra", "-Werror", "-fsyntax-only", "-I",
+                        B.INCLUDE, str(src)], capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr
+
+
+def test_binding_refuses_missing_library(tmp_path):
+    with pytest.raises(RuntimeError, match="not built"):
+        learner.load_library(str(tmp_path / "missing.so"))
+
+
+def drop(p=0.5):
+    return ctypes.byref(learner.pl_drop(p, 1, 2))
+
+
+def refused(lib, rc, text, code=ps.PS_EINVAL):
+    assert rc == code and text in lib.pl_last_error().decode(), (rc, lib.pl_last_error())
+
+
+def test_embedding_refuses(lib):
+    def call(ids=P, id_type=1, tokens=4, table=2 * P, tdt=0, vocab=9, dim=6, ld=6, d=None, out=3 * P,
+             odt=0, old=6):
+        return lib.pl_embedding(ids, id_type, tokens, table, tdt, vocab, dim, ld, 1.0, d, out, odt,
+                                old, None)
+    refused(lib, call(id_type=2), "id type")
+    refused(lib, call(ids=None), "ids: null")
+    refused(lib, call(ids=P + 4), "8-byte")
+    refused(lib, call(table=None), "table: null")
+    refused(lib, call(table=2 * P + 2), "aligned")
+    refused(lib, call(tdt=2), "dtype")
+    refused(lib, call(odt=-1), "dtype")
+    refused(lib, call(ld=5), "row stride")
+    refused(lib, call(old=5), "row stride")
+    refused(lib, call(tokens=-1), "tokens")
+    refused(lib, call(tokens=1 << 32), "tokens")
+    refused(lib, call(vocab=-1), "vocab")
+    refused(lib, call(dim=(1 << 32) + 1, ld=1 << 33, old=1 << 33), "dim")
+    refused(lib, call(d=drop(1.01)), "probability")
+    refused(lib, call(d=drop(float("nan"))), "probability")
+    refused(lib, call(out=2 * P + 4), "overlaps table")
+    refused(lib, call(out=P + 8), "overlaps ids")
+    assert call(tokens=0) == 0 and call(dim=0) == 0   # nothing to do, nothing launched
+
+
+def test_embedding_grad_refuses(lib):
+    need = lib.pl_embedding_grad_workspace(4, 9, 6)
+    assert need > 0
+    # it grows with every size
+    for bigger in ((4000, 9, 6), (4, 9000, 6)):
+        assert lib.pl_embedding_grad_workspace(*bigger) > need
+    for bad in ((-1, 9, 6), (4, 0, 6), (4, 9, -2), (1 << 31, 9, 6), (4, (1 << 31) + 1, 6)):
+        assert lib.pl_embedding_grad_workspace(*bad) == 0
+
+    def call(ids=P, id_type=0, tokens=4, grad=2 * P, gdt=0, gld=6, dim=6, d=None, out=3 * P, odt=0,
+             old=6, vocab=9, ws=4 * P, size=need):
+        return lib.pl_embedding_grad(ids, id_type, tokens, grad, gdt, gld, dim, 1.0, d, out, odt, old,
+                                     vocab, 0, ws, size, None)
+    refused(lib, call(id_type=-1), "id type")
+    refused(lib, call(tokens=1 << 31), "tokens")
+    refused(lib, call(vocab=(1 << 31) + 1), "vocab")
+    refused(lib, call(gld=3), "row stride")
+    refused(lib, call(out=None), "out: null")
+    refused(lib, call(d=drop(-0.1)), "probability")
+    refused(lib, call(size=need - 1), "needed", ps.PS_ENOMEM)
+    refused(lib, call(ws=None), "workspace: null")
+    refused(lib, call(ws=4 * P + 8), "16-byte")
+    refused(lib, call(out=2 * P), "overlaps grad")
+    refused(lib, call(out=4 * P), "overlaps workspace")
+    refused(lib, call(ws=2 * P), "overlaps grad")
+    assert call(vocab=0) == 0 and call(dim=0) == 0
+
+
+def test_dropout_refuses(lib):
+    def call(x=P, dt=0, rows=3, cols=5, ld=5, d=drop(), out=2 * P, old=5):
+        return lib.pl_dropout(x, dt, rows, cols, ld, d, out, old, None)
+    refused(lib, call(d=None), "null")
+    refused(lib, call(x=None), "null")
+    refused(lib, call(dt=7), "dtype")
+    refused(lib, call(ld=4), "row stride")
+    refused(lib, call(rows=1 << 32), "rows")
+    refused(lib, call(cols=-1), "cols")
+    refused(lib, call(out=P + 4), "overlaps")
+    refused(lib, call(out=P, old=6), "overlaps")   # in place with another stride
+    refused(lib, call(d=drop(2.0)), "probability")
+    assert call(rows=0) == 0
+
+
+def fp8(values, scales):
+    return ctypes.byref(learner.pl_fp8(values, scales))
+
+
+def test_fp8_refuses(lib):
+    assert lib.pl_fp8_ld(1) == 128 and lib.pl_fp8_ld(129) == 256 and lib.pl_fp8_ld(0) == 0
+    assert lib.pl_fp8_values_bytes(3, 129) == 768 and lib.pl_fp8_values_bytes(0, 5) == 0
+    assert lib.pl_fp8_scales_bytes(3, 512) == 12 and lib.pl_fp8_scales_bytes(3, 513) == 24
+
+    def quantize(x=P, dt=0, rows=300, cols=200, ld=200, out=fp8(2 * P, 3 * P), out_t=None):
+        return lib.pl_quantize_fp8(x, dt, rows, cols, ld, 0, out, out_t, None)
+    refused(lib, quantize(out=None), "no output")
+    refused(lib, quantize(x=None), "null")
+    refused(lib, quantize(dt=2), "dtype")
+    refused(lib, quantize(ld=199), "row stride")
+    refused(lib, quantize(rows=1 << 31), "rows")
+    refused(lib, quantize(out=fp8(None, 3 * P)), "null")
+    refused(lib, quantize(out=fp8(2 * P + 8, 3 * P)), "16-byte")
+    refused(lib, quantize(out=fp8(P, 3 * P)), "overlaps x")
+    refused(lib, quantize(out_t=fp8(2 * P, 5 * P)), "overlaps")
+    assert quantize(rows=0) == 0
+
+    a, b = fp8(P, 2 * P), fp8(3 * P, 4 * P)
+
+    def matmul(m=8, n=8, k=300, a=a, b=b, bias=None, relu=0, out=5 * P, odt=1, ld=8, acc=0, ws=6 * P,
+               size=1 << 24):
+        return lib.pl_matmul_fp8(m, n, k, a, b, bias, 0, relu, out, odt, ld, acc, ws, size, None)
+    refused(lib, matmul(m=-1), "m:")
+    refused(lib, matmul(k=(1 << 22) + 1), "k:")
+    refused(lib, matmul(a=None), "a: null")
+    refused(lib, matmul(b=fp8(3 * P, None)), "b: null")
+    refused(lib, matmul(odt=3), "dtype")
+    refused(lib, matmul(ld=7), "row stride")
+    refused(lib, matmul(acc=1, relu=1), "accumulate")
+    refused(lib, matmul(acc=1, bias=7 * P), "accumulate")
+    refused(lib, matmul(out=P), "overlaps a")
+    refused(lib, matmul(out=3 * P + 64), "overlaps b")
+    refused(lib, matmul(bias=7 * P, out=7 * P), "overlaps bias")
+    need = lib.pl_matmul_fp8_workspace(8, 8, 100_000, 1)
+    assert need > 0   # few tiles: k is split
+    refused(lib, matmul(k=100_000, b=fp8(8 * P, 16 * P), size=need - 1), "needed", ps.PS_ENOMEM)
+    assert lib.pl_matmul_fp8_workspace(8192, 8192, 8192, 1) == 0
+    assert matmul(m=0) == 0 and matmul(n=0) == 0
+
+
+def test_binding_refuses_host_tensors():
+    x = torch.ones(4, 4)
+    for call in (lambda: learner.dropout(x, learner.Dropout(0.5, 1)),
+                 lambda: learner.embedding(torch.zeros(3, dtype=torch.int64), x),
+                 lambda: learner.quantize_fp8(x)):
+        with pytest.raises(ValueError, match="device tensor"):
+            call()
+    with pytest.raises(TypeError, match="tensor expected"):
+        learner.dropout([1.0], learner.Dropout(0.5, 1))
+
+
+def test_kernels_use_no_scratch_and_no_packed_fp32(tmp_path):
+    running = []
+    for src in B.LEARNER_SOURCES:
+        if src.endswith(".hip"):
+            out = str(tmp_path / (os.path.basename(src) + ".s"))
+            flags = [f for f in B.LEARNER_FLAGS if f != "-fPIC"]
+            running.append((out, subprocess.Popen([B.HIPCC, *flags, "--cuda-device-only", "-S", src, "-o",
+                                                   out], stderr=subprocess.DEVNULL)))
+    assert running
+    for out, p in running:
+        assert p.wait(timeout=600) == 0
+        text = open(out).read()
+        sizes = re.findall(r"\.amdhsa_private_segment_fixed_size (\d+)", text)
+        assert sizes and set(sizes) == {"0"}, out
+        assert not re.search(r"^\s*v_pk_(add|mul|fma)_f32", text, re.M), out
