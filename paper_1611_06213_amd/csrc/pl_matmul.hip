@@ -22,6 +22,8 @@
 // at most 64 rows of a, reads b, by far the larger operand, straight into registers.
 // Where there are too few tiles to fill the card, k is split over workgroups; the parts'
 // sums go to the workspace and `join` adds them up in order.
+#include <algorithm>
+
 #include "pl_device.h"
 
 namespace gadei::learner {
@@ -29,6 +31,7 @@ namespace {
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
@@ -64,10 +67,25 @@ __device__ __forceinline__ f32x4 mfma(const Operand<false> &b, const Operand<fal
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b.v, a.v, c, 0, 0, 0, b.scale, 0, a.scale);
 }
 
+// The same with 32 rows of either operand, of which a lane gives 32 columns of 64.
+__device__ __forceinline__ f32x16 mfma(const Operand<false> &b, const Operand<false> &a, f32x16 c) {
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(b.v, a.v, c, 0, 0, 0, b.scale, 0, a.scale);
+}
+
+__device__ __forceinline__ f32x16 mfma(const Operand<true> &b, const Operand<true> &a, f32x16 c) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b.v[i], a.v[i], c, 0, 0, 0);
+    return c;
+}
+
 __device__ __forceinline__ f32x4 mfma(const Operand<true> &b, const Operand<true> &a, f32x4 c) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b.v[i], a.v[i], c, 0, 0, 0);
     return c;
+}
+
+__device__ __forceinline__ float bias_at(const MatmulArgs &g, uint32_t n) {
+    return g.bias_bf16 ? load1<PS_BF16>(g.bias, n) : load1<PS_F32>(g.bias, n);
 }
 
 // What becomes of a sum: four columns from n on of row m.
@@ -78,8 +96,7 @@ __device__ __forceinline__ void finish(const MatmulArgs &g, f32x4 v, uint32_t m,
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         x[e] = v[e];
-        if (g.bias != nullptr && n + e < g.n)
-            x[e] += g.bias_bf16 ? load1<PS_BF16>(g.bias, n + e) : load1<PS_F32>(g.bias, n + e);
+        if (g.bias != nullptr && n + e < g.n) x[e] += bias_at(g, n + e);
         if (g.relu) x[e] = x[e] < 0.0f ? 0.0f : x[e];   // NaN stays
         if (g.accumulate && n + e < g.n) x[e] += load1<OUT>(g.out, at + e);
     }
@@ -104,8 +121,23 @@ __device__ __forceinline__ void keep(const MatmulArgs &g, f32x4 v, uint32_t part
     *reinterpret_cast<f32x4 *>(g.partial + (static_cast<uint64_t>(part) * g.m + m) * ld + n) = v;
 }
 
-typedef __attribute__((address_space(1))) uint32_t GlobalWord;
-typedef __attribute__((address_space(3))) uint32_t LdsWord;
+// A run of memory that is read by 32-bit offsets: a lane's own, and one that all lanes share
+// (which costs no vector register). What lies outside reads as zero.
+struct Buffer {
+    __amdgpu_buffer_rsrc_t rsrc;
+    Buffer() = default;
+    __device__ __forceinline__ Buffer(const void *p, uint32_t bytes)
+        : rsrc(__builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, static_cast<int>(bytes), 0x27000)) {}
+    static constexpr uint32_t kOutside = 0x80000000u;   // of every buffer
+    // 16 bytes a lane, to LDS at 16 bytes a lane
+    __device__ __forceinline__ void to_lds(uint8_t *to, uint32_t lane, uint32_t shared) const {
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(
+            rsrc, (__attribute__((address_space(3))) void *)to, 16, lane, shared, 0, 0);
+    }
+    __device__ __forceinline__ uint32_t word(uint32_t lane) const {
+        return __builtin_amdgcn_raw_buffer_load_b32(rsrc, lane, 0, 0);
+    }
+};
 
 struct Split {
     uint32_t tiles_m, tiles_n;
@@ -114,113 +146,291 @@ struct Split {
 
 // ------------------------------------------------------------------- tiles
 
-// BM x BN tiles of out by WM x WN waves.
-template <int BM, int BN, int WM, int WN, int OUT>
-__global__ __launch_bounds__(64 * WM * WN) void tiles(MatmulArgs g, Split sp) {
-    constexpr int kWaves = WM * WN, FM = BM / WM / 16, FN = BN / WN / 16;
-    constexpr int kLoads = (BM + BN) / 8 / kWaves;   // a wave loads 8 rows of 128 bytes at once
-    static_assert((BM + BN) % (8 * kWaves) == 0 && BM % (8 * kLoads) == 0, "whole loads");
-    // two buffers that the compiler can tell apart
-    __shared__ __attribute__((aligned(128))) uint8_t even[(BM + BN) * 128];
-    __shared__ __attribute__((aligned(128))) uint8_t odd[(BM + BN) * 128];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const uint32_t tile = blockIdx.x % (sp.tiles_m * sp.tiles_n);
-    const uint32_t part = blockIdx.x / (sp.tiles_m * sp.tiles_n);
-    const uint32_t m0 = tile % sp.tiles_m * BM, n0 = tile / sp.tiles_m * BN;
+// Which tile of which part of k the work unit `unit` is. Workgroups go round the eight XCDs, each
+// with an L2 of its own: an XCD takes a contiguous run of an order that walks bands of eight rows of tiles column by
+// column, so that the 32 tiles that its compute units work on share their rows of a and b.
+__device__ __forceinline__ void place(const Split &sp, uint32_t unit, uint32_t *tile_m, uint32_t *tile_n,
+                                      uint32_t *part) {
+    constexpr uint32_t kXcds = 8, kBand = 8;
+    const uint32_t tiles = sp.tiles_m * sp.tiles_n, all = tiles * sp.parts;
+    const uint32_t xcd = unit % kXcds, each = all / kXcds, more = all % kXcds;
+    const uint32_t t = xcd * each + min(xcd, more) + unit / kXcds;
+    *part = t / tiles;
+    const uint32_t in = t % tiles, band = in / (kBand * sp.tiles_n), at = in % (kBand * sp.tiles_n);
+    const uint32_t height = min(kBand, sp.tiles_m - band * kBand);
+    *tile_m = band * kBand + at % height;
+    *tile_n = at / height;
+}
+
+// Tiles of 64 FM x 64 FN by 2 x 2 waves, each FM x FN instructions of 32 x 32.
+//
+// A step is half a block, 64 columns. LDS holds four steps of either operand, which copies bring
+// there from memory without registers; the registers hold the step that multiplies and the
+// one after it. So in step s, step s + 1 is read from LDS, step s + 4 is copied to where s was,
+// and the copies have three steps to arrive: at the end of a step only those of the one
+// before the last are waited for.
+template <int FM, int FN, int OUT>
+__global__ __launch_bounds__(256) void tiles(MatmulArgs g, Split sp) {
+    constexpr int BM = 64 * FM, BN = 64 * FN;
+    // buffers that the compiler can tell apart: it would wait for all copies before every
+    // read of LDS if it could not
+    __shared__ __attribute__((aligned(128))) uint8_t a0[BM * 64], a1[BM * 64], a2[BM * 64], a3[BM * 64];
+    __shared__ __attribute__((aligned(128))) uint8_t b0[BN * 64], b1[BN * 64], b2[BN * 64], b3[BN * 64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t blocks = (g.k + 127) / 128, ld = blocks * 128;
-    const uint32_t first = part * sp.steps;
-    const uint32_t last = min(blocks, first + sp.steps);   // first < last, as the host splits
+    const int wm = wave % 2 * (32 * FM), wn = wave / 2 * (32 * FN);
+    const int q = lane >> 5, r32 = lane & 31;
 
-    // Rows of the tile: BM of a, then BN of b; rows past the matrix repeat its last. Byte c of
-    // row r lies at 128 r + 16 ((c / 16) ^ (r % 8)) + c % 16, so that the rows that lanes read
-    // together lie in different banks.
-    const bool of_a = wave * kLoads * 8 < BM;
-    const uint8_t *base = of_a ? g.a + static_cast<uint64_t>(m0) * ld : g.b + static_cast<uint64_t>(n0) * ld;
-    uint32_t from[kLoads];
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-        const uint32_t r = (wave * kLoads + i) * 8 + (lane >> 3);
-        const uint32_t row = of_a ? min(r, g.m - 1 - m0) : min(r - BM, g.n - 1 - n0);
-        from[i] = row * ld + (((lane & 7) ^ (lane >> 3)) << 4);
-    }
-    auto fetch = [&](uint8_t *to, uint32_t block) {
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i)
-            __builtin_amdgcn_global_load_lds(
-                (const GlobalWord *)(base + static_cast<uint64_t>(block) * 128 + from[i]),
-                (LdsWord *)(to + (wave * kLoads + i) * 1024), 16, 0, 0);
-    };
+    // A copy takes 16 rows of 64 bytes. Rows past the matrix are outside the buffers' bounds and
+    // read as zeros, as are their scales. 16 bytes c of row r lie at 64 r + 16 (c ^ (r / 4 % 4)),
+    // so that the 16 lanes that LDS serves at once (of rows 0-3, 12-15, 20-23 and 24-27, or of
+    // the other 16) lie in different banks.
+    const uint32_t from = (lane >> 2) * ld + (((lane & 3) ^ ((lane >> 4) & 3)) << 4);
+    const int low = r32 * 64 + (((2 * q) ^ (r32 >> 2 & 3)) << 4);
+    const int high = r32 * 64 + (((2 * q + 1) ^ (r32 >> 2 & 3)) << 4);
 
-    const int wm = wave % WM * (BM / WM), wn = wave / WM * (BN / WN);
-    const int q = lane >> 4, r16 = lane & 15;
-    const int low = r16 * 128 + (((2 * q) ^ (r16 & 7)) << 4);
-    const int high = r16 * 128 + (((2 * q + 1) ^ (r16 & 7)) << 4);
-    uint32_t sa[FM], sb[FN];
-    auto scales = [&](uint32_t block) {   // four blocks' at once
-        const uint32_t *pa = g.sa + static_cast<uint64_t>(block >> 2) * g.m;
-        const uint32_t *pb = g.sb + static_cast<uint64_t>(block >> 2) * g.n;
-#pragma unroll
-        for (int i = 0; i < FM; ++i) sa[i] = pa[min(m0 + wm + 16 * i + r16, g.m - 1)];
-#pragma unroll
-        for (int j = 0; j < FN; ++j) sb[j] = pb[min(n0 + wn + 16 * j + r16, g.n - 1)];
-        const int skip = 8 * (block & 3);
-#pragma unroll
-        for (int i = 0; i < FM; ++i) sa[i] >>= skip;
-#pragma unroll
-        for (int j = 0; j < FN; ++j) sb[j] >>= skip;
+    // a work unit: a tile and a part of k
+    uint32_t m0, n0, part, first, last;
+    Buffer rows_a, rows_b;
+    auto take = [&](uint32_t unit) {
+        uint32_t tile_m, tile_n;
+        place(sp, unit, &tile_m, &tile_n, &part);
+        m0 = tile_m * BM;
+        n0 = tile_n * BN;
+        first = part * sp.steps;
+        last = min(blocks, first + sp.steps);   // first < last, as the host splits
+        rows_a = Buffer(g.a + static_cast<uint64_t>(m0) * ld, min(g.m - m0, uint32_t(BM)) * ld);
+        rows_b = Buffer(g.b + static_cast<uint64_t>(n0) * ld, min(g.n - n0, uint32_t(BN)) * ld);
     };
-    f32x4 acc[FM][FN] = {};
-    auto multiply = [&](const uint8_t *at) {
-        Operand<OUT == PS_F32> fa, fb[FN];
-#pragma unroll
-        for (int j = 0; j < FN; ++j) {
-            const uint8_t *p = at + (BM + wn + 16 * j) * 128;
-            fb[j].set(*reinterpret_cast<const i32x4 *>(p + low),
-                      *reinterpret_cast<const i32x4 *>(p + high), sb[j]);
-        }
-#pragma unroll
-        for (int i = 0; i < FM; ++i) {
-            const uint8_t *p = at + (wm + 16 * i) * 128;
-            fa.set(*reinterpret_cast<const i32x4 *>(p + low),
-                   *reinterpret_cast<const i32x4 *>(p + high), sa[i]);
-#pragma unroll
-            for (int j = 0; j < FN; ++j) acc[i][j] = mfma(fb[j], fa, acc[i][j]);
-        }
-#pragma unroll
-        for (int i = 0; i < FM; ++i) sa[i] >>= 8;
-#pragma unroll
-        for (int j = 0; j < FN; ++j) sb[j] >>= 8;
-    };
-    auto arrived = [] {   // this wave's loads to LDS, then everyone's
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
+    // The wave's copies of a step (of block `block`, half 0 or 1): FM of a, FN of b. Blocks past the
+    // last: no bytes.
+    auto copy = [&](uint8_t *a, uint8_t *b, int i, uint32_t block, int half) {
+        const uint32_t lanes = block < last ? from : Buffer::kOutside;
+        if (i < FM)
+            rows_a.to_lds(a + (wave * FM + i) * 1024, lanes, (wave * FM + i) * 16 * ld + block * 128 + half * 64);
+        else
+            rows_b.to_lds(b + (wave * FN + i - FM) * 1024, lanes,
+                          (wave * FN + i - FM) * 16 * ld + block * 128 + half * 64);
     };
 
-    fetch(even, first);
-    scales(first);
-    arrived();
-    for (uint32_t block = first; block < last; block += 2) {
-        if (block + 1 < last) fetch(odd, block + 1);
-        if (block != first && (block & 3) == 0) scales(block);
-        multiply(even);
-        arrived();
-        if (block + 1 >= last) break;
-        if (block + 2 < last) fetch(even, block + 2);
-        if (((block + 1) & 3) == 0) scales(block + 1);
-        multiply(odd);
-        arrived();
-    }
+    // The scales of four blocks are a word of each row. These are shifted so that the byte of the
+    // step that is being read is the lowest; the next words are loaded a block
+    // ahead.
+    uint32_t sa[FM], sb[FN], next_a[FM], next_b[FN];
+    auto load_words = [&](uint32_t (&a)[FM], uint32_t (&b)[FN], uint32_t block, bool wanted) {
+        const uint64_t group = min(block, blocks - 1) >> 2;
+        const Buffer ga(g.sa + group * g.m, g.m * 4), gb(g.sb + group * g.n, g.n * 4);
+        const uint32_t la = wanted ? (m0 + wm + r32) * 4 : Buffer::kOutside;
+        const uint32_t lb = wanted ? (n0 + wn + r32) * 4 : Buffer::kOutside;
 #pragma unroll
-    for (int i = 0; i < FM; ++i) {
-        const uint32_t m = m0 + wm + 16 * i + r16;
-        if (m >= g.m) continue;
+        for (int i = 0; i < FM; ++i) a[i] = ga.word(la + 128 * i);
 #pragma unroll
-        for (int j = 0; j < FN; ++j) {
-            const uint32_t n = n0 + wn + 16 * j + 4 * q;
-            if (n >= g.n) continue;
-            if (sp.parts == 1) finish<OUT>(g, acc[i][j], m, n);
-            else keep(g, acc[i][j], part, m, n);
+        for (int j = 0; j < FN; ++j) b[j] = gb.word(lb + 128 * j);
+    };
+    auto begin = [&] {   // the first four steps' copies and the first words
+#pragma unroll
+        for (int i = 0; i < FM + FN; ++i) copy(a0, b0, i, first, 0);
+        load_words(sa, sb, first, true);
+        load_words(next_a, next_b, first + 1, ((first + 1) & 3) == 0);
+#pragma unroll
+        for (int i = 0; i < FM + FN; ++i) copy(a1, b1, i, first, 1);
+#pragma unroll
+        for (int i = 0; i < FM + FN; ++i) copy(a2, b2, i, first + 1, 0);
+#pragma unroll
+        for (int i = 0; i < FM + FN; ++i) copy(a3, b3, i, first + 1, 1);
+    };
+
+    using Op = Operand<OUT == PS_F32>;
+    struct Raw { i32x4 lo, hi; };
+    struct Step { Raw a[FM], b[FN]; uint32_t sa[FM], sb[FN]; };
+    f32x16 acc[FM][FN];
+    auto read_a = [&](Step &s, const uint8_t *at, int i) {
+        const uint8_t *p = at + (wm + 32 * i) * 64;
+        s.a[i] = Raw{*reinterpret_cast<const i32x4 *>(p + low), *reinterpret_cast<const i32x4 *>(p + high)};
+        s.sa[i] = sa[i];
+    };
+    auto read_b = [&](Step &s, const uint8_t *at, int j) {
+        const uint8_t *p = at + (wn + 32 * j) * 64;
+        s.b[j] = Raw{*reinterpret_cast<const i32x4 *>(p + low), *reinterpret_cast<const i32x4 *>(p + high)};
+        s.sb[j] = sb[j];
+    };
+    // Multiply `now`, read `next` (from a and b), copy half `half` of block `block` to a_to and b_to.
+    auto step = [&](const Step &now, Step &next, const uint8_t *a, const uint8_t *b, uint8_t *a_to,
+                    uint8_t *b_to, uint32_t block, int half) {
+        // Reads and copies one at a time between the products: the memory pipeline takes a copy every
+        // 16 cycles from four waves, and a wave that has to wait there issues no products. The reads
+        // end early, so that none is waited for at the step's end.
+        constexpr int N = FM + FN, S = FM * FN;
+        Op fa, fb[FN];
+#pragma unroll
+        for (int t = 0; t < S; ++t) {
+            const int i = t / FN, j = t % FN;
+            if (j == 0) fa.set(now.a[i].lo, now.a[i].hi, now.sa[i]);
+            if (i == 0) fb[j].set(now.b[j].lo, now.b[j].hi, now.sb[j]);
+            acc[i][j] = mfma(fb[j], fa, acc[i][j]);
+#pragma unroll
+            for (int c = t * 3 * N / (2 * S); c < (t + 1) * 3 * N / (2 * S) && c < N; ++c) {
+                if (c < FM) read_a(next, a, c);
+                else read_b(next, b, c - FM);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int c = (t * N + N / 2) / S; c < ((t + 1) * N + N / 2) / S && c < N; ++c) copy(a_to, b_to, c, block, half);
+            __builtin_amdgcn_sched_barrier(0);
         }
+        // This wave's copies but those of the last two steps have arrived, and its reads; then
+        // everyone's. Since those copies it has issued 2 (FM + FN) more and the loads of one
+        // block's words.
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(3 * (FM + FN)) : "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+
+    Step x, y;
+    // A block's second step reads the next block's first half, and so takes that block's words;
+    // the words of the block after it are loaded then, if they are of another group. There
+    // is no branch in a step: the compiler would move products across it.
+    auto block = [&](uint32_t k, uint8_t *pa0, uint8_t *pb0, uint8_t *pa1, uint8_t *pb1, uint8_t *pa2,
+                     uint8_t *pb2) {
+        step(x, y, pa1, pb1, pa0, pb0, k + 2, 0);
+        const bool group = ((k + 1) & 3) == 0;
+        const uint32_t keep = k + 1 < last ? 0xffffffffu : 0;   // a block of zeros: any finite scale
+#pragma unroll
+        for (int i = 0; i < FM; ++i) sa[i] = (group ? next_a[i] : sa[i] >> 8) & keep;
+#pragma unroll
+        for (int j = 0; j < FN; ++j) sb[j] = (group ? next_b[j] : sb[j] >> 8) & keep;
+        load_words(next_a, next_b, k + 2, ((k + 2) & 3) == 0);
+        step(y, x, pa2, pb2, pa1, pb1, k + 2, 1);
+    };
+
+    uint32_t unit = blockIdx.x;
+    take(unit);
+    begin();
+    for (;;) {
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j) acc[i][j] = f32x16{};
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * (FM + FN)) : "memory");   // steps 0 and 1
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int i = 0; i < FM; ++i) sa[i] >>= 8 * (first & 3);
+#pragma unroll
+        for (int j = 0; j < FN; ++j) sb[j] >>= 8 * (first & 3);
+#pragma unroll
+        for (int i = 0; i < FM; ++i) read_a(x, a0, i);
+#pragma unroll
+        for (int j = 0; j < FN; ++j) read_b(x, b0, j);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();   // a0 and b0 may be written
+        asm volatile("" ::: "memory");
+        // an odd number of blocks is followed by one of zeros: a loop with a way out in its middle
+        // would have the compiler move all sums from register to register
+        for (uint32_t k = first; k < last; k += 2) {
+            block(k, a0, b0, a1, b1, a2, b2);
+            block(k + 1, a2, b2, a3, b3, a0, b0);
+        }
+
+        // The results. Whole tiles go out from the registers, while the next unit's first copies
+        // are under way.
+        // The lane's number is hidden from the compiler here: it would compute all addresses below
+        // before the loop, and have no registers for them in it.
+        uint32_t lane1 = threadIdx.x & 63;
+        asm volatile("" : "+v"(lane1));
+        const uint32_t q1 = lane1 >> 5, r1 = lane1 & 31;
+        const uint32_t m1 = m0 + wm, n1 = n0 + wn, part1 = part;
+        const bool whole = m0 + BM <= g.m && n0 + BN <= g.n && sp.parts == 1 && !g.accumulate;
+        unit += gridDim.x;
+        const bool more = unit < sp.tiles_m * sp.tiles_n * sp.parts;
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the last copies write zeros to LDS
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        if (whole) {
+            if (more) {
+                take(unit);
+                begin();
+            }
+#pragma unroll
+            for (int j = 0; j < FN; ++j) {
+                // a lane holds row r32's columns 8 e + 4 q + 0..3, e = 0..3
+                f32x4 bias[4] = {};
+                if (g.bias != nullptr) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+#pragma unroll
+                        for (int c = 0; c < 4; ++c)
+                            bias[e][c] = bias_at(g, n1 + 32 * j + 8 * e + 4 * q1 + c);
+                }
+#pragma unroll
+                for (int i = 0; i < FM; ++i) {
+                    f32x4 v[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        v[e] = f32x4{acc[i][j][4 * e], acc[i][j][4 * e + 1], acc[i][j][4 * e + 2],
+                                     acc[i][j][4 * e + 3]} + bias[e];
+                        if (g.relu) {
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) v[e][c] = v[e][c] < 0.0f ? 0.0f : v[e][c];
+                        }
+                    }
+                    const int64_t at = static_cast<int64_t>(m1 + 32 * i + r1) * g.out_ld + n1 + 32 * j;
+                    if constexpr (OUT == PS_F32) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            *reinterpret_cast<f32x4_any *>(static_cast<float *>(g.out) + at + 8 * e + 4 * q1) = v[e];
+                    } else {
+                        // the halves of the wave exchange fours, so that a lane has eight columns
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            u32x4 w;
+#pragma unroll
+                            for (int c = 0; c < 2; ++c) {
+                                const auto p = __builtin_amdgcn_permlane32_swap(
+                                    bf16x2_rne(v[2 * h][2 * c], v[2 * h][2 * c + 1]),
+                                    bf16x2_rne(v[2 * h + 1][2 * c], v[2 * h + 1][2 * c + 1]), false, false);
+                                w[c] = p[0];
+                                w[2 + c] = p[1];
+                            }
+                            *reinterpret_cast<u32x4_any *>(static_cast<uint16_t *>(g.out) + at + 16 * h + 8 * q1) = w;
+                        }
+                    }
+                }
+            }
+        } else {
+            // 32 rows at a time through a part of LDS that is the wave's own: fours of columns,
+            // swizzled.
+            constexpr int kFours = 8 * FN;   // of a row of the wave's
+            static_assert(32 * kFours * 16 <= BM * 64, "a buffer has room for a wave's rows");
+            f32x4 *rows = reinterpret_cast<f32x4 *>(wave == 0 ? a0 : wave == 1 ? a1 : wave == 2 ? a2 : a3);
+#pragma unroll
+            for (int i = 0; i < FM; ++i) {
+#pragma unroll
+                for (int j = 0; j < FN; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        rows[r1 * kFours + ((8 * j + 2 * e + q1) ^ (r1 & 7))] =
+                            f32x4{acc[i][j][4 * e], acc[i][j][4 * e + 1], acc[i][j][4 * e + 2],
+                                  acc[i][j][4 * e + 3]};
+                __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+                for (uint32_t t = lane1; t < 32 * kFours; t += 64) {
+                    const uint32_t r = t / kFours, c = t % kFours;
+                    const uint32_t m = m1 + 32 * i + r, n = n1 + 4 * c;
+                    const f32x4 v = rows[r * kFours + (c ^ (r & 7))];
+                    if (m >= g.m || n >= g.n) continue;
+                    if (sp.parts == 1) finish<OUT>(g, v, m, n);
+                    else keep(g, v, part1, m, n);
+                }
+                __builtin_amdgcn_wave_barrier();
+            }
+            if (more) {
+                __syncthreads();
+                take(unit);
+                begin();
+            }
+        }
+        if (!more) break;
     }
 }
 
@@ -334,6 +544,9 @@ Choice choose(uint64_t m, uint64_t n, uint64_t k, bool wide) {
     if (m <= kSlimRows) {
         c.bm = static_cast<int>(m);
         c.bn = 16;
+    } else if ((m + 255) / 256 * ((n + 255) / 256) * (wide ? 2 : 1) >= kCus) {
+        c.bm = 256;
+        c.bn = wide ? 128 : 256;
     } else {
         c.bm = c.bn = 128;
     }
@@ -369,7 +582,8 @@ hipError_t launch(const MatmulArgs &g, hipStream_t s) {
     if (g.m <= 16) slim<1, OUT><<<blocks, 64 * kSlimWaves, 0, s>>>(g, c.split);
     else if (g.m <= 32) slim<2, OUT><<<blocks, 64 * kSlimWaves, 0, s>>>(g, c.split);
     else if (g.m <= kSlimRows) slim<4, OUT><<<blocks, 64 * kSlimWaves, 0, s>>>(g, c.split);
-    else tiles<128, 128, 2, 2, OUT><<<blocks, 256, 0, s>>>(g, c.split);
+    else if (c.bm == 128) tiles<2, 2, OUT><<<std::min(blocks, 2u * kCus), 256, 0, s>>>(g, c.split);
+    else tiles<4, OUT == PS_F32 ? 2 : 4, OUT><<<std::min(blocks, 1u * kCus), 256, 0, s>>>(g, c.split);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || c.split.parts == 1) return e;
     join<OUT><<<static_cast<uint32_t>(join_blocks), 256, 0, s>>>(g, c.split.parts);
