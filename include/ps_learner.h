@@ -124,6 +124,15 @@ int pl_matmul_fp8(int64_t m, int64_t n, int64_t k, const pl_fp8 *a, const pl_fp8
                   void *stream);
 size_t pl_matmul_fp8_workspace(int64_t m, int64_t n, int64_t k, int out_dtype);
 
+/* A fully connected layer: pl_quantize_fp8 of x (m x k, blocks along its rows), then
+ * pl_matmul_fp8 with the weights w (n x k) -- the same result, in fewer launches where
+ * x is small. */
+int pl_linear_fp8(const void *x, int dtype, int64_t m, int64_t k, int64_t ld, int64_t n,
+                  const pl_fp8 *w, const void *bias, int bias_dtype, int relu, void *out,
+                  int out_dtype, int64_t out_ld, void *workspace, size_t workspace_bytes,
+                  void *stream);
+size_t pl_linear_fp8_workspace(int64_t m, int64_t n, int64_t k, int dtype, int out_dtype);
+
 /* Message for the last failed call on this thread ("" if none). */
 const char *pl_last_error(void);
 

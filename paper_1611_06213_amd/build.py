@@ -22,6 +22,7 @@ LIB = os.path.join(HERE, "libgadeips.so")
 LIB_FMA = os.path.join(HERE, "libgadeips_fma.so")
 FMA_FLAGS = ["-ffp-contract=fast", "-DPS_FP_CONTRACT=1"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
+ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 
 SOURCES = [os.path.join(CSRC, "ps_server.cpp"), os.path.join(CSRC, "ps_protocol.cpp"),
            os.path.join(CSRC, "ps_layout.cpp"), os.path.join(CSRC, "ps_kernels.hip")]
@@ -94,37 +95,57 @@ def build_learner(verbose: bool = False) -> str:
     return LEARNER_LIB
 
 
-# the Python binding's per-step calls (host only; needs torch's headers)
+# the Python bindings' native calls (host only; need torch's headers): the server's
+# per-step calls, and the learner's operators
 BINDING_SRC = os.path.join(CSRC, "ps_binding.cpp")
 BINDING = os.path.join(HERE, "_binding.so")
+LEARNER_BINDING_SRC = os.path.join(CSRC, "pl_binding.cpp")
+LEARNER_BINDING = os.path.join(HERE, "_learner.so")
 
 
-def build_binding(verbose: bool = False) -> str:
+def _binding_cmd(src: str, out: str, flags=(), libs=()):
     import sysconfig
 
     import torch
     t = os.path.dirname(torch.__file__)
-    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-Wall",
-           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", INCLUDE,
-           "-isystem", os.path.join(t, "include"),
-           "-isystem", os.path.join(t, "include", "torch", "csrc", "api", "include"),
-           "-isystem", sysconfig.get_paths()["include"], BINDING_SRC,
-           "-L", os.path.join(t, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10",
-           "-o", BINDING + ".tmp"]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    r = subprocess.run(cmd, capture_output=True, text=True)
-    if r.returncode != 0:
-        sys.stderr.write(r.stdout + r.stderr)
-        raise RuntimeError("g++ failed building the Python binding")
-    os.replace(BINDING + ".tmp", BINDING)
+    return ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-Wall",
+            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *flags, "-I", INCLUDE,
+            "-isystem", os.path.join(t, "include"),
+            "-isystem", os.path.join(t, "include", "torch", "csrc", "api", "include"),
+            "-isystem", sysconfig.get_paths()["include"], src,
+            "-L", os.path.join(t, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", *libs,
+            "-o", out + ".tmp"]
+
+
+def build_binding(verbose: bool = False) -> str:
+    """Both bindings. The learner's links against its library, beside which it lies."""
+    cmds = [(BINDING, _binding_cmd(BINDING_SRC, BINDING)),
+            (LEARNER_BINDING, _binding_cmd(
+                LEARNER_BINDING_SRC, LEARNER_BINDING,
+                ["-D__HIP_PLATFORM_AMD__", "-DUSE_ROCM", "-isystem", os.path.join(ROCM, "include")],
+                ["-lc10_hip", "-L", HERE, "-lgadeilearner", "-Wl,-rpath,$ORIGIN"]))]
+    running = []
+    for out, cmd in cmds:
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        running.append((out, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT,
+                                              text=True)))
+    failed = []
+    for out, p in running:
+        text = p.communicate()[0]
+        if p.returncode != 0:
+            sys.stderr.write(text)
+            failed.append(os.path.basename(out))
+        else:
+            os.replace(out + ".tmp", out)
+    if failed:
+        raise RuntimeError("g++ failed building the Python binding " + ", ".join(failed))
     return BINDING
 
 
 # a plain C program that drives the C ABI without Python (tests/test_c_abi.py)
 C_SMOKE_SRC = os.path.join(ROOT, "tests", "c_abi_smoke.c")
 C_SMOKE = os.path.join(ROOT, "tests", "c_abi_smoke")
-ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 
 
 def build_c_smoke(verbose: bool = False) -> str:

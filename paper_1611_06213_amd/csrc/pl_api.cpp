@@ -101,6 +101,8 @@ int dropping(const pl_drop *drop, Drop *d, float *factor) {
     return PS_OK;
 }
 
+size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
+
 int64_t blocks_of(int64_t cols) { return (cols + 127) / 128; }
 
 int fp8(const char *name, const pl_fp8 *q, int64_t rows, int64_t cols, Span *values, Span *scales) {
@@ -300,4 +302,41 @@ int pl_matmul_fp8(int64_t m, int64_t n, int64_t k, const pl_fp8 *a, const pl_fp8
     g.accumulate = accumulate != 0;
     g.partial = static_cast<float *>(workspace);
     return launched(launch_matmul(g, out_dtype, static_cast<hipStream_t>(stream)), "pl_matmul_fp8");
+}
+
+size_t pl_linear_fp8_workspace(int64_t m, int64_t n, int64_t k, int dtype, int out_dtype) {
+    if (m < 0 || m >= kMax / 2 || n < 0 || n >= kMax / 2 || k < 0 || k > (1 << 22) ||
+        !is_dtype(dtype) || !is_dtype(out_dtype))
+        return 0;
+    return align256(pl_fp8_values_bytes(m, k)) + align256(pl_fp8_scales_bytes(m, k)) +
+           matmul_workspace(m, n, k, out_dtype);
+}
+
+int pl_linear_fp8(const void *x, int dtype, int64_t m, int64_t k, int64_t ld, int64_t n,
+                  const pl_fp8 *w, const void *bias, int bias_dtype, int relu, void *out,
+                  int out_dtype, int64_t out_ld, void *workspace, size_t workspace_bytes,
+                  void *stream) {
+    // the products' checks, with a stand-in for x's 8-bit form, before anything is enqueued
+    Span in[5] = {}, o;
+    if (int rc = size_in("m", m, kMax / 2 - 1)) return rc;
+    if (int rc = size_in("n", n, kMax / 2 - 1)) return rc;
+    if (int rc = size_in("k", k, 1 << 22)) return rc;
+    if (int rc = matrix("x", x, dtype, m, k, ld, &in[0])) return rc;
+    if (int rc = fp8("w", w, n, k, &in[1], &in[2])) return rc;
+    if (bias != nullptr)
+        if (int rc = matrix("bias", bias, bias_dtype, 1, n, n, &in[3])) return rc;
+    if (int rc = matrix("out", out, out_dtype, m, n, out_ld, &o)) return rc;
+    if (m == 0 || n == 0) return PS_OK;
+    const size_t need = pl_linear_fp8_workspace(m, n, k, dtype, out_dtype);
+    if (workspace_bytes < need)
+        return fail(PS_ENOMEM, "workspace of %zu bytes, %zu needed", workspace_bytes, need);
+    if (int rc = plain("workspace", workspace, need, 16, &in[4])) return rc;
+    if (int rc = apart(o, in, 5)) return rc;
+    if (int rc = apart(in[4], in, 4)) return rc;
+    char *ws = static_cast<char *>(workspace);
+    const size_t values = align256(pl_fp8_values_bytes(m, k)), scales = align256(pl_fp8_scales_bytes(m, k));
+    const pl_fp8 q = {ws, reinterpret_cast<uint32_t *>(ws + values)};
+    if (int rc = pl_quantize_fp8(x, dtype, m, k, ld, 0, &q, nullptr, stream)) return rc;
+    return pl_matmul_fp8(m, n, k, &q, w, bias, bias_dtype, relu, out, out_dtype, out_ld, 0,
+                         ws + values + scales, need - values - scales, stream);
 }

@@ -16,6 +16,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import warnings
 from typing import NamedTuple, Optional, Tuple
 
 import torch
@@ -53,6 +54,9 @@ _SIGS = {
     "pl_matmul_fp8": (_INT, [_I64, _I64, _I64, _FP8, _FP8, _VP, _INT, _INT, _VP, _INT, _I64, _INT,
                              _VP, _SIZE, _VP]),
     "pl_matmul_fp8_workspace": (_SIZE, [_I64, _I64, _I64, _INT]),
+    "pl_linear_fp8": (_INT, [_VP, _INT, _I64, _I64, _I64, _I64, _FP8, _VP, _INT, _INT, _VP, _INT, _I64,
+                             _VP, _SIZE, _VP]),
+    "pl_linear_fp8_workspace": (_SIZE, [_I64, _I64, _I64, _INT, _INT]),
     "pl_last_error": (ctypes.c_char_p, []),
 }
 
@@ -82,6 +86,35 @@ def load_library(path: Optional[str] = None):
 def _check(rc: int) -> None:
     if rc != PS_OK:
         raise PSError(rc, load_library().pl_last_error().decode())
+
+
+_native = None   # the native calls' module; False: not built
+
+
+def _native_calls():
+    """The native side of the calls below, or False where it is not built (or built for
+    another torch): they then go through ctypes, which is slower."""
+    global _native
+    if _native is None:
+        load_library()
+        try:
+            from . import _learner
+            _native = _learner
+        except ImportError as e:
+            warnings.warn(f"a learner's calls go through ctypes, which is slower: {e}", RuntimeWarning,
+                          stacklevel=3)
+            _native = False
+    return _native
+
+
+def _done(result) -> bool:
+    """Whether a native call has made the call: it returns None for arguments that it does not
+    take, and the status of a call that was refused."""
+    if result is None:
+        return False
+    if type(result) is int:
+        _check(result)
+    return True
 
 
 _CODES = {torch.float32: PS_F32, torch.bfloat16: PS_BF16}
@@ -152,6 +185,11 @@ def embedding(ids, table, scale: float = 1.0, drop: Optional[Dropout] = None, dt
     An id outside the table (padding) gives zeros. Shape: that of `ids`, then the table's
     columns; of `dtype` (the table's by default), or written to `out`, a matrix of one row
     per id."""
+    native = _native or _native_calls()
+    if native:
+        done = native.embedding(ids, table, scale, drop, dtype or getattr(table, "dtype", None), out)
+        if _done(done):
+            return done
     ids, id_code = _ids(ids)
     src, src_code, src_ld = _matrix("table", table)
     tokens, (vocab, dim) = ids.numel(), table.shape
@@ -172,6 +210,11 @@ def embedding_grad(ids, grad, rows: int, scale: float = 1.0, drop: Optional[Drop
     """The gradient of `embedding` for its table of `rows` rows, from `grad`, that of its
     result (the shape of `ids`, then the columns): every row of it, of `dtype` or written to
     `out`; with `accumulate` added to what `out` holds. Equal calls give equal bits."""
+    native = _native or _native_calls()
+    if native:
+        done = native.embedding_grad(ids, grad, rows, scale, drop, dtype, out, accumulate)
+        if _done(done):
+            return done
     ids, id_code = _ids(ids)
     _on_device("grad", grad)
     tokens = ids.numel()
@@ -199,6 +242,11 @@ def dropout(x, drop: Dropout, out=None):
     """x with dropout, and of a gradient the backward pass. x is a matrix, or anything
     contiguous: then its last dimension is the columns and the others together the rows.
     `out` may be x."""
+    native = _native or _native_calls()
+    if native:
+        done = native.dropout(x, drop, out)
+        if _done(done):
+            return done
     _on_device("x", x)
     if out is not None and (out.shape != x.shape or out.dtype != x.dtype):
         raise ValueError(f"out of {tuple(out.shape)} {out.dtype} for x of {tuple(x.shape)} {x.dtype}")
@@ -228,7 +276,7 @@ class Fp8Matrix:
         blocks = -(-cols // 128)
         self.values = torch.empty((rows, 128 * blocks), dtype=torch.float8_e4m3fn, device=device)
         self.scales = torch.empty((-(-blocks // 4), rows), dtype=torch.int32, device=device)
-        self._as_parameter_ = pl_fp8(self.values.data_ptr(), self.scales.data_ptr())
+        self.parts = (self.values, self.scales, rows, cols)   # what the native calls take
 
     def exponents(self):
         """The exponent of every block: rows x blocks, int32."""
@@ -244,7 +292,7 @@ class Fp8Matrix:
 
 
 def _ref(q: Optional[Fp8Matrix]):
-    return None if q is None else ctypes.byref(q._as_parameter_)
+    return None if q is None else ctypes.byref(pl_fp8(q.values.data_ptr(), q.scales.data_ptr()))
 
 
 def _quantize(x, square: bool, plain: bool, transposed: bool):
@@ -270,10 +318,25 @@ def quantize_fp8_both(x, square: bool = False) -> Tuple[Fp8Matrix, Fp8Matrix]:
     return _quantize(x, square, True, True)
 
 
+def _bias(bias, n: int):
+    """(pointer, dtype code) of a bias of n values; none: (None, any code)."""
+    if bias is None:
+        return None, PS_F32
+    _on_device("bias", bias)
+    if bias.shape != (n,) or not bias.is_contiguous():
+        raise ValueError(f"bias: {n} contiguous values expected, not {tuple(bias.shape)}")
+    return bias.data_ptr(), _code(bias.dtype)
+
+
 def matmul_fp8(a: Fp8Matrix, b: Fp8Matrix, bias=None, relu: bool = False, dtype=torch.bfloat16,
                out=None, accumulate: bool = False):
     """a b^T (+ bias, then max(., 0) with relu), of `dtype` or written to `out`; with
     `accumulate` added to what `out` holds."""
+    native = _native or _native_calls()
+    if native:
+        done = native.product(a.parts, b.parts, bias, relu, dtype, out, accumulate)
+        if _done(done):
+            return done
     (m, k), (n, k2) = a.shape, b.shape
     if k != k2:
         raise ValueError(f"rows of {k} and of {k2} columns")
@@ -284,12 +347,7 @@ def matmul_fp8(a: Fp8Matrix, b: Fp8Matrix, bias=None, relu: bool = False, dtype=
     dst, code, ld = _matrix("out", out, m, n)
     for name, q in (("a", a), ("b", b)):
         _on_device(name, q.values)
-    bias_ptr, bias_code = None, PS_F32
-    if bias is not None:
-        _on_device("bias", bias)
-        if bias.shape != (n,) or not bias.is_contiguous():
-            raise ValueError(f"bias: {n} contiguous values expected, not {tuple(bias.shape)}")
-        bias_ptr, bias_code = bias.data_ptr(), _code(bias.dtype)
+    bias_ptr, bias_code = _bias(bias, n)
     L = load_library()
     need = L.pl_matmul_fp8_workspace(m, n, k, code)
     work = torch.empty(need, dtype=torch.uint8, device=out.device) if need else None
@@ -301,9 +359,24 @@ def matmul_fp8(a: Fp8Matrix, b: Fp8Matrix, bias=None, relu: bool = False, dtype=
 def linear_fp8(x, w: Fp8Matrix, bias=None, relu: bool = False, dtype=torch.bfloat16, out=None):
     """A fully connected layer: x w^T (+ bias, relu). x is quantised along its rows; w is the
     layer's weight (outputs x inputs), quantised (square) once per pull."""
-    if x.dim() != 2 or x.shape[1] != w.shape[1]:
-        raise ValueError(f"x of shape {tuple(x.shape)} for weights of {w.shape}")
-    return matmul_fp8(quantize_fp8(x), w, bias, relu, dtype, out)
+    native = _native or _native_calls()
+    if native:
+        done = native.linear(x, w.parts, bias, relu, dtype, out)
+        if _done(done):
+            return done
+    src, code, src_ld = _matrix("x", x, cols=w.shape[1])
+    m, (n, k) = x.shape[0], w.shape
+    _on_device("w", w.values)
+    if out is None:
+        out = torch.empty((m, n), dtype=dtype, device=x.device)
+    dst, dst_code, dst_ld = _matrix("out", out, m, n)
+    bias_ptr, bias_code = _bias(bias, n)
+    L = load_library()
+    need = L.pl_linear_fp8_workspace(m, n, k, code, dst_code)
+    work = torch.empty(need, dtype=torch.uint8, device=x.device)
+    _check(L.pl_linear_fp8(src, code, m, k, src_ld, n, _ref(w), bias_ptr, bias_code, int(relu), dst,
+                           dst_code, dst_ld, work.data_ptr(), need, _stream()))
+    return out
 
 
 def linear_fp8_grad(x, grad, w_t: Fp8Matrix, dtype=torch.bfloat16, weight_dtype=torch.float32,
@@ -312,6 +385,11 @@ def linear_fp8_grad(x, grad, w_t: Fp8Matrix, dtype=torch.bfloat16, weight_dtype=
     transposed weight, quantised (square); grad is quantised along its rows for the first
     product and along its columns, as x, for the second. `weight_out`, a view into the
     learner's gradient row, is written, or with `accumulate` added to."""
+    native = _native or _native_calls()
+    if native:
+        done = native.linear_grad(x, grad, w_t.parts, dtype, weight_dtype, x_out, weight_out, accumulate)
+        if _done(done):
+            return done
     if x.dim() != 2 or grad.dim() != 2 or x.shape[0] != grad.shape[0] or \
             w_t.shape != (x.shape[1], grad.shape[1]):
         raise ValueError(f"x of {tuple(x.shape)}, grad of {tuple(grad.shape)}, transposed weights "

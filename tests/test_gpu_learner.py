@@ -31,11 +31,18 @@ def torch():
     return torch
 
 
-@pytest.fixture(scope="module")
-def learner(torch):
+@pytest.fixture(scope="module", params=["native", "ctypes"])
+def learner(torch, request):
+    """The binding, with its native calls and without them."""
     from paper_1611_06213_amd import learner
     learner.load_library()
-    return learner
+    assert learner._native_calls(), "the native calls are not built"
+    if request.param == "ctypes":
+        native, learner._native = learner._native, False
+        learner._native_calls, keep = lambda: False, learner._native_calls
+    yield learner
+    if request.param == "ctypes":
+        learner._native, learner._native_calls = native, keep
 
 
 DT = {"f32": "float32", "bf16": "bfloat16", "i32": "int32", "i64": "int64"}
