@@ -56,6 +56,29 @@ __device__ __forceinline__ float load1(const void *p, int64_t i) {
     else return lo_bf16(static_cast<const uint16_t *>(p)[i]);
 }
 
+// The first `count` (1..8) of them; the others are 0.
+template <int DT>
+__device__ __forceinline__ Bits8<DT> load8_some(const void *p, int64_t i, int count) {
+    Bits8<DT> r = {};
+    if constexpr (DT == PS_F32) {
+        const float *q = static_cast<const float *>(p) + i;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (e < count) r.a[e] = q[e];
+            if (4 + e < count) r.b[e] = q[4 + e];
+        }
+    } else {
+        const uint16_t *q = static_cast<const uint16_t *>(p) + i;
+        uint32_t x[8] = {};
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e < count) x[e] = q[e];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r.a[e] = x[2 * e] | x[2 * e + 1] << 16;
+    }
+    return r;
+}
+
 template <int DT>
 __device__ __forceinline__ void widen8(float (&x)[8], const Bits8<DT> &r) {
     if constexpr (DT == PS_F32) {
@@ -80,16 +103,25 @@ __device__ __forceinline__ void store1(void *p, int64_t i, float x) {
     else static_cast<uint16_t *>(p)[i] = static_cast<uint16_t>(bf16x2_rne(x, 0.0f));
 }
 
-template <int DT>
+// NT: not to be kept in the caches.
+template <int DT, bool NT = false>
 __device__ __forceinline__ void store8(void *p, int64_t i, const float (&x)[8]) {
     if constexpr (DT == PS_F32) {
         f32x4_any *q = reinterpret_cast<f32x4_any *>(static_cast<float *>(p) + i);
-        q[0] = f32x4{x[0], x[1], x[2], x[3]};
-        q[1] = f32x4{x[4], x[5], x[6], x[7]};
+        const f32x4 a = {x[0], x[1], x[2], x[3]}, b = {x[4], x[5], x[6], x[7]};
+        if constexpr (NT) {
+            __builtin_nontemporal_store(a, q);
+            __builtin_nontemporal_store(b, q + 1);
+        } else {
+            q[0] = a;
+            q[1] = b;
+        }
     } else {
-        *reinterpret_cast<u32x4_any *>(static_cast<uint16_t *>(p) + i) =
-            u32x4{bf16x2_rne(x[0], x[1]), bf16x2_rne(x[2], x[3]), bf16x2_rne(x[4], x[5]),
-                  bf16x2_rne(x[6], x[7])};
+        u32x4_any *q = reinterpret_cast<u32x4_any *>(static_cast<uint16_t *>(p) + i);
+        const u32x4 a = {bf16x2_rne(x[0], x[1]), bf16x2_rne(x[2], x[3]), bf16x2_rne(x[4], x[5]),
+                         bf16x2_rne(x[6], x[7])};
+        if constexpr (NT) __builtin_nontemporal_store(a, q);
+        else *q = a;
     }
 }
 

@@ -12,8 +12,8 @@
 //         64k 4-byte ids are 256 KB per compute unit, and no pass over global memory
 //         depends on another workgroup. Classes are residues, not ranges, because texts'
 //         frequent ids are neighbours in many vocabularies.
-// sum     A row of at most kPiece tokens is summed by the threads that write it (eight
-//         columns each). The tokens of a longer row are cut into pieces of kPiece, whose
+// sum     A row of at most `piece` tokens is summed by the threads that write it (eight
+//         columns each). The tokens of a longer row are cut into pieces of that many, whose
 //         sums go to the workspace,
 // join    and are added up in order by a last kernel.
 //
@@ -23,10 +23,7 @@
 namespace gadei::learner {
 namespace {
 
-constexpr int kSortThreads = 1024;
-constexpr int kWaves = kSortThreads / 64;
 constexpr int kMaxLocal = 1024;   // ids of one class
-constexpr uint32_t kPiece = 64;   // tokens that one thread adds up
 
 struct Row {
     uint32_t begin, count;   // its part of the sorted list
@@ -38,6 +35,7 @@ struct Piece {
 
 struct Plan {
     int class_bits;
+    uint32_t piece;            // tokens that one thread adds up
     uint32_t classes, local;   // ids of a class, rounded up
     uint32_t pieces;           // room for
     size_t rows_at, perm_at, pieces_at, sums_at, bytes;
@@ -53,8 +51,12 @@ Plan make_plan(int64_t tokens, int64_t vocab, int64_t dim) {
     while (((vocab - 1) >> p.class_bits) >= kMaxLocal) ++p.class_bits;
     p.classes = 1u << p.class_bits;
     p.local = static_cast<uint32_t>((vocab + p.classes - 1) >> p.class_bits);
-    // a row with c > kPiece tokens has ceil(c / kPiece) < 2 c / kPiece pieces
-    p.pieces = static_cast<uint32_t>(2 * tokens / kPiece);
+    // One token after another is latency (with dropout 0.5 us each), and pieces are traffic of
+    // their own: 1824 tokens of 100 columns took 25 us with pieces of 8, 29 of 16, 32 of 32;
+    // 65536 of 4096 478, 419 and 400, and 402 with pieces of 64.
+    p.piece = tokens * dim <= (int64_t(1) << 22) ? 8 : 32;
+    // a row with c > piece tokens has ceil(c / piece) < 2 c / piece pieces
+    p.pieces = tokens <= p.piece ? 0 : static_cast<uint32_t>(2 * tokens / p.piece);
     p.rows_at = 0;
     p.perm_at = align256(sizeof(Row) * p.classes * size_t(p.local));
     p.pieces_at = p.perm_at + align256(sizeof(uint32_t) * size_t(tokens));
@@ -63,19 +65,13 @@ Plan make_plan(int64_t tokens, int64_t vocab, int64_t dim) {
     return p;
 }
 
-template <int IDT>
-__device__ __forceinline__ uint32_t load_id(const void *ids, uint32_t t, uint32_t vocab) {
-    // ids that are no token become 2^32 - 1 (vocab is at most 2^31)
-    if constexpr (IDT == PL_I32) {
-        const uint32_t id = static_cast<const uint32_t *>(ids)[t];
-        return id < vocab ? id : 0xffffffffu;
-    } else {
-        const uint64_t id = static_cast<const uint64_t *>(ids)[t];
-        return id < vocab ? static_cast<uint32_t>(id) : 0xffffffffu;
-    }
-}
+// Ids as unsigned numbers: negative ones are no tokens like all that are too large (vocab is
+// at most 2^31).
+template <int IDT> struct IdBits { using type = uint32_t; };
+template <> struct IdBits<PL_I64> { using type = uint64_t; };
 
-// Sum of x over the workgroup's lanes before this one; `total` is all of them.
+// Sum of x over the lanes of the workgroup's WAVES waves before this one; `total` is all of them.
+template <int WAVES>
 __device__ __forceinline__ uint32_t scan_exclusive(uint32_t x, uint32_t *wave_sums, uint32_t &total) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     uint32_t sum = x;
@@ -88,7 +84,7 @@ __device__ __forceinline__ uint32_t scan_exclusive(uint32_t x, uint32_t *wave_su
     __syncthreads();
     uint32_t before = 0, all = 0;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
+    for (int w = 0; w < WAVES; ++w) {
         const uint32_t y = wave_sums[w];
         if (w < wave) before += y;
         all += y;
@@ -98,133 +94,151 @@ __device__ __forceinline__ uint32_t scan_exclusive(uint32_t x, uint32_t *wave_su
     return before + sum - x;
 }
 
-constexpr int kAhead = 8;   // ids that a thread loads together
+constexpr int kAhead = 16;   // steps whose ids are loaded together
 
-template <int IDT>
-__global__ __launch_bounds__(kSortThreads) void sort_tokens(const void *ids, uint32_t tokens,
-                                                            uint32_t vocab, int class_bits,
-                                                            uint32_t local, Row *rows, uint32_t *perm,
-                                                            Piece *pieces) {
-    __shared__ uint32_t counts[kWaves][kMaxLocal];   // of each wave's part of the ids
-    __shared__ uint32_t wave_sums[kWaves];
-    const uint32_t mine = blockIdx.x, mask = (1u << class_bits) - 1;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    for (uint32_t i = threadIdx.x; i < kWaves * kMaxLocal; i += kSortThreads) (&counts[0][0])[i] = 0;
+// Calls f(step, id) for a wave's steps first, first + 1, .. of 64 ids, in order; ids past the last
+// are 2^32 - 1.
+template <int IDT, class F>
+__device__ __forceinline__ void each_id(const void *ids, uint32_t tokens, uint32_t first, uint32_t steps,
+                                        int lane, F f) {
+    for (uint32_t s = 0; s < steps; s += kAhead) {
+        const uint64_t t0 = 64ull * (first + s);
+        typename IdBits<IDT>::type raw[kAhead];
+        const auto *p = static_cast<const typename IdBits<IDT>::type *>(ids) + t0 + lane;
+        if (s + kAhead <= steps && t0 + 64 * kAhead <= tokens) {   // the same for the whole wave
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) raw[j] = p[64 * j];
+        } else {
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) {
+                raw[j] = ~typename IdBits<IDT>::type(0);
+                if (s + j < steps && t0 + 64 * j + lane < tokens) raw[j] = p[64 * j];
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) f(first + s + j, raw[j]);
+    }
+}
+
+// WAVES waves; a thread does the bookkeeping of kMaxLocal / (64 WAVES) ids.
+template <int IDT, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void sort_tokens(const void *ids, uint32_t tokens, uint32_t vocab,
+                                                          Plan p, Row *rows, uint32_t *perm,
+                                                          Piece *pieces) {
+    using Id = typename IdBits<IDT>::type;
+    constexpr int kEach = kMaxLocal / (64 * WAVES);
+    __shared__ uint32_t counts[WAVES][kMaxLocal];   // of each wave's part of the ids
+    __shared__ uint32_t wave_sums[WAVES];
+    const uint32_t mine = blockIdx.x, mask = p.classes - 1;
+    const int class_bits = p.class_bits;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    for (uint32_t l = threadIdx.x; l < p.local; l += 64 * WAVES)
+        for (int w = 0; w < WAVES; ++w) counts[w][l] = 0;
     __syncthreads();
 
-    // a wave's part of the ids: a run of whole steps of 64
-    const uint32_t steps = (tokens + 64 * kWaves - 1) / (64 * kWaves);
-    const uint64_t part = static_cast<uint64_t>(wave) * steps * 64;
+    // A wave's part of the ids is a run of whole steps of 64. Few instructions an id: what this
+    // kernel takes is the ids times them, on every compute unit.
+    const uint32_t steps = (tokens + 64 * WAVES - 1) / (64 * WAVES), first = wave * steps;
     uint32_t lower = 0;
-    for (uint32_t s = 0; s < steps; s += kAhead) {
-        uint32_t id[kAhead];
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-            const uint64_t t = part + (s + j) * 64ull + lane;
-            id[j] = s + j < steps && t < tokens
-                        ? load_id<IDT>(ids, static_cast<uint32_t>(t), vocab) : 0xffffffffu;
-        }
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-            if (id[j] == 0xffffffffu) continue;
-            const uint32_t c = id[j] & mask;
-            lower += c < mine;
-            if (c == mine) atomicAdd(&counts[wave][id[j] >> class_bits], 1u);
-        }
-    }
+    each_id<IDT>(ids, tokens, first, steps, lane, [&](uint32_t, Id id) {
+        const bool real = id < vocab;
+        const uint32_t low = static_cast<uint32_t>(id), c = low & mask;
+        lower += __popcll(__ballot(real && c < mine));   // in scalar registers
+        if (real && c == mine) atomicAdd(&counts[wave][low >> class_bits], 1u);
+    });
     __syncthreads();
 
     uint32_t base, total;
-    (void)scan_exclusive(lower, wave_sums, base);   // every class below comes before
-    // thread l: the class's id l. Its tokens by wave, then where each wave's begin
-    const uint32_t l = threadIdx.x;
-    uint32_t count = 0;
-    if (l < local)
-        for (int w = 0; w < kWaves; ++w) count += counts[w][l];
-    const uint32_t begin = base + scan_exclusive(count, wave_sums, total);
-    if (l < local) {
-        uint32_t at = begin;
-        for (int w = 0; w < kWaves; ++w) {
+    (void)scan_exclusive<WAVES>(lane == 0 ? lower : 0, wave_sums, base);   // every class below comes before
+    // tokens of a thread's ids, then where each wave's tokens of each id begin
+    const uint32_t l0 = threadIdx.x * kEach;
+    uint32_t count[kEach], all = 0, n[kEach], all_pieces = 0;
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+        count[e] = 0;
+        if (l0 + e < p.local)
+            for (int w = 0; w < WAVES; ++w) count[e] += counts[w][l0 + e];
+        all += count[e];
+        n[e] = count[e] > p.piece ? (count[e] + p.piece - 1) / p.piece : 0;
+        all_pieces += n[e];
+    }
+    uint32_t at = base + scan_exclusive<WAVES>(all, wave_sums, total);
+    // the pieces of long rows lie in the class's part of the list of pieces; the last class's
+    // goes on to the list's end: ids that are no token are in no class
+    uint32_t used = 0, slot = 0, from = 0;
+    if (p.pieces != 0) {
+        from = static_cast<uint32_t>(2ull * base / p.piece);
+        slot = from + scan_exclusive<WAVES>(all_pieces, wave_sums, used);
+    }
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+        const uint32_t l = l0 + e;
+        if (l >= p.local) break;
+        rows[static_cast<uint64_t>(mine) * p.local + l] = Row{at, count[e]};
+        for (uint32_t i = 0; i < n[e]; ++i) {
+            const uint32_t done = i * p.piece;
+            pieces[slot + i] = Piece{(l << class_bits) | mine, at + done,
+                                     count[e] - done < p.piece ? count[e] - done : p.piece, i == 0 ? n[e] : 0};
+        }
+        slot += n[e];
+        for (int w = 0; w < WAVES; ++w) {
             const uint32_t c = counts[w][l];
             counts[w][l] = at;
             at += c;
         }
-        rows[static_cast<uint64_t>(mine) * local + l] = Row{begin, count};
     }
-    // the pieces of long rows, in the class's part of the list of pieces
-    const uint32_t n = count > kPiece ? (count + kPiece - 1) / kPiece : 0;
-    const uint32_t from = static_cast<uint32_t>(2ull * base / kPiece);
-    // the last one goes on to the list's end: ids that are no token are in no class
-    const uint32_t to = static_cast<uint32_t>(
-        2ull * (mine == mask ? tokens : base + total) / kPiece);
-    uint32_t used;
-    const uint32_t slot = from + scan_exclusive(n, wave_sums, used);   // and orders counts[]
-    for (uint32_t i = 0; i < n; ++i) {
-        const uint32_t done = i * kPiece;
-        pieces[slot + i] = Piece{(l << class_bits) | mine, begin + done,
-                                 count - done < kPiece ? count - done : kPiece, i == 0 ? n : 0};
+    if (p.pieces != 0) {
+        const uint32_t to = mine == mask ? p.pieces : static_cast<uint32_t>(2ull * (base + total) / p.piece);
+        for (uint32_t i = from + used + threadIdx.x; i < to; i += 64 * WAVES) pieces[i] = Piece{0, 0, 0, 0};
     }
-    for (uint32_t i = from + used + threadIdx.x; i < to; i += kSortThreads)
-        pieces[i] = Piece{0, 0, 0, 0};
+    __syncthreads();
 
     // second reading: positions into their places, in order within a wave's part
     if (total == 0) return;
-    for (uint32_t s = 0; s < steps; s += kAhead) {
-        uint32_t id[kAhead];
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-            const uint64_t t = part + (s + j) * 64ull + lane;
-            id[j] = s + j < steps && t < tokens
-                        ? load_id<IDT>(ids, static_cast<uint32_t>(t), vocab) : 0xffffffffu;
+    each_id<IDT>(ids, tokens, first, steps, lane, [&](uint32_t step, Id id) {
+        const uint32_t low = static_cast<uint32_t>(id);
+        uint64_t todo = __ballot(id < vocab && (low & mask) == mine);
+        while (todo) {   // one id after the other: all its lanes at once
+            const uint32_t one = __builtin_amdgcn_readlane(low, __ffsll(static_cast<unsigned long long>(todo)) - 1);
+            const uint64_t lanes = todo & __ballot(low == one);
+            const uint32_t at = counts[wave][one >> class_bits];
+            if (lanes >> lane & 1)
+                perm[at + __popcll(lanes & ((1ull << lane) - 1))] = step * 64 + lane;
+            counts[wave][one >> class_bits] = at + __popcll(lanes);   // all lanes alike
+            todo &= ~lanes;
         }
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-            uint64_t todo = __ballot(id[j] != 0xffffffffu && (id[j] & mask) == mine);
-            while (todo) {   // one id after the other: all its lanes at once
-                const uint32_t one = __shfl(id[j], __ffsll(static_cast<unsigned long long>(todo)) - 1);
-                const bool same = id[j] == one;
-                const uint64_t lanes = __ballot(same);
-                const uint32_t at = counts[wave][one >> class_bits];
-                if (same)
-                    perm[at + __popcll(lanes & ((1ull << lane) - 1))] =
-                        static_cast<uint32_t>(part + (s + j) * 64ull + lane);
-                counts[wave][one >> class_bits] = at + __popcll(lanes);   // all lanes alike
-                todo &= ~lanes;
-            }
-        }
-    }
+    });
 }
 
 constexpr int kBlock = 256;
 
 // sum += drop(grad[t]) over `count` tokens of the sorted list, columns col .. col+7.
-template <int G, bool DROP>
+template <int G, bool DROP, int TOGETHER>
 __device__ __forceinline__ void add_tokens(float (&sum)[8], const GradArgs &a, const uint32_t *perm,
                                            uint32_t count, uint32_t group, int columns) {
-    constexpr uint32_t kTogether = 4;
     const int64_t col = 8ll * group;
-    for (uint32_t i = 0; i < count; i += kTogether) {
-        uint32_t t[kTogether];
-        float x[kTogether][8];
+    for (uint32_t i = 0; i < count; i += TOGETHER) {
+        uint32_t t[TOGETHER];
 #pragma unroll
-        for (uint32_t j = 0; j < kTogether; ++j) t[j] = perm[i + j < count ? i + j : i];
+        for (uint32_t j = 0; j < TOGETHER; ++j) t[j] = perm[i + j < count ? i + j : i];
+        Bits8<G> bits[TOGETHER] = {};
         if (columns == 8) {
-            Bits8<G> bits[kTogether];
 #pragma unroll
-            for (uint32_t j = 0; j < kTogether; ++j) bits[j] = load8<G>(a.grad, t[j] * a.grad_ld + col);
-#pragma unroll
-            for (uint32_t j = 0; j < kTogether; ++j) widen8<G>(x[j], bits[j]);
+            for (uint32_t j = 0; j < TOGETHER; ++j)
+                if (i + j < count) bits[j] = load8<G>(a.grad, t[j] * a.grad_ld + col);
         } else {
 #pragma unroll
-            for (uint32_t j = 0; j < kTogether; ++j)
-                load_some<G>(x[j], a.grad, t[j] * a.grad_ld + col, columns);
+            for (uint32_t j = 0; j < TOGETHER; ++j)
+                if (i + j < count) bits[j] = load8_some<G>(a.grad, t[j] * a.grad_ld + col, columns);
         }
 #pragma unroll
-        for (uint32_t j = 0; j < kTogether; ++j) {
+        for (uint32_t j = 0; j < TOGETHER; ++j) {
             if (i + j >= count) break;
-            if constexpr (DROP) drop8(x[j], 1.0f, group, t[j], a.drop);
+            float x[8];
+            widen8<G>(x, bits[j]);
+            if constexpr (DROP) drop8(x, 1.0f, group, t[j], a.drop);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sum[e] += x[j][e];
+            for (int e = 0; e < 8; ++e) sum[e] += x[e];
         }
     }
 }
@@ -243,12 +257,15 @@ __device__ __forceinline__ void write_row(const GradArgs &a, float (&sum)[8], ui
         sum[e] *= a.factor;
         if (a.accumulate) sum[e] += old[e];
     }
-    if (columns == 8) store8<OUT>(a.out, at, sum);
+    if (columns == 8) store8<OUT, true>(a.out, at, sum);
     else store_some<OUT>(a.out, at, sum, columns);
 }
 
-// Blocks of 2^lx groups of eight columns times 256 / 2^lx rows or pieces: first the pieces,
-// which take longest, then the rows.
+// Blocks of 2^lx groups of eight columns times 256 / 2^lx pieces, or that many times kRows rows:
+// first the pieces, which take longest, then the rows. Most rows have no token or one, so a
+// thread has the loads of kRows rows under way together.
+constexpr int kRows = 2;
+
 template <int G, int OUT, bool DROP>
 __global__ __launch_bounds__(kBlock) void sum_rows(GradArgs a, Plan p, int lx, uint32_t tiles_x,
                                                    uint32_t piece_blocks) {
@@ -258,53 +275,107 @@ __global__ __launch_bounds__(kBlock) void sum_rows(GradArgs a, Plan p, int lx, u
     const bool pieces = blockIdx.x < piece_blocks;
     const uint32_t block = pieces ? blockIdx.x : blockIdx.x - piece_blocks;
     const uint32_t group = ((block % tiles_x) << lx) + (threadIdx.x & ((1u << lx) - 1));
-    const uint64_t y = static_cast<uint64_t>(block / tiles_x) * ny + (threadIdx.x >> lx);
     const uint64_t col = 8ull * group;
     if (col >= a.dim) return;
     const int columns = a.dim - col < 8 ? static_cast<int>(a.dim - col) : 8;
-    float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     if (pieces) {
+        const uint64_t y = static_cast<uint64_t>(block / tiles_x) * ny + (threadIdx.x >> lx);
         if (y >= p.pieces) return;
         const Piece piece = reinterpret_cast<const Piece *>(ws + p.pieces_at)[y];
         if (piece.count == 0) return;
-        add_tokens<G, DROP>(sum, a, perm + piece.begin, piece.count, group, columns);
+        float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        add_tokens<G, DROP, 8>(sum, a, perm + piece.begin, piece.count, group, columns);
         float *sums = reinterpret_cast<float *>(static_cast<char *>(a.workspace) + p.sums_at);
         const int64_t at = static_cast<int64_t>(y * a.dim + col);
         if (columns == 8) store8<PS_F32>(sums, at, sum);
         else store_some<PS_F32>(sums, at, sum, columns);
         return;
     }
-    if (y >= a.vocab) return;
-    const uint32_t v = static_cast<uint32_t>(y);
-    const Row row = reinterpret_cast<const Row *>(ws + p.rows_at)[
-        static_cast<uint64_t>(v & (p.classes - 1)) * p.local + (v >> p.class_bits)];
-    if (row.count > kPiece || (row.count == 0 && a.accumulate)) return;
-    add_tokens<G, DROP>(sum, a, perm + row.begin, row.count, group, columns);
-    write_row<OUT>(a, sum, v, group, columns);
+    const uint64_t first = static_cast<uint64_t>(block / tiles_x) * ny * kRows + (threadIdx.x >> lx);
+    Row row[kRows];
+#pragma unroll
+    for (int u = 0; u < kRows; ++u) {
+        const uint64_t v = first + u * ny;
+        row[u] = Row{0, p.piece + 1};   // none, or one of pieces: written by the join
+        if (v < a.vocab)
+            row[u] = reinterpret_cast<const Row *>(ws + p.rows_at)[
+                (v & (p.classes - 1)) * p.local + (v >> p.class_bits)];
+    }
+    uint32_t t[kRows];
+    Bits8<G> bits[kRows] = {};
+#pragma unroll
+    for (int u = 0; u < kRows; ++u)
+        if (row[u].count - 1 < p.piece) t[u] = perm[row[u].begin];   // 1 .. piece tokens
+    if (columns == 8) {
+#pragma unroll
+        for (int u = 0; u < kRows; ++u)
+            if (row[u].count - 1 < p.piece) bits[u] = load8<G>(a.grad, t[u] * a.grad_ld + static_cast<int64_t>(col));
+    } else {
+#pragma unroll
+        for (int u = 0; u < kRows; ++u)
+            if (row[u].count - 1 < p.piece)
+                bits[u] = load8_some<G>(a.grad, t[u] * a.grad_ld + static_cast<int64_t>(col), columns);
+    }
+#pragma unroll
+    for (int u = 0; u < kRows; ++u) {
+        if (row[u].count > p.piece || (row[u].count == 0 && a.accumulate)) continue;
+        float sum[8];
+        widen8<G>(sum, bits[u]);
+        if (row[u].count != 0) {
+            if constexpr (DROP) drop8(sum, 1.0f, group, t[u], a.drop);
+            if (row[u].count > 1)
+                add_tokens<G, DROP, 4>(sum, a, perm + row[u].begin + 1, row[u].count - 1, group, columns);
+        }
+        write_row<OUT>(a, sum, static_cast<uint32_t>(first + u * ny), group, columns);
+    }
 }
 
-// The rows cut into pieces: their sums, in order.
+// The rows cut into pieces: their sums, in order. A workgroup takes kJoinSlots pieces of the list
+// after one another, most of which begin no row; where one does, the threads of one column share
+// its pieces, a run each, and thread 0's adds up the runs.
+constexpr int kJoinGroups = 16, kJoinRuns = kBlock / kJoinGroups;
+constexpr uint32_t kJoinSlots = 16;
+
 template <int OUT>
-__global__ __launch_bounds__(kBlock) void join_pieces(GradArgs a, Plan p, int lx, uint32_t tiles_x) {
+__global__ __launch_bounds__(kBlock) void join_pieces(GradArgs a, Plan p, uint32_t tiles_x) {
+    __shared__ float runs[kJoinRuns][kJoinGroups][8];
     const char *ws = static_cast<const char *>(a.workspace);
-    const uint32_t group = ((blockIdx.x % tiles_x) << lx) + (threadIdx.x & ((1u << lx) - 1));
-    const uint64_t y = static_cast<uint64_t>(blockIdx.x / tiles_x) * (kBlock >> lx) + (threadIdx.x >> lx);
-    const uint64_t col = 8ull * group;
-    if (col >= a.dim || y >= p.pieces) return;
-    const Piece piece = reinterpret_cast<const Piece *>(ws + p.pieces_at)[y];
-    if (piece.of == 0) return;
-    const int columns = a.dim - col < 8 ? static_cast<int>(a.dim - col) : 8;
+    const Piece *list = reinterpret_cast<const Piece *>(ws + p.pieces_at);
     const float *sums = reinterpret_cast<const float *>(ws + p.sums_at);
-    float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    for (uint32_t i = 0; i < piece.of; ++i) {
-        float x[8];
-        const int64_t at = static_cast<int64_t>((y + i) * a.dim + col);
-        if (columns == 8) widen8<PS_F32>(x, load8<PS_F32>(sums, at));
-        else load_some<PS_F32>(x, sums, at, columns);
+    const int g = threadIdx.x % kJoinGroups, run = threadIdx.x / kJoinGroups;
+    const uint32_t group = blockIdx.x % tiles_x * kJoinGroups + g;
+    const uint64_t col = 8ull * group;
+    const int columns = col >= a.dim ? 0 : a.dim - col < 8 ? static_cast<int>(a.dim - col) : 8;
+    const uint32_t slot = blockIdx.x / tiles_x * kJoinSlots;
+    for (uint32_t y = slot; y < slot + kJoinSlots && y < p.pieces; ++y) {
+        const uint32_t of = list[y].of;   // the same for the whole workgroup
+        if (of == 0) continue;
+        const uint32_t each = (of + kJoinRuns - 1) / kJoinRuns;
+        const uint32_t from = min(run * each, of), to = min(from + each, of);
+        float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        if (columns != 0) {
+#pragma unroll 4
+            for (uint32_t i = from; i < to; ++i) {
+                float x[8];
+                const int64_t at = static_cast<int64_t>((y + i) * a.dim + col);
+                if (columns == 8) widen8<PS_F32>(x, load8<PS_F32>(sums, at));
+                else load_some<PS_F32>(x, sums, at, columns);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sum[e] += x[e];
+                for (int e = 0; e < 8; ++e) sum[e] += x[e];
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) runs[run][g][e] = sum[e];
+        __syncthreads();
+        if (run == 0 && columns != 0) {
+            const int used = static_cast<int>((of + each - 1) / each);
+            for (int r = 1; r < used; ++r)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum[e] += runs[r][g][e];
+            write_row<OUT>(a, sum, list[y].row, group, columns);
+        }
+        __syncthreads();
     }
-    write_row<OUT>(a, sum, piece.row, group, columns);
 }
 
 template <int G, int OUT>
@@ -315,7 +386,8 @@ hipError_t launch_sums(const GradArgs &a, const Plan &p, hipStream_t s) {
     const uint32_t tiles_x = static_cast<uint32_t>((groups + (1ull << lx) - 1) >> lx);
     const uint32_t ny = kBlock >> lx;
     const uint64_t piece_blocks = static_cast<uint64_t>((p.pieces + ny - 1) / ny) * tiles_x;
-    const uint64_t blocks = piece_blocks + (static_cast<uint64_t>(a.vocab) + ny - 1) / ny * tiles_x;
+    const uint64_t per = static_cast<uint64_t>(ny) * kRows;
+    const uint64_t blocks = piece_blocks + (a.vocab + per - 1) / per * tiles_x;
     if (blocks > 0xffffffffull / kBlock) return hipErrorInvalidConfiguration;
     const uint32_t pb = static_cast<uint32_t>(piece_blocks);
     if (a.drop.drop != 0)
@@ -323,8 +395,9 @@ hipError_t launch_sums(const GradArgs &a, const Plan &p, hipStream_t s) {
     else
         sum_rows<G, OUT, false><<<static_cast<uint32_t>(blocks), kBlock, 0, s>>>(a, p, lx, tiles_x, pb);
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || pb == 0) return e;
-    join_pieces<OUT><<<pb, kBlock, 0, s>>>(a, p, lx, tiles_x);
+    if (e != hipSuccess || p.pieces == 0) return e;
+    const uint32_t join_x = static_cast<uint32_t>((groups + kJoinGroups - 1) / kJoinGroups);
+    join_pieces<OUT><<<(p.pieces + kJoinSlots - 1) / kJoinSlots * join_x, kBlock, 0, s>>>(a, p, join_x);
     return hipGetLastError();
 }
 
@@ -341,12 +414,16 @@ hipError_t launch_grad(const GradArgs &a, int id_type, int grad_dtype, int out_d
     Row *rows = reinterpret_cast<Row *>(ws + p.rows_at);
     uint32_t *perm = reinterpret_cast<uint32_t *>(ws + p.perm_at);
     Piece *pieces = reinterpret_cast<Piece *>(ws + p.pieces_at);
-    if (id_type == PL_I32)
-        sort_tokens<PL_I32><<<p.classes, kSortThreads, 0, s>>>(a.ids, a.tokens, a.vocab, p.class_bits,
-                                                               p.local, rows, perm, pieces);
-    else
-        sort_tokens<PL_I64><<<p.classes, kSortThreads, 0, s>>>(a.ids, a.tokens, a.vocab, p.class_bits,
-                                                               p.local, rows, perm, pieces);
+    // more waves share the ids of a workgroup, and take longer to start and to be brought together:
+    // 1824 ids PLACEHOLDER
+    const bool few = a.tokens <= 4096;
+    if (id_type == PL_I32) {
+        if (few) sort_tokens<PL_I32, 4><<<p.classes, 256, 0, s>>>(a.ids, a.tokens, a.vocab, p, rows, perm, pieces);
+        else sort_tokens<PL_I32, 16><<<p.classes, 1024, 0, s>>>(a.ids, a.tokens, a.vocab, p, rows, perm, pieces);
+    } else {
+        if (few) sort_tokens<PL_I64, 4><<<p.classes, 256, 0, s>>>(a.ids, a.tokens, a.vocab, p, rows, perm, pieces);
+        else sort_tokens<PL_I64, 16><<<p.classes, 1024, 0, s>>>(a.ids, a.tokens, a.vocab, p, rows, perm, pieces);
+    }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     if (grad_dtype == PS_F32)
