@@ -308,6 +308,7 @@ size_t pl_linear_fp8_workspace(int64_t m, int64_t n, int64_t k, int dtype, int o
     if (m < 0 || m >= kMax / 2 || n < 0 || n >= kMax / 2 || k < 0 || k > (1 << 22) ||
         !is_dtype(dtype) || !is_dtype(out_dtype))
         return 0;
+    if (converts(m, k)) return 0;
     return align256(pl_fp8_values_bytes(m, k)) + align256(pl_fp8_scales_bytes(m, k)) +
            matmul_workspace(m, n, k, out_dtype);
 }
@@ -333,6 +334,23 @@ int pl_linear_fp8(const void *x, int dtype, int64_t m, int64_t k, int64_t ld, in
     if (int rc = plain("workspace", workspace, need, 16, &in[4])) return rc;
     if (int rc = apart(o, in, 5)) return rc;
     if (int rc = apart(in[4], in, 4)) return rc;
+    if (converts(m, k)) {
+        MatmulArgs g{};
+        g.b = static_cast<const uint8_t *>(w->values);
+        g.sb = w->scales;
+        g.bias = bias;
+        g.bias_bf16 = bias != nullptr && bias_dtype == PS_BF16;
+        g.out = out;
+        g.out_ld = out_ld;
+        g.m = static_cast<uint32_t>(m);
+        g.n = static_cast<uint32_t>(n);
+        g.k = static_cast<uint32_t>(k);
+        g.relu = relu != 0;
+        g.x = x;
+        g.x_ld = ld;
+        return launched(launch_convert_matmul(g, dtype, out_dtype, static_cast<hipStream_t>(stream)),
+                        "pl_linear_fp8");
+    }
     char *ws = static_cast<char *>(workspace);
     const size_t values = align256(pl_fp8_values_bytes(m, k)), scales = align256(pl_fp8_scales_bytes(m, k));
     const pl_fp8 q = {ws, reinterpret_cast<uint32_t *>(ws + values)};

@@ -74,8 +74,14 @@ struct MatmulArgs {
     int relu;
     int accumulate;
     float *partial;         // workspace
+    const void *x;          // launch_convert_matmul: what a is made from
+    int64_t x_ld;
 };
 size_t matmul_workspace(int64_t m, int64_t n, int64_t k, int out_dtype);
 hipError_t launch_matmul(const MatmulArgs &a, int out_dtype, hipStream_t s);
+// Whether the product of m x k numbers not yet in 8-bit form is one launch, which needs no a, sa or
+// workspace.
+bool converts(int64_t m, int64_t k);
+hipError_t launch_convert_matmul(const MatmulArgs &a, int x_dtype, int out_dtype, hipStream_t s);
 
 }  // namespace gadei::learner

@@ -19,12 +19,12 @@
 // matter as long as both operands agree, since a block's columns share their scale.
 //
 // Two kernels: `tiles` stages tiles of both operands in LDS, for many rows of a; `slim`, for
-// at most 64 rows of a, reads b, by far the larger operand, straight into registers.
+// at most 32 rows of a, reads b, by far the larger operand, straight into registers.
 // Where there are too few tiles to fill the card, k is split over workgroups; the parts'
 // sums go to the workspace and `join` adds them up in order.
 #include <algorithm>
 
-#include "pl_device.h"
+#include "pl_fp8.h"
 
 namespace gadei::learner {
 namespace {
@@ -133,6 +133,9 @@ struct Buffer {
     __device__ __forceinline__ void to_lds(uint8_t *to, uint32_t lane, uint32_t shared) const {
         __builtin_amdgcn_raw_ptr_buffer_load_lds(
             rsrc, (__attribute__((address_space(3))) void *)to, 16, lane, shared, 0, 0);
+    }
+    __device__ __forceinline__ i32x4 sixteen(uint32_t lane, uint32_t shared) const {
+        return __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, lane, shared, 0));
     }
     __device__ __forceinline__ uint32_t word(uint32_t lane) const {
         return __builtin_amdgcn_raw_buffer_load_b32(rsrc, lane, 0, 0);
@@ -436,70 +439,116 @@ __global__ __launch_bounds__(256) void tiles(MatmulArgs g, Split sp) {
 
 // -------------------------------------------------------------------- slim
 
-// 16 rows of b (columns of out) and up to 16 FM rows of a; the four waves of a workgroup take
-// the blocks of its part of k in turn and add up their sums in LDS.
-constexpr int kSlimWaves = 4;
+// 16 rows of b (columns of out) a workgroup and up to 16 FM rows of a: bound by reading b, once,
+// straight into registers. The waves take the blocks of k in turn, the loads of several blocks under
+// way in each, and add up their sums in LDS, in order: no part of k goes through memory.
+//
+// X >= 0: a is not in 8-bit form yet but given as x. Every workgroup converts all of it, into LDS,
+// while its first rows of b are under way: for few rows that is less than a launch.
+constexpr int kGiven = -1;
+template <int FM>
+constexpr int kAhead = FM == 1 ? 4 : 2;   // blocks whose loads are issued together
 
-template <int FM, int OUT>
-__global__ __launch_bounds__(64 * kSlimWaves) void slim(MatmulArgs g, Split sp) {
-    __shared__ f32x4 sums[kSlimWaves][FM][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+template <int FM, int OUT, int X, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void slim(MatmulArgs g) {
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+    constexpr int A = kAhead<FM>;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int q = lane >> 4, r16 = lane & 15;
-    const uint32_t n0 = blockIdx.x % sp.tiles_n * 16, part = blockIdx.x / sp.tiles_n;
+    const uint32_t n0 = blockIdx.x * 16;
     const uint32_t blocks = (g.k + 127) / 128, ld = blocks * 128;
-    const uint32_t first = part * sp.steps, last = min(blocks, first + sp.steps);
-    const uint32_t rb = min(n0 + r16, g.n - 1);
-    const uint8_t *pb = g.b + static_cast<uint64_t>(rb) * ld + 32 * q;
-    const uint8_t *pa[FM];
-    uint32_t ra[FM];
+    const uint32_t pitch = ld + 16;   // of x's rows in LDS: in different banks
+    uint8_t *const bytes = lds + g.m * pitch;   // x's scales: `blocks` of a row
+    // rows past a matrix, and blocks past the last, read as zeros
+    const Buffer rows_b(g.b + static_cast<uint64_t>(n0) * ld, min(g.n - n0, 16u) * ld);
+    const Buffer rows_a(g.a, g.m * ld);
+    const uint32_t from = r16 * ld + 32 * q;
+
+    struct Ahead {
+        i32x4 b[A][2], a[A][FM][2];
+        uint32_t sb[A], sa[A][FM];
+    } t;
+    auto load = [&](uint32_t block) {
 #pragma unroll
-    for (int i = 0; i < FM; ++i) {
-        ra[i] = min(16u * i + r16, g.m - 1);
-        pa[i] = g.a + static_cast<uint64_t>(ra[i]) * ld + 32 * q;
-    }
-    f32x4 acc[FM] = {};
-    constexpr int kAhead = 4;   // blocks whose loads are issued together
-    for (uint32_t block = first + wave; block < last; block += kSlimWaves * kAhead) {
-        i32x4 b[kAhead][2], a[kAhead][FM][2];
-        uint32_t sb[kAhead], sa[kAhead][FM];
+        for (int j = 0; j < A; ++j) {
+            const uint32_t at = block + j * WAVES;
+            const bool in = at < blocks;
+            const uint32_t lanes = in ? from : Buffer::kOutside;
+            t.b[j][0] = rows_b.sixteen(lanes, at * 128);
+            t.b[j][1] = rows_b.sixteen(lanes, at * 128 + 16);
+            const uint32_t group = in ? at >> 2 : 0;
+            t.sb[j] = Buffer(g.sb + static_cast<uint64_t>(group) * g.n, g.n * 4).word((n0 + r16) * 4);
+            if constexpr (X == kGiven) {
+                const Buffer words(g.sa + static_cast<uint64_t>(group) * g.m, g.m * 4);
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-            const uint32_t at = min(block + j * kSlimWaves, last - 1);
-            const i32x4 *p = reinterpret_cast<const i32x4 *>(pb + static_cast<uint64_t>(at) * 128);
-            b[j][0] = __builtin_nontemporal_load(p);
-            b[j][1] = __builtin_nontemporal_load(p + 1);
-            sb[j] = g.sb[static_cast<uint64_t>(at >> 2) * g.n + rb] >> (8 * (at & 3));
-#pragma unroll
-            for (int i = 0; i < FM; ++i) {
-                const i32x4 *pi = reinterpret_cast<const i32x4 *>(pa[i] + static_cast<uint64_t>(at) * 128);
-                a[j][i][0] = pi[0];
-                a[j][i][1] = pi[1];
-                sa[j][i] = g.sa[static_cast<uint64_t>(at >> 2) * g.m + ra[i]] >> (8 * (at & 3));
+                for (int i = 0; i < FM; ++i) {
+                    t.a[j][i][0] = rows_a.sixteen(lanes, 16 * i * ld + at * 128);
+                    t.a[j][i][1] = rows_a.sixteen(lanes, 16 * i * ld + at * 128 + 16);
+                    t.sa[j][i] = words.word((16 * i + r16) * 4);
+                }
             }
         }
+        __builtin_amdgcn_sched_barrier(0);   // all under way before the first is used
+    };
+    load(wave);
+    if constexpr (X != kGiven) {
+        constexpr int kTogether = 4;
+        const uint32_t group = threadIdx.x >> 4, e = threadIdx.x & 15;   // sixteen lanes a block
+        for (uint32_t i0 = group; i0 < g.m * blocks; i0 += kTogether * 4 * WAVES) {
+            Bits8<X> x[kTogether];
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-            if (block + j * kSlimWaves >= last) break;
+            for (int j = 0; j < kTogether; ++j) {
+                const uint32_t i = i0 + j * 4 * WAVES, m = i / blocks, col = i % blocks * 128 + 8 * e;
+                const int count = m >= g.m || col >= g.k ? 0 : g.k - col >= 8 ? 8 : static_cast<int>(g.k - col);
+                const int64_t at = m * g.x_ld + col;
+                if (count == 8) x[j] = load8<X>(g.x, at);
+                else x[j] = load8_some<X>(g.x, at, count);
+            }
+#pragma unroll
+            for (int j = 0; j < kTogether; ++j) {
+                const uint32_t i = i0 + j * 4 * WAVES, m = i / blocks, col = i % blocks * 128 + 8 * e;
+                const uint32_t byte = scale_byte(most_of_block(most8<X>(x[j])));
+                if (m >= g.m) break;
+                *reinterpret_cast<u32x2 *>(lds + m * pitch + col) =
+                    u32x2{four(x[j], 0, as_scale(byte)), four(x[j], 1, as_scale(byte))};
+                if (e == 0) bytes[i] = static_cast<uint8_t>(byte);
+            }
+        }
+        __syncthreads();
+    }
+    const uint32_t rx = min(uint32_t(r16), g.m - 1);
+    f32x4 acc[FM] = {};
+    for (uint32_t block = wave; block < blocks; block += WAVES * A) {
+#pragma unroll
+        for (int j = 0; j < A; ++j) {
+            const uint32_t at = block + j * WAVES;
+            if (at >= blocks) break;
             Operand<OUT == PS_F32> fb, fa;
-            fb.set(b[j][0], b[j][1], sb[j]);
+            fb.set(t.b[j][0], t.b[j][1], t.sb[j] >> (8 * (at & 3)));
 #pragma unroll
             for (int i = 0; i < FM; ++i) {
-                fa.set(a[j][i][0], a[j][i][1], sa[j][i]);
+                if constexpr (X == kGiven) {
+                    fa.set(t.a[j][i][0], t.a[j][i][1], t.sa[j][i] >> (8 * (at & 3)));
+                } else {
+                    const i32x4 *p = reinterpret_cast<const i32x4 *>(lds + rx * pitch + at * 128 + 32 * q);
+                    fa.set(p[0], p[1], bytes[rx * blocks + at]);
+                }
                 acc[i] = mfma(fb, fa, acc[i]);
             }
         }
+        if (block + WAVES * A < blocks) load(block + WAVES * A);
     }
+    f32x4 *sums = reinterpret_cast<f32x4 *>(lds);
+    if constexpr (X != kGiven) __syncthreads();   // x is read no more
 #pragma unroll
-    for (int i = 0; i < FM; ++i) sums[wave][i][lane] = acc[i];
+    for (int i = 0; i < FM; ++i) sums[(wave * FM + i) * 64 + lane] = acc[i];
     __syncthreads();
-    for (int i = wave; i < FM; i += kSlimWaves) {
-        f32x4 v = sums[0][i][lane];
+    if (wave < FM) {
+        f32x4 v = {0, 0, 0, 0};
 #pragma unroll
-        for (int w = 1; w < kSlimWaves; ++w) v += sums[w][i][lane];
-        const uint32_t m = 16 * i + r16, n = n0 + 4 * q;
-        if (m >= g.m || n >= g.n) continue;
-        if (sp.parts == 1) finish<OUT>(g, v, m, n);
-        else keep(g, v, part, m, n);
+        for (int w = 0; w < WAVES; ++w) v += sums[(w * FM + wave) * 64 + lane];
+        const uint32_t m = 16 * wave + r16, n = n0 + 4 * q;
+        if (m < g.m && n < g.n) finish<OUT>(g, v, m, n);
     }
 }
 
@@ -514,6 +563,7 @@ __global__ __launch_bounds__(256) void join(MatmulArgs g, uint32_t parts) {
     const f32x4 *p = reinterpret_cast<const f32x4 *>(g.partial) + i;
     const uint64_t stride = static_cast<uint64_t>(g.m) * fours;
     f32x4 v = {0, 0, 0, 0};
+#pragma unroll 8
     for (uint32_t s = 0; s < parts; ++s) v += p[s * stride];
     finish<OUT>(g, v, m, n);
 }
@@ -530,59 +580,67 @@ __global__ __launch_bounds__(256) void empty(MatmulArgs g) {
 
 // ---------------------------------------------------------------- choices
 
-constexpr uint32_t kSlimRows = 64;
+// 32 x 4096 x 9216 22 us with either kernel, 64 x 4096 x 9216 25 with tiles and 31 with slim
+constexpr uint32_t kSlimRows = 32;
 constexpr uint32_t kMinSteps = 4;   // blocks of k that a part has at least
+constexpr uint32_t kLds = 65536;    // what a workgroup may ask for at its launch
 
 struct Choice {
     int bm, bn;
     Split split;
 };
 
+// For more than kSlimRows rows of a.
 Choice choose(uint64_t m, uint64_t n, uint64_t k, bool wide) {
     Choice c{};
     const uint64_t blocks = (k + 127) / 128;
-    if (m <= kSlimRows) {
-        c.bm = static_cast<int>(m);
-        c.bn = 16;
-    } else if ((m + 255) / 256 * ((n + 255) / 256) * (wide ? 2 : 1) >= kCus) {
+    if ((m + 255) / 256 * ((n + 255) / 256) * (wide ? 2 : 1) >= kCus) {
         c.bm = 256;
         c.bn = wide ? 128 : 256;
     } else {
         c.bm = c.bn = 128;
     }
-    c.split.tiles_m = m <= kSlimRows ? 1 : static_cast<uint32_t>((m + c.bm - 1) / c.bm);
+    c.split.tiles_m = static_cast<uint32_t>((m + c.bm - 1) / c.bm);
     c.split.tiles_n = static_cast<uint32_t>((n + c.bn - 1) / c.bn);
     // parts of k until every compute unit has a workgroup
     const uint64_t tiles = static_cast<uint64_t>(c.split.tiles_m) * c.split.tiles_n;
-    const uint64_t wanted = m <= kSlimRows ? 2 * kCus : kCus;
-    uint64_t parts = tiles == 0 ? 1 : wanted / tiles;
-    parts = parts < 1 ? 1 : parts;
-    const uint64_t least = m <= kSlimRows ? kMinSteps * kSlimWaves : kMinSteps;
-    if (parts > blocks / least) parts = blocks / least < 1 ? 1 : blocks / least;
+    uint64_t parts = std::max<uint64_t>(1, kCus / tiles);
+    parts = std::min(parts, std::max<uint64_t>(1, blocks / kMinSteps));
     c.split.steps = static_cast<uint32_t>((blocks + parts - 1) / parts);
-    if (c.split.steps == 0) c.split.steps = 1;
+    if (parts > 1) c.split.steps += c.split.steps & 1;   // blocks go in twos
     c.split.parts = static_cast<uint32_t>((blocks + c.split.steps - 1) / c.split.steps);
-    if (c.split.parts < 1) c.split.parts = 1;
     return c;
+}
+
+template <int FM, int OUT, int X>
+hipError_t launch_slim(const MatmulArgs &g, hipStream_t s) {
+    const uint32_t blocks = (g.k + 127) / 128;
+    const uint32_t x = X == kGiven ? 0 : g.m * (blocks * 128 + 16) + g.m * blocks;
+    constexpr uint32_t kSums = FM * 64 * sizeof(f32x4);   // of a wave
+    // Sixteen waves have more of a long row under way, eight leave room for a second workgroup on
+    // the compute unit where rows are many and short: 1 x 4096 x 25088 23.0 us with 16, 24.6 with 8;
+    // 1 x 25088 x 4096 31.7 and 25.0.
+    if (blocks > 64) slim<FM, OUT, X, 16><<<(g.n + 15) / 16, 1024, std::max(16 * kSums, x), s>>>(g);
+    else slim<FM, OUT, X, 8><<<(g.n + 15) / 16, 512, std::max(8 * kSums, x), s>>>(g);
+    return hipGetLastError();
 }
 
 template <int OUT>
 hipError_t launch(const MatmulArgs &g, hipStream_t s) {
     const uint64_t fours = static_cast<uint64_t>(g.m) * ((g.n + 3) / 4);
     const uint64_t join_blocks = (fours + 255) / 256;
-    const Choice c = choose(g.m, g.n, g.k, OUT == PS_F32);
-    const uint64_t grid = static_cast<uint64_t>(c.split.tiles_m) * c.split.tiles_n * c.split.parts;
-    if (join_blocks > 0xffffffffull / 256 || grid > 0xffffffffull / 512)
-        return hipErrorInvalidConfiguration;
-    const uint32_t blocks = static_cast<uint32_t>(grid);
+    if (join_blocks > 0xffffffffull / 256) return hipErrorInvalidConfiguration;
     if (g.k == 0) {
         empty<OUT><<<static_cast<uint32_t>(join_blocks), 256, 0, s>>>(g);
         return hipGetLastError();
     }
-    if (g.m <= 16) slim<1, OUT><<<blocks, 64 * kSlimWaves, 0, s>>>(g, c.split);
-    else if (g.m <= 32) slim<2, OUT><<<blocks, 64 * kSlimWaves, 0, s>>>(g, c.split);
-    else if (g.m <= kSlimRows) slim<4, OUT><<<blocks, 64 * kSlimWaves, 0, s>>>(g, c.split);
-    else if (c.bm == 128) tiles<2, 2, OUT><<<std::min(blocks, 2u * kCus), 256, 0, s>>>(g, c.split);
+    if (g.m <= 16) return launch_slim<1, OUT, kGiven>(g, s);
+    if (g.m <= kSlimRows) return launch_slim<2, OUT, kGiven>(g, s);
+    const Choice c = choose(g.m, g.n, g.k, OUT == PS_F32);
+    const uint64_t units = static_cast<uint64_t>(c.split.tiles_m) * c.split.tiles_n * c.split.parts;
+    if (units > 0xffffffffull / 2) return hipErrorInvalidConfiguration;
+    const uint32_t blocks = static_cast<uint32_t>(units);
+    if (c.bm == 128) tiles<2, 2, OUT><<<std::min(blocks, 2u * kCus), 256, 0, s>>>(g, c.split);
     else tiles<4, OUT == PS_F32 ? 2 : 4, OUT><<<std::min(blocks, 1u * kCus), 256, 0, s>>>(g, c.split);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || c.split.parts == 1) return e;
@@ -593,14 +651,25 @@ hipError_t launch(const MatmulArgs &g, hipStream_t s) {
 }  // namespace
 
 size_t matmul_workspace(int64_t m, int64_t n, int64_t k, int out_dtype) {
-    if (m == 0 || n == 0 || k == 0) return 0;
+    if (m <= kSlimRows || n == 0 || k == 0) return 0;
     const Choice c = choose(m, n, k, out_dtype == PS_F32);
     if (c.split.parts == 1) return 0;
     return sizeof(float) * size_t(c.split.parts) * size_t(m) * ((size_t(n) + 3) & ~size_t(3));
 }
 
+bool converts(int64_t m, int64_t k) {
+    // a row's bytes in LDS, its scales and the padding: PLACEHOLDER measured
+    return m <= 16 && k > 0 && m * ((k + 127) / 128 * 129 + 16) <= kLds;
+}
+
 hipError_t launch_matmul(const MatmulArgs &a, int out_dtype, hipStream_t s) {
     return out_dtype == PS_F32 ? launch<PS_F32>(a, s) : launch<PS_BF16>(a, s);
+}
+
+hipError_t launch_convert_matmul(const MatmulArgs &a, int x_dtype, int out_dtype, hipStream_t s) {
+    if (out_dtype == PS_F32)
+        return x_dtype == PS_F32 ? launch_slim<1, PS_F32, PS_F32>(a, s) : launch_slim<1, PS_F32, PS_BF16>(a, s);
+    return x_dtype == PS_F32 ? launch_slim<1, PS_BF16, PS_F32>(a, s) : launch_slim<1, PS_BF16, PS_BF16>(a, s);
 }
 
 }  // namespace gadei::learner

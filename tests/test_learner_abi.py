@@ -163,9 +163,9 @@ def test_fp8_refuses(lib):
     refused(lib, matmul(out=P), "overlaps a")
     refused(lib, matmul(out=3 * P + 64), "overlaps b")
     refused(lib, matmul(bias=7 * P, out=7 * P), "overlaps bias")
-    need = lib.pl_matmul_fp8_workspace(8, 8, 100_000, 1)
+    need = lib.pl_matmul_fp8_workspace(100, 8, 100_000, 1)
     assert need > 0   # few tiles: k is split
-    refused(lib, matmul(k=100_000, b=fp8(8 * P, 16 * P), size=need - 1), "needed", ps.PS_ENOMEM)
+    refused(lib, matmul(m=100, k=100_000, a=fp8(8 * P, 24 * P), b=fp8(32 * P, 48 * P), size=need - 1), "needed", ps.PS_ENOMEM)
     assert lib.pl_matmul_fp8_workspace(8192, 8192, 8192, 1) == 0
     assert matmul(m=0) == 0 and matmul(n=0) == 0
 
