@@ -21,6 +21,9 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 template <int DT>
 constexpr int kBytes = DT == PS_F32 ? 4 : 2;
 
+// Bytes of a result that are left in the caches (256 MB of last level) for whoever reads it.
+constexpr uint64_t kCached = 64ull << 20;
+
 // bf16 -> fp32 is exact: the bf16 bits are the upper half of the fp32 bits
 __device__ __forceinline__ float lo_bf16(uint32_t u) { return __uint_as_float(u << 16); }
 __device__ __forceinline__ float hi_bf16(uint32_t u) { return __uint_as_float(u & 0xffff0000u); }

@@ -583,7 +583,6 @@ __global__ __launch_bounds__(256) void empty(MatmulArgs g) {
 // 32 x 4096 x 9216 22 us with either kernel, 64 x 4096 x 9216 25 with tiles and 31 with slim
 constexpr uint32_t kSlimRows = 32;
 constexpr uint32_t kMinSteps = 4;   // blocks of k that a part has at least
-constexpr uint32_t kLds = 65536;    // what a workgroup may ask for at its launch
 
 struct Choice {
     int bm, bn;
@@ -658,8 +657,10 @@ size_t matmul_workspace(int64_t m, int64_t n, int64_t k, int out_dtype) {
 }
 
 bool converts(int64_t m, int64_t k) {
-    // a row's bytes in LDS, its scales and the padding: PLACEHOLDER measured
-    return m <= 16 && k > 0 && m * ((k + 127) / 128 * 129 + 16) <= kLds;
+    // A row's bytes in LDS, its scales and the padding. Every workgroup converts all of x: 1 x 4096
+    // (4 KB) took 7.5 us, 9.0 in two launches, 2 x 25088 (50 KB) 24.6 and 25.3, but 16 x 4096 (66 KB)
+    // 13.2 and 10.8, all with 4096 columns of out.
+    return m <= 16 && k > 0 && m * ((k + 127) / 128 * 129 + 16) <= 51200;
 }
 
 hipError_t launch_matmul(const MatmulArgs &a, int out_dtype, hipStream_t s) {
