@@ -17,6 +17,9 @@
 //         sums go to the workspace,
 // join    and are added up in order by a last kernel.
 //
+// Where there are few tokens, launches and latencies take longest, and one kernel does all of it
+// (sum_few).
+//
 // Bound by memory: grad is read once and out written once, rows without tokens included.
 #include "pl_device.h"
 
@@ -379,6 +382,145 @@ __global__ __launch_bounds__(kBlock) void join_pieces(GradArgs a, Plan p, uint32
     }
 }
 
+// Few tokens and narrow rows: everything in one launch. A workgroup takes kSmallRows rows of the
+// table and up to 128 columns; it reads all ids and lists its rows' tokens in LDS, in order, as
+// sort_tokens does. A row of more than kSmallAlone tokens is shared by all threads of a column, a run of its
+// tokens each, and their sums are added up in order.
+constexpr uint32_t kSmallTokens = 4096, kSmallRows = 64, kSmallAlone = 4;
+constexpr int kSmallWaves = kBlock / 64;
+
+template <int IDT, int G, int OUT, bool DROP>
+__global__ __launch_bounds__(kBlock) void sum_few(GradArgs a, int lx, uint32_t tiles_x) {
+    using Id = typename IdBits<IDT>::type;
+    constexpr int kSteps = kSmallTokens / kBlock;   // ids of a lane
+    __shared__ uint32_t counts[kSmallWaves][kSmallRows], begins[kSmallRows + 1], list[kSmallTokens];
+    __shared__ float runs[kBlock][8];
+    __shared__ uint64_t shared_rows;   // bit r: row r is
+    const uint32_t v0 = blockIdx.x / tiles_x * kSmallRows;
+    const uint32_t x = threadIdx.x & ((1u << lx) - 1), y = threadIdx.x >> lx, ny = kBlock >> lx;
+    const uint32_t group = ((blockIdx.x % tiles_x) << lx) + x;
+    const uint64_t col = 8ull * group;
+    const int columns = col >= a.dim ? 0 : a.dim - col < 8 ? static_cast<int>(a.dim - col) : 8;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    counts[wave][lane] = 0;
+
+    // a wave's part of the ids: a run of whole steps of 64, in registers for both readings
+    const uint32_t steps = (a.tokens + kBlock - 1) / kBlock, first = wave * steps;
+    uint32_t row[kSteps];   // of the workgroup's; others are larger
+    {
+        Id raw[kSteps];
+#pragma unroll
+        for (int j = 0; j < kSteps; ++j) {
+            const uint32_t t = 64 * (first + j) + lane;
+            raw[j] = ~Id(0);
+            if (static_cast<uint32_t>(j) < steps && t < a.tokens) raw[j] = static_cast<const Id *>(a.ids)[t];
+        }
+#pragma unroll
+        for (int j = 0; j < kSteps; ++j)
+            row[j] = raw[j] < a.vocab ? static_cast<uint32_t>(raw[j]) - v0 : 0xffffffffu;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kSteps; ++j)
+        if (row[j] < kSmallRows) atomicAdd(&counts[wave][row[j]], 1u);
+    __syncthreads();
+    if (wave == 0) {   // lane l: row l; where each wave's tokens of it begin
+        uint32_t c[kSmallWaves], all = 0;
+#pragma unroll
+        for (int w = 0; w < kSmallWaves; ++w) {
+            c[w] = counts[w][lane];
+            all += c[w];
+        }
+        uint32_t sum = all;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const uint32_t z = __shfl_up(sum, d);
+            if (lane >= d) sum += z;
+        }
+        uint32_t at = sum - all;
+        begins[lane] = at;
+        if (lane == 63) begins[64] = sum;
+        const uint64_t shared = __ballot(all > kSmallAlone);
+        if (lane == 0) shared_rows = shared;
+#pragma unroll
+        for (int w = 0; w < kSmallWaves; ++w) {
+            counts[w][lane] = at;
+            at += c[w];
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kSteps; ++j) {
+        uint64_t todo = __ballot(row[j] < kSmallRows);
+        while (todo) {   // one row after the other: all its lanes at once
+            const uint32_t one = __builtin_amdgcn_readlane(row[j], __ffsll(static_cast<unsigned long long>(todo)) - 1);
+            const uint64_t lanes = todo & __ballot(row[j] == one);
+            const uint32_t at = counts[wave][one];
+            if (lanes >> lane & 1) list[at + __popcll(lanes & ((1ull << lane) - 1))] = 64 * (first + j) + lane;
+            counts[wave][one] = at + __popcll(lanes);   // all lanes alike
+            todo &= ~lanes;
+        }
+    }
+    __syncthreads();
+
+    const uint32_t rows = min(kSmallRows, a.vocab - v0);
+    if (columns != 0) {
+        for (uint32_t r = y; r < rows; r += ny) {
+            const uint32_t from = begins[r], count = begins[r + 1] - from;
+            if (count > kSmallAlone || (count == 0 && a.accumulate)) continue;
+            float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+            add_tokens<G, DROP, 4>(sum, a, list + from, count, group, columns);
+            write_row<OUT>(a, sum, v0 + r, group, columns);
+        }
+    }
+    for (uint64_t todo = shared_rows; todo != 0; todo &= todo - 1) {   // the same for the whole workgroup
+        const uint32_t r = __ffsll(static_cast<unsigned long long>(todo)) - 1;
+        const uint32_t begin = begins[r], count = begins[r + 1] - begin;
+        const uint32_t each = (count + ny - 1) / ny, from = min(y * each, count), to = min(from + each, count);
+        float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        if (columns != 0) add_tokens<G, DROP, 4>(sum, a, list + begin + from, to - from, group, columns);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) runs[threadIdx.x][e] = sum[e];
+        __syncthreads();
+        if (y == 0 && columns != 0) {
+            const uint32_t used = (count + each - 1) / each;
+            for (uint32_t i = 1; i < used; ++i)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum[e] += runs[(i << lx) + x][e];
+            write_row<OUT>(a, sum, v0 + r, group, columns);
+        }
+        __syncthreads();
+    }
+}
+
+template <int IDT, int G, int OUT>
+hipError_t launch_few(const GradArgs &a, hipStream_t s) {
+    const uint64_t groups = (a.dim + 7) / 8;
+    int lx = 0;
+    while (lx < 4 && (1ull << lx) < groups) ++lx;
+    const uint32_t tiles_x = static_cast<uint32_t>((groups + (1ull << lx) - 1) >> lx);
+    const uint64_t blocks = (static_cast<uint64_t>(a.vocab) + kSmallRows - 1) / kSmallRows * tiles_x;
+    if (blocks > 0xffffffffull / kBlock) return hipErrorInvalidConfiguration;
+    const uint32_t n = static_cast<uint32_t>(blocks);
+    if (a.drop.drop != 0) sum_few<IDT, G, OUT, true><<<n, kBlock, 0, s>>>(a, lx, tiles_x);
+    else sum_few<IDT, G, OUT, false><<<n, kBlock, 0, s>>>(a, lx, tiles_x);
+    return hipGetLastError();
+}
+
+template <int IDT>
+hipError_t launch_few_typed(const GradArgs &a, int grad_dtype, int out_dtype, hipStream_t s) {
+    if (grad_dtype == PS_F32)
+        return out_dtype == PS_F32 ? launch_few<IDT, PS_F32, PS_F32>(a, s) : launch_few<IDT, PS_F32, PS_BF16>(a, s);
+    return out_dtype == PS_F32 ? launch_few<IDT, PS_BF16, PS_F32>(a, s) : launch_few<IDT, PS_BF16, PS_BF16>(a, s);
+}
+
+// Every workgroup reads all ids, and rows with many tokens are taken one after the other. In us, in one
+// launch and in three: 2048 tokens of 100 columns into 50000 rows 14 and 25, of 512 into 30000 21 and 30,
+// 4096 of 1024 into 30000 34 and 42; but of 4096 into 30000 163 and 126, and 4096 of 64 into 1000 29 and 21.
+bool few(int64_t tokens, int64_t vocab, int64_t dim) {
+    return tokens <= int64_t(kSmallTokens) && tokens <= vocab && dim <= 1024;
+}
+
 template <int G, int OUT>
 hipError_t launch_sums(const GradArgs &a, const Plan &p, hipStream_t s) {
     const uint64_t groups = (a.dim + 7) / 8;
@@ -405,11 +547,15 @@ hipError_t launch_sums(const GradArgs &a, const Plan &p, hipStream_t s) {
 }  // namespace
 
 size_t grad_workspace(int64_t tokens, int64_t vocab, int64_t dim) {
+    if (few(tokens, vocab, dim)) return 0;
     return make_plan(tokens, vocab, dim).bytes;
 }
 
 hipError_t launch_grad(const GradArgs &a, int id_type, int grad_dtype, int out_dtype,
                        hipStream_t s) {
+    if (few(a.tokens, a.vocab, static_cast<int64_t>(a.dim)))
+        return id_type == PL_I32 ? launch_few_typed<PL_I32>(a, grad_dtype, out_dtype, s)
+                                 : launch_few_typed<PL_I64>(a, grad_dtype, out_dtype, s);
     const Plan p = make_plan(a.tokens, a.vocab, static_cast<int64_t>(a.dim));
     char *ws = static_cast<char *>(a.workspace);
     Row *rows = reinterpret_cast<Row *>(ws + p.rows_at);
@@ -418,12 +564,12 @@ hipError_t launch_grad(const GradArgs &a, int id_type, int grad_dtype, int out_d
     // More waves share the ids of a workgroup, and take longer to start and to be brought together:
     // the whole call over 4096 ids took 25.8 us with four waves and 27.5 with sixteen, over 8192 ids
     // 31.5 and 30.4, over 16384 43 and 36.
-    const bool few = a.tokens <= 4096;
+    const bool short_list = a.tokens <= 4096;
     if (id_type == PL_I32) {
-        if (few) sort_tokens<PL_I32, 4><<<p.classes, 256, 0, s>>>(a.ids, a.tokens, a.vocab, p, rows, perm, pieces);
+        if (short_list) sort_tokens<PL_I32, 4><<<p.classes, 256, 0, s>>>(a.ids, a.tokens, a.vocab, p, rows, perm, pieces);
         else sort_tokens<PL_I32, 16><<<p.classes, 1024, 0, s>>>(a.ids, a.tokens, a.vocab, p, rows, perm, pieces);
     } else {
-        if (few) sort_tokens<PL_I64, 4><<<p.classes, 256, 0, s>>>(a.ids, a.tokens, a.vocab, p, rows, perm, pieces);
+        if (short_list) sort_tokens<PL_I64, 4><<<p.classes, 256, 0, s>>>(a.ids, a.tokens, a.vocab, p, rows, perm, pieces);
         else sort_tokens<PL_I64, 16><<<p.classes, 1024, 0, s>>>(a.ids, a.tokens, a.vocab, p, rows, perm, pieces);
     }
     const hipError_t e = hipGetLastError();
