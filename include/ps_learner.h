@@ -133,6 +133,17 @@ int pl_linear_fp8(const void *x, int dtype, int64_t m, int64_t k, int64_t ld, in
                   void *stream);
 size_t pl_linear_fp8_workspace(int64_t m, int64_t n, int64_t k, int dtype, int out_dtype);
 
+/* The gradients of x w^T (x m x k, w n x k) from grad (m x n), that of the result: out
+ * (m x k) = grad w, from w transposed in 8 bits (w_t, k x n), and weight_out (n x k) = grad^T x,
+ * with accumulate added to what it holds. grad is quantised along its rows for the first
+ * product, grad and x along their columns for the second. m and n <= 2^22. */
+int pl_linear_fp8_grad(const void *x, int x_dtype, int64_t x_ld, const void *grad, int grad_dtype,
+                       int64_t grad_ld, int64_t m, int64_t n, int64_t k, const pl_fp8 *w_t, void *out,
+                       int out_dtype, int64_t out_ld, void *weight_out, int weight_dtype,
+                       int64_t weight_ld, int accumulate, void *workspace, size_t workspace_bytes,
+                       void *stream);
+size_t pl_linear_fp8_grad_workspace(int64_t m, int64_t n, int64_t k, int out_dtype, int weight_dtype);
+
 /* Message for the last failed call on this thread ("" if none). */
 const char *pl_last_error(void);
 

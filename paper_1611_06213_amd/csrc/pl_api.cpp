@@ -3,6 +3,7 @@
 // allocation, nothing that throws.
 #include <hip/hip_runtime_api.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -357,4 +358,99 @@ int pl_linear_fp8(const void *x, int dtype, int64_t m, int64_t k, int64_t ld, in
     if (int rc = pl_quantize_fp8(x, dtype, m, k, ld, 0, &q, nullptr, stream)) return rc;
     return pl_matmul_fp8(m, n, k, &q, w, bias, bias_dtype, relu, out, out_dtype, out_ld, 0,
                          ws + values + scales, need - values - scales, stream);
+}
+
+namespace {
+
+// Where the backward pass has what in its workspace.
+struct GradRoom {
+    size_t g_values, g_scales, t_values, t_scales, x_values, x_scales, product, product_bytes, bytes;
+};
+
+GradRoom grad_room(int64_t m, int64_t n, int64_t k, int out_dtype, int weight_dtype) {
+    GradRoom r{};
+    size_t at = 0;
+    auto take = [&at](size_t bytes) {
+        const size_t was = at;
+        at += align256(bytes);
+        return was;
+    };
+    r.g_values = take(pl_fp8_values_bytes(m, n));
+    r.g_scales = take(pl_fp8_scales_bytes(m, n));
+    r.t_values = take(pl_fp8_values_bytes(n, m));
+    r.t_scales = take(pl_fp8_scales_bytes(n, m));
+    r.x_values = take(pl_fp8_values_bytes(k, m));
+    r.x_scales = take(pl_fp8_scales_bytes(k, m));
+    // one product after the other
+    r.product_bytes = std::max(matmul_workspace(m, k, n, out_dtype), matmul_workspace(n, k, m, weight_dtype));
+    r.product = take(r.product_bytes);
+    r.bytes = at;
+    return r;
+}
+
+}  // namespace
+
+size_t pl_linear_fp8_grad_workspace(int64_t m, int64_t n, int64_t k, int out_dtype, int weight_dtype) {
+    if (m < 0 || m > (1 << 22) || n < 0 || n > (1 << 22) || k < 0 || k >= kMax / 2 ||
+        !is_dtype(out_dtype) || !is_dtype(weight_dtype))
+        return 0;
+    return grad_room(m, n, k, out_dtype, weight_dtype).bytes;
+}
+
+int pl_linear_fp8_grad(const void *x, int x_dtype, int64_t x_ld, const void *grad, int grad_dtype,
+                       int64_t grad_ld, int64_t m, int64_t n, int64_t k, const pl_fp8 *w_t, void *out,
+                       int out_dtype, int64_t out_ld, void *weight_out, int weight_dtype,
+                       int64_t weight_ld, int accumulate, void *workspace, size_t workspace_bytes,
+                       void *stream) {
+    if (int rc = size_in("m", m, 1 << 22)) return rc;
+    if (int rc = size_in("n", n, 1 << 22)) return rc;
+    if (int rc = size_in("k", k, kMax / 2 - 1)) return rc;
+    Span in[5] = {}, o[2];
+    if (int rc = matrix("x", x, x_dtype, m, k, x_ld, &in[0])) return rc;
+    if (int rc = matrix("grad", grad, grad_dtype, m, n, grad_ld, &in[1])) return rc;
+    if (int rc = fp8("w_t", w_t, k, n, &in[2], &in[3])) return rc;
+    if (int rc = matrix("out", out, out_dtype, m, k, out_ld, &o[0])) return rc;
+    if (int rc = matrix("weight_out", weight_out, weight_dtype, n, k, weight_ld, &o[1])) return rc;
+    const GradRoom r = grad_room(m, n, k, out_dtype, weight_dtype);
+    if (workspace_bytes < r.bytes)
+        return fail(PS_ENOMEM, "workspace of %zu bytes, %zu needed", workspace_bytes, r.bytes);
+    if (int rc = plain("workspace", workspace, r.bytes, 16, &in[4])) return rc;
+    if (int rc = apart(o[0], in, 5)) return rc;
+    if (int rc = apart(o[1], in, 5)) return rc;
+    if (int rc = apart(o[0], &o[1], 1)) return rc;
+    if (int rc = apart(in[4], in, 4)) return rc;
+    char *ws = static_cast<char *>(workspace);
+    auto at = [ws](size_t values, size_t scales) {
+        return pl_fp8{ws + values, reinterpret_cast<uint32_t *>(ws + scales)};
+    };
+    const pl_fp8 g = at(r.g_values, r.g_scales), t = at(r.t_values, r.t_scales), xt = at(r.x_values, r.x_scales);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    QuantArgs qg{}, qx{};
+    qg.x = grad;
+    qg.ld = grad_ld;
+    qg.rows = m;
+    qg.cols = n;
+    qg.values = static_cast<uint8_t *>(g.values);
+    qg.scales = g.scales;
+    qg.values_t = static_cast<uint8_t *>(t.values);
+    qg.scales_t = t.scales;
+    qx.x = x;
+    qx.ld = x_ld;
+    qx.rows = m;
+    qx.cols = k;
+    qx.values_t = static_cast<uint8_t *>(xt.values);
+    qx.scales_t = xt.scales;
+    const char *what = "pl_linear_fp8_grad";
+    if (x_dtype == grad_dtype) {
+        if (int rc = launched(launch_quantize_two(qg, qx, x_dtype, false, s), what)) return rc;
+    } else {
+        if (int rc = launched(launch_quantize_two(qg, QuantArgs{}, grad_dtype, false, s), what)) return rc;
+        if (int rc = launched(launch_quantize_two(qx, QuantArgs{}, x_dtype, false, s), what)) return rc;
+    }
+    void *room = r.product_bytes ? ws + r.product : nullptr;
+    if (int rc = pl_matmul_fp8(m, k, n, &g, w_t, nullptr, 0, 0, out, out_dtype, out_ld, 0, room,
+                               r.product_bytes, stream))
+        return rc;
+    return pl_matmul_fp8(n, k, m, &t, &xt, nullptr, 0, 0, weight_out, weight_dtype, weight_ld, accumulate,
+                         room, r.product_bytes, stream);
 }

@@ -138,21 +138,6 @@ bool fp8(PyObject *o, Fp8 *f) {
     return true;
 }
 
-// Room for such a matrix in a run of scratch bytes.
-struct Scratch {
-    size_t size = 0;
-    size_t take(size_t n) {
-        const size_t at = size;
-        size += (n + 255) & ~size_t(255);
-        return at;
-    }
-};
-
-pl_fp8 at_offset(const at::Tensor &t, size_t values, size_t scales) {
-    char *p = static_cast<char *>(t.data_ptr());
-    return pl_fp8{p + values, reinterpret_cast<uint32_t *>(p + scales)};
-}
-
 void *stream() { return c10::hip::getCurrentHIPStream().stream(); }
 
 // Runs `f` (which returns a status and may not touch Python) without the lock.
@@ -311,25 +296,11 @@ PyObject *linear_grad(PyObject *const *a) {
         !result(a[5], a[3], x.rows, x.cols, x.t, &dx) || !result(a[6], a[4], g.cols, x.cols, x.t, &dw))
         Py_RETURN_NONE;
     const int64_t m = x.rows, k = x.cols, n = g.cols;
-    Scratch s;
-    const size_t gv = s.take(pl_fp8_values_bytes(m, n)), gs = s.take(pl_fp8_scales_bytes(m, n));
-    const size_t tv = s.take(pl_fp8_values_bytes(n, m)), ts = s.take(pl_fp8_scales_bytes(n, m));
-    const size_t xv = s.take(pl_fp8_values_bytes(k, m)), xs = s.take(pl_fp8_scales_bytes(k, m));
-    const size_t need_x = pl_matmul_fp8_workspace(m, k, n, dx.dtype);
-    const size_t need_w = pl_matmul_fp8_workspace(n, k, m, dw.dtype);
-    const size_t need = std::max(need_x, need_w), room = s.take(need);
-    const at::Tensor work = bytes(s.size, x.t);
-    const pl_fp8 gq = at_offset(work, gv, gs), gt = at_offset(work, tv, ts), xt = at_offset(work, xv, xs);
-    void *ws = need ? static_cast<char *>(work.data_ptr()) + room : nullptr;
+    const size_t need = pl_linear_fp8_grad_workspace(m, n, k, dx.dtype, dw.dtype);
+    const at::Tensor work = bytes(need, x.t);
     const int rc = unlocked([&] {
-        void *st = stream();
-        int r = pl_quantize_fp8(g.p, g.dtype, m, n, g.ld, 0, &gq, &gt, st);
-        if (r == PS_OK) r = pl_quantize_fp8(x.p, x.dtype, m, k, x.ld, 0, nullptr, &xt, st);
-        if (r == PS_OK)
-            r = pl_matmul_fp8(m, k, n, &gq, &w.q, nullptr, 0, 0, dx.p, dx.dtype, dx.ld, 0, ws, need, st);
-        if (r == PS_OK)
-            r = pl_matmul_fp8(n, k, m, &gt, &xt, nullptr, 0, 0, dw.p, dw.dtype, dw.ld, accumulate, ws, need, st);
-        return r;
+        return pl_linear_fp8_grad(x.p, x.dtype, x.ld, g.p, g.dtype, g.ld, m, n, k, &w.q, dx.p, dx.dtype, dx.ld,
+                                  dw.p, dw.dtype, dw.ld, accumulate, work.data_ptr(), need, stream());
     });
     if (rc != PS_OK) return PyLong_FromLong(rc);
     PyObject *px = give(rc, a[5], dx.t), *pw = give(rc, a[6], dw.t);

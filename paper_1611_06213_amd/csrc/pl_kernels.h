@@ -62,6 +62,8 @@ struct QuantArgs {
     uint32_t *scales, *scales_t;
 };
 hipError_t launch_quantize(const QuantArgs &a, int dtype, bool square, hipStream_t s);
+// Two matrices of one type.
+hipError_t launch_quantize_two(const QuantArgs &a, const QuantArgs &b, int dtype, bool square, hipStream_t s);
 
 struct MatmulArgs {
     const uint8_t *a, *b;

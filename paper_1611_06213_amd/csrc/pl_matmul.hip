@@ -335,15 +335,15 @@ __global__ __launch_bounds__(256) void tiles(MatmulArgs g, Split sp) {
             block(k + 1, a2, b2, a3, b3, a0, b0);
         }
 
-        // The results. Whole tiles go out from the registers, while the next unit's first copies
-        // are under way.
+        // The results. Tiles with all their columns, and parts' sums, go out from the registers,
+        // while the next unit's first copies are under way.
         // The lane's number is hidden from the compiler here: it would compute all addresses below
         // before the loop, and have no registers for them in it.
         uint32_t lane1 = threadIdx.x & 63;
         asm volatile("" : "+v"(lane1));
         const uint32_t q1 = lane1 >> 5, r1 = lane1 & 31;
         const uint32_t m1 = m0 + wm, n1 = n0 + wn, part1 = part;
-        const bool whole = m0 + BM <= g.m && n0 + BN <= g.n && sp.parts == 1 && !g.accumulate;
+        const bool whole = sp.parts > 1 || (n0 + BN <= g.n && !g.accumulate);
         unit += gridDim.x;
         const bool more = unit < sp.tiles_m * sp.tiles_n * sp.parts;
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the last copies write zeros to LDS
@@ -358,7 +358,7 @@ __global__ __launch_bounds__(256) void tiles(MatmulArgs g, Split sp) {
             for (int j = 0; j < FN; ++j) {
                 // a lane holds row r32's columns 8 e + 4 q + 0..3, e = 0..3
                 f32x4 bias[4] = {};
-                if (g.bias != nullptr) {
+                if (g.bias != nullptr && sp.parts == 1) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
 #pragma unroll
@@ -372,16 +372,26 @@ __global__ __launch_bounds__(256) void tiles(MatmulArgs g, Split sp) {
                     for (int e = 0; e < 4; ++e) {
                         v[e] = f32x4{acc[i][j][4 * e], acc[i][j][4 * e + 1], acc[i][j][4 * e + 2],
                                      acc[i][j][4 * e + 3]} + bias[e];
-                        if (g.relu) {
+                        if (g.relu && sp.parts == 1) {
 #pragma unroll
                             for (int c = 0; c < 4; ++c) v[e][c] = v[e][c] < 0.0f ? 0.0f : v[e][c];
                         }
                     }
-                    const int64_t at = static_cast<int64_t>(m1 + 32 * i + r1) * g.out_ld + n1 + 32 * j;
+                    const uint32_t m = m1 + 32 * i + r1;
+                    if (sp.parts > 1) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const uint32_t n = n1 + 32 * j + 8 * e + 4 * q1;
+                            if (m < g.m && n < g.n) keep(g, v[e], part1, m, n);
+                        }
+                        continue;
+                    }
+                    const int64_t at = m * g.out_ld + n1 + 32 * j;
                     if constexpr (OUT == PS_F32) {
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            *reinterpret_cast<f32x4_any *>(static_cast<float *>(g.out) + at + 8 * e + 4 * q1) = v[e];
+                            if (m < g.m)
+                                *reinterpret_cast<f32x4_any *>(static_cast<float *>(g.out) + at + 8 * e + 4 * q1) = v[e];
                     } else {
                         // the halves of the wave exchange fours, so that a lane has eight columns
 #pragma unroll
@@ -395,7 +405,8 @@ __global__ __launch_bounds__(256) void tiles(MatmulArgs g, Split sp) {
                                 w[c] = p[0];
                                 w[2 + c] = p[1];
                             }
-                            *reinterpret_cast<u32x4_any *>(static_cast<uint16_t *>(g.out) + at + 16 * h + 8 * q1) = w;
+                            if (m < g.m)
+                                *reinterpret_cast<u32x4_any *>(static_cast<uint16_t *>(g.out) + at + 16 * h + 8 * q1) = w;
                         }
                     }
                 }
@@ -404,6 +415,7 @@ __global__ __launch_bounds__(256) void tiles(MatmulArgs g, Split sp) {
             // 32 rows at a time through a part of LDS that is the wave's own: fours of columns,
             // swizzled.
             constexpr int kFours = 8 * FN;   // of a row of the wave's
+            static_assert(32 * kFours % 256 == 0, "whole turns");
             static_assert(32 * kFours * 16 <= BM * 64, "a buffer has room for a wave's rows");
             f32x4 *rows = reinterpret_cast<f32x4 *>(wave == 0 ? a0 : wave == 1 ? a1 : wave == 2 ? a2 : a3);
 #pragma unroll
@@ -417,13 +429,18 @@ __global__ __launch_bounds__(256) void tiles(MatmulArgs g, Split sp) {
                                   acc[i][j][4 * e + 3]};
                 __builtin_amdgcn_wave_barrier();
 #pragma unroll 1
-                for (uint32_t t = lane1; t < 32 * kFours; t += 64) {
-                    const uint32_t r = t / kFours, c = t % kFours;
-                    const uint32_t m = m1 + 32 * i + r, n = n1 + 4 * c;
-                    const f32x4 v = rows[r * kFours + (c ^ (r & 7))];
-                    if (m >= g.m || n >= g.n) continue;
-                    if (sp.parts == 1) finish<OUT>(g, v, m, n);
-                    else keep(g, v, part1, m, n);
+                for (uint32_t t = lane1; t < 32 * kFours; t += 4 * 64) {
+                    f32x4 v[4];
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        const uint32_t r = (t + 64 * u) / kFours, c = (t + 64 * u) % kFours;
+                        v[u] = rows[r * kFours + (c ^ (r & 7))];
+                    }
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        const uint32_t m = m1 + 32 * i + (t + 64 * u) / kFours, n = n1 + 4 * ((t + 64 * u) % kFours);
+                        if (m < g.m && n < g.n) finish<OUT>(g, v[u], m, n);
+                    }
                 }
                 __builtin_amdgcn_wave_barrier();
             }
@@ -582,7 +599,6 @@ __global__ __launch_bounds__(256) void empty(MatmulArgs g) {
 
 // 32 x 4096 x 9216 22 us with either kernel, 64 x 4096 x 9216 25 with tiles and 31 with slim
 constexpr uint32_t kSlimRows = 32;
-constexpr uint32_t kMinSteps = 4;   // blocks of k that a part has at least
 
 struct Choice {
     int bm, bn;
@@ -604,7 +620,9 @@ Choice choose(uint64_t m, uint64_t n, uint64_t k, bool wide) {
     // parts of k until every compute unit has a workgroup
     const uint64_t tiles = static_cast<uint64_t>(c.split.tiles_m) * c.split.tiles_n;
     uint64_t parts = std::max<uint64_t>(1, kCus / tiles);
-    parts = std::min(parts, std::max<uint64_t>(1, blocks / kMinSteps));
+    // of four blocks at least, or of eight where the tiles are many (57 x 900 x 1000, 8 tiles: 10.2 us
+    // with parts of four, 13.1 whole; 1000 x 1000 x 1000, 64 tiles: 13.1 and 10.5)
+    parts = std::min(parts, std::max<uint64_t>(1, blocks / (tiles < 32 ? 4 : 8)));
     c.split.steps = static_cast<uint32_t>((blocks + parts - 1) / parts);
     if (parts > 1) c.split.steps += c.split.steps & 1;   // blocks go in twos
     c.split.parts = static_cast<uint32_t>((blocks + c.split.steps - 1) / c.split.steps);

@@ -22,15 +22,24 @@ __device__ __forceinline__ int word_at(int c, int w) {
     return 32 * (c ^ ((c >> 6) & 1)) + (w ^ (((c >> 3) & 7) << 2));
 }
 
+// One matrix, or two of one type in a launch: the workgroups from blocks[0] on take the second's tiles.
+struct Two {
+    QuantArgs q[2];
+    uint32_t tiles_x[2], blocks[2];
+};
+
 template <int X, bool SQUARE>
-__global__ __launch_bounds__(kBlock) void quantize_tile(QuantArgs a, uint32_t tiles_x) {
+__global__ __launch_bounds__(kBlock) void quantize_tile(Two two) {
+    const bool second = blockIdx.x >= two.blocks[0];
+    const QuantArgs &a = two.q[second];
+    const uint32_t tiles_x = two.tiles_x[second], tile = blockIdx.x - (second ? two.blocks[0] : 0);
     using M = Mags<X>;
     constexpr int W = M::kWords;
     __shared__ uint32_t col_max[kTile];
     __shared__ __attribute__((aligned(16))) uint32_t columns[kTile * 32];
     __shared__ uint32_t all_max;
-    const int64_t r0 = static_cast<int64_t>(blockIdx.x / tiles_x) * kTile;
-    const int64_t tile_x = blockIdx.x % tiles_x, c0 = tile_x * kTile;
+    const int64_t r0 = static_cast<int64_t>(tile / tiles_x) * kTile;
+    const int64_t tile_x = tile % tiles_x, c0 = tile_x * kTile;
     const int g = threadIdx.x & 15, y = threadIdx.x >> 4;
     const int64_t col = c0 + 8 * g;
     const int count = a.cols - col >= 8 ? 8 : a.cols > col ? static_cast<int>(a.cols - col) : 0;
@@ -174,16 +183,28 @@ hipError_t launch_quantize(const QuantArgs &a, int dtype, bool square, hipStream
         else quantize_rows<PS_BF16><<<n, kBlock, 0, s>>>(a, w);
         return hipGetLastError();
     }
-    const uint64_t tiles_x = (a.cols + kTile - 1) / kTile;
-    const uint64_t blocks = tiles_x * ((a.rows + kTile - 1) / kTile);
-    if (blocks > 0xffffffffull / kBlock) return hipErrorInvalidConfiguration;
-    const uint32_t n = static_cast<uint32_t>(blocks), tx = static_cast<uint32_t>(tiles_x);
+    return launch_quantize_two(a, QuantArgs{}, dtype, square, s);
+}
+
+hipError_t launch_quantize_two(const QuantArgs &a, const QuantArgs &b, int dtype, bool square, hipStream_t s) {
+    Two two{{a, b}, {}, {}};
+    uint64_t all = 0;
+    for (int i = 0; i < 2; ++i) {
+        const uint64_t x = (two.q[i].cols + kTile - 1) / kTile;
+        const uint64_t blocks = x * ((two.q[i].rows + kTile - 1) / kTile);
+        all += blocks;
+        if (all > 0xffffffffull / kBlock) return hipErrorInvalidConfiguration;
+        two.tiles_x[i] = static_cast<uint32_t>(x);
+        two.blocks[i] = static_cast<uint32_t>(blocks);
+    }
+    if (all == 0) return hipSuccess;
+    const uint32_t n = static_cast<uint32_t>(all);
     if (dtype == PS_F32) {
-        if (square) quantize_tile<PS_F32, true><<<n, kBlock, 0, s>>>(a, tx);
-        else quantize_tile<PS_F32, false><<<n, kBlock, 0, s>>>(a, tx);
+        if (square) quantize_tile<PS_F32, true><<<n, kBlock, 0, s>>>(two);
+        else quantize_tile<PS_F32, false><<<n, kBlock, 0, s>>>(two);
     } else {
-        if (square) quantize_tile<PS_BF16, true><<<n, kBlock, 0, s>>>(a, tx);
-        else quantize_tile<PS_BF16, false><<<n, kBlock, 0, s>>>(a, tx);
+        if (square) quantize_tile<PS_BF16, true><<<n, kBlock, 0, s>>>(two);
+        else quantize_tile<PS_BF16, false><<<n, kBlock, 0, s>>>(two);
     }
     return hipGetLastError();
 }

@@ -57,6 +57,9 @@ _SIGS = {
     "pl_linear_fp8": (_INT, [_VP, _INT, _I64, _I64, _I64, _I64, _FP8, _VP, _INT, _INT, _VP, _INT, _I64,
                              _VP, _SIZE, _VP]),
     "pl_linear_fp8_workspace": (_SIZE, [_I64, _I64, _I64, _INT, _INT]),
+    "pl_linear_fp8_grad": (_INT, [_VP, _INT, _I64, _VP, _INT, _I64, _I64, _I64, _I64, _FP8, _VP, _INT,
+                                  _I64, _VP, _INT, _I64, _INT, _VP, _SIZE, _VP]),
+    "pl_linear_fp8_grad_workspace": (_SIZE, [_I64, _I64, _I64, _INT, _INT]),
     "pl_last_error": (ctypes.c_char_p, []),
 }
 
@@ -390,11 +393,23 @@ def linear_fp8_grad(x, grad, w_t: Fp8Matrix, dtype=torch.bfloat16, weight_dtype=
         done = native.linear_grad(x, grad, w_t.parts, dtype, weight_dtype, x_out, weight_out, accumulate)
         if _done(done):
             return done
-    if x.dim() != 2 or grad.dim() != 2 or x.shape[0] != grad.shape[0] or \
-            w_t.shape != (x.shape[1], grad.shape[1]):
-        raise ValueError(f"x of {tuple(x.shape)}, grad of {tuple(grad.shape)}, transposed weights "
-                         f"of {w_t.shape}")
-    g, g_t = quantize_fp8_both(grad)
-    x_t = quantize_fp8(x, transpose=True)
-    return (matmul_fp8(g, w_t, dtype=dtype, out=x_out),
-            matmul_fp8(g_t, x_t, dtype=weight_dtype, out=weight_out, accumulate=accumulate))
+    k, n = w_t.shape
+    src, code, src_ld = _matrix("x", x, cols=k)
+    m = x.shape[0]
+    grd, grd_code, grd_ld = _matrix("grad", grad, m, n)
+    _on_device("w_t", w_t.values)
+    if x_out is None:
+        x_out = torch.empty((m, k), dtype=dtype, device=x.device)
+    if weight_out is None:
+        if accumulate:
+            raise ValueError("accumulate needs weight_out")
+        weight_out = torch.empty((n, k), dtype=weight_dtype, device=x.device)
+    dst, dst_code, dst_ld = _matrix("x_out", x_out, m, k)
+    wgt, wgt_code, wgt_ld = _matrix("weight_out", weight_out, n, k)
+    L = load_library()
+    need = L.pl_linear_fp8_grad_workspace(m, n, k, dst_code, wgt_code)
+    work = torch.empty(need, dtype=torch.uint8, device=x.device)
+    _check(L.pl_linear_fp8_grad(src, code, src_ld, grd, grd_code, grd_ld, m, n, k, _ref(w_t), dst,
+                                dst_code, dst_ld, wgt, wgt_code, wgt_ld, int(accumulate),
+                                work.data_ptr(), need, _stream()))
+    return x_out, weight_out

@@ -122,7 +122,8 @@ def test_embedding_shapes_and_padding(torch, learner):
 # ------------------------------------------------------------ its gradient
 
 CASES = [(0, 5, 4), (1, 1, 1), (3, 70, 10), (64, 300, 8), (65, 1, 100), (1000, 3, 33),
-         (5000, 700, 24), (4097, 100_000, 5), (300, 2, 2051), (9000, 270_000, 3)]
+         (5000, 700, 24), (4097, 100_000, 5), (300, 2, 2051), (9000, 270_000, 3),
+         (1, 70, 10), (4000, 5000, 33), (4096, 4100, 130), (700, 900, 1021), (700, 900, 1025)]
 
 
 @pytest.mark.parametrize("tokens,vocab,dim", CASES)

@@ -83,15 +83,15 @@ def test_embedding_refuses(lib):
 
 
 def test_embedding_grad_refuses(lib):
-    need = lib.pl_embedding_grad_workspace(4, 9, 6)
+    need = lib.pl_embedding_grad_workspace(40, 9, 6)
     assert need > 0
     # it grows with every size
-    for bigger in ((4000, 9, 6), (4, 9000, 6)):
+    for bigger in ((4000, 9, 6), (40_000, 9000, 6), (4000, 9, 60)):
         assert lib.pl_embedding_grad_workspace(*bigger) > need
-    for bad in ((-1, 9, 6), (4, 0, 6), (4, 9, -2), (1 << 31, 9, 6), (4, (1 << 31) + 1, 6)):
+    for bad in ((-1, 9, 6), (40, 0, 6), (40, 9, -2), (1 << 31, 9, 6), (40, (1 << 31) + 1, 6)):
         assert lib.pl_embedding_grad_workspace(*bad) == 0
 
-    def call(ids=P, id_type=0, tokens=4, grad=2 * P, gdt=0, gld=6, dim=6, d=None, out=3 * P, odt=0,
+    def call(ids=P, id_type=0, tokens=40, grad=2 * P, gdt=0, gld=6, dim=6, d=None, out=3 * P, odt=0,
              old=6, vocab=9, ws=4 * P, size=need):
         return lib.pl_embedding_grad(ids, id_type, tokens, grad, gdt, gld, dim, 1.0, d, out, odt, old,
                                      vocab, 0, ws, size, None)
@@ -196,3 +196,45 @@ def test_kernels_use_no_scratch_and_no_packed_fp32(tmp_path):
         sizes = re.findall(r"\.amdhsa_private_segment_fixed_size (\d+)", text)
         assert sizes and set(sizes) == {"0"}, out
         assert not re.search(r"^\s*v_pk_(add|mul|fma)_f32", text, re.M), out
+
+
+def test_linear_refuses(lib):
+    """The layer and its backward pass check everything before the first launch."""
+    w = fp8(2 * P, 3 * P)
+
+    def linear(x=P, dt=0, m=8, k=300, ld=300, n=16, w=w, bias=None, out=5 * P, odt=1, old=16, ws=6 * P,
+               size=1 << 24):
+        return lib.pl_linear_fp8(x, dt, m, k, ld, n, w, bias, 0, 0, out, odt, old, ws, size, None)
+    refused(lib, linear(m=-1), "m:")
+    refused(lib, linear(k=(1 << 22) + 1, ld=1 << 23), "k:")
+    refused(lib, linear(x=None), "x: null")
+    refused(lib, linear(dt=4), "dtype")
+    refused(lib, linear(ld=299), "row stride")
+    refused(lib, linear(w=fp8(2 * P + 4, 3 * P)), "16-byte")
+    refused(lib, linear(out=P + 64), "overlaps x")
+    refused(lib, linear(out=2 * P), "overlaps w")
+    refused(lib, linear(bias=5 * P), "overlaps bias")
+    need = lib.pl_linear_fp8_workspace(100, 16, 300, 0, 1)
+    assert need > 0 and lib.pl_linear_fp8_workspace(1, 16, 300, 0, 1) == 0   # a few rows: one launch
+    refused(lib, linear(m=100, size=need - 1), "needed", ps.PS_ENOMEM)
+    refused(lib, linear(m=100, ws=None), "workspace: null")
+    refused(lib, linear(m=100, ws=P), "overlaps x")
+    assert linear(m=0) == 0 and linear(n=0) == 0
+
+    need = lib.pl_linear_fp8_grad_workspace(8, 16, 300, 1, 0)
+    assert need > 0
+
+    def grad(x=P, xdt=0, xld=300, g=4 * P, gdt=1, gld=16, m=8, n=16, k=300, w=w, out=5 * P, odt=1, old=300,
+             wout=6 * P, wdt=0, wld=300, ws=8 * P, size=need):
+        return lib.pl_linear_fp8_grad(x, xdt, xld, g, gdt, gld, m, n, k, w, out, odt, old, wout, wdt, wld, 0,
+                                      ws, size, None)
+    refused(lib, grad(m=(1 << 22) + 1), "m:")
+    refused(lib, grad(x=None), "x: null")
+    refused(lib, grad(g=None), "grad: null")
+    refused(lib, grad(gld=15), "row stride")
+    refused(lib, grad(w=None), "w_t: null")
+    refused(lib, grad(wdt=9), "dtype")
+    refused(lib, grad(out=P), "overlaps x")
+    refused(lib, grad(wout=5 * P), "overlaps")
+    refused(lib, grad(size=need - 1), "needed", ps.PS_ENOMEM)
+    refused(lib, grad(ws=4 * P), "overlaps grad")
