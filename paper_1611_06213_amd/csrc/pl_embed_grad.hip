@@ -246,9 +246,11 @@ __device__ __forceinline__ void add_tokens(float (&sum)[8], const GradArgs &a, c
     }
 }
 
+// A result past the caches (true: of a table too large for them) whose 512 columns from the wave's
+// first on are one row's and inside it: stage is the wave's part of LDS. Otherwise null.
 template <int OUT>
 __device__ __forceinline__ void write_row(const GradArgs &a, float (&sum)[8], uint32_t row,
-                                          uint32_t group, int columns) {
+                                          uint32_t group, int columns, f32x4 *stage = nullptr) {
     const int64_t at = row * a.out_ld + 8ll * group;
     float old[8];
     if (a.accumulate) {
@@ -260,34 +262,31 @@ __device__ __forceinline__ void write_row(const GradArgs &a, float (&sum)[8], ui
         sum[e] *= a.factor;
         if (a.accumulate) sum[e] += old[e];
     }
-    if (columns != 8) store_some<OUT>(a.out, at, sum, columns);
-    else if (static_cast<uint64_t>(a.vocab) * a.dim * kBytes<OUT> > kCached) store8<OUT, true>(a.out, at, sum);
-    else store8<OUT>(a.out, at, sum);
+    if (stage != nullptr) store8_lines<OUT>(a.out, at, sum, stage);
+    else if (columns == 8) store8<OUT>(a.out, at, sum);
+    else store_some<OUT>(a.out, at, sum, columns);
 }
 
-// Blocks of 2^lx groups of eight columns times 256 / 2^lx pieces, or that many times kRows rows:
-// first the pieces, which take longest, then the rows. Most rows have no token or one, so a
-// thread has the loads of kRows rows under way together.
-constexpr int kRows = 2;
-
+// Blocks of 2^lx groups of eight columns times 256 / 2^lx pieces or rows: first the pieces, which
+// take longest, then the rows.
 template <int G, int OUT, bool DROP>
 __global__ __launch_bounds__(kBlock) void sum_rows(GradArgs a, Plan p, int lx, uint32_t tiles_x,
-                                                   uint32_t piece_blocks) {
+                                                   uint32_t piece_blocks, bool past_caches) {
+    __shared__ f32x4 stage[OUT == PS_F32 ? 2 * kBlock : 1];
     const char *ws = static_cast<const char *>(a.workspace);
     const uint32_t *perm = reinterpret_cast<const uint32_t *>(ws + p.perm_at);
-    const uint32_t ny = kBlock >> lx;
     const bool pieces = blockIdx.x < piece_blocks;
     const uint32_t block = pieces ? blockIdx.x : blockIdx.x - piece_blocks;
     const uint32_t group = ((block % tiles_x) << lx) + (threadIdx.x & ((1u << lx) - 1));
+    const uint64_t y = static_cast<uint64_t>(block / tiles_x) * (kBlock >> lx) + (threadIdx.x >> lx);
     const uint64_t col = 8ull * group;
     if (col >= a.dim) return;
     const int columns = a.dim - col < 8 ? static_cast<int>(a.dim - col) : 8;
+    float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     if (pieces) {
-        const uint64_t y = static_cast<uint64_t>(block / tiles_x) * ny + (threadIdx.x >> lx);
         if (y >= p.pieces) return;
         const Piece piece = reinterpret_cast<const Piece *>(ws + p.pieces_at)[y];
         if (piece.count == 0) return;
-        float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
         add_tokens<G, DROP, 8>(sum, a, perm + piece.begin, piece.count, group, columns);
         float *sums = reinterpret_cast<float *>(static_cast<char *>(a.workspace) + p.sums_at);
         const int64_t at = static_cast<int64_t>(y * a.dim + col);
@@ -295,43 +294,16 @@ __global__ __launch_bounds__(kBlock) void sum_rows(GradArgs a, Plan p, int lx, u
         else store_some<PS_F32>(sums, at, sum, columns);
         return;
     }
-    const uint64_t first = static_cast<uint64_t>(block / tiles_x) * ny * kRows + (threadIdx.x >> lx);
-    Row row[kRows];
-#pragma unroll
-    for (int u = 0; u < kRows; ++u) {
-        const uint64_t v = first + u * ny;
-        row[u] = Row{0, p.piece + 1};   // none, or one of pieces: written by the join
-        if (v < a.vocab)
-            row[u] = reinterpret_cast<const Row *>(ws + p.rows_at)[
-                (v & (p.classes - 1)) * p.local + (v >> p.class_bits)];
-    }
-    uint32_t t[kRows];
-    Bits8<G> bits[kRows] = {};
-#pragma unroll
-    for (int u = 0; u < kRows; ++u)
-        if (row[u].count - 1 < p.piece) t[u] = perm[row[u].begin];   // 1 .. piece tokens
-    if (columns == 8) {
-#pragma unroll
-        for (int u = 0; u < kRows; ++u)
-            if (row[u].count - 1 < p.piece) bits[u] = load8<G>(a.grad, t[u] * a.grad_ld + static_cast<int64_t>(col));
-    } else {
-#pragma unroll
-        for (int u = 0; u < kRows; ++u)
-            if (row[u].count - 1 < p.piece)
-                bits[u] = load8_some<G>(a.grad, t[u] * a.grad_ld + static_cast<int64_t>(col), columns);
-    }
-#pragma unroll
-    for (int u = 0; u < kRows; ++u) {
-        if (row[u].count > p.piece || (row[u].count == 0 && a.accumulate)) continue;
-        float sum[8];
-        widen8<G>(sum, bits[u]);
-        if (row[u].count != 0) {
-            if constexpr (DROP) drop8(sum, 1.0f, group, t[u], a.drop);
-            if (row[u].count > 1)
-                add_tokens<G, DROP, 4>(sum, a, perm + row[u].begin + 1, row[u].count - 1, group, columns);
-        }
-        write_row<OUT>(a, sum, static_cast<uint32_t>(first + u * ny), group, columns);
-    }
+    if (y >= a.vocab) return;
+    const uint32_t v = static_cast<uint32_t>(y);
+    const Row row = reinterpret_cast<const Row *>(ws + p.rows_at)[
+        static_cast<uint64_t>(v & (p.classes - 1)) * p.local + (v >> p.class_bits)];
+    if (row.count > p.piece || (row.count == 0 && a.accumulate)) return;
+    add_tokens<G, DROP, 4>(sum, a, perm + row.begin, row.count, group, columns);
+    // lx >= 6: a wave's lanes are of one row
+    const bool lines = past_caches && lx >= 6 && col - 8 * (threadIdx.x & 63) + 512 <= a.dim;
+    write_row<OUT>(a, sum, v, group, columns,
+                   lines ? stage + (OUT == PS_F32 ? 2 * (threadIdx.x & ~63u) : 0) : nullptr);
 }
 
 // The rows cut into pieces: their sums, in order. A workgroup takes kJoinSlots pieces of the list
@@ -529,14 +501,14 @@ hipError_t launch_sums(const GradArgs &a, const Plan &p, hipStream_t s) {
     const uint32_t tiles_x = static_cast<uint32_t>((groups + (1ull << lx) - 1) >> lx);
     const uint32_t ny = kBlock >> lx;
     const uint64_t piece_blocks = static_cast<uint64_t>((p.pieces + ny - 1) / ny) * tiles_x;
-    const uint64_t per = static_cast<uint64_t>(ny) * kRows;
-    const uint64_t blocks = piece_blocks + (a.vocab + per - 1) / per * tiles_x;
+    const uint64_t blocks = piece_blocks + (static_cast<uint64_t>(a.vocab) + ny - 1) / ny * tiles_x;
+    const bool past = static_cast<uint64_t>(a.vocab) * a.dim * kBytes<OUT> > kCached;
     if (blocks > 0xffffffffull / kBlock) return hipErrorInvalidConfiguration;
     const uint32_t pb = static_cast<uint32_t>(piece_blocks);
     if (a.drop.drop != 0)
-        sum_rows<G, OUT, true><<<static_cast<uint32_t>(blocks), kBlock, 0, s>>>(a, p, lx, tiles_x, pb);
+        sum_rows<G, OUT, true><<<static_cast<uint32_t>(blocks), kBlock, 0, s>>>(a, p, lx, tiles_x, pb, past);
     else
-        sum_rows<G, OUT, false><<<static_cast<uint32_t>(blocks), kBlock, 0, s>>>(a, p, lx, tiles_x, pb);
+        sum_rows<G, OUT, false><<<static_cast<uint32_t>(blocks), kBlock, 0, s>>>(a, p, lx, tiles_x, pb, past);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.pieces == 0) return e;
     const uint32_t join_x = static_cast<uint32_t>((groups + kJoinGroups - 1) / kJoinGroups);

@@ -21,6 +21,9 @@ __global__ __launch_bounds__(kBlock) void rows_kernel(RowsArgs a, int lx, uint32
     const uint64_t col = 8ull * group;
     if (col >= a.cols) return;
     const int count = a.cols - col < 8 ? static_cast<int>(a.cols - col) : 8;
+    // past the caches: 512 columns of one row, a wave's, at a time
+    __shared__ f32x4 stage[NT && OUT == PS_F32 ? 2 * kBlock : 1];
+    const bool lines = lx >= 6 && col - 8 * (threadIdx.x & 63) + 512 <= a.cols;
 
     int64_t src[ROWS];   // row of x; -1: zeros; -2: past the last row
 #pragma unroll
@@ -67,7 +70,8 @@ __global__ __launch_bounds__(kBlock) void rows_kernel(RowsArgs a, int lx, uint32
             for (int e = 0; e < 8; ++e) x[u][e] = 0.0f;   // not factor * 0: the factor may be NaN
         }
         const int64_t at = static_cast<int64_t>(r) * a.out_ld + static_cast<int64_t>(col);
-        if (count == 8) store8<OUT, NT>(a.out, at, x[u]);
+        if (NT && lines) store8_lines<OUT>(a.out, at, x[u], stage + (OUT == PS_F32 ? 2 * (threadIdx.x & ~63u) : 0));
+        else if (count == 8) store8<OUT>(a.out, at, x[u]);
         else store_some<OUT>(a.out, at, x[u], count);
     }
 }

@@ -232,6 +232,39 @@ def test_dropout_shapes_and_rates(torch, learner):
     assert 0.4 < float((bad == 0).float().mean()) < 0.6
 
 
+@pytest.mark.parametrize("x,out", [("f32", "f32"), ("f32", "bf16"), ("bf16", "f32")])
+def test_results_past_the_caches(torch, learner, x, out):
+    """Results of more than 64 MB are stored in another way: rows of whole waves' columns and not, and
+    nothing around them."""
+    g = gen(torch, 5)
+    for cols in (2048, 2051, 500):
+        rows = (70 << 20) // (cols * (2 if out == "bf16" else 4))
+        ids = torch.randint(-1, 300, (rows,), generator=g, device="cuda")
+        table = randn(torch, g, 300, cols, dtype=dt(torch, x))
+        dst, buf = placed(torch, rows, cols, dt(torch, out), 3, 5, 7.0)
+        learner.embedding(ids, table, 1.5, out=dst)
+        want = torch.where(ids[:, None] >= 0, table.float()[ids.clamp(min=0)] * 1.5, 0.0).to(dt(torch, out))
+        assert torch.equal(dst, want)
+        dst.fill_(7.0)
+        assert bool((buf == 7.0).all())
+        # every table row's gradient from at most one token: no sum, so equal
+        tokens = torch.randperm(rows, generator=g, device="cuda")[:5000]
+        grad = randn(torch, g, 5000, cols, dtype=dt(torch, x))
+        learner.embedding_grad(tokens, grad, rows, 0.5, out=dst)
+        want = torch.zeros_like(want)
+        want[tokens] = (grad.float() * 0.5).to(dt(torch, out))
+        assert torch.equal(dst, want)
+        dst.fill_(7.0)
+        assert bool((buf == 7.0).all())
+        if x == out:
+            drop = learner.Dropout(0.3, 1)
+            src = randn(torch, g, rows, cols)
+            y = learner.dropout(src, drop)
+            small = torch.cat([learner.dropout(torch.cat([src[i:i + 1]] * (i + 1)), drop)[i:]
+                               for i in (0, 1, 63)])   # the same rows of small matrices
+            assert torch.equal(y[[0, 1, 63]], small)
+
+
 # -------------------------------------------------------- 8-bit floating point
 
 @pytest.mark.parametrize("rows,cols", [(1, 1), (1, 128), (3, 129), (130, 100), (257, 700), (128, 512),
