@@ -230,17 +230,23 @@ __global__ __launch_bounds__(256) void tiles(MatmulArgs g, Split sp) {
 #pragma unroll
         for (int j = 0; j < FN; ++j) b[j] = gb.word(lb + 128 * j);
     };
-    auto begin = [&] {   // the first four steps' copies and the first words
+    // The first four steps' copies and the first words. After step 1's come two steps' copies and
+    // one load of words, as after every step's in the loop: its waits count on that.
+    auto begin = [&] {
 #pragma unroll
         for (int i = 0; i < FM + FN; ++i) copy(a0, b0, i, first, 0);
         load_words(sa, sb, first, true);
-        load_words(next_a, next_b, first + 1, ((first + 1) & 3) == 0);
 #pragma unroll
         for (int i = 0; i < FM + FN; ++i) copy(a1, b1, i, first, 1);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < FM + FN; ++i) copy(a2, b2, i, first + 1, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        load_words(next_a, next_b, first + 1, ((first + 1) & 3) == 0);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < FM + FN; ++i) copy(a3, b3, i, first + 1, 1);
+        __builtin_amdgcn_sched_barrier(0);
     };
 
     using Op = Operand<OUT == PS_F32>;
@@ -303,6 +309,7 @@ __global__ __launch_bounds__(256) void tiles(MatmulArgs g, Split sp) {
 #pragma unroll
         for (int j = 0; j < FN; ++j) sb[j] = (group ? next_b[j] : sb[j] >> 8) & keep;
         load_words(next_a, next_b, k + 2, ((k + 2) & 3) == 0);
+        __builtin_amdgcn_sched_barrier(0);
         step(y, x, pa2, pb2, pa1, pb1, k + 2, 1);
     };
 
@@ -314,7 +321,7 @@ __global__ __launch_bounds__(256) void tiles(MatmulArgs g, Split sp) {
         for (int i = 0; i < FM; ++i)
 #pragma unroll
             for (int j = 0; j < FN; ++j) acc[i][j] = f32x16{};
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * (FM + FN)) : "memory");   // steps 0 and 1
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(3 * (FM + FN)) : "memory");   // steps 0 and 1
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
 #pragma unroll

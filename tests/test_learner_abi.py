@@ -181,6 +181,50 @@ def test_binding_refuses_host_tensors():
         learner.dropout([1.0], learner.Dropout(0.5, 1))
 
 
+def waits_of_tiles(text):
+    """The tiled products wait for their copies to LDS by counting what was issued after them. Run
+    through each kernel's memory instructions as compiled: before every barrier of the main loop, all
+    copies but those of the last two steps have arrived."""
+    checked = 0
+    for name in re.findall(r"^(\S*tilesILi\S*):", text, re.M):
+        fm, fn = map(int, re.search(r"tilesILi(\d)ELi(\d)E", name).groups())
+        n = fm + fn   # copies of a step, and words of scales that are loaded together
+        body = text[text.index("\n" + name + ":"):]
+        ops = []
+        for line in body[:body.index(".Lfunc_end")].splitlines():
+            line = line.split(";")[0].strip()
+            if line.startswith("buffer_load_dword"):
+                ops.append("copy" if line.endswith(" lds") else "word")
+            elif re.match(r"(global|flat|scratch)_(load|store)", line):
+                ops.append("other")
+            elif line.startswith("s_waitcnt") and "vmcnt" in line:
+                ops.append(int(re.search(r"vmcnt\((\d+)\)", line).group(1)))
+            elif line.startswith("s_barrier"):
+                ops.append("barrier")
+        # up to the barrier that ends the loop: two before it, then two a block for two blocks
+        barriers = [i for i, op in enumerate(ops) if op == "barrier"]
+        ops = ops[:barriers[5] + 1]
+        assert "other" not in ops, name
+        queue, copies, ended = [], 0, 0
+        for op in ops:
+            if op == "copy":
+                queue.append(copies // n)   # the step that it belongs to
+                copies += 1
+            elif op == "word":
+                queue.append(None)
+            elif op == "barrier":
+                # before step s (0, 1, ..) steps 0 .. s + 1 are there; the first two barriers are before
+                # step 0
+                before = max(0, ended - 1)
+                assert all(step is None or step > before + 1 for step in queue), (name, ended)
+                ended += 1
+            else:
+                del queue[:max(0, len(queue) - op)]
+        assert copies == 8 * n, name
+        checked += 1
+    assert checked == 4
+
+
 def test_kernels_use_no_scratch_and_no_packed_fp32(tmp_path):
     running = []
     for src in B.LEARNER_SOURCES:
@@ -193,6 +237,8 @@ def test_kernels_use_no_scratch_and_no_packed_fp32(tmp_path):
     for out, p in running:
         assert p.wait(timeout=600) == 0
         text = open(out).read()
+        if out.endswith("pl_matmul.hip.s"):
+            waits_of_tiles(text)
         sizes = re.findall(r"\.amdhsa_private_segment_fixed_size (\d+)", text)
         assert sizes and set(sizes) == {"0"}, out
         assert not re.search(r"^\s*v_pk_(add|mul|fma)_f32", text, re.M), out
