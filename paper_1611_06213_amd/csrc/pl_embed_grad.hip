@@ -97,7 +97,7 @@ __device__ __forceinline__ uint32_t scan_exclusive(uint32_t x, uint32_t *wave_su
     return before + sum - x;
 }
 
-constexpr int kAhead = 16;   // steps whose ids are loaded together
+constexpr int kAhead = 8;   // steps whose ids are loaded together
 
 // Calls f(step, id) for a wave's steps first, first + 1, .. of 64 ids, in order; ids past the last
 // are 2^32 - 1.
@@ -216,26 +216,29 @@ __global__ __launch_bounds__(64 * WAVES) void sort_tokens(const void *ids, uint3
 constexpr int kBlock = 256;
 
 // sum += drop(grad[t]) over `count` tokens of the sorted list, columns col .. col+7.
-template <int G, bool DROP, int TOGETHER>
+template <int G, bool DROP>
 __device__ __forceinline__ void add_tokens(float (&sum)[8], const GradArgs &a, const uint32_t *perm,
                                            uint32_t count, uint32_t group, int columns) {
+    // four tokens' loads together: eight leave room for fewer waves (408 us instead of 386 for 65536
+    // tokens of 4096 columns)
+    constexpr uint32_t kTogether = 4;
     const int64_t col = 8ll * group;
-    for (uint32_t i = 0; i < count; i += TOGETHER) {
-        uint32_t t[TOGETHER];
+    for (uint32_t i = 0; i < count; i += kTogether) {
+        uint32_t t[kTogether];
 #pragma unroll
-        for (uint32_t j = 0; j < TOGETHER; ++j) t[j] = perm[i + j < count ? i + j : i];
-        Bits8<G> bits[TOGETHER] = {};
+        for (uint32_t j = 0; j < kTogether; ++j) t[j] = perm[i + j < count ? i + j : i];
+        Bits8<G> bits[kTogether] = {};
         if (columns == 8) {
 #pragma unroll
-            for (uint32_t j = 0; j < TOGETHER; ++j)
+            for (uint32_t j = 0; j < kTogether; ++j)
                 if (i + j < count) bits[j] = load8<G>(a.grad, t[j] * a.grad_ld + col);
         } else {
 #pragma unroll
-            for (uint32_t j = 0; j < TOGETHER; ++j)
+            for (uint32_t j = 0; j < kTogether; ++j)
                 if (i + j < count) bits[j] = load8_some<G>(a.grad, t[j] * a.grad_ld + col, columns);
         }
 #pragma unroll
-        for (uint32_t j = 0; j < TOGETHER; ++j) {
+        for (uint32_t j = 0; j < kTogether; ++j) {
             if (i + j >= count) break;
             float x[8];
             widen8<G>(x, bits[j]);
@@ -287,7 +290,7 @@ __global__ __launch_bounds__(kBlock) void sum_rows(GradArgs a, Plan p, int lx, u
         if (y >= p.pieces) return;
         const Piece piece = reinterpret_cast<const Piece *>(ws + p.pieces_at)[y];
         if (piece.count == 0) return;
-        add_tokens<G, DROP, 8>(sum, a, perm + piece.begin, piece.count, group, columns);
+        add_tokens<G, DROP>(sum, a, perm + piece.begin, piece.count, group, columns);
         float *sums = reinterpret_cast<float *>(static_cast<char *>(a.workspace) + p.sums_at);
         const int64_t at = static_cast<int64_t>(y * a.dim + col);
         if (columns == 8) store8<PS_F32>(sums, at, sum);
@@ -299,7 +302,7 @@ __global__ __launch_bounds__(kBlock) void sum_rows(GradArgs a, Plan p, int lx, u
     const Row row = reinterpret_cast<const Row *>(ws + p.rows_at)[
         static_cast<uint64_t>(v & (p.classes - 1)) * p.local + (v >> p.class_bits)];
     if (row.count > p.piece || (row.count == 0 && a.accumulate)) return;
-    add_tokens<G, DROP, 4>(sum, a, perm + row.begin, row.count, group, columns);
+    add_tokens<G, DROP>(sum, a, perm + row.begin, row.count, group, columns);
     // lx >= 6: a wave's lanes are of one row
     const bool lines = past_caches && lx >= 6 && col - 8 * (threadIdx.x & 63) + 512 <= a.dim;
     write_row<OUT>(a, sum, v, group, columns,
@@ -322,10 +325,11 @@ __global__ __launch_bounds__(kBlock) void join_pieces(GradArgs a, Plan p, uint32
     const uint32_t group = blockIdx.x % tiles_x * kJoinGroups + g;
     const uint64_t col = 8ull * group;
     const int columns = col >= a.dim ? 0 : a.dim - col < 8 ? static_cast<int>(a.dim - col) : 8;
-    const uint32_t slot = blockIdx.x / tiles_x * kJoinSlots;
-    for (uint32_t y = slot; y < slot + kJoinSlots && y < p.pieces; ++y) {
-        const uint32_t of = list[y].of;   // the same for the whole workgroup
-        if (of == 0) continue;
+    const uint32_t slot = blockIdx.x / tiles_x * kJoinSlots, lane = threadIdx.x & 63;
+    const uint32_t mine = lane < kJoinSlots && slot + lane < p.pieces ? list[slot + lane].of : 0;
+    for (uint64_t todo = __ballot(mine != 0); todo != 0; todo &= todo - 1) {   // the same for all waves
+        const int first = __ffsll(static_cast<unsigned long long>(todo)) - 1;
+        const uint32_t y = slot + first, of = __builtin_amdgcn_readlane(mine, first);
         const uint32_t each = (of + kJoinRuns - 1) / kJoinRuns;
         const uint32_t from = min(run * each, of), to = min(from + each, of);
         float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
@@ -441,7 +445,7 @@ __global__ __launch_bounds__(kBlock) void sum_few(GradArgs a, int lx, uint32_t t
             const uint32_t from = begins[r], count = begins[r + 1] - from;
             if (count > kSmallAlone || (count == 0 && a.accumulate)) continue;
             float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-            add_tokens<G, DROP, 4>(sum, a, list + from, count, group, columns);
+            add_tokens<G, DROP>(sum, a, list + from, count, group, columns);
             write_row<OUT>(a, sum, v0 + r, group, columns);
         }
     }
@@ -450,7 +454,7 @@ __global__ __launch_bounds__(kBlock) void sum_few(GradArgs a, int lx, uint32_t t
         const uint32_t begin = begins[r], count = begins[r + 1] - begin;
         const uint32_t each = (count + ny - 1) / ny, from = min(y * each, count), to = min(from + each, count);
         float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-        if (columns != 0) add_tokens<G, DROP, 4>(sum, a, list + begin + from, to - from, group, columns);
+        if (columns != 0) add_tokens<G, DROP>(sum, a, list + begin + from, to - from, group, columns);
 #pragma unroll
         for (int e = 0; e < 8; ++e) runs[threadIdx.x][e] = sum[e];
         __syncthreads();
