@@ -113,7 +113,7 @@ int pl_quantize_fp8(const void *x, int dtype, int64_t rows, int64_t cols, int64_
 /* out = a b^T (+ bias) (then max(., 0) with relu; a NaN stays) for a (m x k) and b (n x k),
  * out m x n; with accumulate added to what out holds. bias: n values or NULL. relu and
  * bias with accumulate are refused. m, n, k may be 0 (k = 0: a sum of no terms);
- * m, n < 2^31, k <= 2^22.
+ * m, n <= 2^28, k <= 2^22.
  *
  * An fp32 result carries fp32 sums. For a bf16 result the 8-bit matrix instructions are
  * used, at twice the rate: they keep 13 bits below the largest of eight products that they
@@ -136,7 +136,7 @@ size_t pl_linear_fp8_workspace(int64_t m, int64_t n, int64_t k, int dtype, int o
 /* The gradients of x w^T (x m x k, w n x k) from grad (m x n), that of the result: out
  * (m x k) = grad w, from w transposed in 8 bits (w_t, k x n), and weight_out (n x k) = grad^T x,
  * with accumulate added to what it holds. grad is quantised along its rows for the first
- * product, grad and x along their columns for the second. m and n <= 2^22. */
+ * product, grad and x along their columns for the second. m, n <= 2^22, k <= 2^28. */
 int pl_linear_fp8_grad(const void *x, int x_dtype, int64_t x_ld, const void *grad, int grad_dtype,
                        int64_t grad_ld, int64_t m, int64_t n, int64_t k, const pl_fp8 *w_t, void *out,
                        int out_dtype, int64_t out_ld, void *weight_out, int weight_dtype,

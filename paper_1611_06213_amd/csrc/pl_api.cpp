@@ -34,6 +34,8 @@ int launched(hipError_t e, const char *what) {
 bool is_dtype(int d) { return d == PS_F32 || d == PS_BF16; }
 size_t dtype_bytes(int d) { return d == PS_F32 ? 4 : 2; }
 constexpr int64_t kMax = int64_t(1) << 32;
+constexpr int64_t kMostRows = int64_t(1) << 28;   // of a product's operands: 4 bytes a row of scales
+constexpr int64_t kMostCols = int64_t(1) << 22;
 
 // A buffer named in a call: bytes from p on, 0 of them for an empty one.
 struct Span {
@@ -259,8 +261,7 @@ int pl_quantize_fp8(const void *x, int dtype, int64_t rows, int64_t cols, int64_
 }
 
 size_t pl_matmul_fp8_workspace(int64_t m, int64_t n, int64_t k, int out_dtype) {
-    if (m < 0 || m >= kMax / 2 || n < 0 || n >= kMax / 2 || k < 0 || k > (1 << 22) ||
-        !is_dtype(out_dtype))
+    if (m < 0 || m > kMostRows || n < 0 || n > kMostRows || k < 0 || k > kMostCols || !is_dtype(out_dtype))
         return 0;
     return matmul_workspace(m, n, k, out_dtype);
 }
@@ -269,9 +270,9 @@ int pl_matmul_fp8(int64_t m, int64_t n, int64_t k, const pl_fp8 *a, const pl_fp8
                   const void *bias, int bias_dtype, int relu, void *out, int out_dtype,
                   int64_t out_ld, int accumulate, void *workspace, size_t workspace_bytes,
                   void *stream) {
-    if (int rc = size_in("m", m, kMax / 2 - 1)) return rc;
-    if (int rc = size_in("n", n, kMax / 2 - 1)) return rc;
-    if (int rc = size_in("k", k, 1 << 22)) return rc;
+    if (int rc = size_in("m", m, kMostRows)) return rc;
+    if (int rc = size_in("n", n, kMostRows)) return rc;
+    if (int rc = size_in("k", k, kMostCols)) return rc;
     if (accumulate && (bias != nullptr || relu))
         return fail(PS_EINVAL, "accumulate with a bias or relu");
     Span in[6] = {}, o;
@@ -306,8 +307,8 @@ int pl_matmul_fp8(int64_t m, int64_t n, int64_t k, const pl_fp8 *a, const pl_fp8
 }
 
 size_t pl_linear_fp8_workspace(int64_t m, int64_t n, int64_t k, int dtype, int out_dtype) {
-    if (m < 0 || m >= kMax / 2 || n < 0 || n >= kMax / 2 || k < 0 || k > (1 << 22) ||
-        !is_dtype(dtype) || !is_dtype(out_dtype))
+    if (m < 0 || m > kMostRows || n < 0 || n > kMostRows || k < 0 || k > kMostCols || !is_dtype(dtype) ||
+        !is_dtype(out_dtype))
         return 0;
     if (converts(m, k)) return 0;
     return align256(pl_fp8_values_bytes(m, k)) + align256(pl_fp8_scales_bytes(m, k)) +
@@ -320,9 +321,9 @@ int pl_linear_fp8(const void *x, int dtype, int64_t m, int64_t k, int64_t ld, in
                   void *stream) {
     // the products' checks, with a stand-in for x's 8-bit form, before anything is enqueued
     Span in[5] = {}, o;
-    if (int rc = size_in("m", m, kMax / 2 - 1)) return rc;
-    if (int rc = size_in("n", n, kMax / 2 - 1)) return rc;
-    if (int rc = size_in("k", k, 1 << 22)) return rc;
+    if (int rc = size_in("m", m, kMostRows)) return rc;
+    if (int rc = size_in("n", n, kMostRows)) return rc;
+    if (int rc = size_in("k", k, kMostCols)) return rc;
     if (int rc = matrix("x", x, dtype, m, k, ld, &in[0])) return rc;
     if (int rc = fp8("w", w, n, k, &in[1], &in[2])) return rc;
     if (bias != nullptr)
@@ -391,7 +392,7 @@ GradRoom grad_room(int64_t m, int64_t n, int64_t k, int out_dtype, int weight_dt
 }  // namespace
 
 size_t pl_linear_fp8_grad_workspace(int64_t m, int64_t n, int64_t k, int out_dtype, int weight_dtype) {
-    if (m < 0 || m > (1 << 22) || n < 0 || n > (1 << 22) || k < 0 || k >= kMax / 2 ||
+    if (m < 0 || m > kMostCols || n < 0 || n > kMostCols || k < 0 || k > kMostRows ||
         !is_dtype(out_dtype) || !is_dtype(weight_dtype))
         return 0;
     return grad_room(m, n, k, out_dtype, weight_dtype).bytes;
@@ -402,9 +403,9 @@ int pl_linear_fp8_grad(const void *x, int x_dtype, int64_t x_ld, const void *gra
                        int out_dtype, int64_t out_ld, void *weight_out, int weight_dtype,
                        int64_t weight_ld, int accumulate, void *workspace, size_t workspace_bytes,
                        void *stream) {
-    if (int rc = size_in("m", m, 1 << 22)) return rc;
-    if (int rc = size_in("n", n, 1 << 22)) return rc;
-    if (int rc = size_in("k", k, kMax / 2 - 1)) return rc;
+    if (int rc = size_in("m", m, kMostCols)) return rc;
+    if (int rc = size_in("n", n, kMostCols)) return rc;
+    if (int rc = size_in("k", k, kMostRows)) return rc;
     Span in[5] = {}, o[2];
     if (int rc = matrix("x", x, x_dtype, m, k, x_ld, &in[0])) return rc;
     if (int rc = matrix("grad", grad, grad_dtype, m, n, grad_ld, &in[1])) return rc;

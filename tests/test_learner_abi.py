@@ -154,6 +154,8 @@ def test_fp8_refuses(lib):
         return lib.pl_matmul_fp8(m, n, k, a, b, bias, 0, relu, out, odt, ld, acc, ws, size, None)
     refused(lib, matmul(m=-1), "m:")
     refused(lib, matmul(k=(1 << 22) + 1), "k:")
+    refused(lib, matmul(m=(1 << 28) + 1), "m:")
+    refused(lib, matmul(n=(1 << 28) + 1), "n:")
     refused(lib, matmul(a=None), "a: null")
     refused(lib, matmul(b=fp8(3 * P, None)), "b: null")
     refused(lib, matmul(odt=3), "dtype")
@@ -275,6 +277,7 @@ def test_linear_refuses(lib):
         return lib.pl_linear_fp8_grad(x, xdt, xld, g, gdt, gld, m, n, k, w, out, odt, old, wout, wdt, wld, 0,
                                       ws, size, None)
     refused(lib, grad(m=(1 << 22) + 1), "m:")
+    refused(lib, grad(k=(1 << 28) + 1, xld=1 << 29, old=1 << 29, wld=1 << 29), "k:")
     refused(lib, grad(x=None), "x: null")
     refused(lib, grad(g=None), "grad: null")
     refused(lib, grad(gld=15), "row stride")
