@@ -260,6 +260,26 @@ int pl_quantize_fp8(const void *x, int dtype, int64_t rows, int64_t cols, int64_
                     "pl_quantize_fp8");
 }
 
+namespace {
+
+MatmulArgs product(int64_t m, int64_t n, int64_t k, const pl_fp8 *a, const pl_fp8 *b, void *out, int64_t out_ld,
+                   void *workspace) {
+    MatmulArgs g{};
+    g.a = static_cast<const uint8_t *>(a->values);
+    g.b = static_cast<const uint8_t *>(b->values);
+    g.sa = a->scales;
+    g.sb = b->scales;
+    g.out = out;
+    g.out_ld = out_ld;
+    g.m = static_cast<uint32_t>(m);
+    g.n = static_cast<uint32_t>(n);
+    g.k = static_cast<uint32_t>(k);
+    g.partial = static_cast<float *>(workspace);
+    return g;
+}
+
+}  // namespace
+
 size_t pl_matmul_fp8_workspace(int64_t m, int64_t n, int64_t k, int out_dtype) {
     if (m < 0 || m > kMostRows || n < 0 || n > kMostRows || k < 0 || k > kMostCols || !is_dtype(out_dtype))
         return 0;
@@ -288,21 +308,11 @@ int pl_matmul_fp8(int64_t m, int64_t n, int64_t k, const pl_fp8 *a, const pl_fp8
     if (int rc = plain("workspace", workspace, need, 16, &in[5])) return rc;
     if (int rc = apart(o, in, 6)) return rc;
     if (int rc = apart(in[5], in, 5)) return rc;
-    MatmulArgs g{};
-    g.a = static_cast<const uint8_t *>(a->values);
-    g.b = static_cast<const uint8_t *>(b->values);
-    g.sa = a->scales;
-    g.sb = b->scales;
+    MatmulArgs g = product(m, n, k, a, b, out, out_ld, workspace);
     g.bias = bias;
     g.bias_bf16 = bias != nullptr && bias_dtype == PS_BF16;
-    g.out = out;
-    g.out_ld = out_ld;
-    g.m = static_cast<uint32_t>(m);
-    g.n = static_cast<uint32_t>(n);
-    g.k = static_cast<uint32_t>(k);
     g.relu = relu != 0;
     g.accumulate = accumulate != 0;
-    g.partial = static_cast<float *>(workspace);
     return launched(launch_matmul(g, out_dtype, static_cast<hipStream_t>(stream)), "pl_matmul_fp8");
 }
 
@@ -319,7 +329,7 @@ int pl_linear_fp8(const void *x, int dtype, int64_t m, int64_t k, int64_t ld, in
                   const pl_fp8 *w, const void *bias, int bias_dtype, int relu, void *out,
                   int out_dtype, int64_t out_ld, void *workspace, size_t workspace_bytes,
                   void *stream) {
-    // the products' checks, with a stand-in for x's 8-bit form, before anything is enqueued
+    // everything is checked before the first launch
     Span in[5] = {}, o;
     if (int rc = size_in("m", m, kMostRows)) return rc;
     if (int rc = size_in("n", n, kMostRows)) return rc;
@@ -337,16 +347,10 @@ int pl_linear_fp8(const void *x, int dtype, int64_t m, int64_t k, int64_t ld, in
     if (int rc = apart(o, in, 5)) return rc;
     if (int rc = apart(in[4], in, 4)) return rc;
     if (converts(m, k)) {
-        MatmulArgs g{};
-        g.b = static_cast<const uint8_t *>(w->values);
-        g.sb = w->scales;
+        const pl_fp8 none = {};
+        MatmulArgs g = product(m, n, k, &none, w, out, out_ld, nullptr);
         g.bias = bias;
         g.bias_bf16 = bias != nullptr && bias_dtype == PS_BF16;
-        g.out = out;
-        g.out_ld = out_ld;
-        g.m = static_cast<uint32_t>(m);
-        g.n = static_cast<uint32_t>(n);
-        g.k = static_cast<uint32_t>(k);
         g.relu = relu != 0;
         g.x = x;
         g.x_ld = ld;
@@ -365,7 +369,9 @@ namespace {
 
 // Where the backward pass has what in its workspace.
 struct GradRoom {
-    size_t g_values, g_scales, t_values, t_scales, x_values, x_scales, product, product_bytes, bytes;
+    size_t g_values, g_scales, t_values, t_scales, x_values, x_scales;
+    size_t out, out_bytes, weight, weight_bytes;   // parts' sums of the two products
+    size_t bytes;
 };
 
 GradRoom grad_room(int64_t m, int64_t n, int64_t k, int out_dtype, int weight_dtype) {
@@ -382,9 +388,8 @@ GradRoom grad_room(int64_t m, int64_t n, int64_t k, int out_dtype, int weight_dt
     r.t_scales = take(pl_fp8_scales_bytes(n, m));
     r.x_values = take(pl_fp8_values_bytes(k, m));
     r.x_scales = take(pl_fp8_scales_bytes(k, m));
-    // one product after the other
-    r.product_bytes = std::max(matmul_workspace(m, k, n, out_dtype), matmul_workspace(n, k, m, weight_dtype));
-    r.product = take(r.product_bytes);
+    r.out = take(r.out_bytes = matmul_workspace(m, k, n, out_dtype));
+    r.weight = take(r.weight_bytes = matmul_workspace(n, k, m, weight_dtype));
     r.bytes = at;
     return r;
 }
@@ -448,10 +453,13 @@ int pl_linear_fp8_grad(const void *x, int x_dtype, int64_t x_ld, const void *gra
         if (int rc = launched(launch_quantize_two(qg, QuantArgs{}, grad_dtype, false, s), what)) return rc;
         if (int rc = launched(launch_quantize_two(qx, QuantArgs{}, x_dtype, false, s), what)) return rc;
     }
-    void *room = r.product_bytes ? ws + r.product : nullptr;
-    if (int rc = pl_matmul_fp8(m, k, n, &g, w_t, nullptr, 0, 0, out, out_dtype, out_ld, 0, room,
-                               r.product_bytes, stream))
-        return rc;
-    return pl_matmul_fp8(n, k, m, &t, &xt, nullptr, 0, 0, weight_out, weight_dtype, weight_ld, accumulate,
-                         room, r.product_bytes, stream);
+    MatmulArgs p = product(m, k, n, &g, w_t, out, out_ld, r.out_bytes ? ws + r.out : nullptr);
+    MatmulArgs pw = product(n, k, m, &t, &xt, weight_out, weight_ld, r.weight_bytes ? ws + r.weight : nullptr);
+    pw.accumulate = accumulate != 0;
+    if (pairs(p, out_dtype, pw, weight_dtype))
+        return launched(launch_matmul_two(p, out_dtype, pw, weight_dtype, s), what);
+    if (p.m != 0 && p.n != 0)
+        if (int rc = launched(launch_matmul(p, out_dtype, s), what)) return rc;
+    if (pw.m == 0 || pw.n == 0) return PS_OK;
+    return launched(launch_matmul(pw, weight_dtype, s), what);
 }

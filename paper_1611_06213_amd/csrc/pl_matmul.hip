@@ -147,6 +147,13 @@ struct Split {
     uint32_t parts, steps;   // of k: number of parts, blocks of 128 of each
 };
 
+// One product, or two in a launch: the workgroups from blocks[0] on are the second's.
+struct Products {
+    MatmulArgs g[2];
+    Split sp[2];
+    uint32_t blocks[2], join_blocks[2];
+};
+
 // ------------------------------------------------------------------- tiles
 
 // Which tile of which part of k the work unit `unit` is. Workgroups go round the eight XCDs, each
@@ -167,18 +174,22 @@ __device__ __forceinline__ void place(const Split &sp, uint32_t unit, uint32_t *
 
 // Tiles of 64 FM x 64 FN by 2 x 2 waves, each FM x FN instructions of 32 x 32.
 //
+// Bound by the matrix pipes and, at large sizes, by power: the clock falls from 2.4 to 1.75 GHz, and
+// the same product of zeros takes three quarters of the time. 8192^3 to bf16 takes 424 to 510 us (2.2
+// to 2.6 PFLOP/s), 16384 x 4096 x 4096 230 (2.4), and to fp32, by bf16 instructions, 460 (1.2). A step of 256 x
+// 256 tiles reads half of what four 128 x 128 tiles read from LDS (8192^3 took 690 us with those), and
+// 256 x 128, for fp32 results, leaves registers for the operands in bf16.
+//
 // A step is half a block, 64 columns. LDS holds four steps of either operand, which copies bring
 // there from memory without registers; the registers hold the step that multiplies and the
 // one after it. So in step s, step s + 1 is read from LDS, step s + 4 is copied to where s was,
 // and the copies have three steps to arrive: at the end of a step only those of the one
 // before the last are waited for.
 template <int FM, int FN, int OUT>
-__global__ __launch_bounds__(256) void tiles(MatmulArgs g, Split sp) {
+__device__ __forceinline__ void take_units(const MatmulArgs &g, const Split &sp, uint32_t unit, uint32_t stride,
+                                           uint8_t *a0, uint8_t *a1, uint8_t *a2, uint8_t *a3, uint8_t *b0,
+                                           uint8_t *b1, uint8_t *b2, uint8_t *b3) {
     constexpr int BM = 64 * FM, BN = 64 * FN;
-    // buffers that the compiler can tell apart: it would wait for all copies before every
-    // read of LDS if it could not
-    __shared__ __attribute__((aligned(128))) uint8_t a0[BM * 64], a1[BM * 64], a2[BM * 64], a3[BM * 64];
-    __shared__ __attribute__((aligned(128))) uint8_t b0[BN * 64], b1[BN * 64], b2[BN * 64], b3[BN * 64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t blocks = (g.k + 127) / 128, ld = blocks * 128;
     const int wm = wave % 2 * (32 * FM), wn = wave / 2 * (32 * FN);
@@ -313,7 +324,7 @@ __global__ __launch_bounds__(256) void tiles(MatmulArgs g, Split sp) {
         step(y, x, pa2, pb2, pa1, pb1, k + 2, 1);
     };
 
-    uint32_t unit = blockIdx.x;
+    asm volatile("; the first unit's copies");
     take(unit);
     begin();
     for (;;) {
@@ -351,7 +362,7 @@ __global__ __launch_bounds__(256) void tiles(MatmulArgs g, Split sp) {
         const uint32_t q1 = lane1 >> 5, r1 = lane1 & 31;
         const uint32_t m1 = m0 + wm, n1 = n0 + wn, part1 = part;
         const bool whole = sp.parts > 1 || (n0 + BN <= g.n && !g.accumulate);
-        unit += gridDim.x;
+        unit += stride;
         const bool more = unit < sp.tiles_m * sp.tiles_n * sp.parts;
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the last copies write zeros to LDS
         __builtin_amdgcn_s_barrier();
@@ -461,11 +472,30 @@ __global__ __launch_bounds__(256) void tiles(MatmulArgs g, Split sp) {
     }
 }
 
+// Small products leave most compute units idle, or wait for their first bytes most of the time. A
+// layer's two backward products in one launch take, quantisation and joining included, 18.7 us instead
+// of 23.4 for 57 x 1000 x 900, 22 instead of 27.6 for 300 x 1000 x 1000, 39 instead of 45.7 for 1000 x 2000 x
+// 2000.
+template <int FM, int FN, int OUT0, int OUT1>
+__global__ __launch_bounds__(256) void tiles(Products both) {
+    constexpr int A = 64 * FM * 64, B = 64 * FN * 64;
+    // buffers that the compiler can tell apart: it would wait for all copies before every
+    // read of LDS if it could not
+    __shared__ __attribute__((aligned(128))) uint8_t a0[A], a1[A], a2[A], a3[A], b0[B], b1[B], b2[B], b3[B];
+    const bool second = blockIdx.x >= both.blocks[0];
+    const uint32_t unit = blockIdx.x - (second ? both.blocks[0] : 0), stride = both.blocks[second];
+    if (OUT0 == OUT1 || !second)
+        take_units<FM, FN, OUT0>(both.g[second], both.sp[second], unit, stride, a0, a1, a2, a3, b0, b1, b2, b3);
+    else
+        take_units<FM, FN, OUT1>(both.g[1], both.sp[1], unit, stride, a0, a1, a2, a3, b0, b1, b2, b3);
+}
+
 // -------------------------------------------------------------------- slim
 
 // 16 rows of b (columns of out) a workgroup and up to 16 FM rows of a: bound by reading b, once,
 // straight into registers. The waves take the blocks of k in turn, the loads of several blocks under
-// way in each, and add up their sums in LDS, in order: no part of k goes through memory.
+// way in each, and add up their sums in LDS, in order: no part of k goes through memory. 1 x 4096 x
+// 25088 takes 20 us (5.1 TB/s of b).
 //
 // X >= 0: a is not in 8-bit form yet but given as x. Every workgroup converts all of it, into LDS,
 // while its first rows of b are under way: for few rows that is less than a launch.
@@ -578,10 +608,13 @@ __global__ __launch_bounds__(64 * WAVES) void slim(MatmulArgs g) {
 
 // -------------------------------------------------------------------- join
 
-template <int OUT>
-__global__ __launch_bounds__(256) void join(MatmulArgs g, uint32_t parts) {
-    const uint32_t fours = (g.n + 3) / 4;
-    const uint64_t i = static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x;
+// The parts' sums, in their order.
+template <int OUT0, int OUT1>
+__global__ __launch_bounds__(256) void join(Products both) {
+    const bool second = blockIdx.x >= both.join_blocks[0];
+    const MatmulArgs &g = both.g[second];
+    const uint32_t fours = (g.n + 3) / 4, parts = both.sp[second].parts;
+    const uint64_t i = static_cast<uint64_t>(blockIdx.x - (second ? both.join_blocks[0] : 0)) * 256 + threadIdx.x;
     if (i >= static_cast<uint64_t>(g.m) * fours) return;
     const uint32_t m = static_cast<uint32_t>(i / fours), n = static_cast<uint32_t>(i % fours) * 4;
     const f32x4 *p = reinterpret_cast<const f32x4 *>(g.partial) + i;
@@ -589,7 +622,8 @@ __global__ __launch_bounds__(256) void join(MatmulArgs g, uint32_t parts) {
     f32x4 v = {0, 0, 0, 0};
 #pragma unroll 8
     for (uint32_t s = 0; s < parts; ++s) v += p[s * stride];
-    finish<OUT>(g, v, m, n);
+    if (OUT0 == OUT1 || !second) finish<OUT0>(g, v, m, n);
+    else finish<OUT1>(g, v, m, n);
 }
 
 // k = 0: sums of no terms.
@@ -649,27 +683,60 @@ hipError_t launch_slim(const MatmulArgs &g, hipStream_t s) {
     return hipGetLastError();
 }
 
+uint64_t join_blocks(const MatmulArgs &g) { return (static_cast<uint64_t>(g.m) * ((g.n + 3) / 4) + 255) / 256; }
+
+// The product's work units; at most `most` workgroups take them.
+bool place_product(const MatmulArgs &g, const Choice &c, uint32_t most, int i, Products *p) {
+    const uint64_t units = static_cast<uint64_t>(c.split.tiles_m) * c.split.tiles_n * c.split.parts;
+    const uint64_t joins = c.split.parts > 1 ? join_blocks(g) : 0;
+    if (units > 0xffffffffull / 2 || joins > 0xffffffffull / 512) return false;
+    p->g[i] = g;
+    p->sp[i] = c.split;
+    p->blocks[i] = std::min(static_cast<uint32_t>(units), most);
+    p->join_blocks[i] = static_cast<uint32_t>(joins);
+    return true;
+}
+
+template <int OUT0, int OUT1>
+hipError_t launch_join(const Products &p, hipStream_t s) {
+    const hipError_t e = hipGetLastError();
+    const uint32_t joins = p.join_blocks[0] + p.join_blocks[1];
+    if (e != hipSuccess || joins == 0) return e;
+    join<OUT0, OUT1><<<joins, 256, 0, s>>>(p);
+    return hipGetLastError();
+}
+
 template <int OUT>
 hipError_t launch(const MatmulArgs &g, hipStream_t s) {
-    const uint64_t fours = static_cast<uint64_t>(g.m) * ((g.n + 3) / 4);
-    const uint64_t join_blocks = (fours + 255) / 256;
-    if (join_blocks > 0xffffffffull / 256) return hipErrorInvalidConfiguration;
     if (g.k == 0) {
-        empty<OUT><<<static_cast<uint32_t>(join_blocks), 256, 0, s>>>(g);
+        if (join_blocks(g) > 0xffffffffull / 256) return hipErrorInvalidConfiguration;
+        empty<OUT><<<static_cast<uint32_t>(join_blocks(g)), 256, 0, s>>>(g);
         return hipGetLastError();
     }
     if (g.m <= 16) return launch_slim<1, OUT, kGiven>(g, s);
     if (g.m <= kSlimRows) return launch_slim<2, OUT, kGiven>(g, s);
     const Choice c = choose(g.m, g.n, g.k, OUT == PS_F32);
-    const uint64_t units = static_cast<uint64_t>(c.split.tiles_m) * c.split.tiles_n * c.split.parts;
-    if (units > 0xffffffffull / 2) return hipErrorInvalidConfiguration;
-    const uint32_t blocks = static_cast<uint32_t>(units);
-    if (c.bm == 128) tiles<2, 2, OUT><<<std::min(blocks, 2u * kCus), 256, 0, s>>>(g, c.split);
-    else tiles<4, OUT == PS_F32 ? 2 : 4, OUT><<<std::min(blocks, 1u * kCus), 256, 0, s>>>(g, c.split);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || c.split.parts == 1) return e;
-    join<OUT><<<static_cast<uint32_t>(join_blocks), 256, 0, s>>>(g, c.split.parts);
-    return hipGetLastError();
+    Products p{};
+    if (!place_product(g, c, c.bm == 128 ? 2 * kCus : kCus, 0, &p)) return hipErrorInvalidConfiguration;
+    if (c.bm == 128) tiles<2, 2, OUT, OUT><<<p.blocks[0], 256, 0, s>>>(p);
+    else tiles<4, OUT == PS_F32 ? 2 : 4, OUT, OUT><<<p.blocks[0], 256, 0, s>>>(p);
+    return launch_join<OUT, OUT>(p, s);
+}
+
+template <int OUT0, int OUT1>
+hipError_t launch_two(const MatmulArgs &a, const MatmulArgs &b, hipStream_t s) {
+    Products p{};
+    if (!place_product(a, choose(a.m, a.n, a.k, OUT0 == PS_F32), kCus, 0, &p) ||
+        !place_product(b, choose(b.m, b.n, b.k, OUT1 == PS_F32), kCus, 1, &p))
+        return hipErrorInvalidConfiguration;
+    tiles<2, 2, OUT0, OUT1><<<p.blocks[0] + p.blocks[1], 256, 0, s>>>(p);
+    return launch_join<OUT0, OUT1>(p, s);
+}
+
+bool is_small(const MatmulArgs &g, int out_dtype) {
+    if (g.m <= kSlimRows || g.n == 0 || g.k == 0) return false;
+    const Choice c = choose(g.m, g.n, g.k, out_dtype == PS_F32);
+    return c.bm == 128 && static_cast<uint64_t>(c.split.tiles_m) * c.split.tiles_n * c.split.parts <= kCus;
 }
 
 }  // namespace
@@ -690,6 +757,16 @@ bool converts(int64_t m, int64_t k) {
 
 hipError_t launch_matmul(const MatmulArgs &a, int out_dtype, hipStream_t s) {
     return out_dtype == PS_F32 ? launch<PS_F32>(a, s) : launch<PS_BF16>(a, s);
+}
+
+bool pairs(const MatmulArgs &a, int a_dtype, const MatmulArgs &b, int b_dtype) {
+    return is_small(a, a_dtype) && is_small(b, b_dtype);
+}
+
+hipError_t launch_matmul_two(const MatmulArgs &a, int a_dtype, const MatmulArgs &b, int b_dtype, hipStream_t s) {
+    if (a_dtype != b_dtype)
+        return a_dtype == PS_BF16 ? launch_two<PS_BF16, PS_F32>(a, b, s) : launch_two<PS_BF16, PS_F32>(b, a, s);
+    return a_dtype == PS_F32 ? launch_two<PS_F32, PS_F32>(a, b, s) : launch_two<PS_BF16, PS_BF16>(a, b, s);
 }
 
 hipError_t launch_convert_matmul(const MatmulArgs &a, int x_dtype, int out_dtype, hipStream_t s) {

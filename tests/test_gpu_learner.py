@@ -411,6 +411,24 @@ def test_linear_grad(torch, learner, m, n, k, x):
     assert torch.equal(into, dw + 2.0) and bool((row[:3] == 2.0).all())
 
 
+@pytest.mark.parametrize("m,n,k", [(57, 1000, 900), (33, 33, 1), (130, 700, 4100), (1025, 129, 40), (20, 500, 500),
+                                   (300, 20, 500), (2100, 2050, 300)])
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("weight", ["f32", "bf16"])
+def test_linear_grad_is_two_products(torch, learner, m, n, k, out, weight):
+    """The same bits as the products one by one, whether or not they go in one launch."""
+    g = gen(torch, m + n)
+    x, grad, w = randn(torch, g, m, k), randn(torch, g, m, n, std=1e-3), randn(torch, g, n, k)
+    w_t = learner.quantize_fp8(w, square=True, transpose=True)
+    into = randn(torch, g, n, k).to(dt(torch, weight))
+    want = learner.matmul_fp8(learner.quantize_fp8(grad, transpose=True), learner.quantize_fp8(x, transpose=True),
+                              out=into.clone(), accumulate=True)
+    want_x = learner.matmul_fp8(learner.quantize_fp8(grad), w_t, dtype=dt(torch, out))
+    dx, dw = learner.linear_fp8_grad(x, grad, w_t, dtype=dt(torch, out), weight_out=into, accumulate=True)
+    assert dx.dtype == dt(torch, out) and torch.equal(dx, want_x)
+    assert dw is into and torch.equal(dw, want)
+
+
 def test_linear_grad_rounding(torch, learner):
     g = gen(torch, 9)
     m, n, k = 300, 200, 500

@@ -192,39 +192,45 @@ def waits_of_tiles(text):
         fm, fn = map(int, re.search(r"tilesILi(\d)ELi(\d)E", name).groups())
         n = fm + fn   # copies of a step, and words of scales that are loaded together
         body = text[text.index("\n" + name + ":"):]
-        ops = []
-        for line in body[:body.index(".Lfunc_end")].splitlines():
-            line = line.split(";")[0].strip()
-            if line.startswith("buffer_load_dword"):
-                ops.append("copy" if line.endswith(" lds") else "word")
-            elif re.match(r"(global|flat|scratch)_(load|store)", line):
-                ops.append("other")
-            elif line.startswith("s_waitcnt") and "vmcnt" in line:
-                ops.append(int(re.search(r"vmcnt\((\d+)\)", line).group(1)))
-            elif line.startswith("s_barrier"):
-                ops.append("barrier")
-        # up to the barrier that ends the loop: two before it, then two a block for two blocks
-        barriers = [i for i, op in enumerate(ops) if op == "barrier"]
-        ops = ops[:barriers[5] + 1]
-        assert "other" not in ops, name
-        queue, copies, ended = [], 0, 0
-        for op in ops:
-            if op == "copy":
-                queue.append(copies // n)   # the step that it belongs to
-                copies += 1
-            elif op == "word":
-                queue.append(None)
-            elif op == "barrier":
-                # before step s (0, 1, ..) steps 0 .. s + 1 are there; the first two barriers are before
-                # step 0
-                before = max(0, ended - 1)
-                assert all(step is None or step > before + 1 for step in queue), (name, ended)
-                ended += 1
-            else:
-                del queue[:max(0, len(queue) - op)]
-        assert copies == 8 * n, name
-        checked += 1
-    assert checked == 4
+        bodies = body[:body.index(".Lfunc_end")].split("; the first unit's copies")[1:]
+        for body in bodies:   # one, or two of a launch with results of two types
+            waits_of_units(body, n, name)
+            checked += 1
+    assert checked == 6
+
+
+def waits_of_units(body, n, name):
+    ops = []
+    for line in body.splitlines():
+        line = line.split(";")[0].strip()
+        if line.startswith("buffer_load_dword"):
+            ops.append("copy" if line.endswith(" lds") else "word")
+        elif re.match(r"(global|flat|scratch)_(load|store)", line):
+            ops.append("other")
+        elif line.startswith("s_waitcnt") and "vmcnt" in line:
+            ops.append(int(re.search(r"vmcnt\((\d+)\)", line).group(1)))
+        elif line.startswith("s_barrier"):
+            ops.append("barrier")
+    # up to the barrier that ends the loop: two before it, then two a block for two blocks
+    barriers = [i for i, op in enumerate(ops) if op == "barrier"]
+    ops = ops[:barriers[5] + 1]
+    assert "other" not in ops, name
+    queue, copies, ended = [], 0, 0
+    for op in ops:
+        if op == "copy":
+            queue.append(copies // n)   # the step that it belongs to
+            copies += 1
+        elif op == "word":
+            queue.append(None)
+        elif op == "barrier":
+            # before step s (0, 1, ..) steps 0 .. s + 1 are there; the first two barriers are before
+            # step 0
+            before = max(0, ended - 1)
+            assert all(step is None or step > before + 1 for step in queue), (name, ended)
+            ended += 1
+        else:
+            del queue[:max(0, len(queue) - op)]
+    assert copies == 8 * n, name
 
 
 def test_kernels_use_no_scratch_and_no_packed_fp32(tmp_path):
