@@ -7,7 +7,7 @@
 //
 // sort    One workgroup per class of ids (id mod the number of classes) reads all
 //         ids: it counts the ids of lower classes (where its part of the sorted list begins)
-//         and its own per id, and on a second reading puts its tokens' positions
+//         and its own per id, writes its tokens down, and then puts their positions
 //         into their places. All workgroups read the same ids, which the L2s hold:
 //         64k 4-byte ids are 256 KB per compute unit, and no pass over global memory
 //         depends on another workgroup. Classes are residues, not ranges, because texts'
@@ -21,14 +21,21 @@
 // (sum_few).
 //
 // Bound by memory: grad is read once and out written once, rows without tokens included. 65536
-// tokens of 4096 bf16 columns into 65536 fp32 rows, with dropout (1.6 GB): 376 us, of which sort 36,
-// sum 330 (4.9 TB/s) and join 12; 1824 tokens of 100 fp32 columns into 50000 rows in one launch of 14.
+// tokens of 4096 bf16 columns into 65536 fp32 rows, with dropout (1.6 GB): 360 us, of which sort 26,
+// sum 320 (5 TB/s) and join 12; 1824 tokens of 100 fp32 columns into 50000 rows in one launch of 14.
 #include "pl_device.h"
 
 namespace gadei::learner {
 namespace {
 
 constexpr int kMaxLocal = 1024;   // ids of one class
+constexpr uint32_t kMaxFound = 1024;   // tokens that a wave writes down
+// Of long lists of ids nothing is written down, as a frequent id's tokens are too many: the call over
+// 65536 ids of 50000 took 65 us with writing and 76 without, over 200000 115 and 146, but over 262144
+// 209 and 177.
+constexpr uint32_t kNoted = 1 << 17;
+constexpr int kPlaceBits = 22;   // of a token in a wave's part of the ids; the rest hold the id in its class
+static_assert(kMaxLocal <= 1 << (32 - kPlaceBits) && kNoted <= 1 << kPlaceBits, "a word each");
 
 struct Row {
     uint32_t begin, count;   // its part of the sorted list
@@ -125,14 +132,38 @@ __device__ __forceinline__ void each_id(const void *ids, uint32_t tokens, uint32
     }
 }
 
+// Puts the positions of some of a wave's lanes (those with a bit in `todo`, one at least) where the next ones of
+// their ids belong; next[local] is where, and moves on. The lanes of an id, its rank among them and
+// how many they are come from ballots, one id after the other; LDS is asked for all ids at once.
+__device__ __forceinline__ void put(uint32_t *next, uint32_t *list, uint64_t todo, uint32_t local, uint32_t position, int lane) {
+    const bool mine = todo >> lane & 1;
+    uint32_t rank = 0, many = 0;
+    int first = lane;
+    while (todo) {
+        const int f = __ffsll(static_cast<unsigned long long>(todo)) - 1;
+        const uint64_t lanes = todo & __ballot(local == static_cast<uint32_t>(__builtin_amdgcn_readlane(local, f)));
+        if (lanes >> lane & 1) {
+            rank = __popcll(lanes & ((1ull << lane) - 1));
+            many = __popcll(lanes);
+            first = f;
+        }
+        todo &= ~lanes;
+    }
+    uint32_t at = 0;
+    if (mine && first == lane) at = atomicAdd(&next[local], many);
+    at = __shfl(at, first);
+    if (mine) list[at + rank] = position;
+}
+
 // WAVES waves; a thread does the bookkeeping of kMaxLocal / (64 WAVES) ids.
-template <int IDT, int WAVES>
+template <int IDT, int WAVES, bool NOTED>
 __global__ __launch_bounds__(64 * WAVES) void sort_tokens(const void *ids, uint32_t tokens, uint32_t vocab,
                                                           Plan p, Row *rows, uint32_t *perm,
                                                           Piece *pieces) {
     using Id = typename IdBits<IDT>::type;
     constexpr int kEach = kMaxLocal / (64 * WAVES);
     __shared__ uint32_t counts[WAVES][kMaxLocal];   // of each wave's part of the ids
+    __shared__ uint32_t found[WAVES][NOTED ? kMaxFound : 1];   // tokens of the class, in order: local id, place in the part
     __shared__ uint32_t wave_sums[WAVES];
     const uint32_t mine = blockIdx.x, mask = p.classes - 1;
     const int class_bits = p.class_bits;
@@ -144,12 +175,20 @@ __global__ __launch_bounds__(64 * WAVES) void sort_tokens(const void *ids, uint3
     // A wave's part of the ids is a run of whole steps of 64. Few instructions an id: what this
     // kernel takes is the ids times them, on every compute unit.
     const uint32_t steps = (tokens + 64 * WAVES - 1) / (64 * WAVES), first = wave * steps;
-    uint32_t lower = 0;
-    each_id<IDT>(ids, tokens, first, steps, lane, [&](uint32_t, Id id) {
+    uint32_t lower = 0, n_found = 0;
+    each_id<IDT>(ids, tokens, first, steps, lane, [&](uint32_t step, Id id) {
         const bool real = id < vocab;
         const uint32_t low = static_cast<uint32_t>(id), c = low & mask;
         lower += __popcll(__ballot(real && c < mine));   // in scalar registers
-        if (real && c == mine) atomicAdd(&counts[wave][low >> class_bits], 1u);
+        const bool hit = real && c == mine;
+        const uint64_t hits = NOTED ? __ballot(hit) : 1;
+        if (hits == 0) return;
+        if (hit) {
+            atomicAdd(&counts[wave][low >> class_bits], 1u);
+            const uint32_t i = n_found + __popcll(hits & ((1ull << lane) - 1));
+            if (NOTED && i < kMaxFound) found[wave][i] = (low >> class_bits) << kPlaceBits | ((step - first) * 64 + lane);
+        }
+        n_found += __popcll(hits);
     });
     __syncthreads();
 
@@ -198,8 +237,17 @@ __global__ __launch_bounds__(64 * WAVES) void sort_tokens(const void *ids, uint3
     }
     __syncthreads();
 
-    // second reading: positions into their places, in order within a wave's part
+    // Positions into their places, in order within a wave's part: those that were written down, or, where they
+    // were too many (in a frequent id's class), found again.
     if (total == 0) return;
+    if (NOTED && n_found <= kMaxFound) {
+        for (uint32_t i = 0; i < n_found; i += 64) {
+            const uint32_t token = i + lane < n_found ? found[wave][i + lane] : 0;
+            put(counts[wave], perm, __ballot(i + lane < n_found), token >> kPlaceBits,
+                first * 64 + (token & ((1u << kPlaceBits) - 1)), lane);
+        }
+        return;
+    }
     each_id<IDT>(ids, tokens, first, steps, lane, [&](uint32_t step, Id id) {
         const uint32_t low = static_cast<uint32_t>(id);
         uint64_t todo = __ballot(id < vocab && (low & mask) == mine);
@@ -522,6 +570,16 @@ hipError_t launch_sums(const GradArgs &a, const Plan &p, hipStream_t s) {
     return hipGetLastError();
 }
 
+template <int IDT>
+void launch_sort(const GradArgs &a, const Plan &p, Row *rows, uint32_t *perm, Piece *pieces, hipStream_t s) {
+    // More waves share the ids of a workgroup, and take longer to start and to be brought together:
+    // the whole call over 4096 ids took 25.8 us with four waves and 27.5 with sixteen, over 8192 ids
+    // 31.5 and 30.4, over 16384 43 and 36.
+    if (a.tokens <= 4096) sort_tokens<IDT, 4, true><<<p.classes, 256, 0, s>>>(a.ids, a.tokens, a.vocab, p, rows, perm, pieces);
+    else if (a.tokens <= kNoted) sort_tokens<IDT, 16, true><<<p.classes, 1024, 0, s>>>(a.ids, a.tokens, a.vocab, p, rows, perm, pieces);
+    else sort_tokens<IDT, 16, false><<<p.classes, 1024, 0, s>>>(a.ids, a.tokens, a.vocab, p, rows, perm, pieces);
+}
+
 }  // namespace
 
 size_t grad_workspace(int64_t tokens, int64_t vocab, int64_t dim) {
@@ -539,17 +597,8 @@ hipError_t launch_grad(const GradArgs &a, int id_type, int grad_dtype, int out_d
     Row *rows = reinterpret_cast<Row *>(ws + p.rows_at);
     uint32_t *perm = reinterpret_cast<uint32_t *>(ws + p.perm_at);
     Piece *pieces = reinterpret_cast<Piece *>(ws + p.pieces_at);
-    // More waves share the ids of a workgroup, and take longer to start and to be brought together:
-    // the whole call over 4096 ids took 25.8 us with four waves and 27.5 with sixteen, over 8192 ids
-    // 31.5 and 30.4, over 16384 43 and 36.
-    const bool short_list = a.tokens <= 4096;
-    if (id_type == PL_I32) {
-        if (short_list) sort_tokens<PL_I32, 4><<<p.classes, 256, 0, s>>>(a.ids, a.tokens, a.vocab, p, rows, perm, pieces);
-        else sort_tokens<PL_I32, 16><<<p.classes, 1024, 0, s>>>(a.ids, a.tokens, a.vocab, p, rows, perm, pieces);
-    } else {
-        if (short_list) sort_tokens<PL_I64, 4><<<p.classes, 256, 0, s>>>(a.ids, a.tokens, a.vocab, p, rows, perm, pieces);
-        else sort_tokens<PL_I64, 16><<<p.classes, 1024, 0, s>>>(a.ids, a.tokens, a.vocab, p, rows, perm, pieces);
-    }
+    if (id_type == PL_I32) launch_sort<PL_I32>(a, p, rows, perm, pieces, s);
+    else launch_sort<PL_I64>(a, p, rows, perm, pieces, s);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     if (grad_dtype == PS_F32)

@@ -165,6 +165,19 @@ def test_embedding_grad_accumulates(torch, learner, out):
     within(got, want, tol + (np.abs(want) + tol) * out_tol(out))
 
 
+@pytest.mark.parametrize("tokens", [131_072, 131_073, 300_001])
+def test_embedding_grad_of_long_lists(torch, learner, tokens):
+    """One id in nine tokens, some rare ones, some no token."""
+    vocab, dim = 30_000, 3
+    g = gen(torch, tokens)
+    ids = torch.randint(-1, vocab + 1, (tokens,), generator=g, device="cuda")
+    ids[torch.rand(tokens, generator=g, device="cuda") < 1 / 9] = 77
+    grad = randn(torch, g, tokens, dim)
+    got = learner.embedding_grad(ids, grad, vocab)
+    want, size, count = ref.embedding_grad(ids, grad, vocab, 1.0)
+    within(got, want, (count[:, None] + 3) * U * size)
+
+
 def test_one_token_everywhere(torch, learner):
     """Every token the same id: the longest sum there is, and all other rows zeros."""
     tokens, vocab, dim = 20_011, 300, 40
