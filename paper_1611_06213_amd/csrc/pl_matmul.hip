@@ -373,23 +373,24 @@ __device__ __forceinline__ void take_units(const MatmulArgs &g, const Split &sp,
                 begin();
             }
 #pragma unroll
-            for (int j = 0; j < FN; ++j) {
+            for (int j0 = 0; j0 < FN; j0 += 2) {   // 64 columns of a row after one another: a line of bf16
                 // a lane holds row r32's columns 8 e + 4 q + 0..3, e = 0..3
-                f32x4 bias[4] = {};
+                f32x4 bias[2][4] = {};
                 if (g.bias != nullptr && sp.parts == 1) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
+                    for (int e = 0; e < 8; ++e)
 #pragma unroll
                         for (int c = 0; c < 4; ++c)
-                            bias[e][c] = bias_at(g, n1 + 32 * j + 8 * e + 4 * q1 + c);
+                            bias[e / 4][e % 4][c] = bias_at(g, n1 + 32 * j0 + 8 * e + 4 * q1 + c);
                 }
 #pragma unroll
-                for (int i = 0; i < FM; ++i) {
+                for (int ij = 0; ij < 2 * FM; ++ij) {
+                    const int i = ij / 2, j = j0 + ij % 2;
                     f32x4 v[4];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         v[e] = f32x4{acc[i][j][4 * e], acc[i][j][4 * e + 1], acc[i][j][4 * e + 2],
-                                     acc[i][j][4 * e + 3]} + bias[e];
+                                     acc[i][j][4 * e + 3]} + bias[ij % 2][e];
                         if (g.relu && sp.parts == 1) {
 #pragma unroll
                             for (int c = 0; c < 4; ++c) v[e][c] = v[e][c] < 0.0f ? 0.0f : v[e][c];
