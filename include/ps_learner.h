@@ -72,7 +72,7 @@ int pl_embedding(const void *ids, int id_type, int64_t tokens, const void *table
  * for every row v (zeros for ids that do not occur), with accumulate added to what
  * out holds instead (rows whose id does not occur are then not touched). The tokens
  * are sorted by id first; a row's terms are then added in an order that depends on
- * the ids alone. tokens < 2^31, vocab <= 2^31. */
+ * the ids and the sizes alone. tokens < 2^31, vocab <= 2^31. */
 int pl_embedding_grad(const void *ids, int id_type, int64_t tokens, const void *grad,
                       int grad_dtype, int64_t grad_ld, int64_t dim, float scale,
                       const pl_drop *drop, void *out, int out_dtype, int64_t out_ld,
