@@ -84,22 +84,41 @@ __device__ __forceinline__ f32x4 mfma(const Operand<true> &b, const Operand<true
     return c;
 }
 
-__device__ __forceinline__ float bias_at(const MatmulArgs &g, uint32_t n) {
-    return g.bias_bf16 ? load1<PS_BF16>(g.bias, n) : load1<PS_F32>(g.bias, n);
+// Four columns from n on of the row that begins at element `row`; zeros from column `end` on.
+template <int DT>
+__device__ __forceinline__ f32x4 load4(const void *p, int64_t row, uint32_t n, uint32_t end) {
+    f32x4 v = {0, 0, 0, 0};
+    if (n + 4 <= end) {
+        if constexpr (DT == PS_F32) {
+            v = *reinterpret_cast<const f32x4_any *>(static_cast<const float *>(p) + row + n);
+        } else {
+            const u32x2 w = *reinterpret_cast<const u32x2_any *>(static_cast<const uint16_t *>(p) + row + n);
+            v = f32x4{__uint_as_float(w[0] << 16), __uint_as_float(w[0] & 0xffff0000u),
+                      __uint_as_float(w[1] << 16), __uint_as_float(w[1] & 0xffff0000u)};
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (n + e < end) v[e] = load1<DT>(p, row + n + e);
+    }
+    return v;
+}
+
+__device__ __forceinline__ f32x4 bias_at(const MatmulArgs &g, uint32_t n) {
+    return g.bias_bf16 ? load4<PS_BF16>(g.bias, 0, n, g.n) : load4<PS_F32>(g.bias, 0, n, g.n);
 }
 
 // What becomes of a sum: four columns from n on of row m.
 template <int OUT>
 __device__ __forceinline__ void finish(const MatmulArgs &g, f32x4 v, uint32_t m, uint32_t n) {
     const int64_t at = m * g.out_ld + n;
-    float x[4];
+    f32x4 x = v;
+    if (g.bias != nullptr) x += bias_at(g, n);
+    if (g.relu) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        x[e] = v[e];
-        if (g.bias != nullptr && n + e < g.n) x[e] += bias_at(g, n + e);
-        if (g.relu) x[e] = x[e] < 0.0f ? 0.0f : x[e];   // NaN stays
-        if (g.accumulate && n + e < g.n) x[e] += load1<OUT>(g.out, at + e);
+        for (int e = 0; e < 4; ++e) x[e] = x[e] < 0.0f ? 0.0f : x[e];   // NaN stays
     }
+    if (g.accumulate) x += load4<OUT>(g.out, m * g.out_ld, n, g.n);
     if (n + 4 <= g.n) {
         if constexpr (OUT == PS_F32)
             *reinterpret_cast<f32x4_any *>(static_cast<float *>(g.out) + at) =
@@ -121,6 +140,33 @@ __device__ __forceinline__ void keep(const MatmulArgs &g, f32x4 v, uint32_t part
     *reinterpret_cast<f32x4 *>(g.partial + (static_cast<uint64_t>(part) * g.m + m) * ld + n) = v;
 }
 
+// 16 bytes of row m's results from column n on; edge: some may lie past the last column.
+template <class T>
+__device__ __forceinline__ void put(const MatmulArgs &g, u32x4 w, uint32_t m, uint32_t n, bool edge) {
+    constexpr uint32_t N = 16 / sizeof(T);
+    T *to = static_cast<T *>(g.out) + m * g.out_ld + n;
+    if (!edge || n + N <= g.n) {
+        *reinterpret_cast<u32x4_any *>(to) = w;
+    } else {
+#pragma unroll
+        for (uint32_t c = 0; c < N; ++c) {
+            if (n + c >= g.n) continue;
+            if constexpr (sizeof(T) == 4) to[c] = __uint_as_float(w[c]);
+            else to[c] = static_cast<T>(w[c / 2] >> (16 * (c % 2)));
+        }
+    }
+}
+
+// Lanes 16 .. 31 and 48 .. 63 of a for lanes 0 .. 15 and 32 .. 47 of b.
+__device__ __forceinline__ void swap_rows(u32x4 &a, u32x4 &b) {
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        const auto p = __builtin_amdgcn_permlane16_swap(a[c], b[c], false, false);
+        a[c] = p[0];
+        b[c] = p[1];
+    }
+}
+
 // A run of memory that is read by 32-bit offsets: a lane's own, and one that all lanes share
 // (which costs no vector register). What lies outside reads as zero.
 struct Buffer {
@@ -139,6 +185,9 @@ struct Buffer {
     }
     __device__ __forceinline__ uint32_t word(uint32_t lane) const {
         return __builtin_amdgcn_raw_buffer_load_b32(rsrc, lane, 0, 0);
+    }
+    __device__ __forceinline__ uint32_t half(uint32_t lane) const {
+        return static_cast<uint16_t>(__builtin_amdgcn_raw_buffer_load_b16(rsrc, lane, 0, 0));
     }
 };
 
@@ -188,7 +237,7 @@ __device__ __forceinline__ void place(const Split &sp, uint32_t unit, uint32_t *
 template <int FM, int FN, int OUT>
 __device__ __forceinline__ void take_units(const MatmulArgs &g, const Split &sp, uint32_t unit, uint32_t stride,
                                            uint8_t *a0, uint8_t *a1, uint8_t *a2, uint8_t *a3, uint8_t *b0,
-                                           uint8_t *b1, uint8_t *b2, uint8_t *b3) {
+                                           uint8_t *b1, uint8_t *b2, uint8_t *b3, float *bias) {
     constexpr int BM = 64 * FM, BN = 64 * FN;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t blocks = (g.k + 127) / 128, ld = blocks * 128;
@@ -241,9 +290,18 @@ __device__ __forceinline__ void take_units(const MatmulArgs &g, const Split &sp,
 #pragma unroll
         for (int j = 0; j < FN; ++j) b[j] = gb.word(lb + 128 * j);
     };
+    // The bias of the thread's column of the tile, zero where there is none; asked for before a unit's
+    // copies, kept in LDS for its end.
+    const Buffer bias32(g.bias, g.bias != nullptr && !g.bias_bf16 ? g.n * 4 : 0);
+    const Buffer bias16(g.bias, g.bias != nullptr && g.bias_bf16 ? g.n * 2 : 0);
+    uint32_t bias_word, bias_half;
+    auto column_bias = [&] { return __uint_as_float(bias_word | bias_half << 16); };
     // The first four steps' copies and the first words. After step 1's come two steps' copies and
     // one load of words, as after every step's in the loop: its waits count on that.
     auto begin = [&] {
+        bias_word = bias32.word((n0 + threadIdx.x) * 4);
+        bias_half = bias16.half((n0 + threadIdx.x) * 2);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < FM + FN; ++i) copy(a0, b0, i, first, 0);
         load_words(sa, sb, first, true);
@@ -353,121 +411,93 @@ __device__ __forceinline__ void take_units(const MatmulArgs &g, const Split &sp,
             block(k + 1, a2, b2, a3, b3, a0, b0);
         }
 
-        // The results. Tiles with all their columns, and parts' sums, go out from the registers,
-        // while the next unit's first copies are under way.
+        // The results go out from the registers, while the next unit's first copies are under way.
         // The lane's number is hidden from the compiler here: it would compute all addresses below
         // before the loop, and have no registers for them in it.
         uint32_t lane1 = threadIdx.x & 63;
         asm volatile("" : "+v"(lane1));
-        const uint32_t q1 = lane1 >> 5, r1 = lane1 & 31;
+        const uint32_t q1 = lane1 >> 5, r1 = lane1 & 31, hi1 = lane1 >> 4 & 1;
         const uint32_t m1 = m0 + wm, n1 = n0 + wn, part1 = part;
-        const bool whole = sp.parts > 1 || (n0 + BN <= g.n && !g.accumulate);
+        const bool edge = n0 + BN > g.n, sums = sp.parts > 1, with_bias = g.bias != nullptr && !sums;
         unit += stride;
         const bool more = unit < sp.tiles_m * sp.tiles_n * sp.parts;
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the last copies write zeros to LDS
+        if (threadIdx.x < BN) bias[threadIdx.x] = column_bias();
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        if (whole) {
-            if (more) {
-                take(unit);
-                begin();
-            }
+        if (more && !g.accumulate) {
+            take(unit);
+            begin();
+        }
+        f32x4 old[2][4] = {};   // what out holds
 #pragma unroll
-            for (int j0 = 0; j0 < FN; j0 += 2) {   // 64 columns of a row after one another: a line of bf16
-                // a lane holds row r32's columns 8 e + 4 q + 0..3, e = 0..3
-                f32x4 bias[2][4] = {};
-                if (g.bias != nullptr && sp.parts == 1) {
+        for (int j0 = 0; j0 < FN; j0 += 2) {   // 64 columns of a row after one another: a line of bf16
+#pragma unroll
+            for (int ij = 0; ij < 2 * FM; ++ij) {
+                const int i = ij / 2, j = j0 + ij % 2;
+                const uint32_t m = m1 + 32 * i + r1;
+                if (g.accumulate && !sums && ij % 2 == 0 && m < g.m) {
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
-#pragma unroll
-                        for (int c = 0; c < 4; ++c)
-                            bias[e / 4][e % 4][c] = bias_at(g, n1 + 32 * j0 + 8 * e + 4 * q1 + c);
+                        old[e / 4][e % 4] = load4<OUT>(g.out, m * g.out_ld, n1 + 32 * j0 + 8 * e + 4 * q1, g.n);
                 }
+                f32x4 v[4];
 #pragma unroll
-                for (int ij = 0; ij < 2 * FM; ++ij) {
-                    const int i = ij / 2, j = j0 + ij % 2;
-                    f32x4 v[4];
+                for (int e = 0; e < 4; ++e) {
+                    // a lane holds row r1's columns 8 e + 4 q1 + 0..3 of each 32
+                    v[e] = f32x4{acc[i][j][4 * e], acc[i][j][4 * e + 1], acc[i][j][4 * e + 2],
+                                 acc[i][j][4 * e + 3]};
+                    if (with_bias) v[e] += *reinterpret_cast<const f32x4 *>(bias + wn + 32 * j + 8 * e + 4 * q1);
+                    if (g.relu && !sums) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        v[e] = f32x4{acc[i][j][4 * e], acc[i][j][4 * e + 1], acc[i][j][4 * e + 2],
-                                     acc[i][j][4 * e + 3]} + bias[ij % 2][e];
-                        if (g.relu && sp.parts == 1) {
-#pragma unroll
-                            for (int c = 0; c < 4; ++c) v[e][c] = v[e][c] < 0.0f ? 0.0f : v[e][c];
-                        }
+                        for (int c = 0; c < 4; ++c) v[e][c] = v[e][c] < 0.0f ? 0.0f : v[e][c];   // NaN stays
                     }
-                    const uint32_t m = m1 + 32 * i + r1;
-                    if (sp.parts > 1) {
+                    if (g.accumulate && !sums) v[e] += old[j - j0][e];
+                }
+                // Lanes exchange so that a store writes 64 neighbouring bytes of each of 16 rows: with 32
+                // bytes of 32 rows, results past the caches were written to memory 1.7 times.
+                if (OUT == PS_F32 || sums) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const uint32_t n = n1 + 32 * j + 8 * e + 4 * q1;
-                            if (m < g.m && n < g.n) keep(g, v[e], part1, m, n);
-                        }
-                        continue;
-                    }
-                    const int64_t at = m * g.out_ld + n1 + 32 * j;
-                    if constexpr (OUT == PS_F32) {
+                    for (int h = 0; h < 2; ++h) {
+                        u32x4 w[2] = {__builtin_bit_cast(u32x4, v[2 * h]), __builtin_bit_cast(u32x4, v[2 * h + 1])};
+                        swap_rows(w[0], w[1]);
+                        const uint32_t n = n1 + 32 * j + 16 * h + 8 * hi1 + 4 * q1;
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (m < g.m)
-                                *reinterpret_cast<f32x4_any *>(static_cast<float *>(g.out) + at + 8 * e + 4 * q1) = v[e];
-                    } else {
-                        // the halves of the wave exchange fours, so that a lane has eight columns
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            u32x4 w;
-#pragma unroll
-                            for (int c = 0; c < 2; ++c) {
-                                const auto p = __builtin_amdgcn_permlane32_swap(
-                                    bf16x2_rne(v[2 * h][2 * c], v[2 * h][2 * c + 1]),
-                                    bf16x2_rne(v[2 * h + 1][2 * c], v[2 * h + 1][2 * c + 1]), false, false);
-                                w[c] = p[0];
-                                w[2 + c] = p[1];
+                        for (int t = 0; t < 2; ++t) {
+                            const uint32_t to = m1 + 32 * i + 16 * t + (lane1 & 15);
+                            if (to < g.m && sums) {
+                                if (n < g.n) keep(g, __builtin_bit_cast(f32x4, w[t]), part1, to, n);
+                            } else if (to < g.m) {
+                                put<float>(g, w[t], to, n, edge);
                             }
-                            if (m < g.m)
-                                *reinterpret_cast<u32x4_any *>(static_cast<uint16_t *>(g.out) + at + 16 * h + 8 * q1) = w;
                         }
                     }
-                }
-            }
-        } else {
-            // 32 rows at a time through a part of LDS that is the wave's own: fours of columns,
-            // swizzled.
-            constexpr int kFours = 8 * FN;   // of a row of the wave's
-            static_assert(32 * kFours % 256 == 0, "whole turns");
-            static_assert(32 * kFours * 16 <= BM * 64, "a buffer has room for a wave's rows");
-            f32x4 *rows = reinterpret_cast<f32x4 *>(wave == 0 ? a0 : wave == 1 ? a1 : wave == 2 ? a2 : a3);
+                } else {
+                    // 16 bytes of bf16 first: the halves of the wave exchange fours
+                    u32x4 w[2];
 #pragma unroll
-            for (int i = 0; i < FM; ++i) {
+                    for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int j = 0; j < FN; ++j)
+                        for (int c = 0; c < 2; ++c) {
+                            const auto p = __builtin_amdgcn_permlane32_swap(
+                                bf16x2_rne(v[2 * h][2 * c], v[2 * h][2 * c + 1]),
+                                bf16x2_rne(v[2 * h + 1][2 * c], v[2 * h + 1][2 * c + 1]), false, false);
+                            w[h][c] = p[0];
+                            w[h][2 + c] = p[1];
+                        }
+                    swap_rows(w[0], w[1]);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        rows[r1 * kFours + ((8 * j + 2 * e + q1) ^ (r1 & 7))] =
-                            f32x4{acc[i][j][4 * e], acc[i][j][4 * e + 1], acc[i][j][4 * e + 2],
-                                  acc[i][j][4 * e + 3]};
-                __builtin_amdgcn_wave_barrier();
-#pragma unroll 1
-                for (uint32_t t = lane1; t < 32 * kFours; t += 4 * 64) {
-                    f32x4 v[4];
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) {
-                        const uint32_t r = (t + 64 * u) / kFours, c = (t + 64 * u) % kFours;
-                        v[u] = rows[r * kFours + (c ^ (r & 7))];
-                    }
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) {
-                        const uint32_t m = m1 + 32 * i + (t + 64 * u) / kFours, n = n1 + 4 * ((t + 64 * u) % kFours);
-                        if (m < g.m && n < g.n) finish<OUT>(g, v[u], m, n);
+                    for (int t = 0; t < 2; ++t) {
+                        const uint32_t to = m1 + 32 * i + 16 * t + (lane1 & 15);
+                        if (to < g.m) put<uint16_t>(g, w[t], to, n1 + 32 * j + 16 * hi1 + 8 * q1, edge);
                     }
                 }
-                __builtin_amdgcn_wave_barrier();
             }
-            if (more) {
-                __syncthreads();
-                take(unit);
-                begin();
-            }
+        }
+        if (more && g.accumulate) {
+            take(unit);
+            begin();
         }
         if (!more) break;
     }
@@ -478,17 +508,20 @@ __device__ __forceinline__ void take_units(const MatmulArgs &g, const Split &sp,
 // of 23.4 for 57 x 1000 x 900, 22 instead of 27.6 for 300 x 1000 x 1000, 39 instead of 45.7 for 1000 x 2000 x
 // 2000.
 template <int FM, int FN, int OUT0, int OUT1>
-__global__ __launch_bounds__(256) void tiles(Products both) {
+__global__ __launch_bounds__(256, FM == 2 ? 2 : 1) void tiles(Products both) {
     constexpr int A = 64 * FM * 64, B = 64 * FN * 64;
     // buffers that the compiler can tell apart: it would wait for all copies before every
     // read of LDS if it could not
     __shared__ __attribute__((aligned(128))) uint8_t a0[A], a1[A], a2[A], a3[A], b0[B], b1[B], b2[B], b3[B];
+    __shared__ __attribute__((aligned(16))) float bias[64 * FN];
     const bool second = blockIdx.x >= both.blocks[0];
     const uint32_t unit = blockIdx.x - (second ? both.blocks[0] : 0), stride = both.blocks[second];
     if (OUT0 == OUT1 || !second)
-        take_units<FM, FN, OUT0>(both.g[second], both.sp[second], unit, stride, a0, a1, a2, a3, b0, b1, b2, b3);
+        take_units<FM, FN, OUT0>(both.g[second], both.sp[second], unit, stride, a0, a1, a2, a3, b0, b1, b2, b3,
+                                   bias);
     else
-        take_units<FM, FN, OUT1>(both.g[1], both.sp[1], unit, stride, a0, a1, a2, a3, b0, b1, b2, b3);
+        take_units<FM, FN, OUT1>(both.g[1], both.sp[1], unit, stride, a0, a1, a2, a3, b0, b1, b2, b3,
+                                   bias);
 }
 
 // -------------------------------------------------------------------- slim
@@ -647,11 +680,30 @@ struct Choice {
     Split split;
 };
 
+// Large tiles read LDS and the caches least, small ones lose less where tiles are few or k is short: a compute
+// unit has one large tile at a time, or two small ones, which cover each other's first loads and last stores. In us, a
+// round of tiles takes so much, and so much more a block of k (fitted to 170 products of random sizes from
+// 512 x 512 x 64 to 16384 x 25088 x 16384). By it the products took 0.6% longer than with the better of both (0.3%
+// to fp32); with large tiles wherever there are 256 of them 9% (15%), always with small ones 10% (0.4%; but
+// 5% for 4096 x 4096 x 16384).
+bool takes_big(uint64_t m, uint64_t n, uint64_t blocks, bool wide) {
+    const uint64_t big = (m + 255) / 256 * ((n + (wide ? 127 : 255)) / (wide ? 128 : 256));
+    const uint64_t small = (m + 127) / 128 * ((n + 127) / 128);
+    if (small <= kCus) return false;   // k is split then
+    const double big_rounds = static_cast<double>((big + kCus - 1) / kCus);
+    const double whole = static_cast<double>((small + 2 * kCus - 1) / (2 * kCus));
+    // the last round of small tiles, if it is not full, has each compute unit to itself
+    const double small_rounds = std::max(1.0, (whole + static_cast<double>(small) / (2 * kCus)) / 2);
+    const double k = static_cast<double>(blocks);
+    return wide ? big_rounds * (8.0 + 1.5 * k) < small_rounds * (6.8 + 1.57 * k)
+                : big_rounds * (11.5 + 1.28 * k) < small_rounds * (4.2 + 1.14 * k);
+}
+
 // For more than kSlimRows rows of a.
 Choice choose(uint64_t m, uint64_t n, uint64_t k, bool wide) {
     Choice c{};
     const uint64_t blocks = (k + 127) / 128;
-    if ((m + 255) / 256 * ((n + 255) / 256) * (wide ? 2 : 1) >= kCus) {
+    if (takes_big(m, n, blocks, wide)) {
         c.bm = 256;
         c.bn = wide ? 128 : 256;
     } else {

@@ -336,7 +336,7 @@ def integers(torch, g, rows, cols):
 
 SIZES = [(1, 1, 1), (1, 16, 128), (1, 1000, 4096), (2, 33, 700), (16, 130, 1024), (17, 64, 129),
          (33, 100, 513), (64, 257, 3000), (65, 129, 128), (100, 1000, 900), (128, 128, 2048),
-         (129, 300, 640), (257, 255, 1280), (300, 520, 8200), (4100, 4099, 257)]
+         (129, 300, 640), (257, 255, 1280), (300, 520, 8200), (4100, 4099, 257), (4090, 4090, 3000)]
 
 
 @pytest.mark.parametrize("m,n,k", SIZES)
