@@ -320,7 +320,7 @@ size_t pl_linear_fp8_workspace(int64_t m, int64_t n, int64_t k, int dtype, int o
     if (m < 0 || m > kMostRows || n < 0 || n > kMostRows || k < 0 || k > kMostCols || !is_dtype(dtype) ||
         !is_dtype(out_dtype))
         return 0;
-    if (converts(m, k)) return 0;
+    if (converts(m, n, k)) return 0;
     return align256(pl_fp8_values_bytes(m, k)) + align256(pl_fp8_scales_bytes(m, k)) +
            matmul_workspace(m, n, k, out_dtype);
 }
@@ -346,7 +346,7 @@ int pl_linear_fp8(const void *x, int dtype, int64_t m, int64_t k, int64_t ld, in
     if (int rc = plain("workspace", workspace, need, 16, &in[4])) return rc;
     if (int rc = apart(o, in, 5)) return rc;
     if (int rc = apart(in[4], in, 4)) return rc;
-    if (converts(m, k)) {
+    if (converts(m, n, k)) {
         const pl_fp8 none = {};
         MatmulArgs g = product(m, n, k, &none, w, out, out_ld, nullptr);
         g.bias = bias;

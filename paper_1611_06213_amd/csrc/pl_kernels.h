@@ -86,7 +86,7 @@ bool pairs(const MatmulArgs &a, int a_dtype, const MatmulArgs &b, int b_dtype);
 hipError_t launch_matmul_two(const MatmulArgs &a, int a_dtype, const MatmulArgs &b, int b_dtype, hipStream_t s);
 // Whether the product of m x k numbers not yet in 8-bit form is one launch, which needs no a, sa or
 // workspace.
-bool converts(int64_t m, int64_t k);
+bool converts(int64_t m, int64_t n, int64_t k);
 hipError_t launch_convert_matmul(const MatmulArgs &a, int x_dtype, int out_dtype, hipStream_t s);
 
 }  // namespace gadei::learner

@@ -538,13 +538,14 @@ template <int FM>
 constexpr int kAhead = FM == 1 ? 4 : 2;   // blocks whose loads are issued together
 
 template <int FM, int OUT, int X, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void slim(MatmulArgs g) {
+__global__ __launch_bounds__(64 * WAVES) void slim(MatmulArgs g, Split sp) {
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     constexpr int A = kAhead<FM>;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int q = lane >> 4, r16 = lane & 15;
-    const uint32_t n0 = blockIdx.x * 16;
+    const uint32_t part = blockIdx.x / sp.tiles_n, n0 = blockIdx.x % sp.tiles_n * 16;
     const uint32_t blocks = (g.k + 127) / 128, ld = blocks * 128;
+    const uint32_t first = part * sp.steps, last = min(blocks, first + sp.steps);
     const uint32_t pitch = ld + 16;   // of x's rows in LDS: in different banks
     uint8_t *const bytes = lds + g.m * pitch;   // x's scales: `blocks` of a row
     // rows past a matrix, and blocks past the last, read as zeros
@@ -560,7 +561,7 @@ __global__ __launch_bounds__(64 * WAVES) void slim(MatmulArgs g) {
 #pragma unroll
         for (int j = 0; j < A; ++j) {
             const uint32_t at = block + j * WAVES;
-            const bool in = at < blocks;
+            const bool in = at < last;
             const uint32_t lanes = in ? from : Buffer::kOutside;
             t.b[j][0] = rows_b.sixteen(lanes, at * 128);
             t.b[j][1] = rows_b.sixteen(lanes, at * 128 + 16);
@@ -578,7 +579,7 @@ __global__ __launch_bounds__(64 * WAVES) void slim(MatmulArgs g) {
         }
         __builtin_amdgcn_sched_barrier(0);   // all under way before the first is used
     };
-    load(wave);
+    load(first + wave);
     if constexpr (X != kGiven) {
         constexpr int kTogether = 4;
         const uint32_t group = threadIdx.x >> 4, e = threadIdx.x & 15;   // sixteen lanes a block
@@ -606,11 +607,11 @@ __global__ __launch_bounds__(64 * WAVES) void slim(MatmulArgs g) {
     }
     const uint32_t rx = min(uint32_t(r16), g.m - 1);
     f32x4 acc[FM] = {};
-    for (uint32_t block = wave; block < blocks; block += WAVES * A) {
+    for (uint32_t block = first + wave; block < last; block += WAVES * A) {
 #pragma unroll
         for (int j = 0; j < A; ++j) {
             const uint32_t at = block + j * WAVES;
-            if (at >= blocks) break;
+            if (at >= last) break;
             Operand<OUT == PS_F32> fb, fa;
             fb.set(t.b[j][0], t.b[j][1], t.sb[j] >> (8 * (at & 3)));
 #pragma unroll
@@ -624,7 +625,7 @@ __global__ __launch_bounds__(64 * WAVES) void slim(MatmulArgs g) {
                 acc[i] = mfma(fb, fa, acc[i]);
             }
         }
-        if (block + WAVES * A < blocks) load(block + WAVES * A);
+        if (block + WAVES * A < last) load(block + WAVES * A);
     }
     f32x4 *sums = reinterpret_cast<f32x4 *>(lds);
     if constexpr (X != kGiven) __syncthreads();   // x is read no more
@@ -636,7 +637,9 @@ __global__ __launch_bounds__(64 * WAVES) void slim(MatmulArgs g) {
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) v += sums[(w * FM + wave) * 64 + lane];
         const uint32_t m = 16 * wave + r16, n = n0 + 4 * q;
-        if (m < g.m && n < g.n) finish<OUT>(g, v, m, n);
+        if (m >= g.m || n >= g.n) return;
+        if (sp.parts > 1) keep(g, v, part, m, n);
+        else finish<OUT>(g, v, m, n);
     }
 }
 
@@ -723,16 +726,38 @@ Choice choose(uint64_t m, uint64_t n, uint64_t k, bool wide) {
     return c;
 }
 
+// Whether slim converts x itself: a row's bytes in LDS, its scales and the padding. Every workgroup converts
+// all of x: 1 x 4096 (4 KB) took 7.5 us, 9.0 in two launches, 2 x 25088 (50 KB) 24.6 and 25.3, but 16 x 4096
+// (66 KB) 13.2 and 10.8, all with 4096 columns of out.
+bool few_bytes(uint64_t m, uint64_t blocks) { return m <= 16 && m * (blocks * 129 + 16) <= 51200; }
+
+// Of slim: where few columns of out leave compute units idle, a long k is split, to a block a wave at least. In us,
+// whole and split, joining included: 3 x 300 x 24000 17.3 and 8.1, 32 x 1000 x 8192 13.3 and 9.3, 3 x 1000 x 8192
+// 7.5 and 7.9, 32 x 300 x 4096 7.8 and 8.1. A split product's x is converted first, which for few bytes pays
+// from 128 blocks on (1 x 70 x 17000 with its conversion 11.8 and 9.8, 1 x 70 x 8192 7.4 and 9.3).
+Split split_slim(uint64_t m, uint64_t n, uint64_t k) {
+    Split sp{};
+    const uint64_t blocks = (k + 127) / 128;
+    sp.tiles_m = 1;
+    sp.tiles_n = static_cast<uint32_t>((n + 15) / 16);
+    const bool whole = blocks < 64 || (blocks < 128 && few_bytes(m, blocks));
+    const uint64_t parts = whole ? 1 : std::max<uint64_t>(1, std::min<uint64_t>(kCus / sp.tiles_n, blocks / 16));
+    sp.steps = static_cast<uint32_t>((blocks + parts - 1) / parts);
+    sp.parts = static_cast<uint32_t>((blocks + sp.steps - 1) / sp.steps);
+    return sp;
+}
+
 template <int FM, int OUT, int X>
-hipError_t launch_slim(const MatmulArgs &g, hipStream_t s) {
+hipError_t launch_slim(const MatmulArgs &g, const Split &sp, hipStream_t s) {
     const uint32_t blocks = (g.k + 127) / 128;
     const uint32_t x = X == kGiven ? 0 : g.m * (blocks * 128 + 16) + g.m * blocks;
     constexpr uint32_t kSums = FM * 64 * sizeof(f32x4);   // of a wave
+    const uint32_t n = sp.tiles_n * sp.parts;
     // Sixteen waves have more of a long row under way, eight leave room for a second workgroup on
     // the compute unit where rows are many and short: 1 x 4096 x 25088 23.0 us with 16, 24.6 with 8;
     // 1 x 25088 x 4096 31.7 and 25.0.
-    if (blocks > 64) slim<FM, OUT, X, 16><<<(g.n + 15) / 16, 1024, std::max(16 * kSums, x), s>>>(g);
-    else slim<FM, OUT, X, 8><<<(g.n + 15) / 16, 512, std::max(8 * kSums, x), s>>>(g);
+    if (sp.steps > 64 || sp.parts > 1) slim<FM, OUT, X, 16><<<n, 1024, std::max(16 * kSums, x), s>>>(g, sp);
+    else slim<FM, OUT, X, 8><<<n, 512, std::max(8 * kSums, x), s>>>(g, sp);
     return hipGetLastError();
 }
 
@@ -766,10 +791,16 @@ hipError_t launch(const MatmulArgs &g, hipStream_t s) {
         empty<OUT><<<static_cast<uint32_t>(join_blocks(g)), 256, 0, s>>>(g);
         return hipGetLastError();
     }
-    if (g.m <= 16) return launch_slim<1, OUT, kGiven>(g, s);
-    if (g.m <= kSlimRows) return launch_slim<2, OUT, kGiven>(g, s);
-    const Choice c = choose(g.m, g.n, g.k, OUT == PS_F32);
     Products p{};
+    if (g.m <= kSlimRows) {
+        Choice c{};
+        c.split = split_slim(g.m, g.n, g.k);
+        if (!place_product(g, c, 0, 0, &p)) return hipErrorInvalidConfiguration;
+        const hipError_t e = g.m <= 16 ? launch_slim<1, OUT, kGiven>(g, c.split, s)
+                                       : launch_slim<2, OUT, kGiven>(g, c.split, s);
+        return e != hipSuccess ? e : launch_join<OUT, OUT>(p, s);
+    }
+    const Choice c = choose(g.m, g.n, g.k, OUT == PS_F32);
     if (!place_product(g, c, c.bm == 128 ? 2 * kCus : kCus, 0, &p)) return hipErrorInvalidConfiguration;
     if (c.bm == 128) tiles<2, 2, OUT, OUT><<<p.blocks[0], 256, 0, s>>>(p);
     else tiles<4, OUT == PS_F32 ? 2 : 4, OUT, OUT><<<p.blocks[0], 256, 0, s>>>(p);
@@ -795,17 +826,14 @@ bool is_small(const MatmulArgs &g, int out_dtype) {
 }  // namespace
 
 size_t matmul_workspace(int64_t m, int64_t n, int64_t k, int out_dtype) {
-    if (m <= kSlimRows || n == 0 || k == 0) return 0;
-    const Choice c = choose(m, n, k, out_dtype == PS_F32);
-    if (c.split.parts == 1) return 0;
-    return sizeof(float) * size_t(c.split.parts) * size_t(m) * ((size_t(n) + 3) & ~size_t(3));
+    if (m == 0 || n == 0 || k == 0) return 0;
+    const uint32_t parts = (m <= kSlimRows ? split_slim(m, n, k) : choose(m, n, k, out_dtype == PS_F32).split).parts;
+    if (parts == 1) return 0;
+    return sizeof(float) * size_t(parts) * size_t(m) * ((size_t(n) + 3) & ~size_t(3));
 }
 
-bool converts(int64_t m, int64_t k) {
-    // A row's bytes in LDS, its scales and the padding. Every workgroup converts all of x: 1 x 4096
-    // (4 KB) took 7.5 us, 9.0 in two launches, 2 x 25088 (50 KB) 24.6 and 25.3, but 16 x 4096 (66 KB)
-    // 13.2 and 10.8, all with 4096 columns of out.
-    return m <= 16 && k > 0 && m * ((k + 127) / 128 * 129 + 16) <= 51200;
+bool converts(int64_t m, int64_t n, int64_t k) {
+    return m > 0 && n > 0 && k > 0 && few_bytes(m, (k + 127) / 128) && split_slim(m, n, k).parts == 1;
 }
 
 hipError_t launch_matmul(const MatmulArgs &a, int out_dtype, hipStream_t s) {
@@ -823,9 +851,12 @@ hipError_t launch_matmul_two(const MatmulArgs &a, int a_dtype, const MatmulArgs 
 }
 
 hipError_t launch_convert_matmul(const MatmulArgs &a, int x_dtype, int out_dtype, hipStream_t s) {
+    Split whole{1, (a.n + 15) / 16, 1, (a.k + 127) / 128};
     if (out_dtype == PS_F32)
-        return x_dtype == PS_F32 ? launch_slim<1, PS_F32, PS_F32>(a, s) : launch_slim<1, PS_F32, PS_BF16>(a, s);
-    return x_dtype == PS_F32 ? launch_slim<1, PS_BF16, PS_F32>(a, s) : launch_slim<1, PS_BF16, PS_BF16>(a, s);
+        return x_dtype == PS_F32 ? launch_slim<1, PS_F32, PS_F32>(a, whole, s)
+                                 : launch_slim<1, PS_F32, PS_BF16>(a, whole, s);
+    return x_dtype == PS_F32 ? launch_slim<1, PS_BF16, PS_F32>(a, whole, s)
+                             : launch_slim<1, PS_BF16, PS_BF16>(a, whole, s);
 }
 
 }  // namespace gadei::learner

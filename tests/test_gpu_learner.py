@@ -334,9 +334,10 @@ def integers(torch, g, rows, cols):
     return torch.randint(-8, 9, (rows, cols), generator=g, device="cuda").float()
 
 
-SIZES = [(1, 1, 1), (1, 16, 128), (1, 1000, 4096), (2, 33, 700), (16, 130, 1024), (17, 64, 129),
-         (33, 100, 513), (64, 257, 3000), (65, 129, 128), (100, 1000, 900), (128, 128, 2048),
-         (129, 300, 640), (257, 255, 1280), (300, 520, 8200), (4100, 4099, 257), (4090, 4090, 3000)]
+SIZES = [(1, 1, 1), (1, 16, 128), (1, 1000, 4096), (1, 70, 17_000), (2, 33, 700), (9, 33, 8193),
+         (16, 130, 1024), (17, 64, 129), (32, 515, 12_345), (33, 100, 513), (64, 257, 3000), (65, 129, 128),
+         (100, 1000, 900), (128, 128, 2048), (129, 300, 640), (257, 255, 1280), (300, 520, 8200),
+         (4100, 4099, 257), (4090, 4090, 3000)]
 
 
 @pytest.mark.parametrize("m,n,k", SIZES)
@@ -366,7 +367,8 @@ def test_matmul_exact(torch, learner, m, n, k, out):
     assert torch.equal(y, (a.double() @ b.double().t() + old).to(dt(torch, out)))
 
 
-@pytest.mark.parametrize("m,n,k", [(1, 512, 9216), (48, 200, 1000), (200, 300, 4096), (1030, 1030, 900)])
+@pytest.mark.parametrize("m,n,k", [(1, 512, 9216), (3, 70, 17_000), (16, 300, 8200), (31, 1000, 8300),
+                                   (48, 200, 1000), (200, 300, 4096), (1030, 1030, 900)])
 def test_matmul_rounding(torch, learner, m, n, k):
     g = gen(torch, k)
     a, b = randn(torch, g, m, k), randn(torch, g, n, k, std=0.05)
