@@ -23,6 +23,8 @@
 // Bound by memory: grad is read once and out written once, rows without tokens included. 65536
 // tokens of 4096 bf16 columns into 65536 fp32 rows, with dropout (1.6 GB): 360 us, of which sort 26,
 // sum 320 (5 TB/s) and join 12; 1824 tokens of 100 fp32 columns into 50000 rows in one launch of 14.
+#include <algorithm>
+
 #include "pl_device.h"
 
 namespace gadei::learner {
@@ -155,6 +157,18 @@ __device__ __forceinline__ void put(uint32_t *next, uint32_t *list, uint64_t tod
     if (mine) list[at + rank] = position;
 }
 
+// A row that is cut into pieces, which lie in the list of pieces from `slot` on.
+struct LongRow {
+    uint32_t row, begin, count, slot;
+};
+constexpr uint32_t kLongRows = 64;   // of a class, whose pieces all threads write
+
+__device__ __forceinline__ void write_pieces(const LongRow &r, uint32_t piece, Piece *pieces, uint32_t i, uint32_t step) {
+    const uint32_t n = (r.count + piece - 1) / piece;
+    for (; i < n; i += step)
+        pieces[r.slot + i] = Piece{r.row, r.begin + i * piece, min(piece, r.count - i * piece), i == 0 ? n : 0};
+}
+
 // WAVES waves; a thread does the bookkeeping of kMaxLocal / (64 WAVES) ids.
 template <int IDT, int WAVES, bool NOTED>
 __global__ __launch_bounds__(64 * WAVES) void sort_tokens(const void *ids, uint32_t tokens, uint32_t vocab,
@@ -165,11 +179,14 @@ __global__ __launch_bounds__(64 * WAVES) void sort_tokens(const void *ids, uint3
     __shared__ uint32_t counts[WAVES][kMaxLocal];   // of each wave's part of the ids
     __shared__ uint32_t found[WAVES][NOTED ? kMaxFound : 1];   // tokens of the class, in order: local id, place in the part
     __shared__ uint32_t wave_sums[WAVES];
+    __shared__ LongRow longs[kLongRows];
+    __shared__ uint32_t n_longs;
     const uint32_t mine = blockIdx.x, mask = p.classes - 1;
     const int class_bits = p.class_bits;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     for (uint32_t l = threadIdx.x; l < p.local; l += 64 * WAVES)
         for (int w = 0; w < WAVES; ++w) counts[w][l] = 0;
+    if (threadIdx.x == 0) n_longs = 0;
     __syncthreads();
 
     // A wave's part of the ids is a run of whole steps of 64. Few instructions an id: what this
@@ -183,8 +200,12 @@ __global__ __launch_bounds__(64 * WAVES) void sort_tokens(const void *ids, uint3
         const bool hit = real && c == mine;
         const uint64_t hits = NOTED ? __ballot(hit) : 1;
         if (hits == 0) return;
+        // many of one id are one addition: LDS would take them one after another
+        const int leader = __ffsll(static_cast<unsigned long long>(hits)) - 1;
+        const uint64_t alike = NOTED ? hits & __ballot(low == static_cast<uint32_t>(__builtin_amdgcn_readlane(low, leader))) : 0;
         if (hit) {
-            atomicAdd(&counts[wave][low >> class_bits], 1u);
+            if (!(alike >> lane & 1)) atomicAdd(&counts[wave][low >> class_bits], 1u);
+            else if (lane == leader) atomicAdd(&counts[wave][low >> class_bits], static_cast<uint32_t>(__popcll(alike)));
             const uint32_t i = n_found + __popcll(hits & ((1ull << lane) - 1));
             if (NOTED && i < kMaxFound) found[wave][i] = (low >> class_bits) << kPlaceBits | ((step - first) * 64 + lane);
         }
@@ -219,10 +240,11 @@ __global__ __launch_bounds__(64 * WAVES) void sort_tokens(const void *ids, uint3
         const uint32_t l = l0 + e;
         if (l >= p.local) break;
         rows[static_cast<uint64_t>(mine) * p.local + l] = Row{at, count[e]};
-        for (uint32_t i = 0; i < n[e]; ++i) {
-            const uint32_t done = i * p.piece;
-            pieces[slot + i] = Piece{(l << class_bits) | mine, at + done,
-                                     count[e] - done < p.piece ? count[e] - done : p.piece, i == 0 ? n[e] : 0};
+        if (n[e] != 0) {
+            const LongRow row = {(l << class_bits) | mine, at, count[e], slot};
+            const uint32_t i = n[e] > 4 ? atomicAdd(&n_longs, 1u) : kLongRows;
+            if (i < kLongRows) longs[i] = row;
+            else write_pieces(row, p.piece, pieces, 0, 1);
         }
         slot += n[e];
         for (int w = 0; w < WAVES; ++w) {
@@ -231,11 +253,12 @@ __global__ __launch_bounds__(64 * WAVES) void sort_tokens(const void *ids, uint3
             at += c;
         }
     }
+    __syncthreads();
+    for (uint32_t i = 0; i < min(n_longs, kLongRows); ++i) write_pieces(longs[i], p.piece, pieces, threadIdx.x, 64 * WAVES);
     if (p.pieces != 0) {
         const uint32_t to = mine == mask ? p.pieces : static_cast<uint32_t>(2ull * (base + total) / p.piece);
         for (uint32_t i = from + used + threadIdx.x; i < to; i += 64 * WAVES) pieces[i] = Piece{0, 0, 0, 0};
     }
-    __syncthreads();
 
     // Positions into their places, in order within a wave's part: those that were written down, or, where they
     // were too many (in a frequent id's class), found again.
@@ -359,20 +382,20 @@ __global__ __launch_bounds__(kBlock) void sum_rows(GradArgs a, Plan p, int lx, u
                    lines ? stage + (OUT == PS_F32 ? 2 * (threadIdx.x & ~63u) : 0) : nullptr);
 }
 
-// The rows cut into pieces: their sums, in order. A workgroup takes kJoinSlots pieces of the list
+// The rows cut into pieces: their sums, in a fixed order. A workgroup takes kJoinSlots pieces of the list
 // after one another, most of which begin no row; where one does, the threads of one column share
-// its pieces, a run each, and thread 0's adds up the runs.
-constexpr int kJoinGroups = 16, kJoinRuns = kBlock / kJoinGroups;
+// its pieces, a run each, and the runs' sums are added up in halves.
+constexpr int kJoinMostGroups = 4;   // log2 of the groups of columns of a workgroup, at most
 constexpr uint32_t kJoinSlots = 16;
 
 template <int OUT>
-__global__ __launch_bounds__(kBlock) void join_pieces(GradArgs a, Plan p, uint32_t tiles_x) {
-    __shared__ float runs[kJoinRuns][kJoinGroups][8];
+__global__ __launch_bounds__(kBlock) void join_pieces(GradArgs a, Plan p, int lx, uint32_t tiles_x) {
+    __shared__ float runs[kBlock][8];
     const char *ws = static_cast<const char *>(a.workspace);
     const Piece *list = reinterpret_cast<const Piece *>(ws + p.pieces_at);
     const float *sums = reinterpret_cast<const float *>(ws + p.sums_at);
-    const int g = threadIdx.x % kJoinGroups, run = threadIdx.x / kJoinGroups;
-    const uint32_t group = blockIdx.x % tiles_x * kJoinGroups + g;
+    const uint32_t run = threadIdx.x >> lx, n_runs = kBlock >> lx;
+    const uint32_t group = (blockIdx.x % tiles_x << lx) + (threadIdx.x & ((1u << lx) - 1));
     const uint64_t col = 8ull * group;
     const int columns = col >= a.dim ? 0 : a.dim - col < 8 ? static_cast<int>(a.dim - col) : 8;
     const uint32_t slot = blockIdx.x / tiles_x * kJoinSlots, lane = threadIdx.x & 63;
@@ -380,7 +403,7 @@ __global__ __launch_bounds__(kBlock) void join_pieces(GradArgs a, Plan p, uint32
     for (uint64_t todo = __ballot(mine != 0); todo != 0; todo &= todo - 1) {   // the same for all waves
         const int first = __ffsll(static_cast<unsigned long long>(todo)) - 1;
         const uint32_t y = slot + first, of = __builtin_amdgcn_readlane(mine, first);
-        const uint32_t each = (of + kJoinRuns - 1) / kJoinRuns;
+        const uint32_t each = (of + n_runs - 1) / n_runs;
         const uint32_t from = min(run * each, of), to = min(from + each, of);
         float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
         if (columns != 0) {
@@ -395,16 +418,16 @@ __global__ __launch_bounds__(kBlock) void join_pieces(GradArgs a, Plan p, uint32
             }
         }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) runs[run][g][e] = sum[e];
+        for (int e = 0; e < 8; ++e) runs[threadIdx.x][e] = sum[e];
         __syncthreads();
-        if (run == 0 && columns != 0) {
-            const int used = static_cast<int>((of + each - 1) / each);
-            for (int r = 1; r < used; ++r)
+        for (uint32_t half = n_runs / 2; half != 0; half /= 2) {
+            if (run < half) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sum[e] += runs[r][g][e];
-            write_row<OUT>(a, sum, list[y].row, group, columns);
+                for (int e = 0; e < 8; ++e) runs[threadIdx.x][e] = sum[e] += runs[threadIdx.x + (half << lx)][e];
+            }
+            __syncthreads();
         }
-        __syncthreads();
+        if (run == 0 && columns != 0) write_row<OUT>(a, sum, list[y].row, group, columns);
     }
 }
 
@@ -565,8 +588,9 @@ hipError_t launch_sums(const GradArgs &a, const Plan &p, hipStream_t s) {
         sum_rows<G, OUT, false><<<static_cast<uint32_t>(blocks), kBlock, 0, s>>>(a, p, lx, tiles_x, pb, past);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.pieces == 0) return e;
-    const uint32_t join_x = static_cast<uint32_t>((groups + kJoinGroups - 1) / kJoinGroups);
-    join_pieces<OUT><<<(p.pieces + kJoinSlots - 1) / kJoinSlots * join_x, kBlock, 0, s>>>(a, p, join_x);
+    const int join_lx = std::min(lx, kJoinMostGroups);
+    const uint32_t join_x = static_cast<uint32_t>((groups + (1ull << join_lx) - 1) >> join_lx);
+    join_pieces<OUT><<<(p.pieces + kJoinSlots - 1) / kJoinSlots * join_x, kBlock, 0, s>>>(a, p, join_lx, join_x);
     return hipGetLastError();
 }
 
