@@ -678,48 +678,62 @@ __global__ __launch_bounds__(256) void empty(MatmulArgs g) {
 // 32 x 4096 x 9216 22 us with either kernel, 64 x 4096 x 9216 25 with tiles and 31 with slim
 constexpr uint32_t kSlimRows = 32;
 
+// Bytes of sums of parts where whole tiles fill the card too.
+constexpr uint64_t kMostSums = uint64_t(1) << 26;
+
 struct Choice {
     int bm, bn;
     Split split;
 };
 
-// Large tiles read LDS and the caches least, small ones lose less where tiles are few or k is short: a compute
-// unit has one large tile at a time, or two small ones, which cover each other's first loads and last stores. In us, a
-// round of tiles takes so much, and so much more a block of k (fitted to 170 products of random sizes from
-// 512 x 512 x 64 to 16384 x 25088 x 16384). By it the products took 0.6% longer than with the better of both (0.3%
-// to fp32); with large tiles wherever there are 256 of them 9% (15%), always with small ones 10% (0.4%; but
-// 5% for 4096 x 4096 x 16384).
-bool takes_big(uint64_t m, uint64_t n, uint64_t blocks, bool wide) {
-    const uint64_t big = (m + 255) / 256 * ((n + (wide ? 127 : 255)) / (wide ? 128 : 256));
-    const uint64_t small = (m + 127) / 128 * ((n + 127) / 128);
-    if (small <= kCus) return false;   // k is split then
-    const double big_rounds = static_cast<double>((big + kCus - 1) / kCus);
-    const double whole = static_cast<double>((small + 2 * kCus - 1) / (2 * kCus));
-    // the last round of small tiles, if it is not full, has each compute unit to itself
-    const double small_rounds = std::max(1.0, (whole + static_cast<double>(small) / (2 * kCus)) / 2);
-    const double k = static_cast<double>(blocks);
-    return wide ? big_rounds * (8.0 + 1.5 * k) < small_rounds * (6.8 + 1.57 * k)
-                : big_rounds * (11.5 + 1.28 * k) < small_rounds * (4.2 + 1.14 * k);
+// What a product takes, in us, by rounds of tiles: a compute unit has one large tile at a time, or two small ones, which
+// cover each other's first loads and last stores; the last ones of many take less, as some have a compute unit each.
+// Fitted to 170 products of random sizes from 512 x 512 x 64 to 16384 x 25088 x 16384.
+double tiles_take(uint64_t m, uint64_t n, uint64_t blocks, bool wide, bool large, uint64_t parts) {
+    const uint64_t bm = large ? 256 : 128, bn = large && !wide ? 256 : 128;
+    const uint64_t units = (m + bm - 1) / bm * ((n + bn - 1) / bn) * parts, at_once = large ? kCus : 2 * kCus;
+    const uint64_t rounds = units / at_once, rest = units % at_once;
+    const double k = static_cast<double>((blocks + parts - 1) / parts);
+    const double start = large ? (wide ? 8.0 : 11.5) : wide ? 6.8 : 4.2;
+    const double block = large ? (wide ? 1.5 : 1.28) : wide ? 1.57 : 1.14, alone = wide ? 0.91 : 0.65;
+    double us = static_cast<double>(rounds) * (start + block * k);
+    if (large) us += rest != 0 ? start + block * k : 0.0;
+    else if (rounds == 0) us += start + (rest <= kCus ? alone : block) * k;
+    else if (rest != 0) us += (start + block * k) * (0.5 + 0.5 * static_cast<double>(rest) / static_cast<double>(at_once));
+    if (parts > 1) us += 4.0 + static_cast<double>(parts * m * n) * 8 / 5e6;   // the parts' sums, written and read
+    return us;
 }
 
 // For more than kSlimRows rows of a.
 Choice choose(uint64_t m, uint64_t n, uint64_t k, bool wide) {
     Choice c{};
-    const uint64_t blocks = (k + 127) / 128;
-    if (takes_big(m, n, blocks, wide)) {
-        c.bm = 256;
-        c.bn = wide ? 128 : 256;
+    const uint64_t blocks = (k + 127) / 128, small = (m + 127) / 128 * ((n + 127) / 128);
+    bool large = false;
+    uint64_t parts = 1;
+    if (small <= kCus / 2) {
+        // parts of k until every compute unit has a workgroup, of four blocks at least, or of eight where
+        // the tiles are many (57 x 900 x 1000, 8 tiles: 10.2 us with parts of four, 13.1 whole; 1000 x
+        // 1000 x 1000, 64 tiles: 13.1 and 10.5)
+        parts = std::min(kCus / small, std::max<uint64_t>(1, blocks / (small < 32 ? 4 : 8)));
     } else {
-        c.bm = c.bn = 128;
+        // Large tiles read LDS and the caches least, small ones lose less where tiles are few or k is
+        // short; parts fill the last round (1280 x 4096 x 22272 195 us whole and 113 in parts, 256 x 21248 x
+        // 24320 275 and 168). Over the fitted sizes, large tiles wherever there are 256 of them took 9%
+        // longer than the better of both (15% to fp32), this rule 0.6%.
+        double least = tiles_take(m, n, blocks, wide, false, 1);
+        for (uint64_t p = 1; p <= 8 && (p == 1 || (blocks / p >= 8 && p * m * n * 4 <= kMostSums)); ++p)
+            for (const bool l : {false, true}) {
+                const double us = tiles_take(m, n, blocks, wide, l, p);
+                if (us >= least) continue;
+                least = us;
+                large = l;
+                parts = p;
+            }
     }
+    c.bm = large ? 256 : 128;
+    c.bn = large && !wide ? 256 : 128;
     c.split.tiles_m = static_cast<uint32_t>((m + c.bm - 1) / c.bm);
     c.split.tiles_n = static_cast<uint32_t>((n + c.bn - 1) / c.bn);
-    // parts of k until every compute unit has a workgroup
-    const uint64_t tiles = static_cast<uint64_t>(c.split.tiles_m) * c.split.tiles_n;
-    uint64_t parts = std::max<uint64_t>(1, kCus / tiles);
-    // of four blocks at least, or of eight where the tiles are many (57 x 900 x 1000, 8 tiles: 10.2 us
-    // with parts of four, 13.1 whole; 1000 x 1000 x 1000, 64 tiles: 13.1 and 10.5)
-    parts = std::min(parts, std::max<uint64_t>(1, blocks / (tiles < 32 ? 4 : 8)));
     c.split.steps = static_cast<uint32_t>((blocks + parts - 1) / parts);
     if (parts > 1) c.split.steps += c.split.steps & 1;   // blocks go in twos
     c.split.parts = static_cast<uint32_t>((blocks + c.split.steps - 1) / c.split.steps);

@@ -337,7 +337,7 @@ def integers(torch, g, rows, cols):
 SIZES = [(1, 1, 1), (1, 16, 128), (1, 1000, 4096), (1, 70, 17_000), (2, 33, 700), (9, 33, 8193),
          (16, 130, 1024), (17, 64, 129), (32, 515, 12_345), (33, 100, 513), (64, 257, 3000), (65, 129, 128),
          (100, 1000, 900), (128, 128, 2048), (129, 300, 640), (257, 255, 1280), (300, 520, 8200),
-         (4100, 4099, 257), (4090, 4090, 3000)]
+         (4100, 4099, 257), (4090, 4090, 3000), (1277, 4090, 9001), (1000, 2000, 2300)]
 
 
 @pytest.mark.parametrize("m,n,k", SIZES)
