@@ -21,8 +21,8 @@
 // (sum_few).
 //
 // Bound by memory: grad is read once and out written once, rows without tokens included. 65536
-// tokens of 4096 bf16 columns into 65536 fp32 rows, with dropout (1.6 GB): 360 us, of which sort 26,
-// sum 320 (5 TB/s) and join 12; 1824 tokens of 100 fp32 columns into 50000 rows in one launch of 14.
+// tokens of 4096 bf16 columns into 65536 fp32 rows, with dropout (1.6 GB): 362 us, of which sort 28,
+// sum 333 (4.9 TB/s) and join 13; 1824 tokens of 100 fp32 columns into 50000 rows in one launch of 14.
 #include <algorithm>
 
 #include "pl_device.h"
@@ -65,10 +65,10 @@ Plan make_plan(int64_t tokens, int64_t vocab, int64_t dim) {
     while (((vocab - 1) >> p.class_bits) >= kMaxLocal) ++p.class_bits;
     p.classes = 1u << p.class_bits;
     p.local = static_cast<uint32_t>((vocab + p.classes - 1) >> p.class_bits);
-    // One token after another is latency (with dropout 0.5 us each), and pieces are traffic of
-    // their own: 1824 tokens of 100 columns took 25 us with pieces of 8, 29 of 16, 32 of 32;
-    // 65536 of 4096 478, 419 and 400, and 402 with pieces of 64.
-    p.piece = tokens * dim <= (int64_t(1) << 22) ? 8 : 32;
+    // One token after another is latency, and pieces are traffic of their own. In us, with dropout, with pieces
+    // of 8 and of 32: 65536 tokens of 100 columns 64 and 75, 32768 of 1000 70 and 73, 65536 of 1200 147 and
+    // 126, 65536 of 4096 409 and 364 (of 64 360).
+    p.piece = tokens * dim < (int64_t(1) << 25) ? 8 : 32;
     // a row with c > piece tokens has ceil(c / piece) < 2 c / piece pieces
     p.pieces = tokens <= p.piece ? 0 : static_cast<uint32_t>(2 * tokens / p.piece);
     p.rows_at = 0;
@@ -563,9 +563,9 @@ hipError_t launch_few_typed(const GradArgs &a, int grad_dtype, int out_dtype, hi
     return out_dtype == PS_F32 ? launch_few<IDT, PS_BF16, PS_F32>(a, s) : launch_few<IDT, PS_BF16, PS_BF16>(a, s);
 }
 
-// Every workgroup reads all ids, and rows with many tokens are taken one after the other. In us, in one
-// launch and in three: 2048 tokens of 100 columns into 50000 rows 14 and 25, of 512 into 30000 21 and 30,
-// 4096 of 1024 into 30000 34 and 42; but of 4096 into 30000 163 and 126, and 4096 of 64 into 1000 29 and 21.
+// Every workgroup reads all ids, and rows with many tokens are taken one after the other. In us, with dropout, in
+// one launch and in three: 1824 tokens of 100 columns into 50000 rows 14 and 22, 2048 of 512 into 30000 21 and
+// 27, 4096 of 1024 into 30000 36 and 36; but of 4096 into 30000 161 and 103, and 4096 of 64 into 1000 30 and 17.
 bool few(int64_t tokens, int64_t vocab, int64_t dim) {
     return tokens <= int64_t(kSmallTokens) && tokens <= vocab && dim <= 1024;
 }
@@ -596,9 +596,8 @@ hipError_t launch_sums(const GradArgs &a, const Plan &p, hipStream_t s) {
 
 template <int IDT>
 void launch_sort(const GradArgs &a, const Plan &p, Row *rows, uint32_t *perm, Piece *pieces, hipStream_t s) {
-    // More waves share the ids of a workgroup, and take longer to start and to be brought together:
-    // the whole call over 4096 ids took 25.8 us with four waves and 27.5 with sixteen, over 8192 ids
-    // 31.5 and 30.4, over 16384 43 and 36.
+    // More waves share the ids of a workgroup, and take longer to start and to be brought together: in us, with
+    // four waves and with sixteen, 2048 ids 17.3 and 18.7, 4096 19.2 and 19.0, 8192 29.3 and 25.7.
     if (a.tokens <= 4096) sort_tokens<IDT, 4, true><<<p.classes, 256, 0, s>>>(a.ids, a.tokens, a.vocab, p, rows, perm, pieces);
     else if (a.tokens <= kNoted) sort_tokens<IDT, 16, true><<<p.classes, 1024, 0, s>>>(a.ids, a.tokens, a.vocab, p, rows, perm, pieces);
     else sort_tokens<IDT, 16, false><<<p.classes, 1024, 0, s>>>(a.ids, a.tokens, a.vocab, p, rows, perm, pieces);

@@ -2,10 +2,10 @@
 //
 // Mathematics: out[r, c] = keep(r, c) * factor * x[src(r), c], src(r) = r or ids[r].
 // Bound by memory: every element is read once and written once. A thread takes eight
-// consecutive columns (one evaluation of the generator gives their eight 16-bit
-// numbers: 20 wide products and 60 other instructions, 3 a column, which the memory's time
-// covers) of one row or four, whose loads are issued together. Dropout of 16384 x 8192 bf16:
-// 80 us, 6.7 TB/s of reads and writes; of 16384 x 4096 fp32 78 us, 6.9 TB/s.
+// consecutive columns (one evaluation of the generator, 20 wide products, gives their eight
+// 16-bit numbers; the memory's time covers it) of one row or four, whose loads are issued
+// together. Dropout of 16384 x 8192 bf16: 80 us, 6.7 TB/s of reads and writes; of 16384 x 4096
+// fp32 78 us, 6.9 TB/s.
 #include "pl_device.h"
 
 namespace gadei::learner {
