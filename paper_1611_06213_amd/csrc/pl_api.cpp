@@ -262,8 +262,8 @@ int pl_quantize_fp8(const void *x, int dtype, int64_t rows, int64_t cols, int64_
 
 namespace {
 
-MatmulArgs product(int64_t m, int64_t n, int64_t k, const pl_fp8 *a, const pl_fp8 *b, void *out, int64_t out_ld,
-                   void *workspace) {
+MatmulArgs product(int64_t m, int64_t n, int64_t k, const pl_fp8 *a, const pl_fp8 *b, void *out,
+                   int64_t out_ld, void *workspace) {
     MatmulArgs g{};
     g.a = static_cast<const uint8_t *>(a->values);
     g.b = static_cast<const uint8_t *>(b->values);
@@ -429,7 +429,8 @@ int pl_linear_fp8_grad(const void *x, int x_dtype, int64_t x_ld, const void *gra
     auto at = [ws](size_t values, size_t scales) {
         return pl_fp8{ws + values, reinterpret_cast<uint32_t *>(ws + scales)};
     };
-    const pl_fp8 g = at(r.g_values, r.g_scales), t = at(r.t_values, r.t_scales), xt = at(r.x_values, r.x_scales);
+    const pl_fp8 g = at(r.g_values, r.g_scales), t = at(r.t_values, r.t_scales);
+    const pl_fp8 xt = at(r.x_values, r.x_scales);
     hipStream_t s = static_cast<hipStream_t>(stream);
     QuantArgs qg{}, qx{};
     qg.x = grad;
@@ -454,7 +455,8 @@ int pl_linear_fp8_grad(const void *x, int x_dtype, int64_t x_ld, const void *gra
         if (int rc = launched(launch_quantize_two(qx, QuantArgs{}, x_dtype, false, s), what)) return rc;
     }
     MatmulArgs p = product(m, k, n, &g, w_t, out, out_ld, r.out_bytes ? ws + r.out : nullptr);
-    MatmulArgs pw = product(n, k, m, &t, &xt, weight_out, weight_ld, r.weight_bytes ? ws + r.weight : nullptr);
+    MatmulArgs pw = product(n, k, m, &t, &xt, weight_out, weight_ld,
+                            r.weight_bytes ? ws + r.weight : nullptr);
     pw.accumulate = accumulate != 0;
     if (pairs(p, out_dtype, pw, weight_dtype))
         return launched(launch_matmul_two(p, out_dtype, pw, weight_dtype, s), what);

@@ -65,9 +65,9 @@ Plan make_plan(int64_t tokens, int64_t vocab, int64_t dim) {
     while (((vocab - 1) >> p.class_bits) >= kMaxLocal) ++p.class_bits;
     p.classes = 1u << p.class_bits;
     p.local = static_cast<uint32_t>((vocab + p.classes - 1) >> p.class_bits);
-    // One token after another is latency, and pieces are traffic of their own. In us, with dropout, with pieces
-    // of 8 and of 32: 65536 tokens of 100 columns 64 and 75, 32768 of 1000 70 and 73, 65536 of 1200 147 and
-    // 126, 65536 of 4096 409 and 364 (of 64 360).
+    // One token after another is latency, and pieces are traffic of their own. In us, with dropout,
+    // with pieces of 8 and of 32: 65536 tokens of 100 columns 64 and 75, 32768 of 1000 70 and 73,
+    // 65536 of 1200 147 and 126, 65536 of 4096 409 and 364 (of 64 360).
     p.piece = tokens * dim < (int64_t(1) << 25) ? 8 : 32;
     // a row with c > piece tokens has ceil(c / piece) < 2 c / piece pieces
     p.pieces = tokens <= p.piece ? 0 : static_cast<uint32_t>(2 * tokens / p.piece);
@@ -134,16 +134,19 @@ __device__ __forceinline__ void each_id(const void *ids, uint32_t tokens, uint32
     }
 }
 
-// Puts the positions of some of a wave's lanes (those with a bit in `todo`, one at least) where the next ones of
-// their ids belong; next[local] is where, and moves on. The lanes of an id, its rank among them and
-// how many they are come from ballots, one id after the other; LDS is asked for all ids at once.
-__device__ __forceinline__ void put(uint32_t *next, uint32_t *list, uint64_t todo, uint32_t local, uint32_t position, int lane) {
+// Puts the positions of some of a wave's lanes (those with a bit in `todo`, one at least) where the
+// next ones of their ids belong; next[local] is where, and moves on. The lanes of an id, its rank
+// among them and how many they are come from ballots, one id after the other; LDS is asked for all
+// ids at once.
+__device__ __forceinline__ void put(uint32_t *next, uint32_t *list, uint64_t todo, uint32_t local,
+                                    uint32_t position, int lane) {
     const bool mine = todo >> lane & 1;
     uint32_t rank = 0, many = 0;
     int first = lane;
     while (todo) {
         const int f = __ffsll(static_cast<unsigned long long>(todo)) - 1;
-        const uint64_t lanes = todo & __ballot(local == static_cast<uint32_t>(__builtin_amdgcn_readlane(local, f)));
+        const uint32_t one = __builtin_amdgcn_readlane(local, f);
+        const uint64_t lanes = todo & __ballot(local == one);
         if (lanes >> lane & 1) {
             rank = __popcll(lanes & ((1ull << lane) - 1));
             many = __popcll(lanes);
@@ -163,10 +166,12 @@ struct LongRow {
 };
 constexpr uint32_t kLongRows = 64;   // of a class, whose pieces all threads write
 
-__device__ __forceinline__ void write_pieces(const LongRow &r, uint32_t piece, Piece *pieces, uint32_t i, uint32_t step) {
+__device__ __forceinline__ void write_pieces(const LongRow &r, uint32_t piece, Piece *pieces, uint32_t i,
+                                             uint32_t step) {
     const uint32_t n = (r.count + piece - 1) / piece;
     for (; i < n; i += step)
-        pieces[r.slot + i] = Piece{r.row, r.begin + i * piece, min(piece, r.count - i * piece), i == 0 ? n : 0};
+        pieces[r.slot + i] =
+            Piece{r.row, r.begin + i * piece, min(piece, r.count - i * piece), i == 0 ? n : 0};
 }
 
 // WAVES waves; a thread does the bookkeeping of kMaxLocal / (64 WAVES) ids.
@@ -177,7 +182,8 @@ __global__ __launch_bounds__(64 * WAVES) void sort_tokens(const void *ids, uint3
     using Id = typename IdBits<IDT>::type;
     constexpr int kEach = kMaxLocal / (64 * WAVES);
     __shared__ uint32_t counts[WAVES][kMaxLocal];   // of each wave's part of the ids
-    __shared__ uint32_t found[WAVES][NOTED ? kMaxFound : 1];   // tokens of the class, in order: local id, place in the part
+    // tokens of the class, in order: id in the class, place in the part
+    __shared__ uint32_t found[WAVES][NOTED ? kMaxFound : 1];
     __shared__ uint32_t wave_sums[WAVES];
     __shared__ LongRow longs[kLongRows];
     __shared__ uint32_t n_longs;
@@ -202,12 +208,14 @@ __global__ __launch_bounds__(64 * WAVES) void sort_tokens(const void *ids, uint3
         if (hits == 0) return;
         // many of one id are one addition: LDS would take them one after another
         const int leader = __ffsll(static_cast<unsigned long long>(hits)) - 1;
-        const uint64_t alike = NOTED ? hits & __ballot(low == static_cast<uint32_t>(__builtin_amdgcn_readlane(low, leader))) : 0;
+        const uint32_t leads = __builtin_amdgcn_readlane(low, leader);
+        const uint64_t alike = NOTED ? hits & __ballot(low == leads) : 0;
         if (hit) {
-            if (!(alike >> lane & 1)) atomicAdd(&counts[wave][low >> class_bits], 1u);
-            else if (lane == leader) atomicAdd(&counts[wave][low >> class_bits], static_cast<uint32_t>(__popcll(alike)));
+            const uint32_t n = alike >> lane & 1 ? static_cast<uint32_t>(__popcll(alike)) : 1u;
+            if (n == 1 || lane == leader) atomicAdd(&counts[wave][low >> class_bits], n);
             const uint32_t i = n_found + __popcll(hits & ((1ull << lane) - 1));
-            if (NOTED && i < kMaxFound) found[wave][i] = (low >> class_bits) << kPlaceBits | ((step - first) * 64 + lane);
+            if (NOTED && i < kMaxFound)
+                found[wave][i] = (low >> class_bits) << kPlaceBits | ((step - first) * 64 + lane);
         }
         n_found += __popcll(hits);
     });
@@ -254,14 +262,15 @@ __global__ __launch_bounds__(64 * WAVES) void sort_tokens(const void *ids, uint3
         }
     }
     __syncthreads();
-    for (uint32_t i = 0; i < min(n_longs, kLongRows); ++i) write_pieces(longs[i], p.piece, pieces, threadIdx.x, 64 * WAVES);
+    for (uint32_t i = 0; i < min(n_longs, kLongRows); ++i)
+        write_pieces(longs[i], p.piece, pieces, threadIdx.x, 64 * WAVES);
     if (p.pieces != 0) {
         const uint32_t to = mine == mask ? p.pieces : static_cast<uint32_t>(2ull * (base + total) / p.piece);
         for (uint32_t i = from + used + threadIdx.x; i < to; i += 64 * WAVES) pieces[i] = Piece{0, 0, 0, 0};
     }
 
-    // Positions into their places, in order within a wave's part: those that were written down, or, where they
-    // were too many (in a frequent id's class), found again.
+    // Positions into their places, in order within a wave's part: those that were written down, or,
+    // where they were too many (in a frequent id's class), found again.
     if (total == 0) return;
     if (NOTED && n_found <= kMaxFound) {
         for (uint32_t i = 0; i < n_found; i += 64) {
@@ -275,7 +284,8 @@ __global__ __launch_bounds__(64 * WAVES) void sort_tokens(const void *ids, uint3
         const uint32_t low = static_cast<uint32_t>(id);
         uint64_t todo = __ballot(id < vocab && (low & mask) == mine);
         while (todo) {   // one id after the other: all its lanes at once
-            const uint32_t one = __builtin_amdgcn_readlane(low, __ffsll(static_cast<unsigned long long>(todo)) - 1);
+            const int f = __ffsll(static_cast<unsigned long long>(todo)) - 1;
+            const uint32_t one = __builtin_amdgcn_readlane(low, f);
             const uint64_t lanes = todo & __ballot(low == one);
             const uint32_t at = counts[wave][one >> class_bits];
             if (lanes >> lane & 1)
@@ -423,7 +433,10 @@ __global__ __launch_bounds__(kBlock) void join_pieces(GradArgs a, Plan p, int lx
         for (uint32_t half = n_runs / 2; half != 0; half /= 2) {
             if (run < half) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) runs[threadIdx.x][e] = sum[e] += runs[threadIdx.x + (half << lx)][e];
+                for (int e = 0; e < 8; ++e) {
+                    sum[e] += runs[threadIdx.x + (half << lx)][e];
+                    runs[threadIdx.x][e] = sum[e];
+                }
             }
             __syncthreads();
         }
@@ -433,8 +446,8 @@ __global__ __launch_bounds__(kBlock) void join_pieces(GradArgs a, Plan p, int lx
 
 // Few tokens and narrow rows: everything in one launch. A workgroup takes kSmallRows rows of the
 // table and up to 128 columns; it reads all ids and lists its rows' tokens in LDS, in order, as
-// sort_tokens does. A row of more than kSmallAlone tokens is shared by all threads of a column, a run of its
-// tokens each, and their sums are added up in order.
+// sort_tokens does. A row of more than kSmallAlone tokens is shared by all threads of a column, a
+// run of its tokens each, and their sums are added up in order.
 constexpr uint32_t kSmallTokens = 4096, kSmallRows = 64, kSmallAlone = 4;
 constexpr int kSmallWaves = kBlock / 64;
 
@@ -502,10 +515,12 @@ __global__ __launch_bounds__(kBlock) void sum_few(GradArgs a, int lx, uint32_t t
     for (int j = 0; j < kSteps; ++j) {
         uint64_t todo = __ballot(row[j] < kSmallRows);
         while (todo) {   // one row after the other: all its lanes at once
-            const uint32_t one = __builtin_amdgcn_readlane(row[j], __ffsll(static_cast<unsigned long long>(todo)) - 1);
+            const int f = __ffsll(static_cast<unsigned long long>(todo)) - 1;
+            const uint32_t one = __builtin_amdgcn_readlane(row[j], f);
             const uint64_t lanes = todo & __ballot(row[j] == one);
             const uint32_t at = counts[wave][one];
-            if (lanes >> lane & 1) list[at + __popcll(lanes & ((1ull << lane) - 1))] = 64 * (first + j) + lane;
+            if (lanes >> lane & 1)
+                list[at + __popcll(lanes & ((1ull << lane) - 1))] = 64 * (first + j) + lane;
             counts[wave][one] = at + __popcll(lanes);   // all lanes alike
             todo &= ~lanes;
         }
@@ -525,7 +540,8 @@ __global__ __launch_bounds__(kBlock) void sum_few(GradArgs a, int lx, uint32_t t
     for (uint64_t todo = shared_rows; todo != 0; todo &= todo - 1) {   // the same for the whole workgroup
         const uint32_t r = __ffsll(static_cast<unsigned long long>(todo)) - 1;
         const uint32_t begin = begins[r], count = begins[r + 1] - begin;
-        const uint32_t each = (count + ny - 1) / ny, from = min(y * each, count), to = min(from + each, count);
+        const uint32_t each = (count + ny - 1) / ny;
+        const uint32_t from = min(y * each, count), to = min(from + each, count);
         float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
         if (columns != 0) add_tokens<G, DROP>(sum, a, list + begin + from, to - from, group, columns);
 #pragma unroll
@@ -559,13 +575,16 @@ hipError_t launch_few(const GradArgs &a, hipStream_t s) {
 template <int IDT>
 hipError_t launch_few_typed(const GradArgs &a, int grad_dtype, int out_dtype, hipStream_t s) {
     if (grad_dtype == PS_F32)
-        return out_dtype == PS_F32 ? launch_few<IDT, PS_F32, PS_F32>(a, s) : launch_few<IDT, PS_F32, PS_BF16>(a, s);
-    return out_dtype == PS_F32 ? launch_few<IDT, PS_BF16, PS_F32>(a, s) : launch_few<IDT, PS_BF16, PS_BF16>(a, s);
+        return out_dtype == PS_F32 ? launch_few<IDT, PS_F32, PS_F32>(a, s)
+                                   : launch_few<IDT, PS_F32, PS_BF16>(a, s);
+    return out_dtype == PS_F32 ? launch_few<IDT, PS_BF16, PS_F32>(a, s)
+                               : launch_few<IDT, PS_BF16, PS_BF16>(a, s);
 }
 
-// Every workgroup reads all ids, and rows with many tokens are taken one after the other. In us, with dropout, in
-// one launch and in three: 1824 tokens of 100 columns into 50000 rows 14 and 22, 2048 of 512 into 30000 21 and
-// 27, 4096 of 1024 into 30000 36 and 36; but of 4096 into 30000 161 and 103, and 4096 of 64 into 1000 30 and 17.
+// Every workgroup reads all ids, and rows with many tokens are taken one after the other. In us,
+// with dropout, in one launch and in three: 1824 tokens of 100 columns into 50000 rows 14 and 22,
+// 2048 of 512 into 30000 21 and 27, 4096 of 1024 into 30000 36 and 36; but of 4096 into 30000 161
+// and 103, and 4096 of 64 into 1000 30 and 17.
 bool few(int64_t tokens, int64_t vocab, int64_t dim) {
     return tokens <= int64_t(kSmallTokens) && tokens <= vocab && dim <= 1024;
 }
@@ -590,17 +609,21 @@ hipError_t launch_sums(const GradArgs &a, const Plan &p, hipStream_t s) {
     if (e != hipSuccess || p.pieces == 0) return e;
     const int join_lx = std::min(lx, kJoinMostGroups);
     const uint32_t join_x = static_cast<uint32_t>((groups + (1ull << join_lx) - 1) >> join_lx);
-    join_pieces<OUT><<<(p.pieces + kJoinSlots - 1) / kJoinSlots * join_x, kBlock, 0, s>>>(a, p, join_lx, join_x);
+    const uint32_t join_blocks = (p.pieces + kJoinSlots - 1) / kJoinSlots * join_x;
+    join_pieces<OUT><<<join_blocks, kBlock, 0, s>>>(a, p, join_lx, join_x);
     return hipGetLastError();
 }
 
 template <int IDT>
 void launch_sort(const GradArgs &a, const Plan &p, Row *rows, uint32_t *perm, Piece *pieces, hipStream_t s) {
-    // More waves share the ids of a workgroup, and take longer to start and to be brought together: in us, with
-    // four waves and with sixteen, 2048 ids 17.3 and 18.7, 4096 19.2 and 19.0, 8192 29.3 and 25.7.
-    if (a.tokens <= 4096) sort_tokens<IDT, 4, true><<<p.classes, 256, 0, s>>>(a.ids, a.tokens, a.vocab, p, rows, perm, pieces);
-    else if (a.tokens <= kNoted) sort_tokens<IDT, 16, true><<<p.classes, 1024, 0, s>>>(a.ids, a.tokens, a.vocab, p, rows, perm, pieces);
-    else sort_tokens<IDT, 16, false><<<p.classes, 1024, 0, s>>>(a.ids, a.tokens, a.vocab, p, rows, perm, pieces);
+    // More waves share the ids of a workgroup, and take longer to start and to be brought together:
+    // in us, with four waves and with sixteen, 2048 ids 17.3 and 18.7, 4096 19.2 and 19.0, 8192
+    // 29.3 and 25.7.
+    const uint32_t n = a.tokens, v = a.vocab;
+    if (n <= 4096) sort_tokens<IDT, 4, true><<<p.classes, 256, 0, s>>>(a.ids, n, v, p, rows, perm, pieces);
+    else if (n <= kNoted)
+        sort_tokens<IDT, 16, true><<<p.classes, 1024, 0, s>>>(a.ids, n, v, p, rows, perm, pieces);
+    else sort_tokens<IDT, 16, false><<<p.classes, 1024, 0, s>>>(a.ids, n, v, p, rows, perm, pieces);
 }
 
 }  // namespace

@@ -83,7 +83,8 @@ size_t matmul_workspace(int64_t m, int64_t n, int64_t k, int out_dtype);
 hipError_t launch_matmul(const MatmulArgs &a, int out_dtype, hipStream_t s);
 // Whether two products go in one launch: small ones, whose workgroups all run at once.
 bool pairs(const MatmulArgs &a, int a_dtype, const MatmulArgs &b, int b_dtype);
-hipError_t launch_matmul_two(const MatmulArgs &a, int a_dtype, const MatmulArgs &b, int b_dtype, hipStream_t s);
+hipError_t launch_matmul_two(const MatmulArgs &a, int a_dtype, const MatmulArgs &b, int b_dtype,
+                             hipStream_t s);
 // Whether the product of m x k numbers not yet in 8-bit form is one launch, which needs no a, sa or
 // workspace.
 bool converts(int64_t m, int64_t n, int64_t k);

@@ -173,7 +173,8 @@ struct Buffer {
     __amdgpu_buffer_rsrc_t rsrc;
     Buffer() = default;
     __device__ __forceinline__ Buffer(const void *p, uint32_t bytes)
-        : rsrc(__builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, static_cast<int>(bytes), 0x27000)) {}
+        : rsrc(__builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, static_cast<int>(bytes),
+                                                 0x27000)) {}
     static constexpr uint32_t kOutside = 0x80000000u;   // of every buffer
     // 16 bytes a lane, to LDS at 16 bytes a lane
     __device__ __forceinline__ void to_lds(uint8_t *to, uint32_t lane, uint32_t shared) const {
@@ -206,8 +207,9 @@ struct Products {
 // ------------------------------------------------------------------- tiles
 
 // Which tile of which part of k the work unit `unit` is. Workgroups go round the eight XCDs, each
-// with an L2 of its own: an XCD takes a contiguous run of an order that walks bands of eight rows of tiles column by
-// column, so that the 32 tiles that its compute units work on share their rows of a and b.
+// with an L2 of its own: an XCD takes a contiguous run of an order that walks bands of eight rows
+// of tiles column by column, so that the 32 tiles that its compute units work on share their rows
+// of a and b.
 __device__ __forceinline__ void place(const Split &sp, uint32_t unit, uint32_t *tile_m, uint32_t *tile_n,
                                       uint32_t *part) {
     constexpr uint32_t kXcds = 8, kBand = 8;
@@ -223,11 +225,12 @@ __device__ __forceinline__ void place(const Split &sp, uint32_t unit, uint32_t *
 
 // Tiles of 64 FM x 64 FN by 2 x 2 waves, each FM x FN instructions of 32 x 32.
 //
-// Bound by the matrix pipes and, at large sizes, by power: the clock falls from 2.4 to 1.75 GHz, and
-// the same product of zeros takes three quarters of the time. 8192^3 to bf16 takes 424 to 510 us (2.2
-// to 2.6 PFLOP/s), 16384 x 4096 x 4096 230 (2.4), and to fp32, by bf16 instructions, 460 (1.2). A step of 256 x
-// 256 tiles reads half of what four 128 x 128 tiles read from LDS (8192^3 took 690 us with those), and
-// 256 x 128, for fp32 results, leaves registers for the operands in bf16.
+// Bound by the matrix pipes and, at large sizes, by power: the clock falls from 2.4 to 1.75 GHz,
+// and the same product of zeros takes three quarters of the time. 8192^3 to bf16 takes 424 to 510
+// us (2.2 to 2.6 PFLOP/s), 16384 x 4096 x 4096 230 (2.4), and to fp32, by bf16 instructions, 460
+// (1.2). A step of 256 x 256 tiles reads half of what four 128 x 128 tiles read from LDS (8192^3
+// took 690 us with those), and 256 x 128, for fp32 results, leaves registers for the operands in
+// bf16.
 //
 // A step is half a block, 64 columns. LDS holds four steps of either operand, which copies bring
 // there from memory without registers; the registers hold the step that multiplies and the
@@ -235,9 +238,10 @@ __device__ __forceinline__ void place(const Split &sp, uint32_t unit, uint32_t *
 // and the copies have three steps to arrive: at the end of a step only those of the one
 // before the last are waited for.
 template <int FM, int FN, int OUT>
-__device__ __forceinline__ void take_units(const MatmulArgs &g, const Split &sp, uint32_t unit, uint32_t stride,
-                                           uint8_t *a0, uint8_t *a1, uint8_t *a2, uint8_t *a3, uint8_t *b0,
-                                           uint8_t *b1, uint8_t *b2, uint8_t *b3, float *bias) {
+__device__ __forceinline__ void take_units(const MatmulArgs &g, const Split &sp, uint32_t unit,
+                                           uint32_t stride, uint8_t *a0, uint8_t *a1, uint8_t *a2,
+                                           uint8_t *a3, uint8_t *b0, uint8_t *b1, uint8_t *b2,
+                                           uint8_t *b3, float *bias) {
     constexpr int BM = 64 * FM, BN = 64 * FN;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t blocks = (g.k + 127) / 128, ld = blocks * 128;
@@ -270,7 +274,8 @@ __device__ __forceinline__ void take_units(const MatmulArgs &g, const Split &sp,
     auto copy = [&](uint8_t *a, uint8_t *b, int i, uint32_t block, int half) {
         const uint32_t lanes = block < last ? from : Buffer::kOutside;
         if (i < FM)
-            rows_a.to_lds(a + (wave * FM + i) * 1024, lanes, (wave * FM + i) * 16 * ld + block * 128 + half * 64);
+            rows_a.to_lds(a + (wave * FM + i) * 1024, lanes,
+                          (wave * FM + i) * 16 * ld + block * 128 + half * 64);
         else
             rows_b.to_lds(b + (wave * FN + i - FM) * 1024, lanes,
                           (wave * FN + i - FM) * 16 * ld + block * 128 + half * 64);
@@ -353,7 +358,8 @@ __device__ __forceinline__ void take_units(const MatmulArgs &g, const Split &sp,
             }
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int c = (t * N + N / 2) / S; c < ((t + 1) * N + N / 2) / S && c < N; ++c) copy(a_to, b_to, c, block, half);
+            for (int c = (t * N + N / 2) / S; c < ((t + 1) * N + N / 2) / S && c < N; ++c)
+                copy(a_to, b_to, c, block, half);
             __builtin_amdgcn_sched_barrier(0);
         }
         // This wave's copies but those of the last two steps have arrived, and its reads; then
@@ -440,7 +446,8 @@ __device__ __forceinline__ void take_units(const MatmulArgs &g, const Split &sp,
                 if (g.accumulate && !sums && ij % 2 == 0 && m < g.m) {
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
-                        old[e / 4][e % 4] = load4<OUT>(g.out, m * g.out_ld, n1 + 32 * j0 + 8 * e + 4 * q1, g.n);
+                        old[e / 4][e % 4] =
+                            load4<OUT>(g.out, m * g.out_ld, n1 + 32 * j0 + 8 * e + 4 * q1, g.n);
                 }
                 f32x4 v[4];
 #pragma unroll
@@ -448,7 +455,8 @@ __device__ __forceinline__ void take_units(const MatmulArgs &g, const Split &sp,
                     // a lane holds row r1's columns 8 e + 4 q1 + 0..3 of each 32
                     v[e] = f32x4{acc[i][j][4 * e], acc[i][j][4 * e + 1], acc[i][j][4 * e + 2],
                                  acc[i][j][4 * e + 3]};
-                    if (with_bias) v[e] += *reinterpret_cast<const f32x4 *>(bias + wn + 32 * j + 8 * e + 4 * q1);
+                    if (with_bias)
+                        v[e] += *reinterpret_cast<const f32x4 *>(bias + wn + 32 * j + 8 * e + 4 * q1);
                     if (g.relu && !sums) {
 #pragma unroll
                         for (int c = 0; c < 4; ++c) v[e][c] = v[e][c] < 0.0f ? 0.0f : v[e][c];   // NaN stays
@@ -460,7 +468,8 @@ __device__ __forceinline__ void take_units(const MatmulArgs &g, const Split &sp,
                 if (OUT == PS_F32 || sums) {
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        u32x4 w[2] = {__builtin_bit_cast(u32x4, v[2 * h]), __builtin_bit_cast(u32x4, v[2 * h + 1])};
+                        u32x4 w[2] = {__builtin_bit_cast(u32x4, v[2 * h]),
+                                      __builtin_bit_cast(u32x4, v[2 * h + 1])};
                         swap_rows(w[0], w[1]);
                         const uint32_t n = n1 + 32 * j + 16 * h + 8 * hi1 + 4 * q1;
 #pragma unroll
@@ -504,9 +513,9 @@ __device__ __forceinline__ void take_units(const MatmulArgs &g, const Split &sp,
 }
 
 // Small products leave most compute units idle, or wait for their first bytes most of the time. A
-// layer's two backward products in one launch take, quantisation and joining included, 18.7 us instead
-// of 23.4 for 57 x 1000 x 900, 22 instead of 27.6 for 300 x 1000 x 1000, 39 instead of 45.7 for 1000 x 2000 x
-// 2000.
+// layer's two backward products in one launch take, quantisation and joining included, 18.7 us
+// instead of 23.4 for 57 x 1000 x 900, 22 instead of 27.6 for 300 x 1000 x 1000, 39 instead of 45.7
+// for 1000 x 2000 x 2000.
 template <int FM, int FN, int OUT0, int OUT1>
 __global__ __launch_bounds__(256, FM == 2 ? 2 : 1) void tiles(Products both) {
     constexpr int A = 64 * FM * 64, B = 64 * FN * 64;
@@ -517,8 +526,8 @@ __global__ __launch_bounds__(256, FM == 2 ? 2 : 1) void tiles(Products both) {
     const bool second = blockIdx.x >= both.blocks[0];
     const uint32_t unit = blockIdx.x - (second ? both.blocks[0] : 0), stride = both.blocks[second];
     if (OUT0 == OUT1 || !second)
-        take_units<FM, FN, OUT0>(both.g[second], both.sp[second], unit, stride, a0, a1, a2, a3, b0, b1, b2, b3,
-                                   bias);
+        take_units<FM, FN, OUT0>(both.g[second], both.sp[second], unit, stride, a0, a1, a2, a3, b0, b1, b2,
+                                 b3, bias);
     else
         take_units<FM, FN, OUT1>(both.g[1], both.sp[1], unit, stride, a0, a1, a2, a3, b0, b1, b2, b3,
                                    bias);
@@ -588,7 +597,7 @@ __global__ __launch_bounds__(64 * WAVES) void slim(MatmulArgs g, Split sp) {
 #pragma unroll
             for (int j = 0; j < kTogether; ++j) {
                 const uint32_t i = i0 + j * 4 * WAVES, m = i / blocks, col = i % blocks * 128 + 8 * e;
-                const int count = m >= g.m || col >= g.k ? 0 : g.k - col >= 8 ? 8 : static_cast<int>(g.k - col);
+                const int count = m >= g.m || col >= g.k ? 0 : static_cast<int>(min(g.k - col, 8u));
                 const int64_t at = m * g.x_ld + col;
                 if (count == 8) x[j] = load8<X>(g.x, at);
                 else x[j] = load8_some<X>(g.x, at, count);
@@ -651,7 +660,8 @@ __global__ __launch_bounds__(256) void join(Products both) {
     const bool second = blockIdx.x >= both.join_blocks[0];
     const MatmulArgs &g = both.g[second];
     const uint32_t fours = (g.n + 3) / 4, parts = both.sp[second].parts;
-    const uint64_t i = static_cast<uint64_t>(blockIdx.x - (second ? both.join_blocks[0] : 0)) * 256 + threadIdx.x;
+    const uint32_t block = blockIdx.x - (second ? both.join_blocks[0] : 0);
+    const uint64_t i = static_cast<uint64_t>(block) * 256 + threadIdx.x;
     if (i >= static_cast<uint64_t>(g.m) * fours) return;
     const uint32_t m = static_cast<uint32_t>(i / fours), n = static_cast<uint32_t>(i % fours) * 4;
     const f32x4 *p = reinterpret_cast<const f32x4 *>(g.partial) + i;
@@ -686,9 +696,10 @@ struct Choice {
     Split split;
 };
 
-// What a product takes, in us, by rounds of tiles: a compute unit has one large tile at a time, or two small ones, which
-// cover each other's first loads and last stores; the last ones of many take less, as some have a compute unit each.
-// Fitted to 170 products of random sizes from 512 x 512 x 64 to 16384 x 25088 x 16384.
+// What a product takes, in us, by rounds of tiles: a compute unit has one large tile at a time, or
+// two small ones, which cover each other's first loads and last stores; the last ones of many take
+// less, as some have a compute unit each. Fitted to 170 products of random sizes from 512 x 512 x
+// 64 to 16384 x 25088 x 16384.
 double tiles_take(uint64_t m, uint64_t n, uint64_t blocks, bool wide, bool large, uint64_t parts) {
     const uint64_t bm = large ? 256 : 128, bn = large && !wide ? 256 : 128;
     const uint64_t units = (m + bm - 1) / bm * ((n + bn - 1) / bn) * parts, at_once = large ? kCus : 2 * kCus;
@@ -699,8 +710,10 @@ double tiles_take(uint64_t m, uint64_t n, uint64_t blocks, bool wide, bool large
     double us = static_cast<double>(rounds) * (start + block * k);
     if (large) us += rest != 0 ? start + block * k : 0.0;
     else if (rounds == 0) us += start + (rest <= kCus ? alone : block) * k;
-    else if (rest != 0) us += (start + block * k) * (0.5 + 0.5 * static_cast<double>(rest) / static_cast<double>(at_once));
-    if (parts > 1) us += 4.0 + static_cast<double>(parts * m * n) * 8 / 5e6;   // the parts' sums, written and read
+    else if (rest != 0)
+        us += (start + block * k) * 0.5 * (1.0 + static_cast<double>(rest) / static_cast<double>(at_once));
+    // the parts' sums, written and read
+    if (parts > 1) us += 4.0 + static_cast<double>(parts * m * n) * 8 / 5e6;
     return us;
 }
 
@@ -716,10 +729,10 @@ Choice choose(uint64_t m, uint64_t n, uint64_t k, bool wide) {
         // 1000 x 1000, 64 tiles: 13.1 and 10.5)
         parts = std::min(kCus / small, std::max<uint64_t>(1, blocks / (small < 32 ? 4 : 8)));
     } else {
-        // Large tiles read LDS and the caches least, small ones lose less where tiles are few or k is
-        // short; parts fill the last round (1280 x 4096 x 22272 195 us whole and 113 in parts, 256 x 21248 x
-        // 24320 275 and 168). Over the fitted sizes, large tiles wherever there are 256 of them took 9%
-        // longer than the better of both (15% to fp32), this rule 0.6%.
+        // Large tiles read LDS and the caches least, small ones lose less where tiles are few or k
+        // is short; parts fill the last round (1280 x 4096 x 22272 195 us whole and 113 in parts,
+        // 256 x 21248 x 24320 275 and 168). Over the fitted sizes, large tiles wherever there are
+        // 256 of them took 9% longer than the better of both (15% to fp32), this rule 0.6%.
         double least = tiles_take(m, n, blocks, wide, false, 1);
         for (uint64_t p = 1; p <= 8 && (p == 1 || (blocks / p >= 8 && p * m * n * 4 <= kMostSums)); ++p)
             for (const bool l : {false, true}) {
@@ -740,22 +753,24 @@ Choice choose(uint64_t m, uint64_t n, uint64_t k, bool wide) {
     return c;
 }
 
-// Whether slim converts x itself: a row's bytes in LDS, its scales and the padding. Every workgroup converts
-// all of x: 1 x 4096 (4 KB) took 7.5 us, 9.0 in two launches, 2 x 25088 (50 KB) 24.6 and 25.3, but 16 x 4096
-// (66 KB) 13.2 and 10.8, all with 4096 columns of out.
+// Whether slim converts x itself: a row's bytes in LDS, its scales and the padding. Every workgroup
+// converts all of x: 1 x 4096 (4 KB) took 7.5 us, 9.0 in two launches, 2 x 25088 (50 KB) 24.6 and
+// 25.3, but 16 x 4096 (66 KB) 13.2 and 10.8, all with 4096 columns of out.
 bool few_bytes(uint64_t m, uint64_t blocks) { return m <= 16 && m * (blocks * 129 + 16) <= 51200; }
 
-// Of slim: where few columns of out leave compute units idle, a long k is split, to a block a wave at least. In us,
-// whole and split, joining included: 3 x 300 x 24000 17.3 and 8.1, 32 x 1000 x 8192 13.3 and 9.3, 3 x 1000 x 8192
-// 7.5 and 7.9, 32 x 300 x 4096 7.8 and 8.1. A split product's x is converted first, which for few bytes pays
-// from 128 blocks on (1 x 70 x 17000 with its conversion 11.8 and 9.8, 1 x 70 x 8192 7.4 and 9.3).
+// Of slim: where few columns of out leave compute units idle, a long k is split, to a block a wave
+// at least. In us, whole and split, joining included: 3 x 300 x 24000 17.3 and 8.1, 32 x 1000 x
+// 8192 13.3 and 9.3, 3 x 1000 x 8192 7.5 and 7.9, 32 x 300 x 4096 7.8 and 8.1. A split product's x
+// is converted first, which for few bytes pays from 128 blocks on (1 x 70 x 17000 with its
+// conversion 11.8 and 9.8, 1 x 70 x 8192 7.4 and 9.3).
 Split split_slim(uint64_t m, uint64_t n, uint64_t k) {
     Split sp{};
     const uint64_t blocks = (k + 127) / 128;
     sp.tiles_m = 1;
     sp.tiles_n = static_cast<uint32_t>((n + 15) / 16);
     const bool whole = blocks < 64 || (blocks < 128 && few_bytes(m, blocks));
-    const uint64_t parts = whole ? 1 : std::max<uint64_t>(1, std::min<uint64_t>(kCus / sp.tiles_n, blocks / 16));
+    const uint64_t many = std::min<uint64_t>(kCus / sp.tiles_n, blocks / 16);
+    const uint64_t parts = whole ? 1 : std::max<uint64_t>(1, many);
     sp.steps = static_cast<uint32_t>((blocks + parts - 1) / parts);
     sp.parts = static_cast<uint32_t>((blocks + sp.steps - 1) / sp.steps);
     return sp;
@@ -775,7 +790,9 @@ hipError_t launch_slim(const MatmulArgs &g, const Split &sp, hipStream_t s) {
     return hipGetLastError();
 }
 
-uint64_t join_blocks(const MatmulArgs &g) { return (static_cast<uint64_t>(g.m) * ((g.n + 3) / 4) + 255) / 256; }
+uint64_t join_blocks(const MatmulArgs &g) {
+    return (static_cast<uint64_t>(g.m) * ((g.n + 3) / 4) + 255) / 256;
+}
 
 // The product's work units; at most `most` workgroups take them.
 bool place_product(const MatmulArgs &g, const Choice &c, uint32_t most, int i, Products *p) {
@@ -841,7 +858,8 @@ bool is_small(const MatmulArgs &g, int out_dtype) {
 
 size_t matmul_workspace(int64_t m, int64_t n, int64_t k, int out_dtype) {
     if (m == 0 || n == 0 || k == 0) return 0;
-    const uint32_t parts = (m <= kSlimRows ? split_slim(m, n, k) : choose(m, n, k, out_dtype == PS_F32).split).parts;
+    const Split split = m <= kSlimRows ? split_slim(m, n, k) : choose(m, n, k, out_dtype == PS_F32).split;
+    const uint32_t parts = split.parts;
     if (parts == 1) return 0;
     return sizeof(float) * size_t(parts) * size_t(m) * ((size_t(n) + 3) & ~size_t(3));
 }
@@ -858,9 +876,11 @@ bool pairs(const MatmulArgs &a, int a_dtype, const MatmulArgs &b, int b_dtype) {
     return is_small(a, a_dtype) && is_small(b, b_dtype);
 }
 
-hipError_t launch_matmul_two(const MatmulArgs &a, int a_dtype, const MatmulArgs &b, int b_dtype, hipStream_t s) {
+hipError_t launch_matmul_two(const MatmulArgs &a, int a_dtype, const MatmulArgs &b, int b_dtype,
+                             hipStream_t s) {
     if (a_dtype != b_dtype)
-        return a_dtype == PS_BF16 ? launch_two<PS_BF16, PS_F32>(a, b, s) : launch_two<PS_BF16, PS_F32>(b, a, s);
+        return a_dtype == PS_BF16 ? launch_two<PS_BF16, PS_F32>(a, b, s)
+                                  : launch_two<PS_BF16, PS_F32>(b, a, s);
     return a_dtype == PS_F32 ? launch_two<PS_F32, PS_F32>(a, b, s) : launch_two<PS_BF16, PS_BF16>(a, b, s);
 }
 

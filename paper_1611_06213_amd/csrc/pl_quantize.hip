@@ -166,7 +166,8 @@ __global__ __launch_bounds__(kBlock) void quantize_rows(QuantArgs a, uint32_t wo
         *reinterpret_cast<u32x2 *>(a.values + (r0 + i) * ld + col) =
             u32x2{four(x[i], 0, as_scale(byte)), four(x[i], 1, as_scale(byte))};
         if ((lane & 15) == 0)
-            reinterpret_cast<uint8_t *>(a.scales + word * a.rows + r0 + i)[lane >> 4] = static_cast<uint8_t>(byte);
+            reinterpret_cast<uint8_t *>(a.scales + word * a.rows + r0 + i)[lane >> 4] =
+                static_cast<uint8_t>(byte);
     }
 }
 
@@ -186,7 +187,8 @@ hipError_t launch_quantize(const QuantArgs &a, int dtype, bool square, hipStream
     return launch_quantize_two(a, QuantArgs{}, dtype, square, s);
 }
 
-hipError_t launch_quantize_two(const QuantArgs &a, const QuantArgs &b, int dtype, bool square, hipStream_t s) {
+hipError_t launch_quantize_two(const QuantArgs &a, const QuantArgs &b, int dtype, bool square,
+                               hipStream_t s) {
     Two two{{a, b}, {}, {}};
     uint64_t all = 0;
     for (int i = 0; i < 2; ++i) {

@@ -72,7 +72,8 @@ __global__ __launch_bounds__(kBlock) void rows_kernel(RowsArgs a, int lx, uint32
             for (int e = 0; e < 8; ++e) x[u][e] = 0.0f;   // not factor * 0: the factor may be NaN
         }
         const int64_t at = static_cast<int64_t>(r) * a.out_ld + static_cast<int64_t>(col);
-        if (NT && lines) store8_lines<OUT>(a.out, at, x[u], stage + (OUT == PS_F32 ? 2 * (threadIdx.x & ~63u) : 0));
+        if (NT && lines)
+            store8_lines<OUT>(a.out, at, x[u], stage + (OUT == PS_F32 ? 2 * (threadIdx.x & ~63u) : 0));
         else if (count == 8) store8<OUT>(a.out, at, x[u]);
         else store_some<OUT>(a.out, at, x[u], count);
     }

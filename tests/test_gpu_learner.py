@@ -426,8 +426,8 @@ def test_linear_grad(torch, learner, m, n, k, x):
     assert torch.equal(into, dw + 2.0) and bool((row[:3] == 2.0).all())
 
 
-@pytest.mark.parametrize("m,n,k", [(57, 1000, 900), (33, 33, 1), (130, 700, 4100), (1025, 129, 40), (20, 500, 500),
-                                   (300, 20, 500), (2100, 2050, 300)])
+@pytest.mark.parametrize("m,n,k", [(57, 1000, 900), (33, 33, 1), (130, 700, 4100), (1025, 129, 40),
+                                   (20, 500, 500), (300, 20, 500), (2100, 2050, 300)])
 @pytest.mark.parametrize("out", ["f32", "bf16"])
 @pytest.mark.parametrize("weight", ["f32", "bf16"])
 def test_linear_grad_is_two_products(torch, learner, m, n, k, out, weight):
@@ -436,8 +436,8 @@ def test_linear_grad_is_two_products(torch, learner, m, n, k, out, weight):
     x, grad, w = randn(torch, g, m, k), randn(torch, g, m, n, std=1e-3), randn(torch, g, n, k)
     w_t = learner.quantize_fp8(w, square=True, transpose=True)
     into = randn(torch, g, n, k).to(dt(torch, weight))
-    want = learner.matmul_fp8(learner.quantize_fp8(grad, transpose=True), learner.quantize_fp8(x, transpose=True),
-                              out=into.clone(), accumulate=True)
+    grad_t, x_t = (learner.quantize_fp8(t, transpose=True) for t in (grad, x))
+    want = learner.matmul_fp8(grad_t, x_t, out=into.clone(), accumulate=True)
     want_x = learner.matmul_fp8(learner.quantize_fp8(grad), w_t, dtype=dt(torch, out))
     dx, dw = learner.linear_fp8_grad(x, grad, w_t, dtype=dt(torch, out), weight_out=into, accumulate=True)
     assert dx.dtype == dt(torch, out) and torch.equal(dx, want_x)
