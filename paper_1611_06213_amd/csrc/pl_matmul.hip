@@ -724,10 +724,20 @@ Choice choose(uint64_t m, uint64_t n, uint64_t k, bool wide) {
     bool large = false;
     uint64_t parts = 1;
     if (small <= kCus / 2) {
-        // parts of k until every compute unit has a workgroup, of four blocks at least, or of eight where
-        // the tiles are many (57 x 900 x 1000, 8 tiles: 10.2 us with parts of four, 13.1 whole; 1000 x
-        // 1000 x 1000, 64 tiles: 13.1 and 10.5)
-        parts = std::min(kCus / small, std::max<uint64_t>(1, blocks / (small < 32 ? 4 : 8)));
+        // Parts of k until every compute unit has a workgroup, unless the joining takes longer: in us,
+        // 64 x 128 x 4096 10.2 in parts of eight blocks and 8.4 of four, 57 x 1000 x 900 to bf16 8.5 in
+        // parts of four and 7.6 whole. To fp32 the latter takes 10.7 and 11.9, but as one of a layer's two
+        // backward products, which take 15.4 and 13.3 together.
+        double least = 0.0;
+        for (uint64_t q = 1; q <= std::min(kCus / small, blocks); ++q) {
+            const uint64_t steps = ((blocks + q - 1) / q + 1) & ~uint64_t(1);
+            const double sums = static_cast<double>(q * m * n) * 8 / 5e6 + 0.2 * static_cast<double>(q);
+            const double join = q == 1 ? 0.0 : 4.0 + sums;
+            const double us = (wide ? 0.9 : 0.5) * static_cast<double>(steps) + join;
+            if (q > 1 && us >= least) continue;
+            least = us;
+            parts = q;
+        }
     } else {
         // Large tiles read LDS and the caches least, small ones lose less where tiles are few or k
         // is short; parts fill the last round (1280 x 4096 x 22272 195 us whole and 113 in parts,
