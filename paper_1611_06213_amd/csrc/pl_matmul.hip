@@ -725,9 +725,9 @@ Choice choose(uint64_t m, uint64_t n, uint64_t k, bool wide) {
     uint64_t parts = 1;
     if (small <= kCus / 2) {
         // Parts of k until every compute unit has a workgroup, unless the joining takes longer: in us,
-        // 64 x 128 x 4096 10.2 in parts of eight blocks and 8.4 of four, 57 x 1000 x 900 to bf16 8.5 in
-        // parts of four and 7.6 whole (a layer's two backward products 15.4 and 13.2), to fp32 9.8 in
-        // parts of two and 12.4 whole.
+        // 64 x 128 x 4096 10.2 in parts of eight blocks and 8.4 of four, 57 x 900 x 1000 to bf16 8.5 in
+        // parts of four and 8.2 whole (with the other backward product and their joining 15.4 and 13.2),
+        // to fp32 9.8 in parts of two and 12.4 whole.
         double least = 0.0;
         for (uint64_t q = 1; q <= std::min(kCus / small, blocks); ++q) {
             const uint64_t steps = ((blocks + q - 1) / q + 1) & ~uint64_t(1);
