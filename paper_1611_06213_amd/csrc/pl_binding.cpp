@@ -121,6 +121,14 @@ bool number(PyObject *o, float *out) {
     return true;
 }
 
+// Any object's truth, as Python has it.
+bool flag(PyObject *o, bool *out) {
+    const int truth = PyObject_IsTrue(o);
+    if (truth < 0) PyErr_Clear();
+    *out = truth > 0;
+    return truth >= 0;
+}
+
 // A matrix in 8-bit form from its parts (values, scales, rows, cols).
 struct Fp8 {
     at::Tensor values, scales;
@@ -203,8 +211,8 @@ PyObject *embedding_grad(PyObject *const *a) {
     int type;
     int64_t rows;
     float scale;
-    const bool accumulate = a[7] == Py_True;
-    if (!ids(a[0], &id, &type) || !matrix(a[1], &grad) || grad.rows != id.numel() ||
+    bool accumulate;
+    if (!flag(a[7], &accumulate) || !ids(a[0], &id, &type) || !matrix(a[1], &grad) || grad.rows != id.numel() ||
         !integer(a[2], &rows) || rows < 0 || !number(a[3], &scale) || !dropping(a[4], &drop) ||
         (accumulate && a[6] == Py_None) || !result(a[6], a[5], rows, grad.cols, grad.t, &out))
         Py_RETURN_NONE;
@@ -251,8 +259,8 @@ PyObject *product(PyObject *const *a) {
     at::Tensor b;
     const void *pb;
     int bias_code;
-    const bool relu = a[3] == Py_True, accumulate = a[6] == Py_True;
-    if (!fp8(a[0], &x) || !fp8(a[1], &w) || x.cols != w.cols || !bias(a[2], w.rows, &b, &pb, &bias_code) ||
+    bool relu, accumulate;
+    if (!flag(a[3], &relu) || !flag(a[6], &accumulate) || !fp8(a[0], &x) || !fp8(a[1], &w) || x.cols != w.cols || !bias(a[2], w.rows, &b, &pb, &bias_code) ||
         (accumulate && a[5] == Py_None) || !result(a[5], a[4], x.rows, w.rows, x.scales, &out))
         Py_RETURN_NONE;
     const size_t need = pl_matmul_fp8_workspace(x.rows, w.rows, x.cols, out.dtype);
@@ -272,8 +280,8 @@ PyObject *linear(PyObject *const *a) {
     at::Tensor b;
     const void *pb;
     int bias_code;
-    const bool relu = a[3] == Py_True;
-    if (!matrix(a[0], &x) || !fp8(a[1], &w) || x.cols != w.cols || !bias(a[2], w.rows, &b, &pb, &bias_code) ||
+    bool relu;
+    if (!flag(a[3], &relu) || !matrix(a[0], &x) || !fp8(a[1], &w) || x.cols != w.cols || !bias(a[2], w.rows, &b, &pb, &bias_code) ||
         !result(a[5], a[4], x.rows, w.rows, x.t, &out))
         Py_RETURN_NONE;
     const size_t need = pl_linear_fp8_workspace(x.rows, w.rows, x.cols, x.dtype, out.dtype);
@@ -290,8 +298,8 @@ PyObject *linear(PyObject *const *a) {
 PyObject *linear_grad(PyObject *const *a) {
     Matrix x, g, dx, dw;
     Fp8 w;   // inputs x outputs
-    const bool accumulate = a[7] == Py_True;
-    if (!matrix(a[0], &x) || !matrix(a[1], &g) || !fp8(a[2], &w) || x.rows != g.rows || w.rows != x.cols ||
+    bool accumulate;
+    if (!flag(a[7], &accumulate) || !matrix(a[0], &x) || !matrix(a[1], &g) || !fp8(a[2], &w) || x.rows != g.rows || w.rows != x.cols ||
         w.cols != g.cols || (accumulate && a[6] == Py_None) ||
         !result(a[5], a[3], x.rows, x.cols, x.t, &dx) || !result(a[6], a[4], g.cols, x.cols, x.t, &dw))
         Py_RETURN_NONE;

@@ -236,7 +236,7 @@ def embedding_grad(ids, grad, rows: int, scale: float = 1.0, drop: Optional[Drop
     need = L.pl_embedding_grad_workspace(tokens, rows, dim)
     work = torch.empty(need, dtype=torch.uint8, device=grad.device)
     _check(L.pl_embedding_grad(ids.data_ptr(), id_code, tokens, src, src_code, src_ld, dim, scale,
-                               _drop(drop), dst, dst_code, dst_ld, rows, int(accumulate),
+                               _drop(drop), dst, dst_code, dst_ld, rows, int(bool(accumulate)),
                                work.data_ptr(), need, _stream()))
     return out
 
@@ -303,7 +303,7 @@ def _quantize(x, square: bool, plain: bool, transposed: bool):
     rows, cols = x.shape
     out = Fp8Matrix(rows, cols, x.device) if plain else None
     out_t = Fp8Matrix(cols, rows, x.device) if transposed else None
-    _check(load_library().pl_quantize_fp8(src, code, rows, cols, ld, int(square), _ref(out),
+    _check(load_library().pl_quantize_fp8(src, code, rows, cols, ld, int(bool(square)), _ref(out),
                                           _ref(out_t), _stream()))
     return out, out_t
 
@@ -354,8 +354,8 @@ def matmul_fp8(a: Fp8Matrix, b: Fp8Matrix, bias=None, relu: bool = False, dtype=
     L = load_library()
     need = L.pl_matmul_fp8_workspace(m, n, k, code)
     work = torch.empty(need, dtype=torch.uint8, device=out.device) if need else None
-    _check(L.pl_matmul_fp8(m, n, k, _ref(a), _ref(b), bias_ptr, bias_code, int(relu), dst, code, ld,
-                           int(accumulate), work.data_ptr() if need else None, need, _stream()))
+    _check(L.pl_matmul_fp8(m, n, k, _ref(a), _ref(b), bias_ptr, bias_code, int(bool(relu)), dst, code, ld,
+                           int(bool(accumulate)), work.data_ptr() if need else None, need, _stream()))
     return out
 
 
@@ -377,7 +377,7 @@ def linear_fp8(x, w: Fp8Matrix, bias=None, relu: bool = False, dtype=torch.bfloa
     L = load_library()
     need = L.pl_linear_fp8_workspace(m, n, k, code, dst_code)
     work = torch.empty(need, dtype=torch.uint8, device=x.device)
-    _check(L.pl_linear_fp8(src, code, m, k, src_ld, n, _ref(w), bias_ptr, bias_code, int(relu), dst,
+    _check(L.pl_linear_fp8(src, code, m, k, src_ld, n, _ref(w), bias_ptr, bias_code, int(bool(relu)), dst,
                            dst_code, dst_ld, work.data_ptr(), need, _stream()))
     return out
 
@@ -410,6 +410,6 @@ def linear_fp8_grad(x, grad, w_t: Fp8Matrix, dtype=torch.bfloat16, weight_dtype=
     need = L.pl_linear_fp8_grad_workspace(m, n, k, dst_code, wgt_code)
     work = torch.empty(need, dtype=torch.uint8, device=x.device)
     _check(L.pl_linear_fp8_grad(src, code, src_ld, grd, grd_code, grd_ld, m, n, k, _ref(w_t), dst,
-                                dst_code, dst_ld, wgt, wgt_code, wgt_ld, int(accumulate),
+                                dst_code, dst_ld, wgt, wgt_code, wgt_ld, int(bool(accumulate)),
                                 work.data_ptr(), need, _stream()))
     return x_out, weight_out

@@ -515,3 +515,33 @@ def test_refusals_on_the_device(torch, learner):
         learner.embedding_grad(torch.zeros(3, 2, dtype=torch.int64, device="cuda"),
                                torch.ones(2, 3, 4, device="cuda"), 5)
 
+
+
+@pytest.mark.parametrize("kind", ["bool", "int", "numpy"])
+def test_flags_by_their_truth(torch, learner, kind):
+    """`relu` and `accumulate` count by their truth, whatever their type."""
+    yes, no = {"bool": (True, False), "int": (1, 0), "numpy": (np.bool_(True), np.bool_(False))}[kind]
+    g = gen(torch, 12)
+    a, b, ids = integers(torch, g, 40, 70), integers(torch, g, 30, 70), torch.arange(40, device="cuda") % 5
+    qa, qb = learner.quantize_fp8(a), learner.quantize_fp8(b)
+    qt = learner.quantize_fp8(b, square=True, transpose=True)
+    y, grad = (a.double() @ b.double().t()).float(), integers(torch, g, 40, 30)
+    dw = (grad.double().t() @ a.double()).float()
+    table = torch.zeros(5, 70, device="cuda").index_add_(0, ids, a)
+    f32 = torch.float32
+    for relu, want in ((yes, y.clamp(min=0)), (no, y)):
+        assert torch.equal(learner.linear_fp8(a, qb, relu=relu, dtype=f32), want)
+        assert torch.equal(learner.matmul_fp8(qa, qb, relu=relu, dtype=f32), want)
+    for add, old in ((yes, 3.0), (no, 0.0)):
+        into = lambda *s: torch.full(s, 3.0, device="cuda")
+        assert torch.equal(learner.matmul_fp8(qa, qb, out=into(40, 30), accumulate=add), y + old)
+        into_dw = learner.linear_fp8_grad(a, grad, qt, weight_out=into(30, 70), accumulate=add)[1]
+        assert torch.equal(into_dw, dw + old)
+        assert torch.equal(learner.embedding_grad(ids, a, 5, out=into(5, 70), accumulate=add), table + old)
+    for call in (lambda: learner.matmul_fp8(qa, qb, accumulate=yes),
+                 lambda: learner.linear_fp8_grad(a, grad, qt, accumulate=yes),
+                 lambda: learner.embedding_grad(ids, a, 5, accumulate=yes)):
+        with pytest.raises(ValueError, match="accumulate needs"):
+            call()
+    with pytest.raises(ps.PSError, match="accumulate"):
+        learner.matmul_fp8(qa, qb, relu=yes, out=into(40, 30), accumulate=yes)
