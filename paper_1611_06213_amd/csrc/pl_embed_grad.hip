@@ -334,9 +334,11 @@ __device__ __forceinline__ void add_tokens(float (&sum)[8], const GradArgs &a, c
 
 // A result past the caches (true: of a table too large for them) whose 512 columns from the wave's
 // first on are one row's and inside it: stage is the wave's part of LDS. Otherwise null.
+// A row without tokens (the sums are zeros) is zeros even where the factor is not finite.
 template <int OUT>
-__device__ __forceinline__ void write_row(const GradArgs &a, float (&sum)[8], uint32_t row,
+__device__ __forceinline__ void write_row(const GradArgs &a, float (&sum)[8], uint32_t tokens, uint32_t row,
                                           uint32_t group, int columns, f32x4 *stage = nullptr) {
+    const float factor = tokens != 0 ? a.factor : 0.0f;
     const int64_t at = row * a.out_ld + 8ll * group;
     float old[8];
     if (a.accumulate) {
@@ -345,7 +347,7 @@ __device__ __forceinline__ void write_row(const GradArgs &a, float (&sum)[8], ui
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        sum[e] *= a.factor;
+        sum[e] *= factor;
         if (a.accumulate) sum[e] += old[e];
     }
     if (stage != nullptr) store8_lines<OUT>(a.out, at, sum, stage);
@@ -388,7 +390,7 @@ __global__ __launch_bounds__(kBlock) void sum_rows(GradArgs a, Plan p, int lx, u
     add_tokens<G, DROP>(sum, a, perm + row.begin, row.count, group, columns);
     // lx >= 6: a wave's lanes are of one row
     const bool lines = past_caches && lx >= 6 && col - 8 * (threadIdx.x & 63) + 512 <= a.dim;
-    write_row<OUT>(a, sum, v, group, columns,
+    write_row<OUT>(a, sum, row.count, v, group, columns,
                    lines ? stage + (OUT == PS_F32 ? 2 * (threadIdx.x & ~63u) : 0) : nullptr);
 }
 
@@ -440,7 +442,7 @@ __global__ __launch_bounds__(kBlock) void join_pieces(GradArgs a, Plan p, int lx
             }
             __syncthreads();
         }
-        if (run == 0 && columns != 0) write_row<OUT>(a, sum, list[y].row, group, columns);
+        if (run == 0 && columns != 0) write_row<OUT>(a, sum, of, list[y].row, group, columns);
     }
 }
 
@@ -534,7 +536,7 @@ __global__ __launch_bounds__(kBlock) void sum_few(GradArgs a, int lx, uint32_t t
             if (count > kSmallAlone || (count == 0 && a.accumulate)) continue;
             float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
             add_tokens<G, DROP>(sum, a, list + from, count, group, columns);
-            write_row<OUT>(a, sum, v0 + r, group, columns);
+            write_row<OUT>(a, sum, count, v0 + r, group, columns);
         }
     }
     for (uint64_t todo = shared_rows; todo != 0; todo &= todo - 1) {   // the same for the whole workgroup
@@ -552,7 +554,7 @@ __global__ __launch_bounds__(kBlock) void sum_few(GradArgs a, int lx, uint32_t t
             for (uint32_t i = 1; i < used; ++i)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) sum[e] += runs[(i << lx) + x][e];
-            write_row<OUT>(a, sum, v0 + r, group, columns);
+            write_row<OUT>(a, sum, count, v0 + r, group, columns);
         }
         __syncthreads();
     }

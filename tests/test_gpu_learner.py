@@ -545,3 +545,23 @@ def test_flags_by_their_truth(torch, learner, kind):
             call()
     with pytest.raises(ps.PSError, match="accumulate"):
         learner.matmul_fp8(qa, qb, relu=yes, out=into(40, 30), accumulate=yes)
+
+
+@pytest.mark.parametrize("tokens,vocab,dim", [(5, 70, 7), (300, 900, 1030), (5000, 700, 24)])
+@pytest.mark.parametrize("scale", [float("nan"), float("inf"), float("-inf")])
+def test_rows_without_tokens_are_zeros(torch, learner, tokens, vocab, dim, scale):
+    """Whatever the scale; rows with tokens carry it. Accumulating, they are not touched."""
+    ids = torch.arange(tokens, device="cuda") % (vocab // 3) * 2
+    grad = torch.ones(tokens, dim, device="cuda")
+    got = learner.embedding_grad(ids, grad, vocab, scale)
+    there = torch.zeros(vocab, dtype=torch.bool, device="cuda")
+    there[ids] = True
+    assert bool((got[~there] == 0).all())
+    want = torch.full_like(got, scale)[there]
+    assert torch.equal(got[there].nan_to_num(), want.nan_to_num())
+    assert bool((got[there].isnan() == want.isnan()).all())
+    old = torch.full_like(got, 5.0)
+    assert bool((learner.embedding_grad(ids, grad, vocab, scale, out=old, accumulate=True)[~there] == 5).all())
+    # and where everything is dropped
+    none = learner.embedding_grad(ids, grad, vocab, float("inf"), learner.Dropout(1.0, 1))
+    assert bool((none[~there] == 0).all())
