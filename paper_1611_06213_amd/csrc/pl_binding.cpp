@@ -48,7 +48,7 @@ bool as_matrix(const at::Tensor &t, Matrix *m) {
     m->rows = t.size(0);
     m->cols = t.size(1);
     if (m->cols > 1 && t.stride(1) != 1) return false;
-    m->ld = m->cols <= 1 ? std::max<int64_t>(t.stride(0), 1) : t.stride(0);
+    m->ld = t.stride(0);   // 0, of rows that share their memory, is refused by the library
     m->p = t.data_ptr();
     m->t = t;
     return true;

@@ -150,7 +150,8 @@ def _matrix(name: str, t, rows: Optional[int] = None, cols: Optional[int] = None
         raise ValueError(f"{name}: a matrix of {want} expected, not {tuple(t.shape)}")
     if t.shape[1] > 1 and t.stride(1) != 1:
         raise ValueError(f"{name}: neighbouring columns are {t.stride(1)} elements apart")
-    return t.data_ptr(), _code(t.dtype), max(t.stride(0), 1) if t.shape[1] <= 1 else t.stride(0)
+    # a row stride of 0, of rows that share their memory, is refused by the library
+    return t.data_ptr(), _code(t.dtype), t.stride(0)
 
 
 def _stream() -> int:

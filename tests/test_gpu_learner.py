@@ -565,3 +565,26 @@ def test_rows_without_tokens_are_zeros(torch, learner, tokens, vocab, dim, scale
     # and where everything is dropped
     none = learner.embedding_grad(ids, grad, vocab, float("inf"), learner.Dropout(1.0, 1))
     assert bool((none[~there] == 0).all())
+
+
+def test_rows_that_share_their_memory(torch, learner):
+    """A column expanded over its rows has a row stride of 0. It is refused, as wider ones are, not
+    taken for a column of neighbours, which lie outside its memory."""
+    one, ids = torch.ones(1, 1, device="cuda"), torch.zeros(300, dtype=torch.int64, device="cuda")
+    many, w = one.expand(300, 1), torch.ones(40, 1, device="cuda")
+    q, drop = learner.quantize_fp8(w), learner.Dropout(0.5, 1)
+    column = torch.ones(300, 1, device="cuda")
+    calls = [lambda: learner.embedding(ids, many), lambda: learner.embedding(ids, one, out=many),
+             lambda: learner.embedding_grad(ids, many, 5), lambda: learner.embedding_grad(ids, column, 300, out=many),
+             lambda: learner.dropout(many, drop), lambda: learner.dropout(column, drop, out=many),
+             lambda: learner.quantize_fp8(many), lambda: learner.linear_fp8(many, q),
+             lambda: learner.matmul_fp8(learner.quantize_fp8(column), learner.quantize_fp8(one), out=many)]
+    for call in calls:
+        with pytest.raises(ps.PSError, match="row stride 0"):
+            call()
+    # one row may have any stride, one column any of at least 1
+    assert learner.dropout(one.expand(1, 1), drop).shape == (1, 1)
+    wide = torch.arange(1200.0, device="cuda").view(300, 4)[:, 1:2]
+    assert torch.equal(learner.embedding(torch.arange(300, device="cuda"), wide), wide)
+    assert torch.equal(learner.embedding(ids, torch.ones(1, 5, device="cuda").as_strided((1, 5), (0, 1))),
+                       torch.ones(300, 5, device="cuda"))

@@ -293,3 +293,12 @@ def test_linear_refuses(lib):
     refused(lib, grad(wout=5 * P), "overlaps")
     refused(lib, grad(size=need - 1), "needed", ps.PS_ENOMEM)
     refused(lib, grad(ws=4 * P), "overlaps grad")
+
+
+def test_binding_gives_the_stride_that_a_tensor_has(monkeypatch):
+    """Rows that share their memory: 0, whatever their columns, which the library refuses."""
+    monkeypatch.setattr(learner, "_on_device", lambda name, t: None)
+    one = torch.ones(1, 1)
+    assert learner._matrix("x", one.expand(300, 1))[2] == 0
+    assert learner._matrix("x", torch.ones(1, 7).expand(300, 7))[2] == 0
+    assert learner._matrix("x", torch.ones(300, 4)[:, :1])[2] == 4
