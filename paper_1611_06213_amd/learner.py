@@ -189,6 +189,8 @@ def embedding(ids, table, scale: float = 1.0, drop: Optional[Dropout] = None, dt
     An id outside the table (padding) gives zeros. Shape: that of `ids`, then the table's
     columns; of `dtype` (the table's by default), or written to `out`, a matrix of one row
     per id."""
+    if out is not None and dtype is not None and getattr(out, "dtype", dtype) != dtype:
+        raise TypeError(f"out is {out.dtype}, not {dtype}")
     native = _native or _native_calls()
     if native:
         done = native.embedding(ids, table, scale, drop, dtype or getattr(table, "dtype", None), out)
@@ -201,8 +203,6 @@ def embedding(ids, table, scale: float = 1.0, drop: Optional[Dropout] = None, dt
     if out is None:
         result = torch.empty((*ids.shape, dim), dtype=dtype or table.dtype, device=table.device)
         out = result.view(tokens, dim)
-    elif dtype is not None and out.dtype != dtype:
-        raise TypeError(f"out is {out.dtype}, not {dtype}")
     dst, dst_code, dst_ld = _matrix("out", out, tokens, dim)
     _check(load_library().pl_embedding(ids.data_ptr(), id_code, tokens, src, src_code, vocab, dim,
                                        src_ld, scale, _drop(drop), dst, dst_code, dst_ld, _stream()))

@@ -588,3 +588,17 @@ def test_rows_that_share_their_memory(torch, learner):
     assert torch.equal(learner.embedding(torch.arange(300, device="cuda"), wide), wide)
     assert torch.equal(learner.embedding(ids, torch.ones(1, 5, device="cuda").as_strided((1, 5), (0, 1))),
                        torch.ones(300, 5, device="cuda"))
+
+
+def test_lookup_into_another_type_than_named(torch, learner):
+    ids, table = torch.zeros(2, dtype=torch.int64, device="cuda"), torch.ones(3, 5, device="cuda")
+    out = torch.zeros(2, 5, device="cuda")
+    with pytest.raises(TypeError, match="out is torch.float32, not torch.bfloat16"):
+        learner.embedding(ids, table, dtype=torch.bfloat16, out=out)
+    assert bool((out == 0).all())
+    assert learner.embedding(ids, table, dtype=torch.float32, out=out) is out and bool((out == 1).all())
+    # without a name, out's own type counts
+    half = torch.zeros(2, 5, dtype=torch.bfloat16, device="cuda")
+    assert learner.embedding(ids, table, out=half) is half and bool((half == 1).all())
+    with pytest.raises(TypeError, match="tensor expected"):
+        learner.embedding(ids, table, dtype=torch.float32, out=[0.0])
