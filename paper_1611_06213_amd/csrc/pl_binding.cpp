@@ -129,6 +129,10 @@ bool flag(PyObject *o, bool *out) {
     return truth >= 0;
 }
 
+bool shape(const at::Tensor &t, int64_t rows, int64_t cols) {
+    return t.dim() == 2 && t.size(0) == rows && t.size(1) == cols && t.is_contiguous();
+}
+
 // A matrix in 8-bit form from its parts (values, scales, rows, cols).
 struct Fp8 {
     at::Tensor values, scales;
@@ -141,6 +145,11 @@ bool fp8(PyObject *o, Fp8 *f) {
     if (!device_tensor(PyTuple_GET_ITEM(o, 0), &f->values) ||
         !device_tensor(PyTuple_GET_ITEM(o, 1), &f->scales) ||
         !integer(PyTuple_GET_ITEM(o, 2), &f->rows) || !integer(PyTuple_GET_ITEM(o, 3), &f->cols))
+        return false;
+    // a caller may have exchanged the tensors for others
+    const int64_t words = (pl_fp8_ld(f->cols) / 128 + 3) / 4;
+    if (f->values.scalar_type() != at::kFloat8_e4m3fn || f->scales.scalar_type() != at::kInt ||
+        !shape(f->values, f->rows, pl_fp8_ld(f->cols)) || !shape(f->scales, words, f->rows))
         return false;
     f->q = pl_fp8{f->values.data_ptr(), static_cast<uint32_t *>(f->scales.data_ptr())};
     return true;
@@ -260,7 +269,8 @@ PyObject *product(PyObject *const *a) {
     const void *pb;
     int bias_code;
     bool relu, accumulate;
-    if (!flag(a[3], &relu) || !flag(a[6], &accumulate) || !fp8(a[0], &x) || !fp8(a[1], &w) || x.cols != w.cols || !bias(a[2], w.rows, &b, &pb, &bias_code) ||
+    if (!flag(a[3], &relu) || !flag(a[6], &accumulate) || !fp8(a[0], &x) || !fp8(a[1], &w) ||
+        x.cols != w.cols || !bias(a[2], w.rows, &b, &pb, &bias_code) ||
         (accumulate && a[5] == Py_None) || !result(a[5], a[4], x.rows, w.rows, x.scales, &out))
         Py_RETURN_NONE;
     const size_t need = pl_matmul_fp8_workspace(x.rows, w.rows, x.cols, out.dtype);
@@ -281,7 +291,8 @@ PyObject *linear(PyObject *const *a) {
     const void *pb;
     int bias_code;
     bool relu;
-    if (!flag(a[3], &relu) || !matrix(a[0], &x) || !fp8(a[1], &w) || x.cols != w.cols || !bias(a[2], w.rows, &b, &pb, &bias_code) ||
+    if (!flag(a[3], &relu) || !matrix(a[0], &x) || !fp8(a[1], &w) || x.cols != w.cols ||
+        !bias(a[2], w.rows, &b, &pb, &bias_code) ||
         !result(a[5], a[4], x.rows, w.rows, x.t, &out))
         Py_RETURN_NONE;
     const size_t need = pl_linear_fp8_workspace(x.rows, w.rows, x.cols, x.dtype, out.dtype);
@@ -299,8 +310,8 @@ PyObject *linear_grad(PyObject *const *a) {
     Matrix x, g, dx, dw;
     Fp8 w;   // inputs x outputs
     bool accumulate;
-    if (!flag(a[7], &accumulate) || !matrix(a[0], &x) || !matrix(a[1], &g) || !fp8(a[2], &w) || x.rows != g.rows || w.rows != x.cols ||
-        w.cols != g.cols || (accumulate && a[6] == Py_None) ||
+    if (!flag(a[7], &accumulate) || !matrix(a[0], &x) || !matrix(a[1], &g) || !fp8(a[2], &w) ||
+        x.rows != g.rows || w.rows != x.cols || w.cols != g.cols || (accumulate && a[6] == Py_None) ||
         !result(a[5], a[3], x.rows, x.cols, x.t, &dx) || !result(a[6], a[4], g.cols, x.cols, x.t, &dw))
         Py_RETURN_NONE;
     const int64_t m = x.rows, k = x.cols, n = g.cols;

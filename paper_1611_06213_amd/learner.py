@@ -280,7 +280,11 @@ class Fp8Matrix:
         blocks = -(-cols // 128)
         self.values = torch.empty((rows, 128 * blocks), dtype=torch.float8_e4m3fn, device=device)
         self.scales = torch.empty((-(-blocks // 4), rows), dtype=torch.int32, device=device)
-        self.parts = (self.values, self.scales, rows, cols)   # what the native calls take
+
+    @property
+    def parts(self):
+        """What the native calls take."""
+        return (self.values, self.scales, *self.shape)
 
     def exponents(self):
         """The exponent of every block: rows x blocks, int32."""
@@ -297,6 +301,19 @@ class Fp8Matrix:
 
 def _ref(q: Optional[Fp8Matrix]):
     return None if q is None else ctypes.byref(pl_fp8(q.values.data_ptr(), q.scales.data_ptr()))
+
+
+def _fp8(name: str, q: Fp8Matrix):
+    """_ref(q) of a caller's matrix, whose tensors may have been exchanged for others."""
+    rows, cols = q.shape
+    blocks = -(-cols // 128)
+    for part, t, dtype, shape in (("values", q.values, torch.float8_e4m3fn, (rows, 128 * blocks)),
+                                  ("scales", q.scales, torch.int32, (-(-blocks // 4), rows))):
+        _on_device(f"{name}.{part}", t)
+        if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
+            raise ValueError(f"{name}.{part}: contiguous {dtype} of {shape} expected, not {t.dtype} of "
+                             f"{tuple(t.shape)}, {t.stride()} elements apart")
+    return _ref(q)
 
 
 def _quantize(x, square: bool, plain: bool, transposed: bool):
@@ -349,13 +366,12 @@ def matmul_fp8(a: Fp8Matrix, b: Fp8Matrix, bias=None, relu: bool = False, dtype=
             raise ValueError("accumulate needs out")
         out = torch.empty((m, n), dtype=dtype, device=a.values.device)
     dst, code, ld = _matrix("out", out, m, n)
-    for name, q in (("a", a), ("b", b)):
-        _on_device(name, q.values)
+    a_ref, b_ref = _fp8("a", a), _fp8("b", b)
     bias_ptr, bias_code = _bias(bias, n)
     L = load_library()
     need = L.pl_matmul_fp8_workspace(m, n, k, code)
     work = torch.empty(need, dtype=torch.uint8, device=out.device) if need else None
-    _check(L.pl_matmul_fp8(m, n, k, _ref(a), _ref(b), bias_ptr, bias_code, int(bool(relu)), dst, code, ld,
+    _check(L.pl_matmul_fp8(m, n, k, a_ref, b_ref, bias_ptr, bias_code, int(bool(relu)), dst, code, ld,
                            int(bool(accumulate)), work.data_ptr() if need else None, need, _stream()))
     return out
 
@@ -370,7 +386,7 @@ def linear_fp8(x, w: Fp8Matrix, bias=None, relu: bool = False, dtype=torch.bfloa
             return done
     src, code, src_ld = _matrix("x", x, cols=w.shape[1])
     m, (n, k) = x.shape[0], w.shape
-    _on_device("w", w.values)
+    w_ref = _fp8("w", w)
     if out is None:
         out = torch.empty((m, n), dtype=dtype, device=x.device)
     dst, dst_code, dst_ld = _matrix("out", out, m, n)
@@ -378,7 +394,7 @@ def linear_fp8(x, w: Fp8Matrix, bias=None, relu: bool = False, dtype=torch.bfloa
     L = load_library()
     need = L.pl_linear_fp8_workspace(m, n, k, code, dst_code)
     work = torch.empty(need, dtype=torch.uint8, device=x.device)
-    _check(L.pl_linear_fp8(src, code, m, k, src_ld, n, _ref(w), bias_ptr, bias_code, int(bool(relu)), dst,
+    _check(L.pl_linear_fp8(src, code, m, k, src_ld, n, w_ref, bias_ptr, bias_code, int(bool(relu)), dst,
                            dst_code, dst_ld, work.data_ptr(), need, _stream()))
     return out
 
@@ -398,7 +414,7 @@ def linear_fp8_grad(x, grad, w_t: Fp8Matrix, dtype=torch.bfloat16, weight_dtype=
     src, code, src_ld = _matrix("x", x, cols=k)
     m = x.shape[0]
     grd, grd_code, grd_ld = _matrix("grad", grad, m, n)
-    _on_device("w_t", w_t.values)
+    w_ref = _fp8("w_t", w_t)
     if x_out is None:
         x_out = torch.empty((m, k), dtype=dtype, device=x.device)
     if weight_out is None:
@@ -410,7 +426,7 @@ def linear_fp8_grad(x, grad, w_t: Fp8Matrix, dtype=torch.bfloat16, weight_dtype=
     L = load_library()
     need = L.pl_linear_fp8_grad_workspace(m, n, k, dst_code, wgt_code)
     work = torch.empty(need, dtype=torch.uint8, device=x.device)
-    _check(L.pl_linear_fp8_grad(src, code, src_ld, grd, grd_code, grd_ld, m, n, k, _ref(w_t), dst,
+    _check(L.pl_linear_fp8_grad(src, code, src_ld, grd, grd_code, grd_ld, m, n, k, w_ref, dst,
                                 dst_code, dst_ld, wgt, wgt_code, wgt_ld, int(bool(accumulate)),
                                 work.data_ptr(), need, _stream()))
     return x_out, weight_out

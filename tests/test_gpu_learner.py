@@ -602,3 +602,36 @@ def test_lookup_into_another_type_than_named(torch, learner):
     assert learner.embedding(ids, table, out=half) is half and bool((half == 1).all())
     with pytest.raises(TypeError, match="tensor expected"):
         learner.embedding(ids, table, dtype=torch.float32, out=[0.0])
+
+
+def test_8_bit_matrix_with_other_tensors(torch, learner):
+    """What a matrix's attributes hold at the call counts, on every path; tensors that do not fit its
+    shape are refused before anything reads them."""
+    g = gen(torch, 21)
+    a, w, grad = integers(torch, g, 40, 200), integers(torch, g, 30, 200), integers(torch, g, 40, 30)
+    f32 = torch.float32
+    calls = [lambda q, t: learner.matmul_fp8(learner.quantize_fp8(a), q, dtype=f32),
+             lambda q, t: learner.matmul_fp8(q, learner.quantize_fp8(a), dtype=f32).t(),
+             lambda q, t: learner.linear_fp8(a, q, dtype=f32),
+             lambda q, t: learner.linear_fp8_grad(a, grad, t, dtype=f32)[0]]
+    other = learner.quantize_fp8_both(w * 2 - 3, square=True)
+    want = [call(*other) for call in calls]
+    for i, call in enumerate(calls):
+        mine = learner.quantize_fp8_both(w, square=True)
+        assert not torch.equal(call(*mine), want[i])
+        for m, o in zip(mine, other):
+            m.values, m.scales = o.values.clone(), o.scales.clone()
+        assert torch.equal(call(*mine), want[i])
+        for part in ("values", "scales"):
+            for bad in (lambda t: t[:-1], lambda t: t.flatten(), lambda t: t.view(torch.uint8),
+                        lambda t: torch.cat([t, t], 1)[:, ::2] if t.dtype == torch.int32 else
+                        torch.cat([t.view(torch.uint8)] * 2, 1)[:, ::2].view(torch.float8_e4m3fn)):
+                mine = learner.quantize_fp8_both(w, square=True)
+                for m in mine:
+                    setattr(m, part, bad(getattr(m, part)))
+                with pytest.raises(ValueError, match=part):
+                    call(*mine)
+        for m in mine:
+            m.values, m.scales = m.values.cpu(), m.scales.cpu()
+        with pytest.raises(ValueError, match="device tensor"):
+            call(*mine)
