@@ -157,14 +157,15 @@ bool fp8(PyObject *o, Fp8 *f) {
 
 void *stream() { return c10::hip::getCurrentHIPStream().stream(); }
 
-// Runs `f` (which returns a status and may not touch Python) without the lock.
+// Runs `f` (which returns a status and may not touch Python) without the lock, which is taken back
+// when `f` throws, too: asking for the stream may.
 template <class F>
 int unlocked(F f) {
-    int rc;
-    Py_BEGIN_ALLOW_THREADS
-    rc = f();
-    Py_END_ALLOW_THREADS
-    return rc;
+    struct Released {
+        PyThreadState *state = PyEval_SaveThread();
+        ~Released() { PyEval_RestoreThread(state); }
+    } released;
+    return f();
 }
 
 PyObject *give(int rc, PyObject *out, const at::Tensor &t) {

@@ -5,6 +5,7 @@ import ctypes
 import os
 import re
 import subprocess
+import sys
 
 import pytest
 import torch
@@ -302,3 +303,29 @@ def test_binding_gives_the_stride_that_a_tensor_has(monkeypatch):
     assert learner._matrix("x", one.expand(300, 1))[2] == 0
     assert learner._matrix("x", torch.ones(1, 7).expand(300, 7))[2] == 0
     assert learner._matrix("x", torch.ones(300, 4)[:, :1])[2] == 4
+
+
+def test_native_calls_take_the_lock_back(tmp_path):
+    """What throws while a call runs without the interpreter's lock comes out with the lock held."""
+    src, out = tmp_path / "throws.cpp", str(tmp_path / "throws.so")
+    src.write_text(f'#include "{B.LEARNER_BINDING_SRC}"\n' + r"""
+static PyObject *throws(PyObject *, PyObject *) {
+    bool thrown = false;
+    try {
+        unlocked([]() -> int { throw std::runtime_error("a HIP error"); });
+    } catch (const std::exception &) { thrown = true; }
+    if (!thrown || !PyGILState_Check()) _exit(3);
+    return PyLong_FromLong(unlocked([] { return PyGILState_Check() ? 1 : 7; }));
+}
+static PyMethodDef own[] = {{"throws", throws, METH_NOARGS, ""}, {nullptr, nullptr, 0, nullptr}};
+static PyModuleDef mod = {PyModuleDef_HEAD_INIT, "throws", nullptr, -1, own, nullptr, nullptr, nullptr, nullptr};
+PyMODINIT_FUNC PyInit_throws(void) { return PyModule_Create(&mod); }
+""")
+    cmd = B._binding_cmd(str(src), out, ["-D__HIP_PLATFORM_AMD__", "-DUSE_ROCM", "-include", "unistd.h", "-isystem",
+                                         os.path.join(B.ROCM, "include")],
+                         ["-lc10_hip", "-L", B.HERE, "-lgadeilearner", "-Wl,-rpath," + B.HERE])
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr
+    os.replace(out + ".tmp", out)
+    code = "import sys, torch; sys.path.insert(0, sys.argv[1]); import throws; sys.exit(throws.throws())"
+    assert subprocess.run([sys.executable, "-c", code, str(tmp_path)]).returncode == 7
