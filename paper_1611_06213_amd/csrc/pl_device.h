@@ -21,6 +21,19 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 template <int DT>
 constexpr int kBytes = DT == PS_F32 ? 4 : 2;
 
+// One dimension of a launch takes fewer than 2^32 threads: more workgroups go on in the second, in rows
+// of kGridRow, the last of which may run past the work.
+constexpr uint32_t kGridRow = 1u << 20;
+
+inline bool grid_of(uint64_t blocks, uint32_t threads, dim3 *grid) {
+    if (blocks > 0xffffffffull - kGridRow) return false;
+    if (blocks <= 0xffffffffull / threads) *grid = dim3(static_cast<uint32_t>(blocks));
+    else *grid = dim3(kGridRow, static_cast<uint32_t>((blocks + kGridRow - 1) / kGridRow));
+    return true;
+}
+
+__device__ __forceinline__ uint32_t block_index() { return blockIdx.x + blockIdx.y * kGridRow; }
+
 // Bytes of a result that are left in the caches (256 MB of last level) for whoever reads it.
 constexpr uint64_t kCached = 64ull << 20;
 

@@ -363,8 +363,8 @@ __global__ __launch_bounds__(kBlock) void sum_rows(GradArgs a, Plan p, int lx, u
     __shared__ f32x4 stage[OUT == PS_F32 ? 2 * kBlock : 1];
     const char *ws = static_cast<const char *>(a.workspace);
     const uint32_t *perm = reinterpret_cast<const uint32_t *>(ws + p.perm_at);
-    const bool pieces = blockIdx.x < piece_blocks;
-    const uint32_t block = pieces ? blockIdx.x : blockIdx.x - piece_blocks;
+    const bool pieces = block_index() < piece_blocks;
+    const uint32_t block = pieces ? block_index() : block_index() - piece_blocks;
     const uint32_t group = ((block % tiles_x) << lx) + (threadIdx.x & ((1u << lx) - 1));
     const uint64_t y = static_cast<uint64_t>(block / tiles_x) * (kBlock >> lx) + (threadIdx.x >> lx);
     const uint64_t col = 8ull * group;
@@ -460,9 +460,10 @@ __global__ __launch_bounds__(kBlock) void sum_few(GradArgs a, int lx, uint32_t t
     __shared__ uint32_t counts[kSmallWaves][kSmallRows], begins[kSmallRows + 1], list[kSmallTokens];
     __shared__ float runs[kBlock][8];
     __shared__ uint64_t shared_rows;   // bit r: row r is
-    const uint32_t v0 = blockIdx.x / tiles_x * kSmallRows;
+    const uint32_t v0 = block_index() / tiles_x * kSmallRows;
+    if (v0 >= a.vocab) return;
     const uint32_t x = threadIdx.x & ((1u << lx) - 1), y = threadIdx.x >> lx, ny = kBlock >> lx;
-    const uint32_t group = ((blockIdx.x % tiles_x) << lx) + x;
+    const uint32_t group = ((block_index() % tiles_x) << lx) + x;
     const uint64_t col = 8ull * group;
     const int columns = col >= a.dim ? 0 : a.dim - col < 8 ? static_cast<int>(a.dim - col) : 8;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -567,10 +568,10 @@ hipError_t launch_few(const GradArgs &a, hipStream_t s) {
     while (lx < 4 && (1ull << lx) < groups) ++lx;
     const uint32_t tiles_x = static_cast<uint32_t>((groups + (1ull << lx) - 1) >> lx);
     const uint64_t blocks = (static_cast<uint64_t>(a.vocab) + kSmallRows - 1) / kSmallRows * tiles_x;
-    if (blocks > 0xffffffffull / kBlock) return hipErrorInvalidConfiguration;
-    const uint32_t n = static_cast<uint32_t>(blocks);
-    if (a.drop.drop != 0) sum_few<IDT, G, OUT, true><<<n, kBlock, 0, s>>>(a, lx, tiles_x);
-    else sum_few<IDT, G, OUT, false><<<n, kBlock, 0, s>>>(a, lx, tiles_x);
+    dim3 grid;
+    if (!grid_of(blocks, kBlock, &grid)) return hipErrorInvalidConfiguration;
+    if (a.drop.drop != 0) sum_few<IDT, G, OUT, true><<<grid, kBlock, 0, s>>>(a, lx, tiles_x);
+    else sum_few<IDT, G, OUT, false><<<grid, kBlock, 0, s>>>(a, lx, tiles_x);
     return hipGetLastError();
 }
 
@@ -601,12 +602,11 @@ hipError_t launch_sums(const GradArgs &a, const Plan &p, hipStream_t s) {
     const uint64_t piece_blocks = static_cast<uint64_t>((p.pieces + ny - 1) / ny) * tiles_x;
     const uint64_t blocks = piece_blocks + (static_cast<uint64_t>(a.vocab) + ny - 1) / ny * tiles_x;
     const bool past = static_cast<uint64_t>(a.vocab) * a.dim * kBytes<OUT> > kCached;
-    if (blocks > 0xffffffffull / kBlock) return hipErrorInvalidConfiguration;
+    dim3 grid;
+    if (!grid_of(blocks, kBlock, &grid)) return hipErrorInvalidConfiguration;
     const uint32_t pb = static_cast<uint32_t>(piece_blocks);
-    if (a.drop.drop != 0)
-        sum_rows<G, OUT, true><<<static_cast<uint32_t>(blocks), kBlock, 0, s>>>(a, p, lx, tiles_x, pb, past);
-    else
-        sum_rows<G, OUT, false><<<static_cast<uint32_t>(blocks), kBlock, 0, s>>>(a, p, lx, tiles_x, pb, past);
+    if (a.drop.drop != 0) sum_rows<G, OUT, true><<<grid, kBlock, 0, s>>>(a, p, lx, tiles_x, pb, past);
+    else sum_rows<G, OUT, false><<<grid, kBlock, 0, s>>>(a, p, lx, tiles_x, pb, past);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.pieces == 0) return e;
     const int join_lx = std::min(lx, kJoinMostGroups);

@@ -552,7 +552,8 @@ __global__ __launch_bounds__(64 * WAVES) void slim(MatmulArgs g, Split sp) {
     constexpr int A = kAhead<FM>;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int q = lane >> 4, r16 = lane & 15;
-    const uint32_t part = blockIdx.x / sp.tiles_n, n0 = blockIdx.x % sp.tiles_n * 16;
+    const uint32_t part = block_index() / sp.tiles_n, n0 = block_index() % sp.tiles_n * 16;
+    if (part >= sp.parts) return;
     const uint32_t blocks = (g.k + 127) / 128, ld = blocks * 128;
     const uint32_t first = part * sp.steps, last = min(blocks, first + sp.steps);
     const uint32_t pitch = ld + 16;   // of x's rows in LDS: in different banks
@@ -677,7 +678,7 @@ __global__ __launch_bounds__(256) void join(Products both) {
 template <int OUT>
 __global__ __launch_bounds__(256) void empty(MatmulArgs g) {
     const uint32_t fours = (g.n + 3) / 4;
-    const uint64_t i = static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x;
+    const uint64_t i = static_cast<uint64_t>(block_index()) * 256 + threadIdx.x;
     if (i >= static_cast<uint64_t>(g.m) * fours) return;
     finish<OUT>(g, f32x4{0, 0, 0, 0}, static_cast<uint32_t>(i / fours),
                 static_cast<uint32_t>(i % fours) * 4);
@@ -791,12 +792,15 @@ hipError_t launch_slim(const MatmulArgs &g, const Split &sp, hipStream_t s) {
     const uint32_t blocks = (g.k + 127) / 128;
     const uint32_t x = X == kGiven ? 0 : g.m * (blocks * 128 + 16) + g.m * blocks;
     constexpr uint32_t kSums = FM * 64 * sizeof(f32x4);   // of a wave
-    const uint32_t n = sp.tiles_n * sp.parts;
+    const bool long_rows = sp.steps > 64 || sp.parts > 1;
+    dim3 grid;
+    if (!grid_of(static_cast<uint64_t>(sp.tiles_n) * sp.parts, long_rows ? 1024 : 512, &grid))
+        return hipErrorInvalidConfiguration;
     // Sixteen waves have more of a long row under way, eight leave room for a second workgroup on
     // the compute unit where rows are many and short: 1 x 4096 x 25088 23.0 us with 16, 24.6 with 8;
     // 1 x 25088 x 4096 31.7 and 25.0.
-    if (sp.steps > 64 || sp.parts > 1) slim<FM, OUT, X, 16><<<n, 1024, std::max(16 * kSums, x), s>>>(g, sp);
-    else slim<FM, OUT, X, 8><<<n, 512, std::max(8 * kSums, x), s>>>(g, sp);
+    if (long_rows) slim<FM, OUT, X, 16><<<grid, 1024, std::max(16 * kSums, x), s>>>(g, sp);
+    else slim<FM, OUT, X, 8><<<grid, 512, std::max(8 * kSums, x), s>>>(g, sp);
     return hipGetLastError();
 }
 
@@ -828,8 +832,9 @@ hipError_t launch_join(const Products &p, hipStream_t s) {
 template <int OUT>
 hipError_t launch(const MatmulArgs &g, hipStream_t s) {
     if (g.k == 0) {
-        if (join_blocks(g) > 0xffffffffull / 256) return hipErrorInvalidConfiguration;
-        empty<OUT><<<static_cast<uint32_t>(join_blocks(g)), 256, 0, s>>>(g);
+        dim3 grid;
+        if (!grid_of(join_blocks(g), 256, &grid)) return hipErrorInvalidConfiguration;
+        empty<OUT><<<grid, 256, 0, s>>>(g);
         return hipGetLastError();
     }
     Products p{};

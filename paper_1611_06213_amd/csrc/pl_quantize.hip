@@ -33,9 +33,10 @@ struct Two {
 
 template <int X, bool SQUARE>
 __global__ __launch_bounds__(kThreads) void quantize_tile(Two two) {
-    const bool second = blockIdx.x >= two.blocks[0];
+    const bool second = block_index() >= two.blocks[0];
     const QuantArgs &a = two.q[second];
-    const uint32_t tiles_x = two.tiles_x[second], tile = blockIdx.x - (second ? two.blocks[0] : 0);
+    const uint32_t tiles_x = two.tiles_x[second], tile = block_index() - (second ? two.blocks[0] : 0);
+    if (tile >= two.blocks[second]) return;
     using M = Mags<X>;
     constexpr int W = M::kWords;
     __shared__ uint32_t col_max[kTile];
@@ -147,8 +148,8 @@ template <int X>
 __global__ __launch_bounds__(kBlock) void quantize_rows(QuantArgs a, uint32_t words) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t ld = (a.cols + 127) / 128 * 128;
-    const uint32_t word = blockIdx.x % words;
-    const int64_t r0 = (static_cast<int64_t>(blockIdx.x / words) * (kBlock / 64) + wave) * kAlong;
+    const uint32_t block = block_index(), word = block % words;
+    const int64_t r0 = (static_cast<int64_t>(block / words) * (kBlock / 64) + wave) * kAlong;
     const int64_t col = 512ll * word + 8 * lane;
     if (col >= ld) return;   // whole blocks, whole sixteens of lanes
     const int count = a.cols - col >= 8 ? 8 : a.cols > col ? static_cast<int>(a.cols - col) : 0;
@@ -178,10 +179,11 @@ hipError_t launch_quantize(const QuantArgs &a, int dtype, bool square, hipStream
         const uint64_t words = (a.cols + 511) / 512;
         constexpr int kPer = kBlock / 64 * kAlong;   // rows of a workgroup
         const uint64_t blocks = words * ((a.rows + kPer - 1) / kPer);
-        if (blocks > 0xffffffffull / kBlock) return hipErrorInvalidConfiguration;
-        const uint32_t n = static_cast<uint32_t>(blocks), w = static_cast<uint32_t>(words);
-        if (dtype == PS_F32) quantize_rows<PS_F32><<<n, kBlock, 0, s>>>(a, w);
-        else quantize_rows<PS_BF16><<<n, kBlock, 0, s>>>(a, w);
+        dim3 grid;
+        if (!grid_of(blocks, kBlock, &grid)) return hipErrorInvalidConfiguration;
+        const uint32_t w = static_cast<uint32_t>(words);
+        if (dtype == PS_F32) quantize_rows<PS_F32><<<grid, kBlock, 0, s>>>(a, w);
+        else quantize_rows<PS_BF16><<<grid, kBlock, 0, s>>>(a, w);
         return hipGetLastError();
     }
     return launch_quantize_two(a, QuantArgs{}, dtype, square, s);
@@ -191,22 +193,22 @@ hipError_t launch_quantize_two(const QuantArgs &a, const QuantArgs &b, int dtype
                                hipStream_t s) {
     Two two{{a, b}, {}, {}};
     uint64_t all = 0;
+    dim3 grid;
     for (int i = 0; i < 2; ++i) {
         const uint64_t x = (two.q[i].cols + kTile - 1) / kTile;
         const uint64_t blocks = x * ((two.q[i].rows + kTile - 1) / kTile);
         all += blocks;
-        if (all > 0xffffffffull / kThreads) return hipErrorInvalidConfiguration;
+        if (!grid_of(all, kThreads, &grid)) return hipErrorInvalidConfiguration;
         two.tiles_x[i] = static_cast<uint32_t>(x);
         two.blocks[i] = static_cast<uint32_t>(blocks);
     }
     if (all == 0) return hipSuccess;
-    const uint32_t n = static_cast<uint32_t>(all);
     if (dtype == PS_F32) {
-        if (square) quantize_tile<PS_F32, true><<<n, kThreads, 0, s>>>(two);
-        else quantize_tile<PS_F32, false><<<n, kThreads, 0, s>>>(two);
+        if (square) quantize_tile<PS_F32, true><<<grid, kThreads, 0, s>>>(two);
+        else quantize_tile<PS_F32, false><<<grid, kThreads, 0, s>>>(two);
     } else {
-        if (square) quantize_tile<PS_BF16, true><<<n, kThreads, 0, s>>>(two);
-        else quantize_tile<PS_BF16, false><<<n, kThreads, 0, s>>>(two);
+        if (square) quantize_tile<PS_BF16, true><<<grid, kThreads, 0, s>>>(two);
+        else quantize_tile<PS_BF16, false><<<grid, kThreads, 0, s>>>(two);
     }
     return hipGetLastError();
 }

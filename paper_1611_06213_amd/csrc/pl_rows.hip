@@ -16,7 +16,7 @@ constexpr int kBlock = 256;
 // The block's threads cover 2^lx groups of eight columns times 256 / 2^lx rows.
 template <int IDT, int X, int OUT, bool DROP, int ROWS, bool NT>
 __global__ __launch_bounds__(kBlock) void rows_kernel(RowsArgs a, int lx, uint32_t tiles_x) {
-    const uint32_t tile_y = blockIdx.x / tiles_x, tile_x = blockIdx.x % tiles_x;
+    const uint32_t block = block_index(), tile_y = block / tiles_x, tile_x = block % tiles_x;
     const uint32_t group = (tile_x << lx) + (threadIdx.x & ((1u << lx) - 1));
     const uint32_t ny = kBlock >> lx;
     const uint64_t first = static_cast<uint64_t>(tile_y) * ny * ROWS + (threadIdx.x >> lx);
@@ -85,8 +85,9 @@ hipError_t launch_shape(const RowsArgs &a, int lx, hipStream_t s) {
     const uint64_t tiles_x = (groups + (1ull << lx) - 1) >> lx;
     const uint64_t rows = static_cast<uint64_t>(kBlock >> lx) * ROWS;
     const uint64_t blocks = tiles_x * ((a.rows + rows - 1) / rows);
-    if (blocks > 0xffffffffull / kBlock) return hipErrorInvalidConfiguration;
-    rows_kernel<IDT, X, OUT, DROP, ROWS, NT><<<static_cast<uint32_t>(blocks), kBlock, 0, s>>>(
+    dim3 grid;
+    if (!grid_of(blocks, kBlock, &grid)) return hipErrorInvalidConfiguration;
+    rows_kernel<IDT, X, OUT, DROP, ROWS, NT><<<grid, kBlock, 0, s>>>(
         a, lx, static_cast<uint32_t>(tiles_x));
     return hipGetLastError();
 }

@@ -635,3 +635,55 @@ def test_8_bit_matrix_with_other_tensors(torch, learner):
             m.values, m.scales = m.values.cpu(), m.scales.cpu()
         with pytest.raises(ValueError, match="device tensor"):
             call(*mine)
+
+
+def only_these(torch, out, rows, want):
+    """Rows of `out` are `want`, all others zeros."""
+    assert torch.equal(out[rows], want)
+    out[rows] = 0
+    step = max(1, (1 << 28) // out.shape[1])
+    assert not any(bool(out[i:i + step].any()) for i in range(0, len(out), step))
+
+
+@pytest.fixture
+def much_memory(torch):
+    torch.cuda.empty_cache()
+    yield
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("vocab,dim", [((1 << 24) + 5, 1025), ((1 << 30) + 70, 1)])
+def test_table_gradients_of_many_workgroups(torch, learner, much_memory, vocab, dim):
+    """More workgroups than one dimension of a launch takes: by sorting, and in one launch."""
+    ids = torch.tensor([vocab - 1, 3, (1 << 24) - 1, 1 << 24, vocab], device="cuda")
+    ids[2:4] %= vocab
+    grad = integers(torch, gen(torch, 1), 5, dim)
+    out = torch.full((vocab, dim), 7.0, dtype=torch.bfloat16, device="cuda")
+    learner.embedding_grad(ids, grad, vocab, out=out)
+    only_these(torch, out, ids[:4], grad[:4].bfloat16())
+
+
+def test_products_of_many_workgroups(torch, learner, much_memory):
+    """The same for quantisation and for few rows times many; products without terms."""
+    n, g = (1 << 27) + 20, gen(torch, 2)
+    w = torch.randint(-8, 9, (n, 1), generator=g, device="cuda", dtype=torch.int8).float()
+    q = learner.quantize_fp8(w)
+    for m in (1, 20):
+        x = integers(torch, g, m, 1)
+        y = learner.linear_fp8(x, q)
+        for i in range(m):
+            assert torch.equal(y[i], (w[:, 0] * x[i, 0]).bfloat16())
+        del y
+    del q
+    rows = (1 << 30) + 200
+    w = torch.randint(-8, 9, (rows, 1), generator=g, device="cuda", dtype=torch.int8).bfloat16()
+    t = learner.quantize_fp8(w, transpose=True)
+    assert torch.equal(t.values[0, :rows].to(torch.bfloat16) * torch.exp2(
+        t.exponents()[0].bfloat16()).repeat_interleave(128)[:rows], w[:, 0])
+    assert not bool(t.values.view(torch.uint8)[0, rows:].any())
+    del w, t
+    m, n = 1 << 17, (1 << 17) + 8
+    out = torch.full((m, n), 7.0, dtype=torch.bfloat16, device="cuda")
+    empty = lambda r: learner.quantize_fp8(torch.ones(r, 0, device="cuda"))
+    learner.matmul_fp8(empty(m), empty(n), out=out)
+    only_these(torch, out, torch.arange(1, device="cuda"), torch.zeros(1, n, dtype=torch.bfloat16, device="cuda"))
