@@ -687,3 +687,47 @@ def test_products_of_many_workgroups(torch, learner, much_memory):
     empty = lambda r: learner.quantize_fp8(torch.ones(r, 0, device="cuda"))
     learner.matmul_fp8(empty(m), empty(n), out=out)
     only_these(torch, out, torch.arange(1, device="cuda"), torch.zeros(1, n, dtype=torch.bfloat16, device="cuda"))
+
+
+def cancelling(torch, g, rows, others, k):
+    """Whole numbers a (rows x k) and b (others x k) with columns of 256 and -256 spread over k, whose
+    products, 65536 of either sign, cancel in every sum. All products and partial sums are whole and
+    below 2^24 (128 large ones, 2^23, and k times 64), so that fp32 sums are exact in any order; sums
+    that lose what lies 16 bits below a large product are not."""
+    a, b = integers(torch, g, rows, k), integers(torch, g, others, k)
+    many = min(128, k // 2) // 2 * 2
+    columns = torch.randperm(k, generator=g, device="cuda")[:many].sort().values
+    sign = lambda *s: torch.randint(0, 2, s, generator=g, device="cuda").float() * 2 - 1
+    s = sign(many)
+    a[:, columns] = 256 * s * sign(rows, 1)
+    b[:, columns] = 256 * s * sign(others, 1) * (1 - 2.0 * (torch.arange(many, device="cuda") % 2))
+    return a, b
+
+
+@pytest.mark.parametrize("m,n,k", SIZES)
+@pytest.mark.parametrize("x", ["f32", "bf16"])
+def test_fp32_results_have_fp32_sums(torch, learner, m, n, k, x):
+    g = gen(torch, m + n + k)
+    a, b = cancelling(torch, g, m, n, k)
+    want = (a.double() @ b.double().t()).float()
+    qb = learner.quantize_fp8(b)
+    assert torch.equal(learner.matmul_fp8(learner.quantize_fp8(a), qb, dtype=torch.float32), want)
+    assert torch.equal(learner.linear_fp8(a.to(dt(torch, x)), qb, dtype=torch.float32), want)
+
+
+@pytest.mark.parametrize("m,n,k", [(57, 1000, 900), (33, 33, 1), (130, 700, 4100), (20, 500, 500),
+                                   (300, 20, 500), (2100, 2050, 300)])
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+def test_fp32_gradients_have_fp32_sums(torch, learner, m, n, k, out):
+    """Alone, and where the other product of a launch has a result in bf16."""
+    g = gen(torch, m + n)
+    t, f32, other = (lambda v: v.t().contiguous()), torch.float32, dt(torch, out)
+    grad, w_t = cancelling(torch, g, m, k, n)   # over the result's columns
+    x = integers(torch, g, m, k)
+    dx = learner.linear_fp8_grad(x, grad, learner.quantize_fp8(t(w_t), square=True, transpose=True), dtype=f32,
+                                 weight_dtype=other)[0]
+    assert torch.equal(dx, (grad.double() @ w_t.double().t()).float())
+    grad_t, x_t = cancelling(torch, g, n, k, m)   # over the rows
+    w = learner.quantize_fp8(integers(torch, g, n, k), square=True, transpose=True)
+    dw = learner.linear_fp8_grad(t(x_t), t(grad_t), w, dtype=other, weight_dtype=f32)[1]
+    assert torch.equal(dw, (grad_t.double() @ x_t.double().t()).float())
