@@ -731,3 +731,68 @@ def test_fp32_gradients_have_fp32_sums(torch, learner, m, n, k, out):
     w = learner.quantize_fp8(integers(torch, g, n, k), square=True, transpose=True)
     dw = learner.linear_fp8_grad(t(x_t), t(grad_t), w, dtype=other, weight_dtype=f32)[1]
     assert torch.equal(dw, (grad_t.double() @ x_t.double().t()).float())
+
+
+def exact_gradient(torch, learner, ids, grad, vocab, drop, out):
+    """Of whole numbers, scale 1/2: every sum is exact in any order. p = 1/2 is a factor of two."""
+    g = grad.double() if drop is None else learner.dropout(grad.float(), drop).double()
+    want = torch.zeros(vocab + 1, grad.shape[1], dtype=torch.float64, device="cuda")
+    real = (ids >= 0) & (ids < vocab)
+    want.index_add_(0, torch.where(real, ids, vocab).long(), g)
+    return (want[:vocab] * 0.5).to(out)
+
+
+@pytest.mark.parametrize("p", [None, 0.5])
+@pytest.mark.parametrize("x,out", [("f32", "f32"), ("bf16", "f32"), ("bf16", "bf16")])
+def test_large_table_gradient(torch, learner, p, x, out):
+    """2^25 elements and more (pieces of 32 tokens) into a table past the caches: rows of one token, of a
+    whole piece, of one more, and of thousands; whole lines of a wave's columns and the rest of a row."""
+    tokens, vocab, dim = 33_000, 40_000, 1030
+    g = gen(torch, 31)
+    ids = torch.randint(0, vocab, (tokens,), generator=g, device="cuda")
+    ids[:9000], ids[9000:9032], ids[9032:9065], ids[9065:9129] = 7, vocab - 1, 300, 301
+    ids[9129:9300] = -1
+    ids = ids[torch.randperm(tokens, generator=g, device="cuda")]
+    grad = integers(torch, g, tokens, dim).to(dt(torch, x))
+    drop = None if p is None else learner.Dropout(p, 8, 9)
+    got = learner.embedding_grad(ids, grad, vocab, 0.5, drop, dtype=dt(torch, out))
+    assert torch.equal(got, exact_gradient(torch, learner, ids, grad, vocab, drop, dt(torch, out)))
+    old = integers(torch, g, vocab, dim).to(dt(torch, out))
+    want = old.double() + exact_gradient(torch, learner, ids, grad, vocab, drop, torch.float64)
+    learner.embedding_grad(ids, grad, vocab, 0.5, drop, out=old, accumulate=True)
+    assert torch.equal(old, want.to(old.dtype))
+
+
+def test_many_frequent_ids_of_one_class(torch, learner):
+    """More ids cut into many pieces than a workgroup of the sort lists: it takes those that are equal
+    modulo a power of two of at least 256."""
+    vocab, dim = 20_000, 24
+    ids = torch.arange(0, vocab, 256, device="cuda").repeat(60)
+    assert len(ids) > 4096 and len(ids.unique()) > 64
+    g = gen(torch, 41)
+    ids = ids[torch.randperm(len(ids), generator=g, device="cuda")].int()
+    grad = integers(torch, g, len(ids), dim)
+    got = learner.embedding_grad(ids, grad, vocab, 0.5)
+    assert torch.equal(got, exact_gradient(torch, learner, ids, grad, vocab, None, torch.float32))
+
+
+@pytest.mark.parametrize("x,out", [("bf16", "bf16"), ("f32", "f32"), ("bf16", "f32")])
+@pytest.mark.parametrize("cols", [2048, 2051])
+def test_dropout_past_the_caches(torch, learner, x, out, cols):
+    """Every element of results of more than 64 MB."""
+    g = gen(torch, 51)
+    rows = (66 << 20) // (cols * (2 if out == "bf16" else 4))
+    drop = learner.Dropout(0.3, (1 << 40) + 3, 5)
+    keep, up = ref.kept(rows, cols, *drop)
+    keep = torch.from_numpy(keep > 0).cuda()
+    ids = torch.randint(-1, 300, (rows,), generator=g, device="cuda")
+    table = randn(torch, g, 300, cols, dtype=dt(torch, x))
+    got = learner.embedding(ids, table, 1.5, drop, dtype=dt(torch, out))
+    factor = float(np.float32(1.5 * up))
+    want = torch.where(keep & (ids >= 0)[:, None], table.float()[ids.clamp(min=0)] * factor, 0.0)
+    assert torch.equal(got, want.to(dt(torch, out)))
+    if x == out:
+        src = randn(torch, g, rows, cols, dtype=dt(torch, x))
+        want = torch.where(keep, src.float() * float(np.float32(up)), 0.0).to(src.dtype)
+        assert torch.equal(learner.dropout(src, drop), want)
+        assert torch.equal(learner.dropout(src, drop, out=src), want)
