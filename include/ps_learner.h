@@ -115,9 +115,12 @@ int pl_quantize_fp8(const void *x, int dtype, int64_t rows, int64_t cols, int64_
  * bias with accumulate are refused. m, n, k may be 0 (k = 0: a sum of no terms);
  * m, n <= 2^28, k <= 2^22.
  *
- * An fp32 result carries fp32 sums. For a bf16 result the 8-bit matrix instructions are
- * used, at twice the rate: they keep 13 bits below the largest of eight products that they
- * add at a time, an error of about 2^-19 of the sum of the products' magnitudes. */
+ * An fp32 result carries fp32 sums of the products of the elements, which count as they are but
+ * in blocks whose scale is below 2^-124, where they are rounded to multiples of 2^-133.
+ *
+ * For a bf16 result the 8-bit matrix instructions are used, at twice the rate: they keep 13 bits
+ * below the largest of eight products that they add at a time, an error of about 2^-19 of
+ * the sum of the products' magnitudes (root mean square). */
 int pl_matmul_fp8(int64_t m, int64_t n, int64_t k, const pl_fp8 *a, const pl_fp8 *b,
                   const void *bias, int bias_dtype, int relu, void *out, int out_dtype,
                   int64_t out_ld, int accumulate, void *workspace, size_t workspace_bytes,

@@ -11,8 +11,10 @@
 //              for the 16 x 16 x 32 form): an error of 2^-19 of the sum of the products'
 //              magnitudes, root mean square, far below bf16's 2^-9 of the result.
 // out in fp32  16 x 16 x 32 on bf16 operands, at half the rate. An 8-bit value times its block's
-//              scale is a bf16 number exactly (one conversion instruction for two of them), and
-//              this instruction's sums are fp32 sums (an error of 2^-27 or less, measured).
+//              scale is a bf16 number exactly for scales from 2^-124 on (one conversion instruction
+//              for two of them; e4m3's least, 2^-9, is then bf16's least, 2^-133, to which the two
+//              smaller scales round), and this instruction's sums are fp32 sums (an error of 2^-27
+//              or less, measured).
 //
 // The first operand is b: then a lane holds four neighbouring columns of out, of one row.
 // Lane l gives row l % 16 of either operand, and 32 of the block's columns; which 32 does not

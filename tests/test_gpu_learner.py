@@ -796,3 +796,25 @@ def test_dropout_past_the_caches(torch, learner, x, out, cols):
         want = torch.where(keep, src.float() * float(np.float32(up)), 0.0).to(src.dtype)
         assert torch.equal(learner.dropout(src, drop), want)
         assert torch.equal(learner.dropout(src, drop, out=src), want)
+
+
+@pytest.mark.parametrize("m", [1, 20, 40, 300])
+@pytest.mark.parametrize("e", [-126, -125, -124, -123, -118])
+def test_products_of_the_smallest_scales(torch, learner, m, e):
+    """Every e4m3 value in blocks of the smallest scales, each times 2^100: bf16 results take the values as
+    they are, fp32 ones too from a scale of 2^-124 on, and to bf16's least number, 2^-133, below."""
+    code = torch.arange(127, dtype=torch.uint8, device="cuda")   # 0 .. 448: the block's largest is its scale's
+    value = code.view(torch.float8_e4m3fn).double() * 2.0 ** e
+    small = torch.zeros(m, 128, device="cuda")
+    small[:, :127] = value.float()   # exact: the least is 2^-135
+    large = torch.zeros(127, 128, device="cuda")
+    large[code.long(), code.long()] = 2.0 ** 100
+    q, ql = learner.quantize_fp8(small), learner.quantize_fp8(large)
+    assert bool((q.exponents() == e).all()) and torch.equal(q.dequantize().double()[:, :127], value.expand(m, 127))
+    want = (value * 2.0 ** 100).expand(m, 127)
+    tol = 2.0 ** -133 * 2.0 ** 100 if e < -124 else 0.0
+    for got in (learner.matmul_fp8(q, ql, dtype=torch.float32), learner.matmul_fp8(ql, q, dtype=torch.float32).t(),
+                learner.linear_fp8(small, ql, dtype=torch.float32)):
+        assert float((got.double() - want).abs().max()) <= tol
+    assert torch.equal(learner.matmul_fp8(q, ql), want.bfloat16())
+    assert torch.equal(learner.matmul_fp8(ql, q).t(), want.bfloat16())
