@@ -289,14 +289,17 @@ class Fp8Matrix:
     def exponents(self):
         """The exponent of every block: rows x blocks, int32."""
         rows, cols = self.shape
-        per_byte = self.scales.view(torch.uint8).view(-1, rows, 4)
-        return per_byte.permute(1, 0, 2).reshape(rows, -1)[:, :-(-cols // 128)].int() - 127
+        words, blocks = self.scales.shape[0], -(-cols // 128)
+        per_byte = self.scales.view(torch.uint8).view(words, rows, 4)
+        return per_byte.permute(1, 0, 2).reshape(rows, 4 * words)[:, :blocks].int() - 127
 
     def dequantize(self):
         """The values that it stands for, in fp32 (exact)."""
         rows, cols = self.shape
+        blocks = -(-cols // 128)
         two = ((self.exponents() + 127) << 23).view(torch.float32)
-        return (self.values.float().view(rows, -1, 128) * two[:, :, None]).view(rows, -1)[:, :cols]
+        values = self.values.float().view(rows, blocks, 128) * two[:, :, None]
+        return values.view(rows, 128 * blocks)[:, :cols]
 
 
 def _ref(q: Optional[Fp8Matrix]):

@@ -818,3 +818,10 @@ def test_products_of_the_smallest_scales(torch, learner, m, e):
         assert float((got.double() - want).abs().max()) <= tol
     assert torch.equal(learner.matmul_fp8(q, ql), want.bfloat16())
     assert torch.equal(learner.matmul_fp8(ql, q).t(), want.bfloat16())
+
+
+@pytest.mark.parametrize("rows,cols", [(0, 5), (5, 0), (0, 0), (0, 700)])
+def test_empty_8_bit_matrices(torch, learner, rows, cols):
+    q, t = learner.quantize_fp8_both(torch.ones(rows, cols, device="cuda"))
+    assert q.dequantize().shape == (rows, cols) and t.dequantize().shape == (cols, rows)
+    assert q.exponents().shape == (rows, -(-cols // 128))
