@@ -154,6 +154,14 @@ def _matrix(name: str, t, rows: Optional[int] = None, cols: Optional[int] = None
     return t.data_ptr(), _code(t.dtype), t.stride(0)
 
 
+def _flat(name: str, t, rows: int, cols: int):
+    try:
+        return t.view(rows, cols)
+    except RuntimeError as e:
+        raise ValueError(f"{name}: its rows, of shape {tuple(t.shape)} with strides {t.stride()}, are not those "
+                         "of a matrix") from e
+
+
 def _stream() -> int:
     return torch.cuda.current_stream().cuda_stream
 
@@ -171,6 +179,9 @@ class Dropout(NamedTuple):
 def _drop(drop: Optional[Dropout]):
     if drop is None:
         return None
+    if not isinstance(drop, tuple) or len(drop) != 3:
+        raise TypeError(f"drop: a Dropout expected, not {type(drop).__name__}")
+    drop = Dropout(*drop)
     if not 0 <= drop.seed < 1 << 64 or not 0 <= drop.offset < 1 << 64:
         raise ValueError("dropout: seed and offset are 64-bit")
     return ctypes.byref(pl_drop(drop.p, drop.seed, drop.offset))
@@ -228,6 +239,8 @@ def embedding_grad(ids, grad, rows: int, scale: float = 1.0, drop: Optional[Drop
         grad = grad.reshape(tokens, grad.shape[-1])
     src, src_code, src_ld = _matrix("grad", grad, rows=tokens)
     dim = grad.shape[1]
+    if rows < 0:
+        raise ValueError(f"{rows} rows")
     if out is None:
         if accumulate:
             raise ValueError("accumulate needs out")
@@ -252,13 +265,15 @@ def dropout(x, drop: Dropout, out=None):
         if _done(done):
             return done
     _on_device("x", x)
+    if out is not None:
+        _on_device("out", out)
     if out is not None and (out.shape != x.shape or out.dtype != x.dtype):
         raise ValueError(f"out of {tuple(out.shape)} {out.dtype} for x of {tuple(x.shape)} {x.dtype}")
     result = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
     if x.dim() != 2:
         cols = x.shape[-1] if x.dim() else 1
         rows = x.numel() // cols if cols else 0
-        x, out = x.view(rows, cols), result.view(rows, cols)
+        x, out = _flat("x", x, rows, cols), _flat("out", result, rows, cols)
     else:
         out = result
     rows, cols = x.shape
@@ -300,6 +315,12 @@ class Fp8Matrix:
         two = ((self.exponents() + 127) << 23).view(torch.float32)
         values = self.values.float().view(rows, blocks, 128) * two[:, :, None]
         return values.view(rows, 128 * blocks)[:, :cols]
+
+
+def _parts(name: str, q):
+    if not isinstance(q, Fp8Matrix):
+        raise TypeError(f"{name}: an Fp8Matrix expected, not {type(q).__name__}")
+    return q.parts
 
 
 def _ref(q: Optional[Fp8Matrix]):
@@ -356,9 +377,10 @@ def matmul_fp8(a: Fp8Matrix, b: Fp8Matrix, bias=None, relu: bool = False, dtype=
                out=None, accumulate: bool = False):
     """a b^T (+ bias, then max(., 0) with relu), of `dtype` or written to `out`; with
     `accumulate` added to what `out` holds."""
+    a_parts, b_parts = _parts("a", a), _parts("b", b)
     native = _native or _native_calls()
     if native:
-        done = native.product(a.parts, b.parts, bias, relu, dtype, out, accumulate)
+        done = native.product(a_parts, b_parts, bias, relu, dtype, out, accumulate)
         if _done(done):
             return done
     (m, k), (n, k2) = a.shape, b.shape
@@ -382,9 +404,10 @@ def matmul_fp8(a: Fp8Matrix, b: Fp8Matrix, bias=None, relu: bool = False, dtype=
 def linear_fp8(x, w: Fp8Matrix, bias=None, relu: bool = False, dtype=torch.bfloat16, out=None):
     """A fully connected layer: x w^T (+ bias, relu). x is quantised along its rows; w is the
     layer's weight (outputs x inputs), quantised (square) once per pull."""
+    w_parts = _parts("w", w)
     native = _native or _native_calls()
     if native:
-        done = native.linear(x, w.parts, bias, relu, dtype, out)
+        done = native.linear(x, w_parts, bias, relu, dtype, out)
         if _done(done):
             return done
     src, code, src_ld = _matrix("x", x, cols=w.shape[1])
@@ -408,9 +431,10 @@ def linear_fp8_grad(x, grad, w_t: Fp8Matrix, dtype=torch.bfloat16, weight_dtype=
     transposed weight, quantised (square); grad is quantised along its rows for the first
     product and along its columns, as x, for the second. `weight_out`, a view into the
     learner's gradient row, is written, or with `accumulate` added to."""
+    w_parts = _parts("w_t", w_t)
     native = _native or _native_calls()
     if native:
-        done = native.linear_grad(x, grad, w_t.parts, dtype, weight_dtype, x_out, weight_out, accumulate)
+        done = native.linear_grad(x, grad, w_parts, dtype, weight_dtype, x_out, weight_out, accumulate)
         if _done(done):
             return done
     k, n = w_t.shape

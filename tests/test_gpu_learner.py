@@ -825,3 +825,26 @@ def test_empty_8_bit_matrices(torch, learner, rows, cols):
     q, t = learner.quantize_fp8_both(torch.ones(rows, cols, device="cuda"))
     assert q.dequantize().shape == (rows, cols) and t.dequantize().shape == (cols, rows)
     assert q.exponents().shape == (rows, -(-cols // 128))
+
+
+def test_refused_arguments_raise_what_is_said(torch, learner):
+    """TypeError or ValueError, as the binding documents."""
+    x, ids = torch.ones(4, 6, device="cuda"), torch.zeros(4, dtype=torch.int64, device="cuda")
+    q, drop = learner.quantize_fp8(x), learner.Dropout(0.5, 1)
+    for call in (lambda: learner.matmul_fp8(x, q), lambda: learner.matmul_fp8(q, x), lambda: learner.linear_fp8(x, x),
+                 lambda: learner.linear_fp8_grad(x, x, x), lambda: learner.linear_fp8(x, None),
+                 lambda: learner.dropout(x, 0.5), lambda: learner.embedding(ids, x, drop=0.5),
+                 lambda: learner.dropout(x, ("p", 1, 2)), lambda: learner.dropout(x, drop, out=[1.0]),
+                 lambda: learner.embedding_grad(ids, [1.0], 5), lambda: learner.quantize_fp8([1.0])):
+        with pytest.raises(TypeError):
+            call()
+    y = torch.ones(4, 6, 8, device="cuda")
+    for call in (lambda: learner.dropout(y.transpose(0, 1), drop), lambda: learner.dropout(x.flatten()[::2], drop),
+                 lambda: learner.dropout(y, drop, out=torch.ones(6, 4, 8, device="cuda").transpose(0, 1)),
+                 lambda: learner.embedding_grad(ids, x, -1), lambda: learner.dropout(x, drop, out=x.cpu())):
+        with pytest.raises(ValueError):
+            call()
+    # a plain triple names a dropout, rows of a matrix in more dimensions need not be neighbours
+    assert torch.equal(learner.dropout(x, (0.5, 1, 0)), learner.dropout(x, drop))
+    part = torch.ones(4, 3, 12, device="cuda")[:, :, :8]
+    assert torch.equal(learner.dropout(part, drop), learner.dropout(part.contiguous(), drop))
