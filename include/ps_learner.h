@@ -20,8 +20,9 @@
  *     input or another output, except that pl_dropout may work in place (out == x
  *     with equal strides).
  *   - Element types are PS_F32 and PS_BF16. Sums are held in fp32 and rounded once
- *     to the output's type (nearest even). Results do not depend on scheduling:
- *     equal calls give equal bits.
+ *     to the output's type (nearest even); an 8-bit product with a bf16 result loses more
+ *     (see pl_matmul_fp8). Results do not depend on scheduling: equal calls give equal
+ *     bits.
  *
  * Status codes and their names are ps.h's: PS_OK, PS_EINVAL (a refused argument;
  * nothing was enqueued), PS_ENOMEM (workspace too small; nothing was enqueued),
@@ -106,7 +107,7 @@ size_t pl_fp8_scales_bytes(int64_t rows, int64_t cols);
  * be NULL; x is read once for both. square: one scale for each 128 x 128 tile of x instead
  * (for weights: both layouts then hold the same values). A block's scale is the least
  * 2^e, e >= -126, with max|x| <= 448 * 2^e over its finite elements; elements are rounded
- * to nearest even. NaN and infinities become NaN. */
+ * to nearest even. NaN and infinities become NaN. rows, cols < 2^31. */
 int pl_quantize_fp8(const void *x, int dtype, int64_t rows, int64_t cols, int64_t ld, int square,
                     const pl_fp8 *out, const pl_fp8 *out_t, void *stream);
 
@@ -118,9 +119,10 @@ int pl_quantize_fp8(const void *x, int dtype, int64_t rows, int64_t cols, int64_
  * An fp32 result carries fp32 sums of the products of the elements, which count as they are but
  * in blocks whose scale is below 2^-124, where they are rounded to multiples of 2^-133.
  *
- * For a bf16 result the 8-bit matrix instructions are used, at twice the rate: they keep 13 bits
- * below the largest of eight products that they add at a time, an error of about 2^-19 of
- * the sum of the products' magnitudes (root mean square). */
+ * For a bf16 result the 8-bit matrix instructions are used, at twice the rate: of eight products that
+ * they add at a time they keep 13 bits below the largest, and add the eights' sums in fp32. That is an
+ * error of about 2^-19 of the sum of the products' magnitudes (root mean square), which bf16's
+ * rounding covers unless large products cancel. Where they may, take an fp32 result. */
 int pl_matmul_fp8(int64_t m, int64_t n, int64_t k, const pl_fp8 *a, const pl_fp8 *b,
                   const void *bias, int bias_dtype, int relu, void *out, int out_dtype,
                   int64_t out_ld, int accumulate, void *workspace, size_t workspace_bytes,
@@ -139,7 +141,8 @@ size_t pl_linear_fp8_workspace(int64_t m, int64_t n, int64_t k, int dtype, int o
 /* The gradients of x w^T (x m x k, w n x k) from grad (m x n), that of the result: out
  * (m x k) = grad w, from w transposed in 8 bits (w_t, k x n), and weight_out (n x k) = grad^T x,
  * with accumulate added to what it holds. grad is quantised along its rows for the first
- * product, grad and x along their columns for the second. m, n <= 2^22, k <= 2^28. */
+ * product, grad and x along their columns for the second. m, n <= 2^22, k <= 2^28. Each result's
+ * sums are as pl_matmul_fp8 has them for its type. */
 int pl_linear_fp8_grad(const void *x, int x_dtype, int64_t x_ld, const void *grad, int grad_dtype,
                        int64_t grad_ld, int64_t m, int64_t n, int64_t k, const pl_fp8 *w_t, void *out,
                        int out_dtype, int64_t out_ld, void *weight_out, int weight_dtype,

@@ -6,6 +6,10 @@ in 8-bit floating point with a scale per block of 128, and dropout. Weights are
 read where they lie in a replica (any view with unit column stride), weight
 gradients are written where they belong in a gradient row.
 
+No call records anything for autograd: a result does not require a gradient, whatever its
+arguments do. The backward pass is a call of its own (`embedding_grad`, `linear_fp8_grad`,
+`dropout` again).
+
 Every call enqueues its kernels on torch's current stream and returns without
 waiting; as with torch's own operators, a tensor last used on another stream is
 for the caller to order and to record. Refused arguments raise `TypeError` or
@@ -309,7 +313,8 @@ class Fp8Matrix:
         return per_byte.permute(1, 0, 2).reshape(rows, 4 * words)[:, :blocks].int() - 127
 
     def dequantize(self):
-        """The values that it stands for, in fp32 (exact)."""
+        """The values that it stands for, in fp32 (exact; 2^128, to which numbers next to fp32's
+        largest round, is infinity)."""
         rows, cols = self.shape
         blocks = -(-cols // 128)
         two = ((self.exponents() + 127) << 23).view(torch.float32)
@@ -376,7 +381,11 @@ def _bias(bias, n: int):
 def matmul_fp8(a: Fp8Matrix, b: Fp8Matrix, bias=None, relu: bool = False, dtype=torch.bfloat16,
                out=None, accumulate: bool = False):
     """a b^T (+ bias, then max(., 0) with relu), of `dtype` or written to `out`; with
-    `accumulate` added to what `out` holds."""
+    `accumulate` added to what `out` holds.
+
+    Results in fp32 have fp32 sums. Those in bf16 are summed by the 8-bit matrix instructions,
+    twice as fast: of eight products at a time they keep 13 bits below the largest, which bf16's
+    rounding covers unless large products cancel."""
     a_parts, b_parts = _parts("a", a), _parts("b", b)
     native = _native or _native_calls()
     if native:
@@ -403,7 +412,8 @@ def matmul_fp8(a: Fp8Matrix, b: Fp8Matrix, bias=None, relu: bool = False, dtype=
 
 def linear_fp8(x, w: Fp8Matrix, bias=None, relu: bool = False, dtype=torch.bfloat16, out=None):
     """A fully connected layer: x w^T (+ bias, relu). x is quantised along its rows; w is the
-    layer's weight (outputs x inputs), quantised (square) once per pull."""
+    layer's weight (outputs x inputs), quantised (square) once per pull. Sums are those of
+    `matmul_fp8` for the result's type."""
     w_parts = _parts("w", w)
     native = _native or _native_calls()
     if native:
@@ -430,7 +440,8 @@ def linear_fp8_grad(x, grad, w_t: Fp8Matrix, dtype=torch.bfloat16, weight_dtype=
     """Gradients of x w^T from `grad`, that of the result: (for x, for w). w_t is the
     transposed weight, quantised (square); grad is quantised along its rows for the first
     product and along its columns, as x, for the second. `weight_out`, a view into the
-    learner's gradient row, is written, or with `accumulate` added to."""
+    learner's gradient row, is written, or with `accumulate` added to. Sums are those of
+    `matmul_fp8` for each result's type."""
     w_parts = _parts("w_t", w_t)
     native = _native or _native_calls()
     if native:
