@@ -119,8 +119,8 @@ int pl_quantize_fp8(const void *x, int dtype, int64_t rows, int64_t cols, int64_
  * An fp32 result carries fp32 sums of the products of the elements, which count as they are but
  * in blocks whose scale is below 2^-124, where they are rounded to multiples of 2^-133.
  *
- * For a bf16 result the 8-bit matrix instructions are used, at twice the rate: of eight products that
- * they add at a time they keep 13 bits below the largest, and add the eights' sums in fp32. That is an
+ * For a bf16 result the 8-bit matrix instructions are used, at twice the rate: of eight neighbouring
+ * products they keep 13 bits below the largest, and they add the eights' sums in fp32. That is an
  * error of about 2^-19 of the sum of the products' magnitudes (root mean square), which bf16's
  * rounding covers unless large products cancel. Where they may, take an fp32 result. */
 int pl_matmul_fp8(int64_t m, int64_t n, int64_t k, const pl_fp8 *a, const pl_fp8 *b,

@@ -848,3 +848,21 @@ def test_refused_arguments_raise_what_is_said(torch, learner):
     assert torch.equal(learner.dropout(x, (0.5, 1, 0)), learner.dropout(x, drop))
     part = torch.ones(4, 3, 12, device="cuda")[:, :, :8]
     assert torch.equal(learner.dropout(part, drop), learner.dropout(part.contiguous(), drop))
+
+
+@pytest.mark.parametrize("rows", [16, 128])
+@pytest.mark.parametrize("first,second", [(0, 1), (0, 64), (5, 37), (40, 100)])
+def test_what_bf16_results_keep(torch, learner, rows, first, second):
+    """Beside products of 2^16 and -2^16 that cancel, smaller ones of the same eight neighbours are kept
+    from 2^3 on (13 bits), and all of other eights."""
+    other = [i for i in range(128) if i not in (first, second)]
+    b = torch.ones(64, 128, device="cuda")
+    b[:, first], b[:, second] = 256, -256
+    qb = learner.quantize_fp8(b)
+    for small in (8.0, 1.0):
+        a = torch.zeros(128, 128, device="cuda")
+        a[:, first] = a[:, second] = 256
+        a[other, other] = small
+        y = torch.cat([learner.matmul_fp8(learner.quantize_fp8(a[i:i + rows]), qb) for i in range(0, 128, rows)])
+        kept = [i for i in other if small == 8 or i // 8 not in (first // 8, second // 8)]
+        assert bool((y[kept] == small).all()), small
