@@ -144,7 +144,8 @@ __device__ __forceinline__ void store8(void *p, int64_t i, const float (&x)[8]) 
 // store8 past the caches by all 64 lanes of a wave, whose elements are 512 neighbours: lane l's
 // begin at i = first + 8 l. Stores past the caches should fill whole lines, and those of fp32, 16 of
 // a lane's 32 bytes at a time, would not: they go through `stage`, 2 KB of LDS of the wave's own.
-// (536 MB of fp32 rows by the gradient of an embedding: 231 us with plain stores, 151 so.)
+// (The gradient of an embedding from 32768 tokens of 4096 bf16 columns into 536 MB of fp32 rows:
+// 208 us with plain stores, 165 so.)
 template <int DT>
 __device__ __forceinline__ void store8_lines(void *p, int64_t i, const float (&x)[8], f32x4 *stage) {
     if constexpr (DT == PS_F32) {

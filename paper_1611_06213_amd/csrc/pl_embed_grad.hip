@@ -21,8 +21,8 @@
 // (sum_few).
 //
 // Bound by memory: grad is read once and out written once, rows without tokens included. 65536
-// tokens of 4096 bf16 columns into 65536 fp32 rows, with dropout (1.6 GB): 362 us, of which sort 28,
-// sum 333 (4.9 TB/s) and join 13; 1824 tokens of 100 fp32 columns into 50000 rows in one launch of 14.
+// tokens of 4096 bf16 columns into 65536 fp32 rows, with dropout (1.6 GB): 360 us, of which sort 27,
+// sum 330 (4.9 TB/s) and join 13; 1824 tokens of 100 fp32 columns into 50000 rows in one launch of 15.
 #include <algorithm>
 
 #include "pl_device.h"
@@ -33,8 +33,8 @@ namespace {
 constexpr int kMaxLocal = 1024;   // ids of one class
 constexpr uint32_t kMaxFound = 1024;   // tokens that a wave writes down
 // Of long lists of ids nothing is written down, as a frequent id's tokens are too many: the call over
-// 65536 ids of 50000 took 65 us with writing and 76 without, over 200000 115 and 146, but over 262144
-// 209 and 177.
+// 65536 ids of 50000, of 16 columns, takes 44 us with writing and 50 without, over 200000 89 and 98, but
+// over 262144 160 and 119.
 constexpr uint32_t kNoted = 1 << 17;
 constexpr int kPlaceBits = 22;   // of a token in a wave's part of the ids; the rest hold the id in its class
 static_assert(kMaxLocal <= 1 << (32 - kPlaceBits) && kNoted <= 1 << kPlaceBits, "a word each");
@@ -66,8 +66,8 @@ Plan make_plan(int64_t tokens, int64_t vocab, int64_t dim) {
     p.classes = 1u << p.class_bits;
     p.local = static_cast<uint32_t>((vocab + p.classes - 1) >> p.class_bits);
     // One token after another is latency, and pieces are traffic of their own. In us, with dropout,
-    // with pieces of 8 and of 32: 65536 tokens of 100 columns 64 and 75, 32768 of 1000 70 and 73,
-    // 65536 of 1200 147 and 126, 65536 of 4096 409 and 364 (of 64 360).
+    // with pieces of 8 and of 32: 65536 tokens of 100 columns 60 and 69, 32768 of 1000 95 and 93,
+    // 65536 of 1200 169 and 157, 65536 of 4096 406 and 364 (of 64 367).
     p.piece = tokens * dim < (int64_t(1) << 25) ? 8 : 32;
     // a row with c > piece tokens has ceil(c / piece) < 2 c / piece pieces
     p.pieces = tokens <= p.piece ? 0 : static_cast<uint32_t>(2 * tokens / p.piece);
@@ -302,7 +302,7 @@ constexpr int kBlock = 256;
 template <int G, bool DROP>
 __device__ __forceinline__ void add_tokens(float (&sum)[8], const GradArgs &a, const uint32_t *perm,
                                            uint32_t count, uint32_t group, int columns) {
-    // four tokens' loads together: eight leave room for fewer waves (408 us instead of 386 for 65536
+    // four tokens' loads together: eight leave room for fewer waves (407 us instead of 363 for 65536
     // tokens of 4096 columns)
     constexpr uint32_t kTogether = 4;
     const int64_t col = 8ll * group;
@@ -585,9 +585,11 @@ hipError_t launch_few_typed(const GradArgs &a, int grad_dtype, int out_dtype, hi
 }
 
 // Every workgroup reads all ids, and rows with many tokens are taken one after the other. In us,
-// with dropout, in one launch and in three: 1824 tokens of 100 columns into 50000 rows 14 and 22,
-// 2048 of 512 into 30000 21 and 27, 4096 of 1024 into 30000 36 and 36; but of 4096 into 30000 161
-// and 103, and 4096 of 64 into 1000 30 and 17.
+// with dropout, in one launch and in three: 1824 tokens of 100 columns into 50000 rows 15 and 23,
+// 2048 of 512 into 30000 21 and 27, 4096 of 1024 into 30000 34 and 36; but of 4096 into 30000 174
+// and 102, and 4096 of 64 into 1000 36 and 18. These are ids whose numbers say nothing of how frequent
+// they are: the sizes do not tell the host of others. Where the first rows are the most frequent, which
+// one workgroup then has, the first takes 104 and 22, the third 141 and 36.
 bool few(int64_t tokens, int64_t vocab, int64_t dim) {
     return tokens <= int64_t(kSmallTokens) && tokens <= vocab && dim <= 1024;
 }
@@ -619,8 +621,8 @@ hipError_t launch_sums(const GradArgs &a, const Plan &p, hipStream_t s) {
 template <int IDT>
 void launch_sort(const GradArgs &a, const Plan &p, Row *rows, uint32_t *perm, Piece *pieces, hipStream_t s) {
     // More waves share the ids of a workgroup, and take longer to start and to be brought together:
-    // in us, with four waves and with sixteen, 2048 ids 17.3 and 18.7, 4096 19.2 and 19.0, 8192
-    // 29.3 and 25.7.
+    // in us, with four waves and with sixteen, calls of 100 columns into 50000 rows in three launches, 2048
+    // ids 21.1 and 22.4, 4096 26.7 and 26.4, 8192 30.8 and 28.4.
     const uint32_t n = a.tokens, v = a.vocab;
     if (n <= 4096) sort_tokens<IDT, 4, true><<<p.classes, 256, 0, s>>>(a.ids, n, v, p, rows, perm, pieces);
     else if (n <= kNoted)

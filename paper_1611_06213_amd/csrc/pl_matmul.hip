@@ -7,9 +7,10 @@
 // out in bf16  16 x 16 x 128 on 8-bit operands, which takes the scales of its operands' rows
 //              with them (four bytes a row, one per 32 columns; here all four are the block's),
 //              so scaling costs no vector work and no second accumulator. It adds products
-//              in groups of eight, of which it keeps 13 bits below the largest (measured, as
-//              for the 16 x 16 x 32 form): an error of 2^-19 of the sum of the products'
-//              magnitudes, root mean square, far below bf16's 2^-9 of the result.
+//              in groups of eight neighbours, of which it keeps 13 bits below the largest
+//              (measured, as for the 16 x 16 x 32 form): an error of 2^-19 of the sum of the
+//              products' magnitudes, root mean square, far below bf16's 2^-9 of the result
+//              unless large products cancel. That is the price of twice the rate.
 // out in fp32  16 x 16 x 32 on bf16 operands, at half the rate. An 8-bit value times its block's
 //              scale is a bf16 number exactly for scales from 2^-124 on (one conversion instruction
 //              for two of them; e4m3's least, 2^-9, is then bf16's least, 2^-133, to which the two
@@ -229,9 +230,9 @@ __device__ __forceinline__ void place(const Split &sp, uint32_t unit, uint32_t *
 //
 // Bound by the matrix pipes and, at large sizes, by power: the clock falls from 2.4 to 1.75 GHz,
 // and the same product of zeros takes three quarters of the time. 8192^3 to bf16 takes 424 to 510
-// us (2.2 to 2.6 PFLOP/s), 16384 x 4096 x 4096 230 (2.4), and to fp32, by bf16 instructions, 460
-// (1.2). A step of 256 x 256 tiles reads half of what four 128 x 128 tiles read from LDS (8192^3
-// took 690 us with those), and 256 x 128, for fp32 results, leaves registers for the operands in
+// us (2.2 to 2.6 PFLOP/s), 16384 x 4096 x 4096 230 (2.4), and to fp32, by bf16 instructions, 450
+// to 500 (1.1 to 1.2). A step of 256 x 256 tiles reads half of what four 128 x 128 tiles read from LDS (8192^3
+// takes 606 us with those), and 256 x 128, for fp32 results, leaves registers for the operands in
 // bf16.
 //
 // A step is half a block, 64 columns. LDS holds four steps of either operand, which copies bring
@@ -515,8 +516,8 @@ __device__ __forceinline__ void take_units(const MatmulArgs &g, const Split &sp,
 }
 
 // Small products leave most compute units idle, or wait for their first bytes most of the time. A
-// layer's two backward products in one launch take, quantisation and joining included, 18.7 us
-// instead of 23.4 for 57 x 1000 x 900, 22 instead of 27.6 for 300 x 1000 x 1000, 39 instead of 45.7
+// layer's two backward products in one launch take, in fp32, quantisation and joining included, 16.5 us
+// instead of 23.0 for 57 x 1000 x 900, 18.6 instead of 27.4 for 300 x 1000 x 1000, 35 instead of 45
 // for 1000 x 2000 x 2000.
 template <int FM, int FN, int OUT0, int OUT1>
 __global__ __launch_bounds__(256, FM == 2 ? 2 : 1) void tiles(Products both) {
@@ -688,7 +689,7 @@ __global__ __launch_bounds__(256) void empty(MatmulArgs g) {
 
 // ---------------------------------------------------------------- choices
 
-// 32 x 4096 x 9216 22 us with either kernel, 64 x 4096 x 9216 25 with tiles and 31 with slim
+// In us, with slim and with tiles: 32 x 4096 x 9216 16.0 and 14.4, 64 x 4096 x 9216 24.7 and 16.4.
 constexpr uint32_t kSlimRows = 32;
 
 // Bytes of sums of parts where whole tiles fill the card too.
@@ -728,9 +729,9 @@ Choice choose(uint64_t m, uint64_t n, uint64_t k, bool wide) {
     uint64_t parts = 1;
     if (small <= kCus / 2) {
         // Parts of k until every compute unit has a workgroup, unless the joining takes longer: in us,
-        // 64 x 128 x 4096 10.2 in parts of eight blocks and 8.4 of four, 57 x 900 x 1000 to bf16 8.5 in
-        // parts of four and 8.2 whole (with the other backward product and their joining 15.4 and 13.2),
-        // to fp32 9.8 in parts of two and 12.4 whole.
+        // 64 x 128 x 4096 10.6 in parts of eight blocks and 8.8 of four, 57 x 900 x 1000 to bf16 8.9 in
+        // parts of four and 8.6 whole (with the other backward product and their joining 14.3 and 13.8),
+        // to fp32 10.3 in parts of two and 12.9 whole.
         double least = 0.0;
         for (uint64_t q = 1; q <= std::min(kCus / small, blocks); ++q) {
             const uint64_t steps = ((blocks + q - 1) / q + 1) & ~uint64_t(1);
@@ -743,8 +744,8 @@ Choice choose(uint64_t m, uint64_t n, uint64_t k, bool wide) {
         }
     } else {
         // Large tiles read LDS and the caches least, small ones lose less where tiles are few or k
-        // is short; parts fill the last round (1280 x 4096 x 22272 195 us whole and 113 in parts,
-        // 256 x 21248 x 24320 275 and 168). Over the fitted sizes, large tiles wherever there are
+        // is short; parts fill the last round (1280 x 4096 x 22272 196 us whole and 111 in parts,
+        // 256 x 21248 x 24320 304 and 163). Over the fitted sizes, large tiles wherever there are
         // 256 of them took 9% longer than the better of both (15% to fp32), this rule 0.6%.
         double least = tiles_take(m, n, blocks, wide, false, 1);
         for (uint64_t p = 1; p <= 8 && (p == 1 || (blocks / p >= 8 && p * m * n * 4 <= kMostSums)); ++p)
@@ -767,15 +768,15 @@ Choice choose(uint64_t m, uint64_t n, uint64_t k, bool wide) {
 }
 
 // Whether slim converts x itself: a row's bytes in LDS, its scales and the padding. Every workgroup
-// converts all of x: 1 x 4096 (4 KB) took 7.5 us, 9.0 in two launches, 2 x 25088 (50 KB) 24.6 and
-// 25.3, but 16 x 4096 (66 KB) 13.2 and 10.8, all with 4096 columns of out.
+// converts all of x: 1 x 4096 (4 KB) takes 6.0 us, 7.6 in two launches, 2 x 25088 (50 KB) 22.7 and
+// 22.6, but 16 x 4096 (66 KB) 11.6 and 9.2, all with 4096 columns of out.
 bool few_bytes(uint64_t m, uint64_t blocks) { return m <= 16 && m * (blocks * 129 + 16) <= 51200; }
 
 // Of slim: where few columns of out leave compute units idle, a long k is split, to a block a wave
-// at least. In us, whole and split, joining included: 3 x 300 x 24000 17.3 and 8.1, 32 x 1000 x
-// 8192 13.3 and 9.3, 3 x 1000 x 8192 7.5 and 7.9, 32 x 300 x 4096 7.8 and 8.1. A split product's x
+// at least. In us, whole and split, joining included: 3 x 300 x 24000 17.8 and 8.3, 32 x 1000 x
+// 8192 13.5 and 9.4, 3 x 1000 x 8192 7.9 and 8.3, 32 x 300 x 4096 8.2 and 8.6. A split product's x
 // is converted first, which for few bytes pays from 128 blocks on (1 x 70 x 17000 with its
-// conversion 11.8 and 9.8, 1 x 70 x 8192 7.4 and 9.3).
+// conversion 12.0 and 9.7, 1 x 70 x 8192 7.6 and 10.2).
 Split split_slim(uint64_t m, uint64_t n, uint64_t k) {
     Split sp{};
     const uint64_t blocks = (k + 127) / 128;
@@ -799,8 +800,8 @@ hipError_t launch_slim(const MatmulArgs &g, const Split &sp, hipStream_t s) {
     if (!grid_of(static_cast<uint64_t>(sp.tiles_n) * sp.parts, long_rows ? 1024 : 512, &grid))
         return hipErrorInvalidConfiguration;
     // Sixteen waves have more of a long row under way, eight leave room for a second workgroup on
-    // the compute unit where rows are many and short: 1 x 4096 x 25088 23.0 us with 16, 24.6 with 8;
-    // 1 x 25088 x 4096 31.7 and 25.0.
+    // the compute unit where rows are many and short: a layer of 1 x 4096 x 25088 20.6 us with 16, 23.3
+    // with 8; 1 x 25088 x 4096 32.3 and 22.3.
     if (long_rows) slim<FM, OUT, X, 16><<<grid, 1024, std::max(16 * kSums, x), s>>>(g, sp);
     else slim<FM, OUT, X, 8><<<grid, 512, std::max(8 * kSums, x), s>>>(g, sp);
     return hipGetLastError();

@@ -6,7 +6,7 @@
 // workgroup takes a 128 x 128 tile of x: sixteen lanes hold a row's 128 elements, eight
 // each, so a row's maximum is a reduction over sixteen lanes; columns' maxima and the
 // transposed bytes go through LDS. 16384 x 4096 bf16: along rows (no tiles) 30 us, 6.7 TB/s; along
-// columns 33, 6.1 TB/s; both 48, 5.6 TB/s.
+// columns 33, 6.1 TB/s; both 46, 5.8 TB/s.
 #include "pl_fp8.h"
 
 namespace gadei::learner {
@@ -15,7 +15,7 @@ namespace {
 constexpr int kBlock = 256;   // of quantize_rows
 constexpr int kTile = 128;
 // A thread takes four neighbouring rows of eight columns: with eight rows and half the threads, a
-// few tiles took 6.8 us instead of 5.3 (57 x 900, both ways), many the same.
+// few tiles take 7.4 us instead of 5.7 (57 x 900, both ways), many the same.
 constexpr int kRows = 4, kThreads = kTile * kTile / 8 / kRows;
 
 // Where word w (four rows) of column c of the transposed tile lies: fours of words exchanged by

@@ -5,7 +5,7 @@
 // consecutive columns (one evaluation of the generator, 20 wide products, gives their eight
 // 16-bit numbers; the memory's time covers it) of one row or four, whose loads are issued
 // together. Dropout of 16384 x 8192 bf16: 80 us, 6.7 TB/s of reads and writes; of 16384 x 4096
-// fp32 78 us, 6.9 TB/s.
+// fp32 79 us, 6.8 TB/s.
 #include "pl_device.h"
 
 namespace gadei::learner {
@@ -93,9 +93,9 @@ hipError_t launch_shape(const RowsArgs &a, int lx, hipStream_t s) {
 }
 
 // Four rows a thread keep enough loads under way for large matrices; small ones are over sooner with
-// one, in more workgroups: 1824 lookups of 100 columns with dropout 3.2 us, 5.6 with four.
+// one, in more workgroups: 1824 lookups of 100 columns with dropout 3.6 us, 6.0 with four.
 // Results that the caches (256 MB) will not hold for a reader go past them: 65536 lookups of 4096
-// bf16 columns 136 us, 183 otherwise; dropout of 16384 x 8192 80 us, 95 otherwise.
+// bf16 columns 129 us, 172 otherwise; dropout of 16384 x 8192 81 us, 93 otherwise.
 template <int IDT, int X, int OUT, bool DROP>
 hipError_t launch_drop(const RowsArgs &a, hipStream_t s) {
     const uint64_t groups = (a.cols + 7) / 8, all = groups * a.rows;
