@@ -2,7 +2,8 @@
  * ps_learner.h -- C ABI of a learner's operators on one gfx950 GPU: what a
  * learner computes between a pull and a push with the layers that hold most of
  * the server's parameters (ps.h): embedding tables and fully connected layers,
- * and the dropout between them.
+ * the dropout between them, the norms around a residual block of them; the AdamW step
+ * that a learner makes of a gradient; and layers in 8-bit integers, for answers.
  *
  *   - A learner pulls a replica, reads its layers' weights where they lie in it
  *     (any element boundary), and writes their gradients where they belong in its
@@ -149,6 +150,125 @@ int pl_linear_fp8_grad(const void *x, int x_dtype, int64_t x_ld, const void *gra
                        int64_t weight_ld, int accumulate, void *workspace, size_t workspace_bytes,
                        void *stream);
 size_t pl_linear_fp8_grad_workspace(int64_t m, int64_t n, int64_t k, int out_dtype, int weight_dtype);
+
+/* ---- The norms after and before a block of layers in a residual stack.
+ *
+ * With N(v) = v / sqrt(mean(v^2) + eps) over a row, x the stream and y the block's output:
+ *   out = scale * x + gate * after * N(y)       (after NULL: gate * y; gate NULL: no gate)
+ *   normed = before * N(out)                    (the next block's input; before NULL: N(out))
+ * or, with y NULL (out, gate, after NULL too, scale 1), normed = before * N(x) alone.
+ *
+ * x and out are of x_dtype, y and normed of y_dtype, after and before (cols values) of
+ * weight_dtype. `gate` has `gates` rows of cols values, of gate_dtype, each for rows / gates
+ * neighbouring rows (one sequence's, say; 1: for all; rows: one each); rows is a multiple of it.
+ * Either output may be NULL, out only without a block. normed is that of the sums before they
+ * are rounded to out's type. eps > 0. Squares are summed in fp32: a row whose sum of squares
+ * passes 3.4e38 is normed to zeros. rows < 2^31, cols <= 2^31. */
+int pl_norm(const void *x, int x_dtype, int64_t x_ld, const void *y, int y_dtype, int64_t y_ld,
+            int64_t rows, int64_t cols, const void *gate, int gate_dtype, int64_t gates,
+            int64_t gate_ld, const void *after, const void *before, int weight_dtype, float scale,
+            float eps, void *out, int64_t out_ld, void *normed, int64_t normed_ld, void *stream);
+
+/* Its gradients, from `grad`, that of out (x_dtype), and `normed_grad`, that of normed (y_dtype);
+ * either may be NULL (zeros), not both. h is what pl_norm wrote to out (without a block: x).
+ * x_out (x_dtype) and, with a block, y_out (y_dtype) are written; gate_out, after_out and before_out
+ * (of weight_out_dtype; gate_out has the gate's rows) if they are not NULL, with accumulate added to
+ * what they hold. Without a block x_out = grad + the gradient of the norm. */
+int pl_norm_grad(const void *h, int x_dtype, int64_t h_ld, const void *y, int y_dtype, int64_t y_ld,
+                 const void *grad, int64_t grad_ld, const void *normed_grad, int64_t normed_grad_ld,
+                 int64_t rows, int64_t cols, const void *gate, int gate_dtype, int64_t gates,
+                 int64_t gate_ld, const void *after, const void *before, int weight_dtype,
+                 float scale, float eps, void *x_out, int64_t x_out_ld, void *y_out,
+                 int64_t y_out_ld, void *gate_out, int64_t gate_out_ld, void *after_out,
+                 void *before_out, int weight_out_dtype, int accumulate, void *workspace,
+                 size_t workspace_bytes, void *stream);
+size_t pl_norm_grad_workspace(int64_t rows, int64_t cols);
+
+/* ---- A matrix in 8-bit integers with a scale for each row (a token's activations, or a
+ * channel's weights): element (r, c) = values[r * pl_int8_ld(cols) + c] * scales[r]. The scale is
+ * most / 127, most the largest magnitude of the row or 2^-100 if that is larger; elements times
+ * 127 (1 / most), each step in fp32, are rounded to nearest even. A row with a NaN or an infinity has the scale NaN. The
+ * values' rows are padded with zeros to multiples of 128. Both arrays lie on 16-byte boundaries. */
+typedef struct pl_int8 {
+    int8_t *values;   /* pl_int8_values_bytes(rows, cols) bytes */
+    float *scales;    /* rows */
+} pl_int8;
+int64_t pl_int8_ld(int64_t cols);
+size_t pl_int8_values_bytes(int64_t rows, int64_t cols);
+
+/* x (rows x cols) as 8-bit integers. rows <= 2^28, cols <= 2^17. */
+int pl_quantize_int8(const void *x, int dtype, int64_t rows, int64_t cols, int64_t ld,
+                     const pl_int8 *out, void *stream);
+
+/* out = a b^T (+ bias) (then max(., 0) with relu; a NaN stays) for a (m x k) and b (n x k), out
+ * m x n. Sums of products of integers are exact, so an element depends on its rows of a and b
+ * alone, not on how many others there are; then it is the sum times a's scale, times b's, plus
+ * the bias, each step in fp32 (whose range the first may pass before the second). bias: n values or NULL. m, n, k may be 0;
+ * m, n <= 2^28, k <= 2^17. */
+int pl_matmul_int8(int64_t m, int64_t n, int64_t k, const pl_int8 *a, const pl_int8 *b,
+                   const void *bias, int bias_dtype, int relu, void *out, int out_dtype,
+                   int64_t out_ld, void *workspace, size_t workspace_bytes, void *stream);
+size_t pl_matmul_int8_workspace(int64_t m, int64_t n, int64_t k);
+
+/* A fully connected layer: pl_quantize_int8 of x (m x k), then pl_matmul_int8 with the weights w
+ * (n x k) -- the same result, in fewer launches where x is small. */
+int pl_linear_int8(const void *x, int dtype, int64_t m, int64_t k, int64_t ld, int64_t n,
+                   const pl_int8 *w, const void *bias, int bias_dtype, int relu, void *out,
+                   int out_dtype, int64_t out_ld, void *workspace, size_t workspace_bytes,
+                   void *stream);
+size_t pl_linear_int8_workspace(int64_t m, int64_t n, int64_t k);
+
+/* ---- One AdamW step over many tensors.
+ *
+ * Of each element, with t = steps made before + 1, all in fp32:
+ *   g = factor * grad;  m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2
+ *   step = lr (m / (1 - beta1^t) / (sqrt(v / (1 - beta2^t)) + eps) + decay * weight)
+ * and weight -= step; or, with push, grad = step and the weights are only read: a learner pushes
+ * it to a server with lr 1 and momentum 0, which makes the step when it applies it.
+ *
+ * The states m and v are vectors of pl_adamw_room() elements that hold tensor after tensor, each
+ * from a multiple of 128 elements on; what lies between is zeros and stays so. New ones are
+ * zeros. Weights are fp32 (with push also bf16), gradients fp32 or bf16, all of a type.
+ *
+ * bits = 32: the states are fp32. bits = 8: a byte an element, and for each 128 elements a byte s
+ * in m_scales and v_scales, the exponent field of the block's largest magnitude as an fp32 number,
+ * plus 1 if its fraction is above 7/8. An element's code is that of |x| 2^(15-s) (v: 2^(31-s)) as
+ * an fp32 number's bits, plus 16 r, shifted right by 20, m's with the sign as its upper bit; a
+ * positive v's is 1 at least. r is a random number of 16 bits, so that what is kept has the
+ * expectation of what was computed: for element j of the vectors word j & 3 of Philox4x32-7 (as
+ * above, with seven rounds), of the counter (j >> 2 low, high, t low, high) and the key (seed low,
+ * high); its low half for m, its high half for v. s = 255 (a NaN or an infinity in the block, or a
+ * magnitude above 1.875 * 2^127): the whole block is NaN.
+ *
+ * A plan says where the tensors are. pl_adamw_plan writes it to host memory, whence the caller
+ * copies it to device memory (16-byte aligned), which counts the steps made and belongs to the
+ * optimizer from then on: a captured step that is replayed counts on. Steps of one plan are made
+ * one after another. Every call that names a plan has the same tensors' types, push and parts. */
+typedef struct pl_adamw_tensor {
+    void *weight, *grad;   /* count elements each */
+    int64_t count;
+    float decay;
+} pl_adamw_tensor;
+int64_t pl_adamw_room(const pl_adamw_tensor *tensors, int64_t n);    /* -1: refused */
+int64_t pl_adamw_parts(const pl_adamw_tensor *tensors, int64_t n);   /* -1: refused */
+size_t pl_adamw_plan_bytes(int64_t parts);
+
+/* `steps`: made before. What is written may overlap nothing. */
+int pl_adamw_plan(const pl_adamw_tensor *tensors, int64_t n, int weight_dtype, int grad_dtype,
+                  int push, int64_t steps, void *plan, size_t plan_bytes);
+/* The steps made, from a plan of one part or more copied back to host memory. */
+int64_t pl_adamw_steps(const void *plan);
+
+/* lr_at and factor_at: numbers in device memory that are read instead of lr and factor; or NULL. */
+int pl_adamw_step(void *plan, int64_t parts, int weight_dtype, int grad_dtype, int push, int bits,
+                  int64_t room, void *m, void *v, uint8_t *m_scales, uint8_t *v_scales,
+                  double beta1, double beta2, float eps, float lr, const float *lr_at,
+                  float factor, const float *factor_at, uint64_t seed, void *stream);
+
+/* What states in 8 bits stand for, room elements each of `dtype` (exact in either, but below 2^-133
+ * in bf16 and 2^-149 in fp32). */
+int pl_adamw_moments(int64_t room, const void *m, const void *v, const uint8_t *m_scales,
+                     const uint8_t *v_scales, void *m_out, void *v_out, int dtype, void *stream);
 
 /* Message for the last failed call on this thread ("" if none). */
 const char *pl_last_error(void);

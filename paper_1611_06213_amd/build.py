@@ -62,7 +62,8 @@ def build_all(verbose: bool = False):
 # per source, compiled side by side.
 LEARNER_LIB = os.path.join(HERE, "libgadeilearner.so")
 LEARNER_SOURCES = [os.path.join(CSRC, s) for s in (
-    "pl_api.cpp", "pl_rows.hip", "pl_embed_grad.hip", "pl_quantize.hip", "pl_matmul.hip")]
+    "pl_api.cpp", "pl_rows.hip", "pl_embed_grad.hip", "pl_quantize.hip", "pl_matmul.hip",
+    "pl_matmul_int8.hip", "pl_norm.hip", "pl_adamw.hip")]
 LEARNER_FLAGS = [f for f in FLAGS if not f.startswith("-ffp-contract=") and f != "-shared"]
 
 

@@ -1,0 +1,271 @@
+// One AdamW step over many tensors.
+//
+// Mathematics, of each element, t = steps made + 1:
+//
+//   m = b1 m + (1 - b1) f g        v = b2 v + (1 - b2) (f g)^2
+//   step = lr (m up / (sqrt(v) root + eps) + decay w)
+//   up = 1 / (1 - b1^t), root = (1 - b2^t)^-1/2
+//
+// and w - step for w, or the step in g's place. Products and sums of m and v round one by one, so
+// that what is kept of them in 8 bits is a function of the arguments alone.
+//
+// States in 8 bits, for each 128 elements one exponent: magnitudes are numbers of 3 fraction bits
+// and 4 exponent bits (m, with a sign) or 5 (v, whose root so spans 2^17: an element far below its
+// block's largest keeps a denominator). Scaled so that the format's least normal number is fp32's,
+// a number's bits without the last 20 are its code, subnormal ones included: rounding is one
+// addition of random bits and a shift. The rounding is random because a mean that moves by (1 -
+// b2) of itself a step, 2^-10, would never leave a number of 3 fraction bits if rounded to nearest.
+// A positive v is never rounded to 0, below which m / sqrt(v) has no bound.
+//
+// Bound by memory in 32 bits, by memory and vector instructions in 8.
+#include "pl_device.h"
+
+namespace gadei::learner {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kFour = 4;   // neighbouring elements a lane
+
+typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
+typedef u16x4 u16x4_any __attribute__((aligned(2)));
+
+// Philox4x32-7: as pl_device.h's philox with seven rounds, the fewest that its authors found to pass
+// their tests; a word an element.
+__device__ __forceinline__ u32x4 random4(uint64_t j, uint64_t t, uint64_t seed) {
+    uint32_t c0 = static_cast<uint32_t>(j), c1 = static_cast<uint32_t>(j >> 32);
+    uint32_t c2 = static_cast<uint32_t>(t), c3 = static_cast<uint32_t>(t >> 32);
+    uint32_t k0 = static_cast<uint32_t>(seed), k1 = static_cast<uint32_t>(seed >> 32);
+#pragma unroll
+    for (int i = 0; i < 7; ++i) {
+        const uint64_t p0 = static_cast<uint64_t>(0xD2511F53u) * c0;
+        const uint64_t p1 = static_cast<uint64_t>(0xCD9E8D57u) * c2;
+        c0 = static_cast<uint32_t>(p1 >> 32) ^ c1 ^ k0;
+        c2 = static_cast<uint32_t>(p0 >> 32) ^ c3 ^ k1;
+        c1 = static_cast<uint32_t>(p1);
+        c3 = static_cast<uint32_t>(p0);
+        k0 += 0x9E3779B9u;
+        k1 += 0xBB67AE85u;
+    }
+    return u32x4{c0, c1, c2, c3};
+}
+
+// Four elements as loaded; those past `count` are 0.
+template <int DT>
+__device__ __forceinline__ f32x4 load4(const void *p, int64_t i, int count) {
+    f32x4 x = {0, 0, 0, 0};
+    if (count >= kFour) {
+        if constexpr (DT == PS_F32) {
+            x = *reinterpret_cast<const f32x4_any *>(static_cast<const float *>(p) + i);
+        } else {
+            const u32x2 w = *reinterpret_cast<const u32x2_any *>(static_cast<const uint16_t *>(p) + i);
+            x = f32x4{lo_bf16(w[0]), hi_bf16(w[0]), lo_bf16(w[1]), hi_bf16(w[1])};
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < kFour; ++e)
+            if (e < count) x[e] = load1<DT>(p, i + e);
+    }
+    return x;
+}
+
+template <int DT>
+__device__ __forceinline__ void store4(void *p, int64_t i, f32x4 x, int count) {
+    if (count >= kFour) {
+        if constexpr (DT == PS_F32)
+            *reinterpret_cast<f32x4_any *>(static_cast<float *>(p) + i) = x;
+        else
+            *reinterpret_cast<u32x2_any *>(static_cast<uint16_t *>(p) + i) =
+                u32x2{bf16x2_rne(x[0], x[1]), bf16x2_rne(x[2], x[3])};
+    } else {
+#pragma unroll
+        for (int e = 0; e < kFour; ++e)
+            if (e < count) store1<DT>(p, i + e, x[e]);
+    }
+}
+
+// The byte of a block whose largest magnitude has these bits: the exponent field, one more above
+// 1.875 times its power of two, which is the largest code. 255: not finite, or above 1.875 * 2^127.
+__device__ __forceinline__ uint32_t block_byte(uint32_t bits) { return (bits + 0xfffffu) >> 23; }
+constexpr uint32_t kBad = 255;
+
+template <bool SIGNED>
+__device__ __forceinline__ float decode(uint32_t code, int byte) {
+    if constexpr (SIGNED) {
+        const float x = ldexpf(__uint_as_float((code & 0x7fu) << 20), byte - 15);
+        return __uint_as_float(__float_as_uint(x) | (code & 0x80u) << 24);
+    }
+    return ldexpf(__uint_as_float(code << 20), byte - 31);
+}
+
+// r: 16 random bits.
+template <bool SIGNED>
+__device__ __forceinline__ uint32_t encode(float x, int byte, uint32_t r) {
+    const uint32_t bits = __float_as_uint(x) & 0x7fffffffu;
+    const uint32_t scaled = __float_as_uint(ldexpf(__uint_as_float(bits), (SIGNED ? 15 : 31) - byte));
+    const uint32_t code = (scaled + 16 * r) >> 20;
+    if constexpr (SIGNED) return code | (__float_as_uint(x) >> 24 & 0x80u);
+    return max(code, min(bits, 1u));
+}
+
+// The largest of the 32 lanes that hold a block.
+__device__ __forceinline__ uint32_t most_of_32(uint32_t m) {
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) m = max(m, static_cast<uint32_t>(__shfl_xor(m, d)));
+    return m;
+}
+
+struct Factors {
+    uint64_t t;
+    float up, root, lr, factor;
+};
+
+template <int W, int G, int BITS, bool PUSH>
+__global__ __launch_bounds__(kThreads) void adamw(AdamwArgs a) {
+#pragma clang fp contract(off)
+    __shared__ Factors shared;
+    const uint64_t index = block_index();
+    if (index >= a.parts) return;
+    AdamwPart *const part = a.plan + index;
+    if (threadIdx.x == 0) {
+        // Each part counts the steps for itself: the count of a captured step goes on when it is
+        // replayed, and no part waits for another.
+        const int64_t t = part->steps + 1;
+        part->steps = t;
+        Factors f;
+        f.t = static_cast<uint64_t>(t);
+        f.up = static_cast<float>(1.0 / (1.0 - exp2(static_cast<double>(t) * a.log2_beta1)));
+        f.root = static_cast<float>(1.0 / sqrt(1.0 - exp2(static_cast<double>(t) * a.log2_beta2)));
+        f.lr = a.lr_at != nullptr ? *a.lr_at : a.lr;
+        f.factor = a.factor_at != nullptr ? *a.factor_at : a.factor;
+        shared = f;
+    }
+    __syncthreads();
+    const Factors f = shared;
+    void *const w = part->weight, *const g = part->grad;
+    const int64_t first = part->at;   // of the states
+    const int count = static_cast<int>(part->count);
+    const float decay = part->decay;
+    const int room = (count + 127) & ~127;
+    for (int i = threadIdx.x * kFour; i < room; i += kThreads * kFour) {
+        const int left = count - i;
+        const f32x4 x = load4<W>(w, i, left);
+        f32x4 d = load4<G>(g, i, left);
+        f32x4 m, v;
+        uint32_t cm, cv;
+        int bm = 0, bv = 0;
+        const int64_t at = first + i;
+        if constexpr (BITS == 32) {
+            m = *reinterpret_cast<const f32x4 *>(static_cast<const float *>(a.m) + at);
+            v = *reinterpret_cast<const f32x4 *>(static_cast<const float *>(a.v) + at);
+        } else {
+            cm = *reinterpret_cast<const uint32_t *>(static_cast<const uint8_t *>(a.m) + at);
+            cv = *reinterpret_cast<const uint32_t *>(static_cast<const uint8_t *>(a.v) + at);
+            bm = a.m_scales[at >> 7];
+            bv = a.v_scales[at >> 7];
+#pragma unroll
+            for (int e = 0; e < kFour; ++e) {
+                m[e] = decode<true>(cm >> 8 * e & 0xff, bm);
+                v[e] = decode<false>(cv >> 8 * e & 0xff, bv);
+                if (bm == kBad) m[e] = __builtin_nanf("");
+                if (bv == kBad) v[e] = __builtin_nanf("");
+            }
+        }
+        f32x4 y;
+#pragma unroll
+        for (int e = 0; e < kFour; ++e) {
+            const float ge = d[e] * f.factor;
+            m[e] = a.beta1 * m[e] + a.rest1 * ge;
+            v[e] = a.beta2 * v[e] + a.rest2 * (ge * ge);
+            const float step = f.lr * (m[e] * f.up / (sqrtf(v[e]) * f.root + a.eps) + decay * x[e]);
+            y[e] = PUSH ? step : x[e] - step;
+        }
+        if constexpr (PUSH) store4<G>(g, i, y, left);
+        else store4<W>(w, i, y, left);
+        if constexpr (BITS == 32) {
+            *reinterpret_cast<f32x4 *>(static_cast<float *>(a.m) + at) = m;
+            *reinterpret_cast<f32x4 *>(static_cast<float *>(a.v) + at) = v;
+        } else {
+            uint32_t mm = 0, mv = 0;
+#pragma unroll
+            for (int e = 0; e < kFour; ++e) {
+                mm = max(mm, __float_as_uint(m[e]) & 0x7fffffffu);
+                mv = max(mv, __float_as_uint(v[e]) & 0x7fffffffu);
+            }
+            bm = block_byte(most_of_32(mm));
+            bv = block_byte(most_of_32(mv));
+            const u32x4 r = random4(static_cast<uint64_t>(at) >> 2, f.t, a.seed);
+            cm = cv = 0;
+#pragma unroll
+            for (int e = 0; e < kFour; ++e) {
+                cm |= encode<true>(m[e], bm, r[e] & 0xffffu) << 8 * e;
+                cv |= encode<false>(v[e], bv, r[e] >> 16) << 8 * e;
+            }
+            *reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(a.m) + at) = cm;
+            *reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(a.v) + at) = cv;
+            if ((threadIdx.x & 31) == 0) {
+                a.m_scales[at >> 7] = static_cast<uint8_t>(bm);
+                a.v_scales[at >> 7] = static_cast<uint8_t>(bv);
+            }
+        }
+    }
+}
+
+// The values of states in 8 bits, sixteen lanes a block.
+template <bool SIGNED, int OUT>
+__device__ __forceinline__ void values(const uint8_t *codes, const uint8_t *scales, void *out, uint64_t at) {
+    const u32x2 c = *reinterpret_cast<const u32x2 *>(codes + at);
+    const int byte = scales[at >> 7];
+    float x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        x[e] = decode<SIGNED>(c[e >> 2] >> 8 * (e & 3) & 0xff, byte);
+        if (byte == kBad) x[e] = __builtin_nanf("");
+    }
+    store8<OUT>(out, static_cast<int64_t>(at), x);
+}
+
+template <int OUT>
+__global__ __launch_bounds__(kThreads) void moments(MomentsArgs a) {
+    const uint64_t at = (static_cast<uint64_t>(block_index()) * kThreads + threadIdx.x) * 8;
+    if (at >= a.room) return;
+    values<true, OUT>(a.m, a.m_scales, a.m_out, at);
+    values<false, OUT>(a.v, a.v_scales, a.v_out, at);
+}
+
+template <int W, int G, int BITS, bool PUSH>
+hipError_t launch(const AdamwArgs &a, hipStream_t s) {
+    dim3 grid;
+    if (!grid_of(a.parts, kThreads, &grid)) return hipErrorInvalidConfiguration;
+    adamw<W, G, BITS, PUSH><<<grid, kThreads, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+template <int W, int G, bool PUSH>
+hipError_t launch_bits(const AdamwArgs &a, int bits, hipStream_t s) {
+    return bits == 8 ? launch<W, G, 8, PUSH>(a, s) : launch<W, G, 32, PUSH>(a, s);
+}
+
+}  // namespace
+
+uint32_t adamw_part(int64_t room) { return room >= int64_t(1) << 24 ? 8192 : 2048; }
+
+hipError_t launch_adamw(const AdamwArgs &a, int weight_dtype, int grad_dtype, int bits, bool push, hipStream_t s) {
+    if (!push)
+        return grad_dtype == PS_F32 ? launch_bits<PS_F32, PS_F32, false>(a, bits, s)
+                                    : launch_bits<PS_F32, PS_BF16, false>(a, bits, s);
+    if (weight_dtype == PS_F32)
+        return grad_dtype == PS_F32 ? launch_bits<PS_F32, PS_F32, true>(a, bits, s)
+                                    : launch_bits<PS_F32, PS_BF16, true>(a, bits, s);
+    return grad_dtype == PS_F32 ? launch_bits<PS_BF16, PS_F32, true>(a, bits, s)
+                                : launch_bits<PS_BF16, PS_BF16, true>(a, bits, s);
+}
+
+hipError_t launch_moments(const MomentsArgs &a, int dtype, hipStream_t s) {
+    dim3 grid;
+    if (!grid_of((a.room / 8 + kThreads - 1) / kThreads, kThreads, &grid)) return hipErrorInvalidConfiguration;
+    if (dtype == PS_F32) moments<PS_F32><<<grid, kThreads, 0, s>>>(a);
+    else moments<PS_BF16><<<grid, kThreads, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace gadei::learner

@@ -332,6 +332,230 @@ PyObject *linear_grad(PyObject *const *a) {
     return Py_BuildValue("(NN)", px, pw);
 }
 
+// `cols` contiguous values of a type that `*code` may already name (>= 0), or none.
+bool values(PyObject *o, int64_t cols, at::Tensor *t, void **p, int *code) {
+    *p = nullptr;
+    if (o == Py_None) return true;
+    int own;
+    if (!device_tensor(o, t) || t->dim() != 1 || t->size(0) != cols || !t->is_contiguous() ||
+        !code_of(t->scalar_type(), &own) || (*code >= 0 && own != *code))
+        return false;
+    *code = own;
+    *p = t->data_ptr();
+    return true;
+}
+
+// A gate: `cols` values for all rows, or a matrix; or none.
+struct Gate {
+    at::Tensor t;
+    void *p = nullptr;
+    int dtype = PS_F32;
+    int64_t rows = 0, ld = 0;
+};
+
+bool gate(PyObject *o, int64_t cols, Gate *g) {
+    if (o == Py_None) return true;
+    Matrix m;
+    if (!device_tensor(o, &g->t) || !as_matrix(g->t.dim() == 1 ? g->t.unsqueeze(0) : g->t, &m) || m.cols != cols)
+        return false;
+    g->p = m.p;
+    g->dtype = m.dtype;
+    g->rows = m.rows;
+    g->ld = m.ld;
+    return true;
+}
+
+// rows x cols of `code`: `out` if it is not None, else new.
+bool like(PyObject *out, int64_t rows, int64_t cols, int code, const at::Tensor &on, Matrix *m) {
+    if (out == Py_None)
+        return as_matrix(at::empty({rows, cols}, on.options().dtype(code == PS_F32 ? at::kFloat : at::kBFloat16)), m);
+    return matrix(out, m) && m->rows == rows && m->cols == cols && m->dtype == code;
+}
+
+// A new reference to `out`, or to the tensor that was made instead.
+PyObject *same(PyObject *out, const at::Tensor &t) {
+    if (out == Py_None) return THPVariable_Wrap(t);
+    Py_INCREF(out);
+    return out;
+}
+
+// norm(x, y, gate, after, before, scale, eps, dtype, out, normed_out): h and z, or without a y z
+PyObject *norm(PyObject *const *a) {
+    Matrix x, y, out, normed;
+    Gate g;
+    at::Tensor ta, tb;
+    void *after, *before;
+    float scale, eps;
+    int code = -1;
+    const bool block = a[1] != Py_None, next = !block || a[4] != Py_None;
+    // empty tensors have no address: the Python route
+    if (!matrix(a[0], &x) || x.rows == 0 || x.cols == 0) Py_RETURN_NONE;
+    if (block && (!matrix(a[1], &y) || y.rows != x.rows || y.cols != x.cols)) Py_RETURN_NONE;
+    if (!gate(a[2], x.cols, &g) || !values(a[3], x.cols, &ta, &after, &code) ||
+        !values(a[4], x.cols, &tb, &before, &code) || !number(a[5], &scale) || !number(a[6], &eps))
+        Py_RETURN_NONE;
+    int y_code = y.dtype;
+    if (!block) {
+        y_code = x.dtype;
+        if (a[7] != Py_None && (!THPDtype_Check(a[7]) ||
+                                !code_of(reinterpret_cast<THPDtype *>(a[7])->scalar_type, &y_code)))
+            Py_RETURN_NONE;
+        if (a[9] != Py_None && a[7] == Py_None) {
+            Matrix m;
+            if (!matrix(a[9], &m)) Py_RETURN_NONE;
+            y_code = m.dtype;
+        }
+    }
+    if ((block ? !like(a[8], x.rows, x.cols, x.dtype, x.t, &out) : a[8] != Py_None) ||
+        (next ? !like(a[9], x.rows, x.cols, y_code, x.t, &normed) : a[9] != Py_None))
+        Py_RETURN_NONE;
+    const int rc = unlocked([&] {
+        return pl_norm(x.p, x.dtype, x.ld, y.p, y_code, y.ld, x.rows, x.cols, g.p, g.dtype, g.rows, g.ld, after,
+                       before, code < 0 ? PS_F32 : code, scale, eps, out.p, out.ld, normed.p, normed.ld, stream());
+    });
+    if (rc != PS_OK) return PyLong_FromLong(rc);
+    PyObject *z = Py_None;
+    if (next) z = same(a[9], normed.t);
+    else Py_INCREF(z);
+    if (!block || z == nullptr) return z;
+    PyObject *h = same(a[8], out.t);
+    if (h == nullptr) {
+        Py_DECREF(z);
+        return nullptr;
+    }
+    return Py_BuildValue("(NN)", h, z);
+}
+
+// Where the gradient of `of` (None: there is none) goes; *code: of all that are named.
+bool weight_out(PyObject *out, PyObject *of, const at::Tensor &like, int *code, bool accumulate, at::ScalarType dtype,
+                at::Tensor *t, Matrix *m) {
+    if (of == Py_None) return out == Py_None;
+    if (out == Py_None) {
+        if (accumulate) return false;
+        *t = at::empty(like.sizes(), like.options().dtype(dtype));
+    } else if (!device_tensor(out, t) || t->sizes() != like.sizes() || (t->dim() == 1 && !t->is_contiguous())) {
+        return false;
+    }
+    if (!as_matrix(t->dim() == 1 ? t->unsqueeze(0) : *t, m) || (*code >= 0 && m->dtype != *code)) return false;
+    *code = m->dtype;
+    return true;
+}
+
+// norm_grad(h, y, grad, normed_grad, gate, after, before, scale, eps, weight_dtype, x_out, y_out, gate_out,
+// after_out, before_out, accumulate): gradients for x, y, gate, after, before
+PyObject *norm_grad(PyObject *const *a) {
+    Matrix h, y, dh, dz, dx, dy, out[3];
+    Gate g;
+    at::Tensor ta, tb, made[3];
+    void *after, *before;
+    float scale, eps;
+    bool accumulate;
+    int code = -1, out_code = -1;
+    const bool block = a[1] != Py_None, next = a[3] != Py_None;
+    if (!flag(a[15], &accumulate) || !matrix(a[0], &h) || h.rows == 0 || h.cols == 0) Py_RETURN_NONE;
+    auto fits = [&](PyObject *o, Matrix *m) { return matrix(o, m) && m->rows == h.rows && m->cols == h.cols; };
+    if ((block && !fits(a[1], &y)) || (a[2] != Py_None && (!fits(a[2], &dh) || dh.dtype != h.dtype)) ||
+        (next && (!fits(a[3], &dz) || (block && dz.dtype != y.dtype))) || (!next && a[6] != Py_None))
+        Py_RETURN_NONE;
+    const int y_code = block ? y.dtype : next ? dz.dtype : h.dtype;
+    if (!gate(a[4], h.cols, &g) || !values(a[5], h.cols, &ta, &after, &code) ||
+        !values(a[6], h.cols, &tb, &before, &code) || !number(a[7], &scale) || !number(a[8], &eps) ||
+        !THPDtype_Check(a[9]) || !like(a[10], h.rows, h.cols, h.dtype, h.t, &dx) ||
+        (block ? !like(a[11], h.rows, h.cols, y.dtype, h.t, &dy) : a[11] != Py_None))
+        Py_RETURN_NONE;
+    const at::ScalarType dtype = reinterpret_cast<THPDtype *>(a[9])->scalar_type;
+    const at::Tensor *of[3] = {&g.t, &ta, &tb};
+    for (int i = 0; i < 3; ++i)
+        if (!weight_out(a[12 + i], a[4 + i], *of[i], &out_code, accumulate, dtype, &made[i], &out[i])) Py_RETURN_NONE;
+    const size_t need = pl_norm_grad_workspace(h.rows, h.cols);
+    const at::Tensor work = bytes(need, h.t);
+    const int rc = unlocked([&] {
+        return pl_norm_grad(h.p, h.dtype, h.ld, y.p, y_code, y.ld, dh.p, dh.ld, dz.p, dz.ld, h.rows, h.cols, g.p,
+                            g.dtype, g.rows, g.ld, after, before, code < 0 ? PS_F32 : code, scale, eps, dx.p, dx.ld,
+                            dy.p, dy.ld, out[0].p, out[0].ld, out[1].p, out[2].p, out_code < 0 ? PS_F32 : out_code,
+                            accumulate, work.data_ptr(), need, stream());
+    });
+    if (rc != PS_OK) return PyLong_FromLong(rc);
+    PyObject *result = PyTuple_New(5);
+    if (result == nullptr) return nullptr;
+    const at::Tensor *given[5] = {&dx.t, block ? &dy.t : nullptr, g.p ? &made[0] : nullptr, after ? &made[1] : nullptr,
+                                  before ? &made[2] : nullptr};
+    for (int i = 0; i < 5; ++i) {
+        PyObject *o = Py_None;
+        if (given[i] != nullptr) o = same(a[10 + i], *given[i]);
+        else Py_INCREF(o);
+        if (o == nullptr) {
+            Py_DECREF(result);
+            return nullptr;
+        }
+        PyTuple_SET_ITEM(result, i, o);
+    }
+    return result;
+}
+
+// A matrix of 8-bit integers from its parts (values, scales, rows, cols).
+struct Int8 {
+    at::Tensor values, scales;
+    pl_int8 q;
+    int64_t rows = 0, cols = 0;
+};
+
+bool int8(PyObject *o, Int8 *f) {
+    if (!PyTuple_CheckExact(o) || PyTuple_GET_SIZE(o) != 4) return false;
+    if (!device_tensor(PyTuple_GET_ITEM(o, 0), &f->values) || !device_tensor(PyTuple_GET_ITEM(o, 1), &f->scales) ||
+        !integer(PyTuple_GET_ITEM(o, 2), &f->rows) || !integer(PyTuple_GET_ITEM(o, 3), &f->cols))
+        return false;
+    // a caller may have exchanged the tensors for others
+    if (f->values.scalar_type() != at::kChar || f->scales.scalar_type() != at::kFloat ||
+        !shape(f->values, f->rows, pl_int8_ld(f->cols)) || f->scales.dim() != 1 || f->scales.size(0) != f->rows ||
+        !f->scales.is_contiguous())
+        return false;
+    f->q = pl_int8{static_cast<int8_t *>(f->values.data_ptr()), static_cast<float *>(f->scales.data_ptr())};
+    return true;
+}
+
+// product_int8(a, b, bias, relu, dtype, out), a and b parts of matrices of integers
+PyObject *product_int8(PyObject *const *a) {
+    Int8 x, w;
+    Matrix out;
+    at::Tensor b;
+    const void *pb;
+    int bias_code;
+    bool relu;
+    if (!flag(a[3], &relu) || !int8(a[0], &x) || !int8(a[1], &w) || x.cols != w.cols ||
+        !bias(a[2], w.rows, &b, &pb, &bias_code) || !result(a[5], a[4], x.rows, w.rows, x.scales, &out))
+        Py_RETURN_NONE;
+    const size_t need = pl_matmul_int8_workspace(x.rows, w.rows, x.cols);
+    at::Tensor work;
+    if (need) work = bytes(need, out.t);
+    const int rc = unlocked([&] {
+        return pl_matmul_int8(x.rows, w.rows, x.cols, &x.q, &w.q, pb, bias_code, relu, out.p, out.dtype, out.ld,
+                              need ? work.data_ptr() : nullptr, need, stream());
+    });
+    return give(rc, a[5], out.t);
+}
+
+// linear_int8(x, w, bias, relu, dtype, out), w the parts of a matrix of integers
+PyObject *linear_int8(PyObject *const *a) {
+    Matrix x, out;
+    Int8 w;
+    at::Tensor b;
+    const void *pb;
+    int bias_code;
+    bool relu;
+    if (!flag(a[3], &relu) || !matrix(a[0], &x) || !int8(a[1], &w) || x.cols != w.cols ||
+        !bias(a[2], w.rows, &b, &pb, &bias_code) || !result(a[5], a[4], x.rows, w.rows, x.t, &out))
+        Py_RETURN_NONE;
+    const size_t need = pl_linear_int8_workspace(x.rows, w.rows, x.cols);
+    at::Tensor work;
+    if (need) work = bytes(need, out.t);
+    const int rc = unlocked([&] {
+        return pl_linear_int8(x.p, x.dtype, x.rows, x.cols, x.ld, w.rows, &w.q, pb, bias_code, relu, out.p, out.dtype,
+                              out.ld, need ? work.data_ptr() : nullptr, need, stream());
+    });
+    return give(rc, a[5], out.t);
+}
+
 #define ENTRY(name, f, count, doc)                                                                  \
     {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(entry<f, count>)), METH_FASTCALL, doc}
 
@@ -344,6 +568,12 @@ PyMethodDef methods[] = {
     ENTRY("linear", linear, 6, "linear(x, w, bias, relu, dtype, out)"),
     ENTRY("linear_grad", linear_grad, 8,
           "linear_grad(x, grad, w_t, dtype, weight_dtype, x_out, weight_out, accumulate)"),
+    ENTRY("norm", norm, 10, "norm(x, y, gate, after, before, scale, eps, dtype, out, normed_out)"),
+    ENTRY("norm_grad", norm_grad, 16,
+          "norm_grad(h, y, grad, normed_grad, gate, after, before, scale, eps, weight_dtype, x_out, y_out, "
+          "gate_out, after_out, before_out, accumulate)"),
+    ENTRY("product_int8", product_int8, 6, "product_int8(a, b, bias, relu, dtype, out)"),
+    ENTRY("linear_int8", linear_int8, 6, "linear_int8(x, w, bias, relu, dtype, out)"),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_learner", nullptr, -1, methods,

@@ -90,4 +90,95 @@ hipError_t launch_matmul_two(const MatmulArgs &a, int a_dtype, const MatmulArgs 
 bool converts(int64_t m, int64_t n, int64_t k);
 hipError_t launch_convert_matmul(const MatmulArgs &a, int x_dtype, int out_dtype, hipStream_t s);
 
+// One AdamW step. A plan has an entry for each workgroup, which counts the steps made.
+struct AdamwPart {
+    void *weight, *grad;   // the part's first elements
+    int64_t at;            // where they are in the states, a multiple of 128
+    int64_t steps;
+    uint32_t count;
+    float decay;
+};
+struct AdamwArgs {
+    AdamwPart *plan;
+    uint64_t parts;
+    void *m, *v;                     // fp32 or 8-bit codes
+    uint8_t *m_scales, *v_scales;    // of codes, a byte for each 128
+    double log2_beta1, log2_beta2;
+    float beta1, beta2, rest1, rest2, eps, lr, factor;   // rest = 1 - beta
+    const float *lr_at, *factor_at;  // on the device, or null
+    uint64_t seed;
+};
+uint32_t adamw_part(int64_t room);   // elements of a part, at most, a multiple of 128
+hipError_t launch_adamw(const AdamwArgs &a, int weight_dtype, int grad_dtype, int bits, bool push, hipStream_t s);
+
+struct MomentsArgs {
+    const uint8_t *m, *v, *m_scales, *v_scales;
+    void *m_out, *v_out;
+    uint64_t room;   // a multiple of 128
+};
+hipError_t launch_moments(const MomentsArgs &a, int dtype, hipStream_t s);
+
+// The norms after and before a block. Matrices of `rows` x `cols`; vectors may be null.
+struct NormArgs {
+    const void *x, *y;               // y null: no block
+    int64_t x_ld, y_ld;
+    uint32_t rows, per_gate;         // rows that share a row of the gate
+    uint64_t cols;
+    const void *gate, *after, *before;
+    int64_t gate_ld;
+    int gate_bf16, weight_bf16;
+    float scale, eps;
+    void *out, *normed;              // either may be null
+    int64_t out_ld, normed_ld;
+};
+hipError_t launch_norm(const NormArgs &a, int x_dtype, int y_dtype, hipStream_t s);
+
+struct NormGradArgs {
+    const void *h, *y, *dh, *dz;     // y, dh, dz may be null
+    int64_t h_ld, y_ld, dh_ld, dz_ld;
+    uint32_t rows, per_gate, gates;
+    uint64_t cols;
+    const void *gate, *after, *before;
+    int64_t gate_ld;
+    int gate_bf16, weight_bf16;
+    float scale, eps;
+    void *dx, *dy;
+    int64_t dx_ld, dy_ld;
+    void *dgate, *dafter, *dbefore;  // of one type
+    int64_t dgate_ld;
+    int out_bf16, accumulate;
+    void *workspace;
+};
+size_t norm_grad_workspace(int64_t rows, int64_t cols);
+hipError_t launch_norm_grad(const NormGradArgs &a, int x_dtype, int y_dtype, hipStream_t s);
+
+// Products of 8-bit integers with a scale for each row of either factor.
+struct Int8QuantArgs {
+    const void *x;
+    int64_t ld, rows, cols;
+    int8_t *values;
+    float *scales;
+};
+hipError_t launch_quantize_int8(const Int8QuantArgs &a, int dtype, hipStream_t s);
+
+struct Int8Args {
+    const int8_t *a, *b;
+    const float *sa, *sb;
+    const void *bias;
+    void *out;
+    int64_t out_ld;
+    uint32_t m, n, k;       // k: real columns; rows are padded to whole blocks of 128
+    int bias_bf16;
+    int relu;
+    int32_t *partial;       // workspace
+    const void *x;          // where a is null: what it is made from
+    int64_t x_ld;
+    int x_bf16;
+};
+size_t int8_workspace(int64_t m, int64_t n, int64_t k);
+// Whether the product of m x k numbers that are not integers yet is one launch, which needs no a, sa
+// or workspace.
+bool int8_converts(int64_t m, int64_t n, int64_t k);
+hipError_t launch_int8(const Int8Args &a, int out_dtype, hipStream_t s);
+
 }  // namespace gadei::learner
