@@ -18,6 +18,7 @@
 // matrix is read and written once; longer rows are read again. Sums over rows stay in registers over
 // a worker's rows, go to the workspace and are joined in order.
 #include <algorithm>
+#include <type_traits>
 
 #include "pl_device.h"
 
@@ -27,57 +28,122 @@ namespace {
 constexpr int kJoinCols = 32, kJoinRows = 8;   // of a workgroup of `join`
 constexpr int kSums = 6;
 constexpr uint64_t kRowCols = 8 * 1024;        // of a row that 1024 threads hold, eight columns each
-constexpr uint64_t kGradCols = 8 * 512;        // backward: 512, for their registers
 
-// Eight columns of a vector of weights, or ones where there is none; past `count`: zeros.
-__device__ __forceinline__ void vector8(float (&w)[8], const void *p, int bf16, int64_t at, int count) {
+// Where a row begins; the same for all lanes of a wave, so that a lane's address is a 32-bit offset.
+template <int DT>
+__device__ __forceinline__ const void *row_of(const void *p, uint32_t row, int64_t ld) {
+    return static_cast<const char *>(p) + static_cast<int64_t>(row) * ld * kBytes<DT>;
+}
+template <int DT>
+__device__ __forceinline__ void *row_of(void *p, uint32_t row, int64_t ld) {
+    return static_cast<char *>(p) + static_cast<int64_t>(row) * ld * kBytes<DT>;
+}
+
+// The wave's threadIdx.y.
+__device__ __forceinline__ uint32_t wave_y() { return __builtin_amdgcn_readfirstlane(threadIdx.y); }
+
+// A lane's column, which the compiler takes for another one each time: it would keep a 64-bit address a lane
+// for every matrix, where a row's address and 32 bits a lane do.
+__device__ __forceinline__ uint32_t now(uint32_t col) {
+    asm volatile("" : "+v"(col));
+    return col;
+}
+
+// Eight columns as loaded: zeros past `count`.
+template <int DT, bool EIGHTS>
+__device__ __forceinline__ Bits8<DT> bits8(const void *p, uint32_t at, int count) {
+    if (count == 8) return load8<DT>(p, at);
+    if constexpr (EIGHTS) return Bits8<DT>{};
+    else return load8_some<DT>(p, at, count);
+}
+
+// Of a vector of weights, or ones where there is none.
+template <bool EIGHTS>
+__device__ __forceinline__ void vector8(float (&w)[8], const void *p, int bf16, uint32_t at, int count) {
     if (p == nullptr) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) w[e] = 1.0f;
     } else if (bf16) {
-        widen8<PS_BF16>(w, count == 8 ? load8<PS_BF16>(p, at) : load8_some<PS_BF16>(p, at, count));
+        widen8<PS_BF16>(w, bits8<PS_BF16, EIGHTS>(p, at, count));
     } else {
-        widen8<PS_F32>(w, count == 8 ? load8<PS_F32>(p, at) : load8_some<PS_F32>(p, at, count));
+        widen8<PS_F32>(w, bits8<PS_F32, EIGHTS>(p, at, count));
     }
 }
 
+// The same bits, which the compiler takes for others: it would keep what it has widened of them through
+// a row's reduction, in twice the registers.
+__device__ __forceinline__ void anew(Bits8<PS_BF16> &x) { asm volatile("" : "+v"(x.a)); }
+__device__ __forceinline__ void anew(Bits8<PS_F32> &) {}
+
 template <int DT>
-__device__ __forceinline__ void row8(float (&x)[8], const void *p, int64_t at, int count) {
-    widen8<DT>(x, count == 8 ? load8<DT>(p, at) : load8_some<DT>(p, at, count));
+__device__ __forceinline__ void row8(float (&x)[8], const void *p, uint32_t at, int count) {
+    widen8<DT>(x, bits8<DT, false>(p, at, count));
 }
 
 template <int DT>
-__device__ __forceinline__ void put8(void *p, int64_t at, const float (&x)[8], int count) {
+__device__ __forceinline__ void put8(void *p, uint32_t at, const float (&x)[8], int count) {
     if (count == 8) store8<DT>(p, at, x);
     else store_some<DT>(p, at, x, count);
 }
 
+// Results of a row. (Stores past the caches take as long: 16384 x 8192 bf16 218 us with either.)
+template <int DT, bool EIGHTS>
+__device__ __forceinline__ void put_row8(void *p, uint32_t at, const float (&x)[8], int count) {
+    if (count == 0) return;
+    if constexpr (EIGHTS) store8<DT>(p, at, x);
+    else put8<DT>(p, at, x, count);
+}
+
+// How many of a thread's eight columns there are. EIGHTS: all or none, as rows are multiples of eight.
+template <bool EIGHTS>
 __device__ __forceinline__ int count_at(uint64_t cols, uint64_t col) {
+    if (EIGHTS) return col < cols ? 8 : 0;
     return cols >= col + 8 ? 8 : cols > col ? static_cast<int>(cols - col) : 0;
 }
 
+// Sums over the sixteen lanes of a row of lanes, in all of them.
+__device__ __forceinline__ float sum16(float x) {
+    auto rotated = [](float v, auto by) {
+        return __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(v), 0x120 + decltype(by)::value, 0xf, 0xf, true));
+    };
+    x += rotated(x, std::integral_constant<int, 8>());
+    x += rotated(x, std::integral_constant<int, 4>());
+    x += rotated(x, std::integral_constant<int, 2>());
+    x += rotated(x, std::integral_constant<int, 1>());
+    return x;
+}
+
+__device__ __forceinline__ float sum64(float x) {
+    x = sum16(x);
+    const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+    const auto q = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(q[0]) + __uint_as_float(q[1]);
+}
+
 // Sums over the threads of a row: a wave, or a whole workgroup, whose waves' sums go through `lds`
-// (two places in turn, so that one barrier is enough).
+// (two places in turn, so that one barrier is enough). There, sixteen lanes add up each sum.
 template <int K>
 __device__ __forceinline__ void sum_row(float (&s)[K], float *lds, int *turn) {
 #pragma unroll
-    for (int k = 0; k < K; ++k)
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) s[k] += __shfl_xor(s[k], d);
-    const int waves = static_cast<int>(blockDim.x) >> 6;
+    for (int k = 0; k < K; ++k) s[k] = sum64(s[k]);
+    const int waves = static_cast<int>(blockDim.x) >> 6, lane = static_cast<int>(threadIdx.x) & 63;
     if (waves == 1) return;
     float *at = lds + *turn * 16 * kSums;
     *turn ^= 1;
-    if ((threadIdx.x & 63) == 0) {
+    if (lane == 0) {
 #pragma unroll
-        for (int k = 0; k < K; ++k) at[(threadIdx.x >> 6) * K + k] = s[k];
+        for (int k = 0; k < K; ++k) at[16 * k + (threadIdx.x >> 6)] = s[k];
     }
     __syncthreads();
+    const int wave = lane & 15, first = lane >> 4;
 #pragma unroll
-    for (int k = 0; k < K; ++k) s[k] = 0.0f;
-    for (int w = 0; w < waves; ++w)
+    for (int k0 = 0; k0 < K; k0 += 4) {
+        const float v = sum16(wave < waves && k0 + first < K ? at[16 * (k0 + first) + wave] : 0.0f);
 #pragma unroll
-        for (int k = 0; k < K; ++k) s[k] += at[w * K + k];
+        for (int k = k0; k < K && k < k0 + 4; ++k)
+            s[k] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), 16 * (k - k0)));
+    }
 }
 
 __device__ __forceinline__ float inverse_root(float sum, uint64_t cols, float eps) {
@@ -86,89 +152,141 @@ __device__ __forceinline__ float inverse_root(float sum, uint64_t cols, float ep
 
 // ----------------------------------------------------------------- forward
 
-// What the block leaves in the stream: h of eight columns, from y times ry.
-template <int X>
-__device__ __forceinline__ void stream8(float (&h)[8], const NormArgs &a, const float (&y)[8], float ry,
-                                        uint32_t row, uint64_t col, int count) {
-    float x[8], after[8], gate[8];
-    row8<X>(x, a.x, row * a.x_ld + static_cast<int64_t>(col), count);
-    vector8(after, a.after, a.weight_bf16, static_cast<int64_t>(col), count);
-    vector8(gate, a.gate, a.gate_bf16, row / a.per_gate * a.gate_ld + static_cast<int64_t>(col), count);
+__device__ __forceinline__ void times8(float (&a)[8], const float (&b)[8]) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) h[e] = a.scale * x[e] + y[e] * ry * after[e] * gate[e];
+    for (int e = 0; e < 8; ++e) a[e] *= b[e];
 }
 
-template <int X, int Y, int N, bool BLOCK>
-__global__ __launch_bounds__(1024) void norm(NormArgs a) {
+// The row of the gate that is row `row`'s.
+template <bool EIGHTS, class Args>
+__device__ __forceinline__ void gate8(float (&w)[8], const Args &a, uint32_t row, uint32_t col, int count) {
+    const void *const gate = a.gate_bf16 ? row_of<PS_BF16>(a.gate, row / a.per_gate, a.gate_ld)
+                                         : row_of<PS_F32>(a.gate, row / a.per_gate, a.gate_ld);
+    vector8<EIGHTS>(w, a.gate == nullptr ? nullptr : gate, a.gate_bf16, col, count);
+}
+
+// after * gate.
+template <bool EIGHTS, class Args>
+__device__ __forceinline__ void branch_scale(float (&w)[8], const Args &a, uint32_t row, uint32_t col, int count) {
+    float gate[8];
+    vector8<EIGHTS>(w, a.after, a.weight_bf16, col, count);
+    gate8<EIGHTS>(gate, a, row, col, count);
+    times8(w, gate);
+}
+
+// What the block leaves in the stream: h of eight columns.
+template <int X>
+__device__ __forceinline__ void stream8(float (&h)[8], const NormArgs &a, const Bits8<X> &x_bits, const float (&y)[8],
+                                        float ry, const float (&w)[8]) {
+    float x[8];
+    widen8<X>(x, x_bits);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) h[e] = a.scale * x[e] + y[e] * ry * w[e];
+}
+
+// A worker, a wave or a workgroup, takes `rows_each` rows one after another, the next one's loads under
+// way; the vectors stay in registers.
+template <int X, int Y, int N, bool BLOCK, bool EIGHTS>
+__global__ __launch_bounds__(1024) void norm(NormArgs a, uint32_t rows_each) {
     __shared__ float lds[2 * 16 * kSums];
     int turn = 0;
-    const uint64_t row64 = static_cast<uint64_t>(block_index()) * blockDim.y + threadIdx.y;
-    if (row64 >= a.rows) return;   // a whole wave, of those that no barrier waits for
-    const uint32_t row = static_cast<uint32_t>(row64);
-    float h[N][8];
-    float y[N][8];
-    float s[1] = {0.0f};
-    if constexpr (BLOCK) {
+    const uint64_t first = (static_cast<uint64_t>(block_index()) * blockDim.y + wave_y()) * rows_each;
+    if (first >= a.rows) return;   // a whole wave, of those that no barrier waits for
+    const uint32_t last = static_cast<uint32_t>(min(static_cast<uint64_t>(a.rows), first + rows_each));
+    uint32_t col[N];
+    int count[N];
+    float branch[N][8], before[N][8];
+    Bits8<X> next_x[N];
+    Bits8<Y> next_y[N];
+    auto load = [&](uint32_t row) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const uint64_t col = 8 * (threadIdx.x + static_cast<uint64_t>(i) * blockDim.x);
-            row8<Y>(y[i], a.y, row * a.y_ld + static_cast<int64_t>(col), count_at(a.cols, col));
-#pragma unroll
-            for (int e = 0; e < 8; ++e) s[0] += y[i][e] * y[i][e];
+            next_x[i] = bits8<X, EIGHTS>(row_of<X>(a.x, row, a.x_ld), now(col[i]), count[i]);
+            if constexpr (BLOCK) next_y[i] = bits8<Y, EIGHTS>(row_of<Y>(a.y, row, a.y_ld), now(col[i]), count[i]);
         }
-        float ry = 1.0f;
-        if (a.after != nullptr) {
-            sum_row(s, lds, &turn);
-            ry = inverse_root(s[0], a.cols, a.eps);
-        }
-        s[0] = 0.0f;
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const uint64_t col = 8 * (threadIdx.x + static_cast<uint64_t>(i) * blockDim.x);
-            const int count = count_at(a.cols, col);
-            stream8<X>(h[i], a, y[i], ry, row, col, count);
-            if (count) put8<X>(a.out, row * a.out_ld + static_cast<int64_t>(col), h[i], count);
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const uint64_t col = 8 * (threadIdx.x + static_cast<uint64_t>(i) * blockDim.x);
-            row8<X>(h[i], a.x, row * a.x_ld + static_cast<int64_t>(col), count_at(a.cols, col));
-        }
-    }
-    if (a.normed == nullptr) return;
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) s[0] += h[i][e] * h[i][e];
-    sum_row(s, lds, &turn);
-    const float rh = inverse_root(s[0], a.cols, a.eps);
+    };
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        const uint64_t col = 8 * (threadIdx.x + static_cast<uint64_t>(i) * blockDim.x);
-        const int count = count_at(a.cols, col);
-        float w[8];
-        vector8(w, a.before, a.weight_bf16, static_cast<int64_t>(col), count);
+        col[i] = 8 * (threadIdx.x + i * blockDim.x);
+        count[i] = count_at<EIGHTS>(a.cols, col[i]);
+    }
+    load(static_cast<uint32_t>(first));
 #pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] *= h[i][e] * rh;
-        if (count) put8<Y>(a.normed, row * a.normed_ld + static_cast<int64_t>(col), w, count);
+    for (int i = 0; i < N; ++i) vector8<EIGHTS>(before[i], a.before, a.weight_bf16, col[i], count[i]);
+    uint32_t gate_ends = static_cast<uint32_t>(first);
+    for (uint32_t row = static_cast<uint32_t>(first); row < last; ++row) {
+        if (BLOCK && row >= gate_ends) {
+            // of all rows where there is no gate
+            gate_ends = a.gate == nullptr ? a.rows : (row / a.per_gate + 1) * a.per_gate;
+#pragma unroll
+            for (int i = 0; i < N; ++i) branch_scale<EIGHTS>(branch[i], a, row, now(col[i]), count[i]);
+        }
+        float h[N][8];
+        Bits8<X> x[N];
+        Bits8<Y> y[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            x[i] = next_x[i];
+            if constexpr (BLOCK) y[i] = next_y[i];
+        }
+        if (row + 1 < last) load(row + 1);
+        float s[1] = {0.0f};
+        if constexpr (BLOCK) {
+            float ry = 1.0f;
+            if (a.after != nullptr) {
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    float v[8];
+                    widen8<Y>(v, y[i]);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) s[0] += v[e] * v[e];
+                    anew(y[i]);
+                }
+                sum_row(s, lds, &turn);
+                ry = inverse_root(s[0], a.cols, a.eps);
+                s[0] = 0.0f;
+            }
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                float v[8];
+                widen8<Y>(v, y[i]);
+                stream8<X>(h[i], a, x[i], v, ry, branch[i]);
+                put_row8<X, EIGHTS>(row_of<X>(a.out, row, a.out_ld), now(col[i]), h[i], count[i]);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) widen8<X>(h[i], x[i]);
+        }
+        if (a.normed == nullptr) continue;
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s[0] += h[i][e] * h[i][e];
+        sum_row(s, lds, &turn);
+        const float rh = inverse_root(s[0], a.cols, a.eps);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) h[i][e] *= rh * before[i][e];
+            put_row8<Y, EIGHTS>(row_of<Y>(a.normed, row, a.normed_ld), now(col[i]), h[i], count[i]);
+        }
     }
 }
 
 // Longer rows: a workgroup a row, which it reads again for each sum.
 template <int X, int Y, bool BLOCK>
 __global__ __launch_bounds__(1024) void norm_long(NormArgs a) {
+    constexpr bool EIGHTS = false;
     __shared__ float lds[2 * 16 * kSums];
     int turn = 0;
-    const uint64_t row64 = block_index();
-    if (row64 >= a.rows) return;
-    const uint32_t row = static_cast<uint32_t>(row64);
-    const uint64_t first = 8 * threadIdx.x, step = 8 * blockDim.x;
+    const uint32_t row = block_index();
+    if (row >= a.rows) return;
+    const uint32_t first = 8 * threadIdx.x, step = 8 * blockDim.x;
     float s[1] = {0.0f}, ry = 1.0f;
     if (BLOCK && a.after != nullptr) {
-        for (uint64_t col = first; col < a.cols; col += step) {
+        for (uint32_t col = first; col < a.cols; col += step) {
             float y[8];
-            row8<Y>(y, a.y, row * a.y_ld + static_cast<int64_t>(col), count_at(a.cols, col));
+            row8<Y>(y, row_of<Y>(a.y, row, a.y_ld), col, count_at<EIGHTS>(a.cols, col));
 #pragma unroll
             for (int e = 0; e < 8; ++e) s[0] += y[e] * y[e];
         }
@@ -176,34 +294,35 @@ __global__ __launch_bounds__(1024) void norm_long(NormArgs a) {
         ry = inverse_root(s[0], a.cols, a.eps);
         s[0] = 0.0f;
     }
-    auto stream = [&](float (&h)[8], uint64_t col, int count) {
+    auto stream = [&](float (&h)[8], uint32_t col, int count) {
         if constexpr (BLOCK) {
-            float y[8];
-            row8<Y>(y, a.y, row * a.y_ld + static_cast<int64_t>(col), count);
-            stream8<X>(h, a, y, ry, row, col, count);
+            float y[8], w[8];
+            row8<Y>(y, row_of<Y>(a.y, row, a.y_ld), col, count);
+            branch_scale<EIGHTS>(w, a, row, col, count);
+            stream8<X>(h, a, bits8<X, EIGHTS>(row_of<X>(a.x, row, a.x_ld), col, count), y, ry, w);
         } else {
-            row8<X>(h, a.x, row * a.x_ld + static_cast<int64_t>(col), count);
+            row8<X>(h, row_of<X>(a.x, row, a.x_ld), col, count);
         }
     };
-    for (uint64_t col = first; col < a.cols; col += step) {
-        const int count = count_at(a.cols, col);
+    for (uint32_t col = first; col < a.cols; col += step) {
+        const int count = count_at<EIGHTS>(a.cols, col);
         float h[8];
         stream(h, col, count);
-        if (BLOCK) put8<X>(a.out, row * a.out_ld + static_cast<int64_t>(col), h, count);
+        if (BLOCK) put8<X>(row_of<X>(a.out, row, a.out_ld), col, h, count);
 #pragma unroll
         for (int e = 0; e < 8; ++e) s[0] += h[e] * h[e];
     }
     if (a.normed == nullptr) return;
     sum_row(s, lds, &turn);
     const float rh = inverse_root(s[0], a.cols, a.eps);
-    for (uint64_t col = first; col < a.cols; col += step) {
-        const int count = count_at(a.cols, col);
+    for (uint32_t col = first; col < a.cols; col += step) {
+        const int count = count_at<EIGHTS>(a.cols, col);
         float h[8], w[8];
         stream(h, col, count);
-        vector8(w, a.before, a.weight_bf16, static_cast<int64_t>(col), count);
+        vector8<EIGHTS>(w, a.before, a.weight_bf16, col, count);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] *= h[e] * rh;
-        put8<Y>(a.normed, row * a.normed_ld + static_cast<int64_t>(col), w, count);
+        for (int e = 0; e < 8; ++e) h[e] *= rh * w[e];
+        put8<Y>(row_of<Y>(a.normed, row, a.normed_ld), col, h, count);
     }
 }
 
@@ -219,50 +338,54 @@ struct Split {
     f32x4 *rows_of;           // of rows that no worker holds: rh, k1, ry, k2 of each
 };
 
-// Eight columns of a row and of the vectors.
-template <int X, int Y, bool BLOCK>
-struct Eight {
-    float h[8], u[8], dz[8], before[8], y[8], dh[8], after[8], gate[8];
-    __device__ __forceinline__ void load(const NormGradArgs &a, uint32_t row, uint64_t col, int count) {
-        const int64_t c = static_cast<int64_t>(col);
-        row8<X>(h, a.h, row * a.h_ld + c, count);
-        if (a.dz != nullptr) {
-            row8<Y>(dz, a.dz, row * a.dz_ld + c, count);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) dz[e] = 0.0f;
-        }
-        vector8(before, a.before, a.weight_bf16, c, count);
-        if constexpr (BLOCK) {
-            row8<Y>(y, a.y, row * a.y_ld + c, count);
-            vector8(after, a.after, a.weight_bf16, c, count);
-            vector8(gate, a.gate, a.gate_bf16, row / a.per_gate * a.gate_ld + c, count);
-        }
-        if (a.dh != nullptr) {
-            row8<X>(dh, a.dh, row * a.dh_ld + c, count);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) dh[e] = 0.0f;
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) u[e] = dz[e] * before[e];
-    }
-    // h h, u h; y y, and of p = gate after y: p dh, p u, p h
-    __device__ __forceinline__ void sums(float (&s)[kSums]) const {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            s[0] += h[e] * h[e];
-            s[1] += u[e] * h[e];
-            if constexpr (BLOCK) {
-                const float p = gate[e] * after[e] * y[e];
-                s[2] += y[e] * y[e];
-                s[3] += p * dh[e];
-                s[4] += p * u[e];
-                s[5] += p * h[e];
-            }
-        }
+// Eight columns of a row, as loaded.
+template <int X, int Y, bool BLOCK, bool EIGHTS>
+struct RowBits {
+    Bits8<X> h, dh;
+    Bits8<Y> y, dz;
+    __device__ __forceinline__ void load(const NormGradArgs &a, uint32_t row, uint32_t col, int count) {
+        h = bits8<X, EIGHTS>(row_of<X>(a.h, row, a.h_ld), col, count);
+        if constexpr (BLOCK) y = bits8<Y, EIGHTS>(row_of<Y>(a.y, row, a.y_ld), col, count);
+        dh = a.dh != nullptr ? bits8<X, EIGHTS>(row_of<X>(a.dh, row, a.dh_ld), col, count) : Bits8<X>{};
+        dz = a.dz != nullptr ? bits8<Y, EIGHTS>(row_of<Y>(a.dz, row, a.dz_ld), col, count) : Bits8<Y>{};
     }
 };
+
+// What a thread keeps of its columns: the vectors, and sums over rows. In a gate's rows the gradients
+// of the gate and of after share the sum of dH N(y), times after and times the gate.
+struct Columns {
+    float branch[8];                 // after * gate
+    float d_before[8], d_branch[8];
+    f32x4 *before, *d_after;         // in LDS, the thread's own: two fours each, `apart` from one another
+    uint32_t apart;
+};
+
+// h h, u h; y y, and of p = gate after y: p dh, p u, p h
+template <int X, int Y, bool BLOCK, bool EIGHTS>
+__device__ __forceinline__ void add_sums(float (&s)[kSums], const RowBits<X, Y, BLOCK, EIGHTS> &v, const Columns &c) {
+    float h[8], dz[8];
+    widen8<X>(h, v.h);
+    widen8<Y>(dz, v.dz);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        dz[e] *= c.before[e / 4 * c.apart][e % 4];
+        s[0] += h[e] * h[e];
+        s[1] += dz[e] * h[e];
+    }
+    if constexpr (BLOCK) {
+        float y[8], dh[8];
+        widen8<Y>(y, v.y);
+        widen8<X>(dh, v.dh);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float p = c.branch[e] * y[e];
+            s[2] += y[e] * y[e];
+            s[3] += p * dh[e];
+            s[4] += p * dz[e];
+            s[5] += p * h[e];
+        }
+    }
+}
 
 // rh, k1 = rh^2 mean(u h), ry, k2 = ry^2 mean(v y). Without a norm before or after: 0, 0 and 1, 0.
 __device__ __forceinline__ f32x4 row_factors(const NormGradArgs &a, const float (&s)[kSums]) {
@@ -279,39 +402,37 @@ __device__ __forceinline__ f32x4 row_factors(const NormGradArgs &a, const float 
     return r;
 }
 
-struct Gradients {
-    float before[8], after[8], gate[8];   // sums over rows
-    __device__ __forceinline__ void zero(float (&x)[8]) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = 0.0f;
-    }
-};
-
-template <int X, int Y, bool BLOCK>
-__device__ __forceinline__ void take_row(const NormGradArgs &a, const Eight<X, Y, BLOCK> &v, f32x4 r,
-                                         uint32_t row, uint64_t col, int count, Gradients &sum) {
-    float dx[8], dy[8];
+template <int X, int Y, bool BLOCK, bool EIGHTS>
+__device__ __forceinline__ void take_row(const NormGradArgs &a, const RowBits<X, Y, BLOCK, EIGHTS> &v, f32x4 r, uint32_t row,
+                                         uint32_t col, int count, Columns &c) {
+    float h[8], dz[8], d[8];
+    widen8<X>(h, v.h);
+    widen8<Y>(dz, v.dz);
+    widen8<X>(d, v.dh);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        const float d = v.dh[e] + r[0] * (v.u[e] - v.h[e] * r[1]);
-        dx[e] = a.scale * d;
-        sum.before[e] += v.dz[e] * (v.h[e] * r[0]);
-        if constexpr (BLOCK) {
-            const float n = v.y[e] * r[2], g = d * v.gate[e];
-            sum.gate[e] += d * (n * v.after[e]);
-            sum.after[e] += g * n;
-            dy[e] = r[2] * (g * v.after[e] - v.y[e] * r[3]);
-        }
+        d[e] += r[0] * (dz[e] * c.before[e / 4 * c.apart][e % 4] - h[e] * r[1]);
+        c.d_before[e] += dz[e] * (h[e] * r[0]);
+        h[e] = a.scale * d[e];
     }
-    if (count == 0) return;
-    put8<X>(a.dx, row * a.dx_ld + static_cast<int64_t>(col), dx, count);
-    if constexpr (BLOCK) put8<Y>(a.dy, row * a.dy_ld + static_cast<int64_t>(col), dy, count);
+    put_row8<X, EIGHTS>(row_of<X>(a.dx, row, a.dx_ld), col, h, count);
+    if constexpr (BLOCK) {
+        float y[8];
+        widen8<Y>(y, v.y);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            c.d_branch[e] += d[e] * (y[e] * r[2]);
+            d[e] = r[2] * (d[e] * c.branch[e] - y[e] * r[3]);
+        }
+        put_row8<Y, EIGHTS>(row_of<Y>(a.dy, row, a.dy_ld), col, d, count);
+    }
 }
 
-__device__ __forceinline__ void put_result(const NormGradArgs &a, void *p, int64_t at, float (&x)[8], int count) {
+template <bool EIGHTS>
+__device__ __forceinline__ void put_result(const NormGradArgs &a, void *p, uint32_t at, float (&x)[8], int count) {
     if (a.accumulate) {
         float old[8];
-        vector8(old, p, a.out_bf16, at, count);
+        vector8<EIGHTS>(old, p, a.out_bf16, at, count);
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] += old[e];
     }
@@ -319,67 +440,121 @@ __device__ __forceinline__ void put_result(const NormGradArgs &a, void *p, int64
     else put8<PS_F32>(p, at, x, count);
 }
 
-// The gate's sum when its last row, or the worker's, has been taken.
+// The first of a gate's rows among the worker's (without a gate: of all rows); when they end.
+template <bool EIGHTS>
+__device__ __forceinline__ uint32_t begin_gate(const NormGradArgs &a, uint32_t row, uint32_t last, uint32_t col,
+                                               int count, Columns &c) {
+    branch_scale<EIGHTS>(c.branch, a, row, col, count);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) c.d_branch[e] = 0.0f;
+    return a.gate == nullptr ? last : min(last, (row / a.per_gate + 1) * a.per_gate);
+}
+
+// The last of them has been taken, before `end`.
+template <bool EIGHTS>
 __device__ __forceinline__ void end_gate(const NormGradArgs &a, const Split &sp, uint32_t worker, uint32_t first,
-                                         uint32_t row, uint32_t last, uint64_t col, int count, Gradients &sum) {
-    if (a.dgate == nullptr) return;
-    const uint32_t gate = row / a.per_gate;
-    const uint64_t begins = static_cast<uint64_t>(gate) * a.per_gate, ends = begins + a.per_gate;
-    if (row + 1 != ends && row + 1 != last) return;
-    if (count) {
-        if (begins >= first && ends <= last) {
-            put_result(a, a.dgate, gate * a.dgate_ld + static_cast<int64_t>(col), sum.gate, count);
-        } else {
-            const uint64_t slot = 2 * static_cast<uint64_t>(worker) + (begins >= first ? 1 : 0);
-            store8<PS_F32>(sp.gate, static_cast<int64_t>(slot * sp.pitch + col), sum.gate);
-        }
+                                         uint32_t last, uint32_t end, uint32_t col, int count, Columns &c) {
+    float w[8];
+    if (a.dafter != nullptr) {
+        gate8<EIGHTS>(w, a, end - 1, col, count);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) c.d_after[e / 4 * c.apart][e % 4] += w[e] * c.d_branch[e];
     }
-    sum.zero(sum.gate);
+    if (a.dgate == nullptr || count == 0) return;
+    vector8<EIGHTS>(w, a.after, a.weight_bf16, col, count);
+    times8(c.d_branch, w);
+    const uint32_t gate = (end - 1) / a.per_gate;
+    const uint64_t begins = static_cast<uint64_t>(gate) * a.per_gate, ends = begins + a.per_gate;
+    if (begins >= first && ends <= last) {
+        put_result<EIGHTS>(a, a.out_bf16 ? row_of<PS_BF16>(a.dgate, gate, a.dgate_ld) : row_of<PS_F32>(a.dgate, gate, a.dgate_ld),
+                   col, c.d_branch, count);
+    } else {
+        const uint64_t slot = 2 * static_cast<uint64_t>(worker) + (begins >= first ? 1 : 0);
+        store8<PS_F32>(sp.gate + slot * sp.pitch, col, c.d_branch);
+    }
 }
 
-__device__ __forceinline__ void end_worker(const NormGradArgs &a, const Split &sp, uint32_t worker, uint64_t col,
-                                           int count, const Gradients &sum) {
+template <bool EIGHTS>
+__device__ __forceinline__ void begin_worker(const NormGradArgs &a, uint32_t col, int count, Columns &c) {
+    float w[8];
+    vector8<EIGHTS>(w, a.before, a.weight_bf16, col, count);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        c.before[e / 4 * c.apart][e % 4] = w[e];
+        c.branch[e] = c.d_before[e] = c.d_branch[e] = 0.0f;
+    }
+    c.d_after[0] = c.d_after[c.apart] = f32x4{0, 0, 0, 0};
+}
+
+__device__ __forceinline__ void end_worker(const NormGradArgs &a, const Split &sp, uint32_t worker, uint32_t col,
+                                           int count, const Columns &c) {
     if (count == 0) return;
-    const int64_t at = static_cast<int64_t>(worker * sp.pitch + col);
-    if (a.dbefore != nullptr) store8<PS_F32>(sp.before, at, sum.before);
-    if (a.dafter != nullptr) store8<PS_F32>(sp.after, at, sum.after);
+    const uint64_t at = worker * sp.pitch;
+    if (a.dbefore != nullptr) store8<PS_F32>(sp.before + at, col, c.d_before);
+    if (a.dafter == nullptr) return;
+    const f32x4 x = c.d_after[0], y = c.d_after[c.apart];
+    const float sum[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+    store8<PS_F32>(sp.after + at, col, sum);
 }
 
-// A worker is a wave or a workgroup, its rows in registers one after another.
-template <int X, int Y, bool BLOCK, int THREADS>
-__global__ __launch_bounds__(THREADS) void norm_grad(NormGradArgs a, Split sp) {
+// A worker is a wave or a workgroup; it takes its rows one after another, the next one's loads under way.
+template <int X, int Y, bool BLOCK, bool EIGHTS>
+__global__ __launch_bounds__(1024, 4) void norm_grad(NormGradArgs a, Split sp) {
     __shared__ float lds[2 * 16 * kSums];
+    extern __shared__ f32x4 own[];   // four a thread
     int turn = 0;
-    const uint32_t worker = block_index() * blockDim.y + threadIdx.y;
+    const uint32_t worker = block_index() * blockDim.y + wave_y();
     if (worker >= sp.workers) return;   // a whole wave, of those that no barrier waits for
     const uint32_t first = worker * sp.rows, last = min(a.rows - first, sp.rows) + first;
-    const uint64_t col = 8 * threadIdx.x;
-    const int count = count_at(a.cols, col);
-    Gradients sum = {};
-    for (uint32_t row = first; row < last; ++row) {
-        Eight<X, Y, BLOCK> v;
-        v.load(a, row, col, count);
-        float s[kSums] = {};
-        v.sums(s);
-        sum_row(s, lds, &turn);
-        take_row(a, v, row_factors(a, s), row, col, count, sum);
-        end_gate(a, sp, worker, first, row, last, col, count, sum);
+    const uint32_t col = 8 * threadIdx.x;
+    const int count = count_at<EIGHTS>(a.cols, col);
+    RowBits<X, Y, BLOCK, EIGHTS> next;
+    next.load(a, first, col, count);
+    Columns c;
+    c.apart = blockDim.x * blockDim.y;
+    c.before = own + threadIdx.y * blockDim.x + threadIdx.x;
+    c.d_after = c.before + 2 * c.apart;
+    begin_worker<EIGHTS>(a, col, count, c);
+    for (uint32_t row = first; row < last;) {
+        const uint32_t end = BLOCK ? begin_gate<EIGHTS>(a, row, last, now(col), count, c) : last;
+        for (; row < end; ++row) {
+            RowBits<X, Y, BLOCK, EIGHTS> v = next;
+            if (row + 1 < last) next.load(a, row + 1, now(col), count);
+            float s[kSums] = {};
+            add_sums(s, v, c);
+            sum_row(s, lds, &turn);
+            anew(v.h);
+            anew(v.dh);
+            anew(v.dz);
+            if constexpr (BLOCK) anew(v.y);
+            take_row(a, v, row_factors(a, s), row, now(col), count, c);
+        }
+        if constexpr (BLOCK) end_gate<EIGHTS>(a, sp, worker, first, last, end, now(col), count, c);
     }
-    end_worker(a, sp, worker, col, count, sum);
+    end_worker(a, sp, worker, col, count, c);
 }
 
 // Longer rows: first their sums, a workgroup a row, ...
 template <int X, int Y, bool BLOCK>
 __global__ __launch_bounds__(1024) void row_sums(NormGradArgs a, Split sp) {
+    constexpr bool EIGHTS = false;
     __shared__ float lds[2 * 16 * kSums];
     int turn = 0;
-    const uint64_t row = block_index();
+    const uint32_t row = block_index();
     if (row >= a.rows) return;
     float s[kSums] = {};
-    for (uint64_t col = 8 * threadIdx.x; col < a.cols; col += 8 * blockDim.x) {
-        Eight<X, Y, BLOCK> v;
-        v.load(a, static_cast<uint32_t>(row), col, count_at(a.cols, col));
-        v.sums(s);
+    for (uint32_t col = 8 * threadIdx.x; col < a.cols; col += 8 * blockDim.x) {
+        const int count = count_at<EIGHTS>(a.cols, col);
+        RowBits<X, Y, BLOCK, EIGHTS> v;
+        v.load(a, row, col, count);
+        Columns c;
+        float w[8];
+        vector8<EIGHTS>(w, a.before, a.weight_bf16, col, count);
+        f32x4 before[2] = {{w[0], w[1], w[2], w[3]}, {w[4], w[5], w[6], w[7]}};
+        c.before = before;
+        c.apart = 1;
+        if constexpr (BLOCK) branch_scale<EIGHTS>(c.branch, a, row, col, count);
+        add_sums(s, v, c);
     }
     sum_row(s, lds, &turn);
     if (threadIdx.x == 0) sp.rows_of[row] = row_factors(a, s);
@@ -388,25 +563,34 @@ __global__ __launch_bounds__(1024) void row_sums(NormGradArgs a, Split sp) {
 // ... then strips of columns.
 template <int X, int Y, bool BLOCK>
 __global__ __launch_bounds__(256) void norm_grad_long(NormGradArgs a, Split sp, uint32_t strips) {
+    constexpr bool EIGHTS = false;
+    __shared__ f32x4 own[4 * 256];
     const uint64_t worker64 = block_index() / strips;
     if (worker64 >= sp.workers) return;
     const uint32_t worker = static_cast<uint32_t>(worker64);
     const uint32_t first = worker * sp.rows, last = min(a.rows - first, sp.rows) + first;
-    const uint64_t col = 8 * (threadIdx.x + 256ull * (block_index() % strips));
-    const int count = count_at(a.cols, col);
-    Gradients sum = {};
-    for (uint32_t row = first; row < last; ++row) {
-        Eight<X, Y, BLOCK> v;
-        v.load(a, row, col, count);
-        take_row(a, v, sp.rows_of[row], row, col, count, sum);
-        end_gate(a, sp, worker, first, row, last, col, count, sum);
+    const uint32_t col = 8 * (threadIdx.x + 256 * (block_index() % strips));
+    const int count = count_at<EIGHTS>(a.cols, col);
+    Columns c;
+    c.apart = 256;
+    c.before = own + threadIdx.x;
+    c.d_after = c.before + 2 * c.apart;
+    begin_worker<EIGHTS>(a, col, count, c);
+    for (uint32_t row = first; row < last;) {
+        const uint32_t end = BLOCK ? begin_gate<EIGHTS>(a, row, last, now(col), count, c) : last;
+        for (; row < end; ++row) {
+            RowBits<X, Y, BLOCK, EIGHTS> v;
+            v.load(a, row, now(col), count);
+            take_row(a, v, sp.rows_of[row], row, now(col), count, c);
+        }
+        if constexpr (BLOCK) end_gate<EIGHTS>(a, sp, worker, first, last, end, now(col), count, c);
     }
-    end_worker(a, sp, worker, col, count, sum);
+    end_worker(a, sp, worker, col, count, c);
 }
 
-// The workers' sums, in order: y = 0 and 1 dbefore and dafter, from 2 on the gate that goes from
-// worker y - 2 into the next.
-__global__ __launch_bounds__(kJoinCols * kJoinRows) void join(NormGradArgs a, Split sp) {
+// The workers' sums, in order: y = 0 and 1 dbefore and dafter, from 2 on the gates whose rows are more
+// than one worker's: of a few gates gate y - 2, else the one that goes from worker y - 2 into the next.
+__global__ __launch_bounds__(kJoinCols * kJoinRows) void join(NormGradArgs a, Split sp, bool few_gates) {
     __shared__ float lds[kJoinRows][kJoinCols];
     const int x = threadIdx.x % kJoinCols, y = threadIdx.x / kJoinCols;
     const uint64_t col = static_cast<uint64_t>(blockIdx.x) * kJoinCols + x;
@@ -418,13 +602,15 @@ __global__ __launch_bounds__(kJoinCols * kJoinRows) void join(NormGradArgs a, Sp
     uint64_t pitch = sp.pitch;
     float v = 0.0f;
     if (blockIdx.y >= 2) {
-        from = blockIdx.y - 2;
-        const uint64_t boundary = static_cast<uint64_t>(from + 1) * sp.rows, gate = boundary / a.per_gate;
+        const uint64_t i = blockIdx.y - 2, boundary = (i + 1) * sp.rows;
+        const uint64_t gate = few_gates ? i : boundary / a.per_gate;
         const uint64_t begins = gate * a.per_gate, ends = begins + a.per_gate;
-        // none crosses here, or it does not begin in this worker's rows
-        if (begins == boundary || begins < boundary - sp.rows) return;
-        at += static_cast<int64_t>(gate) * a.dgate_ld;
+        // no gate crosses this boundary, or it does not begin in this worker's rows
+        if (!few_gates && (begins == boundary || begins < boundary - sp.rows)) return;
+        from = static_cast<uint32_t>(begins / sp.rows);
         to = static_cast<uint32_t>((ends - 1) / sp.rows) + 1;
+        if (to == from + 1) return;
+        at += static_cast<int64_t>(gate) * a.dgate_ld;
         p = sp.gate;
         pitch = 2 * sp.pitch;
         if (y == 0 && col < a.cols) v = p[(2ull * from + 1) * sp.pitch + col];
@@ -456,22 +642,32 @@ __global__ __launch_bounds__(256) void no_rows(NormGradArgs a) {
 
 // --------------------------------------------------------------- launches
 
-// Threads of a row of so many columns, eight a thread.
-uint32_t threads_of(uint64_t cols) {
-    uint32_t t = 64;
-    while (t < 1024 && 8ull * t < cols) t *= 2;
-    return t;
-}
+// Threads of a row of so many columns, eight a thread: whole waves.
+uint32_t threads_of(uint64_t cols) { return static_cast<uint32_t>(64 * std::min<uint64_t>(16, (cols + 511) / 512)); }
 
 template <int X, int Y, bool BLOCK>
 hipError_t launch(const NormArgs &a, hipStream_t s) {
     const uint32_t threads = threads_of(a.cols);
-    const uint32_t together = threads == 64 ? 4 : 1;   // rows of a workgroup
+    const uint32_t together = threads == 64 ? 4 : 1;   // workers of a workgroup
     dim3 grid;
-    if (!grid_of((a.rows + together - 1ull) / together, threads * together, &grid)) return hipErrorInvalidConfiguration;
-    if (a.cols <= kRowCols) norm<X, Y, 1, BLOCK><<<grid, dim3(threads, together), 0, s>>>(a);
-    else if (a.cols <= 2 * kRowCols) norm<X, Y, 2, BLOCK><<<grid, threads, 0, s>>>(a);
-    else norm_long<X, Y, BLOCK><<<grid, threads, 0, s>>>(a);
+    if (a.cols > 2 * kRowCols) {
+        if (!grid_of(a.rows, threads, &grid)) return hipErrorInvalidConfiguration;
+        norm_long<X, Y, BLOCK><<<grid, threads, 0, s>>>(a);
+        return hipGetLastError();
+    }
+    // In us, with one row a worker, with as many workers as the card has room for, and with 4096: 16384 x
+    // 8192 bf16 246, 215 and 195, without a gate 208, 216 and 197; 16384 x 5000 190, 166 and 148; but rows
+    // of a wave, 200000 x 512, 139, 168 and 170.
+    const uint64_t most = threads == 64 ? ~uint64_t(0) >> 1 : 4096;
+    const uint32_t each = static_cast<uint32_t>((a.rows + most - 1) / most);
+    if (!grid_of((a.rows + each - 1ull) / each / together + 1, threads * together, &grid))
+        return hipErrorInvalidConfiguration;
+    const dim3 block(threads, together);
+    const bool eights = a.cols % 8 == 0;
+    if (a.cols > kRowCols && eights) norm<X, Y, 2, BLOCK, true><<<grid, block, 0, s>>>(a, each);
+    else if (a.cols > kRowCols) norm<X, Y, 2, BLOCK, false><<<grid, block, 0, s>>>(a, each);
+    else if (eights) norm<X, Y, 1, BLOCK, true><<<grid, block, 0, s>>>(a, each);
+    else norm<X, Y, 1, BLOCK, false><<<grid, block, 0, s>>>(a, each);
     return hipGetLastError();
 }
 
@@ -488,7 +684,9 @@ Split split(uint64_t rows, uint64_t cols) {
     Split sp{};
     sp.pitch = (cols + 7) & ~uint64_t(7);
     if (rows == 0) return sp;
-    const uint64_t most = cols > kGradCols ? 64 : std::max<uint64_t>(256, 2048 * 64 / threads_of(cols));
+    // In us with 256, 512, 1024 and 2048 workers, their sums' joining included: 16384 x 4096 bf16 166, 175,
+    // 187 and 198; 32768 x 1024 165, 122, 95 and 110; 100000 x 512 392, 209, 137 and 148
+    const uint64_t most = cols > kRowCols ? 64 : std::clamp<uint64_t>(2048 * 64 / threads_of(cols), 256, 1024);
     sp.rows = static_cast<uint32_t>((rows + most - 1) / most);
     sp.workers = static_cast<uint32_t>((rows + sp.rows - 1) / sp.rows);
     return sp;
@@ -511,11 +709,13 @@ hipError_t launch(const NormGradArgs &a, hipStream_t s) {
             if (!grid_of((a.gates * a.cols + 255) / 256, 256, &grid)) return hipErrorInvalidConfiguration;
             no_rows<<<grid, 256, 0, s>>>(a);
         }
-    } else if (a.cols <= kGradCols) {
+    } else if (a.cols <= kRowCols) {
         const uint32_t together = threads == 64 ? 4 : 1;
         grid = dim3((sp.workers + together - 1) / together);
-        if (threads <= 256) norm_grad<X, Y, BLOCK, 256><<<grid, dim3(threads, together), 0, s>>>(a, sp);
-        else norm_grad<X, Y, BLOCK, 512><<<grid, threads, 0, s>>>(a, sp);
+        const dim3 block(threads, together);
+        const uint32_t own = 4 * sizeof(f32x4) * threads * together;
+        if (a.cols % 8 == 0) norm_grad<X, Y, BLOCK, true><<<grid, block, own, s>>>(a, sp);
+        else norm_grad<X, Y, BLOCK, false><<<grid, block, own, s>>>(a, sp);
     } else {
         if (!grid_of(a.rows, 1024, &grid)) return hipErrorInvalidConfiguration;
         row_sums<X, Y, BLOCK><<<grid, 1024, 0, s>>>(a, sp);
@@ -526,8 +726,10 @@ hipError_t launch(const NormGradArgs &a, hipStream_t s) {
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     const bool gates = a.dgate != nullptr && a.rows != 0 && sp.rows % a.per_gate != 0;
     if (a.dbefore == nullptr && a.dafter == nullptr && !gates) return hipSuccess;
-    grid = dim3(static_cast<uint32_t>((a.cols + kJoinCols - 1) / kJoinCols), gates ? 1 + sp.workers : 2);
-    join<<<grid, kJoinCols * kJoinRows, 0, s>>>(a, sp);
+    const bool few_gates = a.gates < sp.workers;
+    grid = dim3(static_cast<uint32_t>((a.cols + kJoinCols - 1) / kJoinCols),
+                gates ? 2 + (few_gates ? a.gates : sp.workers - 1) : 2);
+    join<<<grid, kJoinCols * kJoinRows, 0, s>>>(a, sp, few_gates);
     return hipGetLastError();
 }
 
@@ -547,7 +749,7 @@ hipError_t launch_norm(const NormArgs &a, int x_dtype, int y_dtype, hipStream_t 
 size_t norm_grad_workspace(int64_t rows, int64_t cols) {
     const Split sp = split(rows, cols);
     return 4 * align256(sizeof(float) * sp.workers * sp.pitch) +
-           (static_cast<uint64_t>(cols) > kGradCols ? sizeof(f32x4) * static_cast<size_t>(rows) : 0);
+           (static_cast<uint64_t>(cols) > kRowCols ? sizeof(f32x4) * static_cast<size_t>(rows) : 0);
 }
 
 hipError_t launch_norm_grad(const NormGradArgs &a, int x_dtype, int y_dtype, hipStream_t s) {
