@@ -24,7 +24,8 @@ namespace gadei::learner {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kFour = 4;   // neighbouring elements a lane
+constexpr int kFour = 4;    // neighbouring elements a lane
+constexpr int kFours = 2;   // of them
 
 typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
 typedef u16x4 u16x4_any __attribute__((aligned(2)));
@@ -107,11 +108,14 @@ __device__ __forceinline__ uint32_t encode(float x, int byte, uint32_t r) {
     return max(code, min(bits, 1u));
 }
 
-// The largest of the 32 lanes that hold a block.
+// The largest of the 32 lanes that hold a block: sixteen by rotations, then the two rows of lanes.
 __device__ __forceinline__ uint32_t most_of_32(uint32_t m) {
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) m = max(m, static_cast<uint32_t>(__shfl_xor(m, d)));
-    return m;
+    m = max(m, static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(m, 0x128, 0xf, 0xf, true)));
+    m = max(m, static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(m, 0x124, 0xf, 0xf, true)));
+    m = max(m, static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(m, 0x122, 0xf, 0xf, true)));
+    m = max(m, static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(m, 0x121, 0xf, 0xf, true)));
+    const auto p = __builtin_amdgcn_permlane16_swap(m, m, false, false);
+    return max(p[0], p[1]);
 }
 
 struct Factors {
@@ -119,6 +123,15 @@ struct Factors {
     float up, root, lr, factor;
 };
 
+// Four elements of a lane, as loaded.
+template <int W, int G, int BITS>
+struct Four {
+    f32x4 w, g, m, v;          // m and v in 32 bits
+    uint32_t cm, cv, bm, bv;   // in 8
+};
+
+// A workgroup makes the step of one part, whose loads are all under way while one wave computes the
+// factors that depend on the number of the step.
 template <int W, int G, int BITS, bool PUSH>
 __global__ __launch_bounds__(kThreads) void adamw(AdamwArgs a) {
 #pragma clang fp contract(off)
@@ -126,58 +139,74 @@ __global__ __launch_bounds__(kThreads) void adamw(AdamwArgs a) {
     const uint64_t index = block_index();
     if (index >= a.parts) return;
     AdamwPart *const part = a.plan + index;
-    if (threadIdx.x == 0) {
-        // Each part counts the steps for itself: the count of a captured step goes on when it is
-        // replayed, and no part waits for another.
-        const int64_t t = part->steps + 1;
-        part->steps = t;
-        Factors f;
-        f.t = static_cast<uint64_t>(t);
-        f.up = static_cast<float>(1.0 / (1.0 - exp2(static_cast<double>(t) * a.log2_beta1)));
-        f.root = static_cast<float>(1.0 / sqrt(1.0 - exp2(static_cast<double>(t) * a.log2_beta2)));
-        f.lr = a.lr_at != nullptr ? *a.lr_at : a.lr;
-        f.factor = a.factor_at != nullptr ? *a.factor_at : a.factor;
-        shared = f;
-    }
-    __syncthreads();
-    const Factors f = shared;
     void *const w = part->weight, *const g = part->grad;
     const int64_t first = part->at;   // of the states
     const int count = static_cast<int>(part->count);
     const float decay = part->decay;
     const int room = (count + 127) & ~127;
-    for (int i = threadIdx.x * kFour; i < room; i += kThreads * kFour) {
-        const int left = count - i;
-        const f32x4 x = load4<W>(w, i, left);
-        f32x4 d = load4<G>(g, i, left);
-        f32x4 m, v;
-        uint32_t cm, cv;
-        int bm = 0, bv = 0;
-        const int64_t at = first + i;
+    Four<W, G, BITS> x[kFours];
+#pragma unroll
+    for (int j = 0; j < kFours; ++j) {
+        const int i = (threadIdx.x + j * kThreads) * kFour;
+        if (i >= room) continue;
+        x[j].w = load4<W>(w, i, count - i);
+        x[j].g = load4<G>(g, i, count - i);
         if constexpr (BITS == 32) {
-            m = *reinterpret_cast<const f32x4 *>(static_cast<const float *>(a.m) + at);
-            v = *reinterpret_cast<const f32x4 *>(static_cast<const float *>(a.v) + at);
+            x[j].m = *reinterpret_cast<const f32x4 *>(static_cast<const float *>(a.m) + first + i);
+            x[j].v = *reinterpret_cast<const f32x4 *>(static_cast<const float *>(a.v) + first + i);
         } else {
-            cm = *reinterpret_cast<const uint32_t *>(static_cast<const uint8_t *>(a.m) + at);
-            cv = *reinterpret_cast<const uint32_t *>(static_cast<const uint8_t *>(a.v) + at);
-            bm = a.m_scales[at >> 7];
-            bv = a.v_scales[at >> 7];
+            x[j].cm = *reinterpret_cast<const uint32_t *>(static_cast<const uint8_t *>(a.m) + first + i);
+            x[j].cv = *reinterpret_cast<const uint32_t *>(static_cast<const uint8_t *>(a.v) + first + i);
+            x[j].bm = a.m_scales[(first + i) >> 7];
+            x[j].bv = a.v_scales[(first + i) >> 7];
+        }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (threadIdx.x < 2) {
+        // Each part counts the steps for itself: the count of a captured step goes on when it is
+        // replayed, and no part waits for another.
+        const int64_t t = part->steps + 1;
+        const double rest = 1.0 - exp2(static_cast<double>(t) * (threadIdx.x == 0 ? a.log2_beta1 : a.log2_beta2));
+        if (threadIdx.x == 0) {
+            part->steps = t;
+            shared.t = static_cast<uint64_t>(t);
+            shared.up = static_cast<float>(1.0 / rest);
+            shared.lr = a.lr_at != nullptr ? *a.lr_at : a.lr;
+            shared.factor = a.factor_at != nullptr ? *a.factor_at : a.factor;
+        } else {
+            shared.root = static_cast<float>(1.0 / sqrt(rest));
+        }
+    }
+    __syncthreads();
+    const Factors f = shared;
+#pragma unroll
+    for (int j = 0; j < kFours; ++j) {
+        const int i = (threadIdx.x + j * kThreads) * kFour, left = count - i;
+        if (i >= room) continue;
+        const int64_t at = first + i;
+        f32x4 m = x[j].m, v = x[j].v, y;
+        if constexpr (BITS == 8) {
+            const int bm = static_cast<int>(x[j].bm), bv = static_cast<int>(x[j].bv);
 #pragma unroll
             for (int e = 0; e < kFour; ++e) {
-                m[e] = decode<true>(cm >> 8 * e & 0xff, bm);
-                v[e] = decode<false>(cv >> 8 * e & 0xff, bv);
-                if (bm == kBad) m[e] = __builtin_nanf("");
-                if (bv == kBad) v[e] = __builtin_nanf("");
+                m[e] = decode<true>(x[j].cm >> 8 * e & 0xff, bm);
+                v[e] = decode<false>(x[j].cv >> 8 * e & 0xff, bv);
+            }
+            if (bm == kBad || bv == kBad) {   // rare
+#pragma unroll
+                for (int e = 0; e < kFour; ++e) {
+                    if (bm == kBad) m[e] = __builtin_nanf("");
+                    if (bv == kBad) v[e] = __builtin_nanf("");
+                }
             }
         }
-        f32x4 y;
 #pragma unroll
         for (int e = 0; e < kFour; ++e) {
-            const float ge = d[e] * f.factor;
+            const float ge = x[j].g[e] * f.factor;
             m[e] = a.beta1 * m[e] + a.rest1 * ge;
             v[e] = a.beta2 * v[e] + a.rest2 * (ge * ge);
-            const float step = f.lr * (m[e] * f.up / (sqrtf(v[e]) * f.root + a.eps) + decay * x[e]);
-            y[e] = PUSH ? step : x[e] - step;
+            const float step = f.lr * (m[e] * f.up / (sqrtf(v[e]) * f.root + a.eps) + decay * x[j].w[e]);
+            y[e] = PUSH ? step : x[j].w[e] - step;
         }
         if constexpr (PUSH) store4<G>(g, i, y, left);
         else store4<W>(w, i, y, left);
@@ -191,10 +220,9 @@ __global__ __launch_bounds__(kThreads) void adamw(AdamwArgs a) {
                 mm = max(mm, __float_as_uint(m[e]) & 0x7fffffffu);
                 mv = max(mv, __float_as_uint(v[e]) & 0x7fffffffu);
             }
-            bm = block_byte(most_of_32(mm));
-            bv = block_byte(most_of_32(mv));
+            const int bm = static_cast<int>(block_byte(most_of_32(mm))), bv = static_cast<int>(block_byte(most_of_32(mv)));
             const u32x4 r = random4(static_cast<uint64_t>(at) >> 2, f.t, a.seed);
-            cm = cv = 0;
+            uint32_t cm = 0, cv = 0;
 #pragma unroll
             for (int e = 0; e < kFour; ++e) {
                 cm |= encode<true>(m[e], bm, r[e] & 0xffffu) << 8 * e;
@@ -247,7 +275,7 @@ hipError_t launch_bits(const AdamwArgs &a, int bits, hipStream_t s) {
 
 }  // namespace
 
-uint32_t adamw_part(int64_t room) { return room >= int64_t(1) << 24 ? 8192 : 2048; }
+uint32_t adamw_part() { return kThreads * kFour * kFours; }
 
 hipError_t launch_adamw(const AdamwArgs &a, int weight_dtype, int grad_dtype, int bits, bool push, hipStream_t s) {
     if (!push)

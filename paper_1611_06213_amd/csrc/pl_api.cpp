@@ -815,7 +815,7 @@ int64_t pl_adamw_room(const pl_adamw_tensor *tensors, int64_t n) { return adamw_
 int64_t pl_adamw_parts(const pl_adamw_tensor *tensors, int64_t n) {
     const int64_t room = adamw_room(tensors, n);
     if (room < 0) return -1;
-    const int64_t most = adamw_part(room);
+    const int64_t most = adamw_part();
     int64_t parts = 0;
     for (int64_t i = 0; i < n; ++i) parts += (tensors[i].count + most - 1) / most;
     return parts;
@@ -850,7 +850,7 @@ int pl_adamw_plan(const pl_adamw_tensor *tensors, int64_t n, int weight_dtype, i
     } catch (const std::bad_alloc &) {
         return fail(PS_ENOMEM, "no memory for the check of %lld tensors", static_cast<long long>(n));
     }
-    const int64_t most = adamw_part(adamw_room(tensors, n));
+    const int64_t most = adamw_part();
     char *to = static_cast<char *>(plan);
     int64_t at = 0;
     for (int64_t i = 0; i < n; ++i) {

@@ -108,7 +108,7 @@ struct AdamwArgs {
     const float *lr_at, *factor_at;  // on the device, or null
     uint64_t seed;
 };
-uint32_t adamw_part(int64_t room);   // elements of a part, at most, a multiple of 128
+uint32_t adamw_part();   // elements of a part, at most, a multiple of 128
 hipError_t launch_adamw(const AdamwArgs &a, int weight_dtype, int grad_dtype, int bits, bool push, hipStream_t s);
 
 struct MomentsArgs {
