@@ -556,6 +556,88 @@ PyObject *linear_int8(PyObject *const *a) {
     return give(rc, a[5], out.t);
 }
 
+// An optimizer's states: m, v and, of 8 bits, their scales (else None), which a caller may have exchanged.
+struct States {
+    void *p[4] = {};
+    at::Tensor t[4];
+};
+
+bool states(PyObject *const *a, int64_t room, int64_t bits, States *s) {
+    for (int i = 0; i < 4; ++i) {
+        if (i >= 2 && bits == 32) break;
+        if (!device_tensor(a[i], &s->t[i]) || !s->t[i].is_contiguous() ||
+            s->t[i].scalar_type() != (bits == 32 ? at::kFloat : at::kByte) ||
+            s->t[i].numel() != (i < 2 ? room : room / 128))
+            return false;
+        s->p[i] = s->t[i].data_ptr();
+    }
+    return true;
+}
+
+// A number, or one fp32 on the device.
+bool number_or_tensor(PyObject *o, float *x, at::Tensor *t, const float **at) {
+    *at = nullptr;
+    *x = 0.0f;
+    if (number(o, x)) return true;
+    if (!device_tensor(o, t) || t->scalar_type() != at::kFloat || t->numel() != 1) return false;
+    *at = static_cast<const float *>(t->data_ptr());
+    return true;
+}
+
+// adamw_step(m, v, m_scales, v_scales, plan, (parts, room, weight code, grad code, push, bits, seed), beta1,
+// beta2, eps, lr, factor): None if it is not made, else its status
+PyObject *adamw_step(PyObject *const *a) {
+    int64_t k[6];
+    if (!PyTuple_CheckExact(a[5]) || PyTuple_GET_SIZE(a[5]) != 7) Py_RETURN_NONE;
+    for (int i = 0; i < 6; ++i)
+        if (!integer(PyTuple_GET_ITEM(a[5], i), &k[i])) Py_RETURN_NONE;
+    const uint64_t seed = PyLong_AsUnsignedLongLong(PyTuple_GET_ITEM(a[5], 6));
+    const double beta1 = PyFloat_AsDouble(a[6]), beta2 = PyFloat_AsDouble(a[7]);
+    if (PyErr_Occurred()) {
+        PyErr_Clear();
+        Py_RETURN_NONE;
+    }
+    States s;
+    at::Tensor plan, tl, tf;
+    float eps, lr, factor;
+    const float *lr_at, *factor_at;
+    if (!states(a, k[1], k[5], &s) || !device_tensor(a[4], &plan) || !plan.is_contiguous() ||
+        plan.scalar_type() != at::kByte || static_cast<size_t>(plan.numel()) != pl_adamw_plan_bytes(k[0]) ||
+        !number(a[8], &eps) || !number_or_tensor(a[9], &lr, &tl, &lr_at) ||
+        !number_or_tensor(a[10], &factor, &tf, &factor_at))
+        Py_RETURN_NONE;
+    return PyLong_FromLong(unlocked([&] {
+        return pl_adamw_step(plan.data_ptr(), k[0], static_cast<int>(k[2]), static_cast<int>(k[3]),
+                             static_cast<int>(k[4]), static_cast<int>(k[5]), k[1], s.p[0], s.p[1],
+                             static_cast<uint8_t *>(s.p[2]), static_cast<uint8_t *>(s.p[3]), beta1, beta2, eps, lr,
+                             lr_at, factor, factor_at, seed, stream());
+    }));
+}
+
+// adamw_moments(m, v, m_scales, v_scales, room, dtype), of states in 8 bits: m and v of dtype
+PyObject *adamw_moments(PyObject *const *a) {
+    States s;
+    int64_t room;
+    int code;
+    if (!integer(a[4], &room) || !states(a, room, 8, &s) || !THPDtype_Check(a[5]) ||
+        !code_of(reinterpret_cast<THPDtype *>(a[5])->scalar_type, &code))
+        Py_RETURN_NONE;
+    const auto options = s.t[0].options().dtype(code == PS_F32 ? at::kFloat : at::kBFloat16);
+    const at::Tensor m = at::empty({room}, options), v = at::empty({room}, options);
+    const int rc = unlocked([&] {
+        return pl_adamw_moments(room, s.p[0], s.p[1], static_cast<uint8_t *>(s.p[2]), static_cast<uint8_t *>(s.p[3]),
+                                m.data_ptr(), v.data_ptr(), code, stream());
+    });
+    if (rc != PS_OK) return PyLong_FromLong(rc);
+    PyObject *pm = THPVariable_Wrap(m), *pv = THPVariable_Wrap(v);
+    if (pm == nullptr || pv == nullptr) {
+        Py_XDECREF(pm);
+        Py_XDECREF(pv);
+        return nullptr;
+    }
+    return Py_BuildValue("(NN)", pm, pv);
+}
+
 #define ENTRY(name, f, count, doc)                                                                  \
     {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(entry<f, count>)), METH_FASTCALL, doc}
 
@@ -574,6 +656,9 @@ PyMethodDef methods[] = {
           "gate_out, after_out, before_out, accumulate)"),
     ENTRY("product_int8", product_int8, 6, "product_int8(a, b, bias, relu, dtype, out)"),
     ENTRY("linear_int8", linear_int8, 6, "linear_int8(x, w, bias, relu, dtype, out)"),
+    ENTRY("adamw_step", adamw_step, 11,
+          "adamw_step(m, v, m_scales, v_scales, plan, fixed, beta1, beta2, eps, lr, factor)"),
+    ENTRY("adamw_moments", adamw_moments, 6, "adamw_moments(m, v, m_scales, v_scales, room, dtype)"),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_learner", nullptr, -1, methods,

@@ -854,6 +854,8 @@ class AdamW:
             self.m_scales, self.v_scales = (torch.zeros(self._room // 128, dtype=torch.uint8, device=self.device)
                                             for _ in range(2))
         self.plan = plan.to(self.device)
+        # what does not change, as the native call takes it
+        self._fixed = (self._parts, self._room, *self._codes, int(self.push), bits, seed)
 
     def _plan(self, steps: int):
         L = load_library()
@@ -868,13 +870,26 @@ class AdamW:
                              f"cuda:{torch.cuda.current_device()}")
 
     def _states(self):
-        """Their addresses, as the library takes them."""
-        scales = (None, None) if self.bits == 32 else (self.m_scales.data_ptr(), self.v_scales.data_ptr())
-        return (self.m.data_ptr(), self.v.data_ptr(), *scales)
+        """Their addresses, as the library takes them; a caller may have exchanged the tensors for others."""
+        kind, out = torch.float32 if self.bits == 32 else torch.uint8, []
+        for name, n in (("m", self._room), ("v", self._room), ("m_scales", self._room // 128),
+                        ("v_scales", self._room // 128))[:2 if self.bits == 32 else 4]:
+            t = getattr(self, name)
+            _on_device(name, t)
+            if t.dtype != kind or t.numel() != n or not t.is_contiguous():
+                raise ValueError(f"{name}: {n} contiguous elements of {kind} expected, not {t.dtype} of {tuple(t.shape)}")
+            out.append(t.data_ptr())
+        return out if self.bits == 8 else out + [None, None]
 
     def step(self, lr, factor=1.0) -> None:
         """One step. `lr`, and `factor`, by which gradients are multiplied first (of a clipped norm, or of a scaled
         loss): numbers, or fp32 tensors of one element on the device, read when the step is made."""
+        native = _native or _native_calls()
+        if native:
+            done = native.adamw_step(self.m, self.v, self.m_scales, self.v_scales, self.plan, self._fixed, *self.betas,
+                                     self.eps, lr, factor)
+            if _done(done):
+                return
         self._here()
         numbers = []
         for name, x in (("lr", lr), ("factor", factor)):
@@ -885,6 +900,10 @@ class AdamW:
                 numbers += [0.0, x.data_ptr()]
             else:
                 numbers += [x, None]
+        _on_device("plan", self.plan)
+        if self.plan.numel() != load_library().pl_adamw_plan_bytes(self._parts) or self.plan.dtype != torch.uint8 or \
+                not self.plan.is_contiguous():
+            raise ValueError(f"plan: not this optimizer's, but {self.plan.dtype} of {tuple(self.plan.shape)}")
         _check(load_library().pl_adamw_step(
             self.plan.data_ptr(), self._parts, *self._codes, int(self.push), self.bits, self._room, *self._states(),
             *self.betas, self.eps, *numbers, self.seed, _stream()))
@@ -903,6 +922,11 @@ class AdamW:
         self._here()
         if self.bits == 32:
             return self.m.to(dtype), self.v.to(dtype)
+        native = _native or _native_calls()
+        if native:
+            done = native.adamw_moments(self.m, self.v, self.m_scales, self.v_scales, self._room, dtype)
+            if _done(done):
+                return done
         m, v = (torch.empty(self._room, dtype=dtype, device=self.device) for _ in range(2))
         _check(load_library().pl_adamw_moments(self._room, *self._states(), m.data_ptr(), v.data_ptr(), _code(dtype),
                                                _stream()))

@@ -4,15 +4,11 @@ import pytest
 
 from tests import adamw_ref
 from tests import learner_ref as ref
-from tests.test_gpu_learner import B16, U, dt, gen, randn, torch  # noqa: F401
+from tests.test_gpu_learner import B16, U, dt, gen, learner, randn, torch  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
 
-@pytest.fixture(scope="module")
-def learner(torch):  # noqa: F811
-    from paper_1611_06213_amd import learner
-    return learner
 
 
 class Tensors:
@@ -258,6 +254,13 @@ def test_refusals(torch, learner):  # noqa: F811
     from paper_1611_06213_amd import ps
     w, g = torch.ones(100, device="cuda"), torch.ones(100, device="cuda")
     A = learner.AdamW
+
+    def exchanged(bits, **parts):
+        opt = A([w], [g], bits=bits)
+        for k, t in parts.items():
+            setattr(opt, k, t)
+        return opt
+
     bad = [
         (ValueError, lambda: A([], [])),
         (ValueError, lambda: A([w], [])),
@@ -284,6 +287,13 @@ def test_refusals(torch, learner):  # noqa: F811
         (ValueError, lambda: A([w], [g]).load(A([w[:10]], [g[:10]]).state() | {"m": torch.zeros(1, device="cuda")})),
         (ValueError, lambda: A([w], [g], bits=8).load(A([w], [g]).state())),
         (TypeError, lambda: A([w], [g], bits=8).moments(torch.float16)),
+        (ValueError, lambda: exchanged(8, m=torch.zeros(127, device="cuda", dtype=torch.uint8)).step(0.1)),
+        (ValueError, lambda: exchanged(8, v_scales=torch.zeros(1, device="cuda")).step(0.1)),
+        (ValueError, lambda: exchanged(32, v=torch.zeros(128, device="cuda", dtype=torch.bfloat16)).step(0.1)),
+        (ValueError, lambda: exchanged(32, m=torch.zeros(128)).step(0.1)),
+        (ValueError, lambda: exchanged(8, v=torch.zeros(256, device="cuda", dtype=torch.uint8)[::2]).moments()),
+        (ValueError, lambda: exchanged(8, plan=torch.zeros(40, dtype=torch.uint8)).step(0.1)),
+        (ValueError, lambda: exchanged(8, plan=torch.zeros(39, device="cuda", dtype=torch.uint8)).step(0.1)),
     ]
     for i, (error, call) in enumerate(bad):
         with pytest.raises(error):
