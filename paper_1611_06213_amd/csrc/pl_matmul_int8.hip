@@ -11,7 +11,7 @@
 // operand is b: then a lane holds four neighbouring columns of out, of one row.
 //
 // Two kernels: `tiles` stages tiles of both operands in LDS, for many rows of a; `slim`, for at most
-// 32 rows of a, reads b straight into registers. Where there are too few tiles to fill the card, k is
+// 64 rows of a, reads b straight into registers. Where there are too few tiles to fill the card, k is
 // split over workgroups; the parts' sums go to the workspace and `join` adds them up.
 #include <algorithm>
 
@@ -411,12 +411,12 @@ __global__ __launch_bounds__(256, F == 2 ? 2 : 1) void tiles(Int8Args g, Split s
 // its first rows of b are under way: for few rows that is less than a launch.
 constexpr int kGiven = -1;
 template <int FM>
-constexpr int kAhead = FM == 1 ? 4 : 2;   // blocks whose loads are issued together
+constexpr int kAhead = FM == 1 ? 4 : FM == 2 ? 2 : 1;   // blocks whose loads are issued together
 
 template <int FM, int OUT, int X, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void slim(Int8Args g, Split sp) {
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
-    __shared__ uint32_t most[16];
+    __shared__ uint32_t most[16 * FM];
     constexpr int A = kAhead<FM>;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int q = lane >> 4, r16 = lane & 15;
@@ -450,7 +450,7 @@ __global__ __launch_bounds__(64 * WAVES) void slim(Int8Args g, Split sp) {
     };
     load(first + wave);
     if constexpr (X != kGiven) {
-        if (threadIdx.x < 16) most[threadIdx.x] = 0;
+        if (threadIdx.x < 16 * FM) most[threadIdx.x] = 0;
         __syncthreads();
         // eights of all rows, sixteen lanes a block; the first kKept of a thread stay in registers
         const uint32_t eights = g.m * blocks * 16;
@@ -488,7 +488,6 @@ __global__ __launch_bounds__(64 * WAVES) void slim(Int8Args g, Split sp) {
         }
         __syncthreads();
     }
-    const uint32_t rx = min(uint32_t(r16), g.m - 1);
     i32x4 acc[FM] = {};
     for (uint32_t block = first + wave; block < last; block += WAVES * A) {
 #pragma unroll
@@ -502,7 +501,8 @@ __global__ __launch_bounds__(64 * WAVES) void slim(Int8Args g, Split sp) {
                     lo = t.a[j][i][0];
                     hi = t.a[j][i][1];
                 } else {
-                    const i32x4 *p = reinterpret_cast<const i32x4 *>(lds + rx * pitch + at * 128 + 32 * q);
+                    const uint32_t row = min(16u * i + r16, g.m - 1);
+                    const i32x4 *p = reinterpret_cast<const i32x4 *>(lds + row * pitch + at * 128 + 32 * q);
                     lo = p[0];
                     hi = p[1];
                 }
@@ -553,7 +553,6 @@ __global__ __launch_bounds__(256) void join(Int8Args g, uint32_t parts) {
 
 // ---------------------------------------------------------------- choices
 
-constexpr uint32_t kSlimRows = 32;
 // Bytes of sums of parts where whole tiles fill the card too.
 constexpr uint64_t kMostSums = uint64_t(1) << 26;
 
@@ -580,7 +579,6 @@ double tiles_take(uint64_t m, uint64_t n, uint64_t blocks, bool large, uint64_t 
     return us;
 }
 
-// For more than kSlimRows rows of a.
 Choice choose(uint64_t m, uint64_t n, uint64_t k) {
     Choice c{};
     const uint64_t blocks = (k + 127) / 128, small = (m + 127) / 128 * ((n + 127) / 128);
@@ -615,9 +613,23 @@ Choice choose(uint64_t m, uint64_t n, uint64_t k) {
     return c;
 }
 
-// Whether slim converts x itself: a row's bytes in LDS and the padding. Every workgroup converts all of
-// x.
-bool few_bytes(uint64_t m, uint64_t blocks) { return m <= 16 && m * (blocks * 128 + 16) <= 51200; }
+// Few rows: slim reads b once, past LDS, and rows of a for every 16 columns of out. In us, a layer with slim
+// and with tiles: 32 x 1000 x 9216 13.6 and 14.6, 64 x 4096 x 4096 15.3 and 16.4, 24 x 4096 x 9216 17.5 and
+// 17.4, 64 x 4096 x 9216 27.0 and 19.6, 1 x 25088 x 4096 24.0 and 28.6, 1 x 25088 x 1000 14.2 and 11.7: fitted
+// to 104 sizes, of which the rule takes 0.7% longer than the better of both.
+constexpr uint64_t kSlimRows = 64;
+
+bool is_slim(uint64_t m, uint64_t n, uint64_t k) {
+    const double m1 = static_cast<double>(m), n1 = static_cast<double>(n), k1 = static_cast<double>(k);
+    return m <= kSlimRows && n1 * (1.0 + (m1 - 10.0) * k1 / 53000.0) <= 16700.0;
+}
+
+// Whether slim converts x itself: a row's bytes in LDS and the padding. Every workgroup converts all of x: in
+// us, so and in two launches, 16 x 1000 x 900 6.2 and 8.6, 4 x 4096 x 9216 12.3 and 13.3, 24 x 1000 x 900 8.7
+// and 8.1, 1 x 25088 x 4096 24.9 and 24.0.
+bool few_bytes(uint64_t m, uint64_t n, uint64_t blocks) {
+    return m <= 16 && n <= 8192 && m * (blocks * 128 + 16) <= 51200;
+}
 
 // Of slim: where few columns of out leave compute units idle, a long k is split, to a block a wave at
 // least.
@@ -626,7 +638,7 @@ Split split_slim(uint64_t m, uint64_t n, uint64_t k) {
     const uint64_t blocks = (k + 127) / 128;
     sp.tiles_m = 1;
     sp.tiles_n = static_cast<uint32_t>((n + 15) / 16);
-    const bool whole = blocks < 64 || (blocks < 128 && few_bytes(m, blocks));
+    const bool whole = blocks < 64 || (blocks < 128 && few_bytes(m, n, blocks));
     const uint64_t many = std::min<uint64_t>(kCus / sp.tiles_n, blocks / 16);
     const uint64_t parts = whole ? 1 : std::max<uint64_t>(1, many);
     sp.steps = static_cast<uint32_t>((blocks + parts - 1) / parts);
@@ -635,7 +647,7 @@ Split split_slim(uint64_t m, uint64_t n, uint64_t k) {
 }
 
 Split split_of(uint64_t m, uint64_t n, uint64_t k) {
-    return m <= kSlimRows ? split_slim(m, n, k) : choose(m, n, k).split;
+    return is_slim(m, n, k) ? split_slim(m, n, k) : choose(m, n, k).split;
 }
 
 template <int FM, int OUT, int X>
@@ -643,7 +655,8 @@ hipError_t launch_slim(const Int8Args &g, const Split &sp, hipStream_t s) {
     const uint32_t blocks = (g.k + 127) / 128;
     const uint32_t x = X == kGiven ? 0 : g.m * (blocks * 128 + 16);
     constexpr uint32_t kSums = FM * 64 * sizeof(i32x4);   // of a wave
-    const bool long_rows = sp.steps > 64 || sp.parts > 1;
+    // sixteen waves keep twice as much of x, too
+    const bool long_rows = sp.steps > 64 || sp.parts > 1 || (X != kGiven && g.m * blocks * 16 > kKept * 512);
     dim3 grid;
     if (!grid_of(static_cast<uint64_t>(sp.tiles_n) * sp.parts, long_rows ? 1024 : 512, &grid))
         return hipErrorInvalidConfiguration;
@@ -668,11 +681,13 @@ hipError_t launch(const Int8Args &g, hipStream_t s) {
     if (g.k == 0) return launch_join<OUT>(g, 0, s);
     Split sp;
     hipError_t e;
-    if (g.m <= kSlimRows) {
+    if (is_slim(g.m, g.n, g.k)) {
         sp = split_slim(g.m, g.n, g.k);
         if (g.a == nullptr)
             return g.x_bf16 ? launch_slim<1, OUT, PS_BF16>(g, sp, s) : launch_slim<1, OUT, PS_F32>(g, sp, s);
-        e = g.m <= 16 ? launch_slim<1, OUT, kGiven>(g, sp, s) : launch_slim<2, OUT, kGiven>(g, sp, s);
+        e = g.m <= 16   ? launch_slim<1, OUT, kGiven>(g, sp, s)
+            : g.m <= 32 ? launch_slim<2, OUT, kGiven>(g, sp, s)
+                        : launch_slim<4, OUT, kGiven>(g, sp, s);
     } else {
         const Choice c = choose(g.m, g.n, g.k);
         sp = c.split;
@@ -706,7 +721,8 @@ size_t int8_workspace(int64_t m, int64_t n, int64_t k) {
 }
 
 bool int8_converts(int64_t m, int64_t n, int64_t k) {
-    return m > 0 && n > 0 && k > 0 && few_bytes(m, (k + 127) / 128) && split_slim(m, n, k).parts == 1;
+    return m > 0 && n > 0 && k > 0 && few_bytes(m, n, (k + 127) / 128) && is_slim(m, n, k) &&
+           split_slim(m, n, k).parts == 1;
 }
 
 hipError_t launch_int8(const Int8Args &g, int out_dtype, hipStream_t s) {
