@@ -21,8 +21,6 @@
 namespace gadei::learner {
 namespace {
 
-typedef int i32x16 __attribute__((ext_vector_type(16)));
-
 // ---------------------------------------------------------------- integers
 
 constexpr float kLeast = 0x1p-100f;   // below it a row's largest would have no inverse in fp32
@@ -160,7 +158,32 @@ __device__ __forceinline__ void keep(const Int8Args &g, i32x4 v, uint32_t part, 
 
 // ------------------------------------------------------------------- tiles
 
-// Tiles of 64 F x 64 F by 2 x 2 waves, each F x F blocks of 32 x 32.
+// Of s_waitcnt: until so many copies and loads, and reads of LDS, are under way. By the builtin, which tells
+// the compiler: it would wait for its reads once more.
+constexpr int wait(int vm, int lgkm) { return (vm & 15) | (vm >> 4) << 14 | 7 << 4 | lgkm << 8; }
+constexpr int kAnyReads = 15;
+constexpr int kSums = -2;   // for OUT: parts' sums
+
+// c += b a^T, with c where it is: from the builtin the compiler makes moves of sums from register to register in
+// the loop over k (8192^3 438 us with it, 419 so). It knows nothing of this instruction's time, so `settle`
+// comes between it and any other use of c.
+__device__ __forceinline__ void mfma(i32x4 &c, const i32x4 &b, const i32x4 &a) {
+    asm volatile("v_mfma_i32_16x16x64_i8 %0, %1, %2, %0" : "+a"(c) : "v"(b), "v"(a));
+}
+
+// What was written to the sums before this, by products or by moves, is there after it.
+template <int F>
+__device__ __forceinline__ void settle(i32x4 (&acc)[F][F][2][2]) {
+    auto tie = [&] {
+#pragma unroll
+        for (int i = 0; i < 4 * F * F; ++i) asm volatile("" : "+a"(acc[i / (4 * F)][i / 4 % F][i / 2 % 2][i % 2]));
+    };
+    tie();
+    asm volatile("s_nop 15\n\ts_nop 15");
+    tie();
+}
+
+// Tiles of 64 F x 64 F by 2 x 2 waves, each F x F times four blocks of 16 x 16.
 //
 // A step is 64 columns of k. LDS holds four steps of either operand, which copies bring there from
 // memory without registers; the registers hold the step that multiplies and the one after it. So in
@@ -178,14 +201,14 @@ __global__ __launch_bounds__(256, F == 2 ? 2 : 1) void tiles(Int8Args g, Split s
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t blocks = (g.k + 127) / 128, ld = blocks * 128;
     const int wm = wave % 2 * (32 * F), wn = wave / 2 * (32 * F);
-    const int q = lane >> 5, r32 = lane & 31;
+    const int q = lane >> 4, r16 = lane & 15;
 
     // A copy takes 16 rows of 64 bytes. Rows past the matrix are outside the buffers' bounds and read
-    // as zeros. 16 bytes c of row r lie at 64 r + 16 (c ^ (r / 4 % 4)), so that the 16 lanes that LDS
-    // serves at once lie in different banks.
-    const uint32_t from = (lane >> 2) * ld + (((lane & 3) ^ ((lane >> 4) & 3)) << 4);
-    const int low = r32 * 64 + (((2 * q) ^ (r32 >> 2 & 3)) << 4);
-    const int high = r32 * 64 + (((2 * q + 1) ^ (r32 >> 2 & 3)) << 4);
+    // as zeros. 16 bytes c of row r lie at 64 r + 16 (c ^ (-r / 4 % 4)), so that the 16 lanes that LDS
+    // serves at once (0-3, 12-15, 20-23 and 24-27, and their like) lie in different banks. A lane reads
+    // 16 bytes of rows r16 and, 16 rows further, r16 + 16.
+    const uint32_t from = (lane >> 2) * ld + (((lane & 3) ^ (-(lane >> 4) & 3)) << 4);
+    const int low = r16 * 64 + ((q ^ (-(r16 >> 2) & 3)) << 4), high = low + 16 * 64;
 
     // a work unit: a tile and a part of k
     uint32_t m0, n0, part, first, last;
@@ -237,7 +260,7 @@ __global__ __launch_bounds__(256, F == 2 ? 2 : 1) void tiles(Int8Args g, Split s
 
     struct Raw { i32x4 lo, hi; };
     struct Step { Raw a[F], b[F]; };
-    i32x16 acc[F][F];
+    i32x4 acc[F][F][2][2];   // of 16 columns and 16 rows of out each
     auto read_a = [&](Step &s, const uint8_t *at, int i) {
         const uint8_t *p = at + (wm + 32 * i) * 64;
         s.a[i] = Raw{*reinterpret_cast<const i32x4 *>(p + low), *reinterpret_cast<const i32x4 *>(p + high)};
@@ -256,8 +279,11 @@ __global__ __launch_bounds__(256, F == 2 ? 2 : 1) void tiles(Int8Args g, Split s
 #pragma unroll
         for (int t = 0; t < S; ++t) {
             const int i = t / F, j = t % F;
-            acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(now.b[j].lo, now.a[i].lo, acc[i][j], 0, 0, 0);
-            acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(now.b[j].hi, now.a[i].hi, acc[i][j], 0, 0, 0);
+#pragma unroll
+            for (int hb = 0; hb < 2; ++hb)
+#pragma unroll
+                for (int ha = 0; ha < 2; ++ha)
+                    mfma(acc[i][j][hb][ha], hb ? now.b[j].hi : now.b[j].lo, ha ? now.a[i].hi : now.a[i].lo);
 #pragma unroll
             for (int c = t * 3 * N / (2 * S); c < (t + 1) * 3 * N / (2 * S) && c < N; ++c) {
                 if (c < F) read_a(next, a, c);
@@ -271,7 +297,8 @@ __global__ __launch_bounds__(256, F == 2 ? 2 : 1) void tiles(Int8Args g, Split s
         }
         // This wave's copies but those of the last two steps have arrived, and its reads; then
         // everyone's.
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * N) : "memory");
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(wait(2 * N, 0));
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
@@ -288,18 +315,21 @@ __global__ __launch_bounds__(256, F == 2 ? 2 : 1) void tiles(Int8Args g, Split s
     take(unit);
     begin();
     for (;;) {
+        int zero = 0;
+        asm volatile("" : "+v"(zero));   // the compiler would keep zeros in registers from unit to unit
 #pragma unroll
-        for (int i = 0; i < F; ++i)
-#pragma unroll
-            for (int j = 0; j < F; ++j) acc[i][j] = i32x16{};
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * N) : "memory");   // steps 0 and 1
+        for (int i = 0; i < 4 * F * F; ++i) acc[i / (4 * F)][i / 4 % F][i / 2 % 2][i % 2] = i32x4{zero, zero, zero, zero};
+        settle(acc);
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(wait(2 * N, kAnyReads));   // steps 0 and 1
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
 #pragma unroll
         for (int i = 0; i < F; ++i) read_a(x, a0, i);
 #pragma unroll
         for (int j = 0; j < F; ++j) read_b(x, b0, j);
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(wait(63, 0));
         __builtin_amdgcn_s_barrier();   // a0 and b0 may be written
         asm volatile("" ::: "memory");
         // an odd number of blocks is followed by one of zeros: a loop with a way out in its middle
@@ -309,11 +339,12 @@ __global__ __launch_bounds__(256, F == 2 ? 2 : 1) void tiles(Int8Args g, Split s
             block(k + 1, a2, b2, a3, b3, a0, b0);
         }
 
+        settle(acc);
         // The results go out from the registers, while the next unit's first copies are under way.
         const uint32_t lane1 = lane_now(), thread = 64 * wave + lane1;
-        const uint32_t q1 = lane1 >> 5, r1 = lane1 & 31, hi1 = lane1 >> 4 & 1;
+        const uint32_t q1 = lane1 >> 4, r1 = lane1 & 15;
         const uint32_t m1 = m0 + wm, n1 = n0 + wn, part1 = part;
-        const bool edge = n0 + B > g.n, sums = sp.parts > 1, with_bias = g.bias != nullptr;
+        const bool edge = n0 + B > g.n, with_bias = OUT != kSums && g.bias != nullptr;
         unit += gridDim.x;
         const bool more = unit < sp.tiles_m * sp.tiles_n * sp.parts;
         const float *const rows_of = row_scales + turn * B + wm + r1, *const columns_of = scales + turn * B + wn;
@@ -322,9 +353,11 @@ __global__ __launch_bounds__(256, F == 2 ? 2 : 1) void tiles(Int8Args g, Split s
         const Buffer bias16(g.bias, with_bias && g.bias_bf16 ? g.n * 2 : 0);
         const uint32_t bias_word = bias32.word((n0 + thread) * 4);
         const uint32_t bias_half = bias16.half((n0 + thread) * 2);
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the last copies write zeros to LDS
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(wait(0, 0));   // the last copies write zeros to LDS
         if (thread < B) biases[thread] = __uint_as_float(bias_word | bias_half << 16);
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(wait(63, 0));
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         if (more) {
@@ -332,69 +365,57 @@ __global__ __launch_bounds__(256, F == 2 ? 2 : 1) void tiles(Int8Args g, Split s
             take(unit);
             begin();
         }
+        // a lane holds columns 4 q1 + 0..3 of row r1 of each 16 x 16
 #pragma unroll
         for (int j0 = 0; j0 < F; j0 += 2) {   // 64 columns of a row after one another: a line of bf16
 #pragma unroll
-            for (int ij = 0; ij < 2 * F; ++ij) {
-                const int i = ij / 2, j = j0 + ij % 2;
-                f32x4 v[4];
+            for (int ij = 0; ij < 4 * F; ++ij) {
+                const int i = ij / 4, ha = ij / 2 % 2, j = j0 + ij % 2;
+                const uint32_t to = m1 + 32 * i + 16 * ha + r1, n = n1 + 32 * j;
+                f32x4 v[2];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
+                for (int hb = 0; hb < 2; ++hb) {
 #pragma clang fp contract(off)
-                    // as `scaled` has it, in fewer registers; a lane holds row r1's columns 8 e + 4 q1 + 0..3 of each 32
-                    const i32x4 sum = {acc[i][j][4 * e], acc[i][j][4 * e + 1], acc[i][j][4 * e + 2],
-                                       acc[i][j][4 * e + 3]};
-                    if (sums) {
-                        v[e] = __builtin_bit_cast(f32x4, sum);
+                    // as `scaled` has it, in fewer registers
+                    const i32x4 sum = acc[i][j][hb][ha];
+                    if constexpr (OUT == kSums) {
+                        v[hb] = __builtin_bit_cast(f32x4, sum);
                         continue;
                     }
-                    const uint32_t c = 32 * j + 8 * e + 4 * q1;
+                    const uint32_t c = 32 * j + 16 * hb + 4 * q1;
                     const f32x4 sb = *reinterpret_cast<const f32x4 *>(columns_of + c);
 #pragma unroll
-                    for (int d = 0; d < 4; ++d) v[e][d] = static_cast<float>(sum[d]) * rows_of[32 * i] * sb[d];
-                    if (with_bias) v[e] += *reinterpret_cast<const f32x4 *>(biases + wn + c);
+                    for (int d = 0; d < 4; ++d) v[hb][d] = static_cast<float>(sum[d]) * rows_of[32 * i + 16 * ha] * sb[d];
+                    if (with_bias) v[hb] += *reinterpret_cast<const f32x4 *>(biases + wn + c);
                     if (g.relu) {
 #pragma unroll
-                        for (int d = 0; d < 4; ++d) v[e][d] = v[e][d] < 0.0f ? 0.0f : v[e][d];   // NaN stays
+                        for (int d = 0; d < 4; ++d) v[hb][d] = v[hb][d] < 0.0f ? 0.0f : v[hb][d];   // NaN stays
                     }
                 }
-                // Lanes exchange so that a store writes 64 neighbouring bytes of each of 16 rows.
-                if (OUT == PS_F32 || sums) {
+                if (to >= g.m) continue;
+                if constexpr (OUT == kSums) {
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        u32x4 w[2] = {__builtin_bit_cast(u32x4, v[2 * h]), __builtin_bit_cast(u32x4, v[2 * h + 1])};
-                        swap_rows(w[0], w[1]);
-                        const uint32_t n = n1 + 32 * j + 16 * h + 8 * hi1 + 4 * q1;
+                    for (int hb = 0; hb < 2; ++hb)
+                        if (n + 16 * hb + 4 * q1 < g.n) keep(g, __builtin_bit_cast(i32x4, v[hb]), part1, to, n + 16 * hb + 4 * q1);
+                } else if constexpr (OUT == PS_F32) {
 #pragma unroll
-                        for (int t = 0; t < 2; ++t) {
-                            const uint32_t to = m1 + 32 * i + 16 * t + (lane1 & 15);
-                            if (to < g.m && sums) {
-                                if (n < g.n) keep(g, __builtin_bit_cast(i32x4, w[t]), part1, to, n);
-                            } else if (to < g.m) {
-                                put<float>(g, w[t], to, n, edge);
-                            }
-                        }
-                    }
+                    for (int hb = 0; hb < 2; ++hb)
+                        put<float>(g, __builtin_bit_cast(u32x4, v[hb]), to, n + 16 * hb + 4 * q1, edge);
                 } else {
-                    // 16 bytes of bf16 first: the halves of the wave exchange fours
-                    u32x4 w[2];
+                    // Eights of bf16 first: of the two rows of lanes that hold neighbouring fours, one takes
+                    // both of the first sixteen columns, the other both of the second.
+                    u32x4 w;
 #pragma unroll
-                    for (int h = 0; h < 2; ++h)
-#pragma unroll
-                        for (int c = 0; c < 2; ++c) {
-                            const auto p = __builtin_amdgcn_permlane32_swap(
-                                bf16x2_rne(v[2 * h][2 * c], v[2 * h][2 * c + 1]),
-                                bf16x2_rne(v[2 * h + 1][2 * c], v[2 * h + 1][2 * c + 1]), false, false);
-                            w[h][c] = p[0];
-                            w[h][2 + c] = p[1];
-                        }
-                    swap_rows(w[0], w[1]);
-#pragma unroll
-                    for (int t = 0; t < 2; ++t) {
-                        const uint32_t to = m1 + 32 * i + 16 * t + (lane1 & 15);
-                        if (to < g.m) put<uint16_t>(g, w[t], to, n1 + 32 * j + 16 * hi1 + 8 * q1, edge);
+                    for (int c = 0; c < 2; ++c) {
+                        const auto p = __builtin_amdgcn_permlane16_swap(bf16x2_rne(v[0][2 * c], v[0][2 * c + 1]),
+                                                                        bf16x2_rne(v[1][2 * c], v[1][2 * c + 1]), false,
+                                                                        false);
+                        w[c] = p[0];
+                        w[2 + c] = p[1];
                     }
+                    put<uint16_t>(g, w, to, n + 16 * (q1 & 1) + 4 * (q1 & 2), edge);
                 }
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
         if (!more) break;
@@ -694,7 +715,9 @@ hipError_t launch(const Int8Args &g, hipStream_t s) {
         const uint64_t units = static_cast<uint64_t>(sp.tiles_m) * sp.tiles_n * sp.parts;
         if (units > 0xffffffffull / 2) return hipErrorInvalidConfiguration;
         const uint32_t at_once = c.large ? kCus : 2 * kCus, grid = std::min(static_cast<uint32_t>(units), at_once);
-        if (c.large) tiles<4, OUT><<<grid, 256, 0, s>>>(g, sp);
+        if (sp.parts > 1 && c.large) tiles<4, kSums><<<grid, 256, 0, s>>>(g, sp);
+        else if (sp.parts > 1) tiles<2, kSums><<<grid, 256, 0, s>>>(g, sp);
+        else if (c.large) tiles<4, OUT><<<grid, 256, 0, s>>>(g, sp);
         else tiles<2, OUT><<<grid, 256, 0, s>>>(g, sp);
         e = hipGetLastError();
     }

@@ -310,4 +310,4 @@ def test_waits_for_copies(tmp_path):
                 del queue[:max(0, len(queue) - op)]
         assert copies == 8 * n, name
         checked += 1
-    assert checked == 4
+    assert checked == 6
