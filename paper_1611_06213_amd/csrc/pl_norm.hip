@@ -25,7 +25,7 @@
 namespace gadei::learner {
 namespace {
 
-constexpr int kJoinCols = 32, kJoinRows = 8;   // of a workgroup of `join`
+constexpr int kJoinCols = 32;   // of a workgroup of `join`
 constexpr int kSums = 6;
 constexpr uint64_t kRowCols = 8 * 1024;        // of a row that 1024 threads hold, eight columns each
 
@@ -49,7 +49,7 @@ __device__ __forceinline__ uint32_t now(uint32_t col) {
     return col;
 }
 
-// Eight columns as loaded: zeros past `count`.
+// Eight columns as loaded: zeros past `count`. EIGHTS: all of them or none.
 template <int DT, bool EIGHTS>
 __device__ __forceinline__ Bits8<DT> bits8(const void *p, uint32_t at, int count) {
     if (count == 8) return load8<DT>(p, at);
@@ -94,11 +94,32 @@ __device__ __forceinline__ void put_row8(void *p, uint32_t at, const float (&x)[
     else put8<DT>(p, at, x, count);
 }
 
-// How many of a thread's eight columns there are. EIGHTS: all or none, as rows are multiples of eight.
-template <bool EIGHTS>
 __device__ __forceinline__ int count_at(uint64_t cols, uint64_t col) {
-    if (EIGHTS) return col < cols ? 8 : 0;
     return cols >= col + 8 ? 8 : cols > col ? static_cast<int>(cols - col) : 0;
+}
+
+// A thread's eight columns of a row of at least as many, all or none of them. The row's last thread goes back to
+// where there are eight: its first `twice` are its neighbour's too. It leaves them out of sums over the row;
+// their results are the same bits from both. ODD: the row's columns are not eights.
+struct Place {
+    uint32_t col;
+    int count, twice;
+    template <bool ODD>
+    __device__ __forceinline__ static Place of(uint32_t thread, uint64_t cols) {
+        const uint32_t col = 8 * thread, n = static_cast<uint32_t>(cols);
+        const bool in = col < n;
+        if constexpr (!ODD) return Place{col, in ? 8 : 0, 0};
+        const uint32_t from = in ? min(col, n - 8) : col;
+        return Place{from, in ? 8 : 0, static_cast<int>(col - from)};
+    }
+};
+
+template <bool ODD>
+__device__ __forceinline__ void leave_out(float (&x)[8], int twice) {
+    if constexpr (ODD) {
+#pragma unroll
+        for (int e = 0; e < 7; ++e) x[e] = e < twice ? 0.0f : x[e];
+    }
 }
 
 // Sums over the sixteen lanes of a row of lanes, in all of them.
@@ -186,15 +207,16 @@ __device__ __forceinline__ void stream8(float (&h)[8], const NormArgs &a, const 
 
 // A worker, a wave or a workgroup, takes `rows_each` rows one after another, the next one's loads under
 // way; the vectors stay in registers.
-template <int X, int Y, int N, bool BLOCK, bool EIGHTS>
+template <int X, int Y, int N, bool BLOCK, bool ODD>
 __global__ __launch_bounds__(1024) void norm(NormArgs a, uint32_t rows_each) {
+    constexpr bool EIGHTS = true;
     __shared__ float lds[2 * 16 * kSums];
     int turn = 0;
     const uint64_t first = (static_cast<uint64_t>(block_index()) * blockDim.y + wave_y()) * rows_each;
     if (first >= a.rows) return;   // a whole wave, of those that no barrier waits for
     const uint32_t last = static_cast<uint32_t>(min(static_cast<uint64_t>(a.rows), first + rows_each));
     uint32_t col[N];
-    int count[N];
+    int count[N], twice[N];
     float branch[N][8], before[N][8];
     Bits8<X> next_x[N];
     Bits8<Y> next_y[N];
@@ -207,8 +229,10 @@ __global__ __launch_bounds__(1024) void norm(NormArgs a, uint32_t rows_each) {
     };
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        col[i] = 8 * (threadIdx.x + i * blockDim.x);
-        count[i] = count_at<EIGHTS>(a.cols, col[i]);
+        const Place place = Place::of<ODD>(threadIdx.x + i * blockDim.x, a.cols);
+        col[i] = place.col;
+        count[i] = place.count;
+        twice[i] = place.twice;
     }
     load(static_cast<uint32_t>(first));
 #pragma unroll
@@ -238,6 +262,7 @@ __global__ __launch_bounds__(1024) void norm(NormArgs a, uint32_t rows_each) {
                 for (int i = 0; i < N; ++i) {
                     float v[8];
                     widen8<Y>(v, y[i]);
+                    leave_out<ODD>(v, twice[i]);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) s[0] += v[e] * v[e];
                     anew(y[i]);
@@ -261,7 +286,7 @@ __global__ __launch_bounds__(1024) void norm(NormArgs a, uint32_t rows_each) {
 #pragma unroll
         for (int i = 0; i < N; ++i)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) s[0] += h[i][e] * h[i][e];
+            for (int e = 0; e < 8; ++e) s[0] += ODD && e < twice[i] ? 0.0f : h[i][e] * h[i][e];
         sum_row(s, lds, &turn);
         const float rh = inverse_root(s[0], a.cols, a.eps);
 #pragma unroll
@@ -273,7 +298,7 @@ __global__ __launch_bounds__(1024) void norm(NormArgs a, uint32_t rows_each) {
     }
 }
 
-// Longer rows: a workgroup a row, which it reads again for each sum.
+// Longer rows, and those of fewer than eight columns: a workgroup a row, which it reads again for each sum.
 template <int X, int Y, bool BLOCK>
 __global__ __launch_bounds__(1024) void norm_long(NormArgs a) {
     constexpr bool EIGHTS = false;
@@ -286,7 +311,7 @@ __global__ __launch_bounds__(1024) void norm_long(NormArgs a) {
     if (BLOCK && a.after != nullptr) {
         for (uint32_t col = first; col < a.cols; col += step) {
             float y[8];
-            row8<Y>(y, row_of<Y>(a.y, row, a.y_ld), col, count_at<EIGHTS>(a.cols, col));
+            row8<Y>(y, row_of<Y>(a.y, row, a.y_ld), col, count_at(a.cols, col));
 #pragma unroll
             for (int e = 0; e < 8; ++e) s[0] += y[e] * y[e];
         }
@@ -305,7 +330,7 @@ __global__ __launch_bounds__(1024) void norm_long(NormArgs a) {
         }
     };
     for (uint32_t col = first; col < a.cols; col += step) {
-        const int count = count_at<EIGHTS>(a.cols, col);
+        const int count = count_at(a.cols, col);
         float h[8];
         stream(h, col, count);
         if (BLOCK) put8<X>(row_of<X>(a.out, row, a.out_ld), col, h, count);
@@ -316,7 +341,7 @@ __global__ __launch_bounds__(1024) void norm_long(NormArgs a) {
     sum_row(s, lds, &turn);
     const float rh = inverse_root(s[0], a.cols, a.eps);
     for (uint32_t col = first; col < a.cols; col += step) {
-        const int count = count_at<EIGHTS>(a.cols, col);
+        const int count = count_at(a.cols, col);
         float h[8], w[8];
         stream(h, col, count);
         vector8<EIGHTS>(w, a.before, a.weight_bf16, col, count);
@@ -361,27 +386,27 @@ struct Columns {
 };
 
 // h h, u h; y y, and of p = gate after y: p dh, p u, p h
-template <int X, int Y, bool BLOCK, bool EIGHTS>
-__device__ __forceinline__ void add_sums(float (&s)[kSums], const RowBits<X, Y, BLOCK, EIGHTS> &v, const Columns &c) {
-    float h[8], dz[8];
+template <bool ODD, int X, int Y, bool BLOCK, bool EIGHTS>
+__device__ __forceinline__ void add_sums(float (&s)[kSums], const RowBits<X, Y, BLOCK, EIGHTS> &v, const Columns &c,
+                                         int twice) {
+    float h[8], dz[8], y[8], dh[8];
     widen8<X>(h, v.h);
     widen8<Y>(dz, v.dz);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        dz[e] *= c.before[e / 4 * c.apart][e % 4];
-        s[0] += h[e] * h[e];
-        s[1] += dz[e] * h[e];
-    }
     if constexpr (BLOCK) {
-        float y[8], dh[8];
         widen8<Y>(y, v.y);
         widen8<X>(dh, v.dh);
+    }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
+    for (int e = 0; e < 8; ++e) {
+        if (ODD && e < twice) continue;
+        const float u = dz[e] * c.before[e / 4 * c.apart][e % 4];
+        s[0] += h[e] * h[e];
+        s[1] += u * h[e];
+        if constexpr (BLOCK) {
             const float p = c.branch[e] * y[e];
             s[2] += y[e] * y[e];
             s[3] += p * dh[e];
-            s[4] += p * dz[e];
+            s[4] += p * u;
             s[5] += p * h[e];
         }
     }
@@ -428,16 +453,24 @@ __device__ __forceinline__ void take_row(const NormGradArgs &a, const RowBits<X,
     }
 }
 
+// twice: of them, what the neighbour adds to what is there.
 template <bool EIGHTS>
-__device__ __forceinline__ void put_result(const NormGradArgs &a, void *p, uint32_t at, float (&x)[8], int count) {
+__device__ __forceinline__ void put_result(const NormGradArgs &a, void *p, uint32_t at, float (&x)[8], int count,
+                                           int twice) {
     if (a.accumulate) {
         float old[8];
         vector8<EIGHTS>(old, p, a.out_bf16, at, count);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] += old[e];
+        for (int e = 0; e < 8; ++e) {
+            if (e < twice || e >= count) continue;
+            if (a.out_bf16) store1<PS_BF16>(p, at + e, old[e] + x[e]);
+            else store1<PS_F32>(p, at + e, old[e] + x[e]);
+        }
+    } else if (a.out_bf16) {
+        put8<PS_BF16>(p, at, x, count);
+    } else {
+        put8<PS_F32>(p, at, x, count);
     }
-    if (a.out_bf16) put8<PS_BF16>(p, at, x, count);
-    else put8<PS_F32>(p, at, x, count);
 }
 
 // The first of a gate's rows among the worker's (without a gate: of all rows); when they end.
@@ -453,7 +486,7 @@ __device__ __forceinline__ uint32_t begin_gate(const NormGradArgs &a, uint32_t r
 // The last of them has been taken, before `end`.
 template <bool EIGHTS>
 __device__ __forceinline__ void end_gate(const NormGradArgs &a, const Split &sp, uint32_t worker, uint32_t first,
-                                         uint32_t last, uint32_t end, uint32_t col, int count, Columns &c) {
+                                         uint32_t last, uint32_t end, uint32_t col, int count, int twice, Columns &c) {
     float w[8];
     if (a.dafter != nullptr) {
         gate8<EIGHTS>(w, a, end - 1, col, count);
@@ -467,7 +500,7 @@ __device__ __forceinline__ void end_gate(const NormGradArgs &a, const Split &sp,
     const uint64_t begins = static_cast<uint64_t>(gate) * a.per_gate, ends = begins + a.per_gate;
     if (begins >= first && ends <= last) {
         put_result<EIGHTS>(a, a.out_bf16 ? row_of<PS_BF16>(a.dgate, gate, a.dgate_ld) : row_of<PS_F32>(a.dgate, gate, a.dgate_ld),
-                   col, c.d_branch, count);
+                   col, c.d_branch, count, twice);
     } else {
         const uint64_t slot = 2 * static_cast<uint64_t>(worker) + (begins >= first ? 1 : 0);
         store8<PS_F32>(sp.gate + slot * sp.pitch, col, c.d_branch);
@@ -498,16 +531,18 @@ __device__ __forceinline__ void end_worker(const NormGradArgs &a, const Split &s
 }
 
 // A worker is a wave or a workgroup; it takes its rows one after another, the next one's loads under way.
-template <int X, int Y, bool BLOCK, bool EIGHTS>
+template <int X, int Y, bool BLOCK, bool ODD>
 __global__ __launch_bounds__(1024, 4) void norm_grad(NormGradArgs a, Split sp) {
+    constexpr bool EIGHTS = true;
     __shared__ float lds[2 * 16 * kSums];
     extern __shared__ f32x4 own[];   // four a thread
     int turn = 0;
     const uint32_t worker = block_index() * blockDim.y + wave_y();
     if (worker >= sp.workers) return;   // a whole wave, of those that no barrier waits for
     const uint32_t first = worker * sp.rows, last = min(a.rows - first, sp.rows) + first;
-    const uint32_t col = 8 * threadIdx.x;
-    const int count = count_at<EIGHTS>(a.cols, col);
+    const Place place = Place::of<ODD>(threadIdx.x, a.cols);
+    const uint32_t col = place.col;
+    const int count = place.count, twice = place.twice;
     RowBits<X, Y, BLOCK, EIGHTS> next;
     next.load(a, first, col, count);
     Columns c;
@@ -521,7 +556,7 @@ __global__ __launch_bounds__(1024, 4) void norm_grad(NormGradArgs a, Split sp) {
             RowBits<X, Y, BLOCK, EIGHTS> v = next;
             if (row + 1 < last) next.load(a, row + 1, now(col), count);
             float s[kSums] = {};
-            add_sums(s, v, c);
+            add_sums<ODD>(s, v, c, twice);
             sum_row(s, lds, &turn);
             anew(v.h);
             anew(v.dh);
@@ -529,12 +564,12 @@ __global__ __launch_bounds__(1024, 4) void norm_grad(NormGradArgs a, Split sp) {
             if constexpr (BLOCK) anew(v.y);
             take_row(a, v, row_factors(a, s), row, now(col), count, c);
         }
-        if constexpr (BLOCK) end_gate<EIGHTS>(a, sp, worker, first, last, end, now(col), count, c);
+        if constexpr (BLOCK) end_gate<EIGHTS>(a, sp, worker, first, last, end, now(col), count, twice, c);
     }
     end_worker(a, sp, worker, col, count, c);
 }
 
-// Longer rows: first their sums, a workgroup a row, ...
+// Longer rows, and those of fewer than eight columns: first their sums, a workgroup a row, ...
 template <int X, int Y, bool BLOCK>
 __global__ __launch_bounds__(1024) void row_sums(NormGradArgs a, Split sp) {
     constexpr bool EIGHTS = false;
@@ -544,7 +579,7 @@ __global__ __launch_bounds__(1024) void row_sums(NormGradArgs a, Split sp) {
     if (row >= a.rows) return;
     float s[kSums] = {};
     for (uint32_t col = 8 * threadIdx.x; col < a.cols; col += 8 * blockDim.x) {
-        const int count = count_at<EIGHTS>(a.cols, col);
+        const int count = count_at(a.cols, col);
         RowBits<X, Y, BLOCK, EIGHTS> v;
         v.load(a, row, col, count);
         Columns c;
@@ -554,7 +589,7 @@ __global__ __launch_bounds__(1024) void row_sums(NormGradArgs a, Split sp) {
         c.before = before;
         c.apart = 1;
         if constexpr (BLOCK) branch_scale<EIGHTS>(c.branch, a, row, col, count);
-        add_sums(s, v, c);
+        add_sums<false>(s, v, c, 0);
     }
     sum_row(s, lds, &turn);
     if (threadIdx.x == 0) sp.rows_of[row] = row_factors(a, s);
@@ -570,7 +605,7 @@ __global__ __launch_bounds__(256) void norm_grad_long(NormGradArgs a, Split sp, 
     const uint32_t worker = static_cast<uint32_t>(worker64);
     const uint32_t first = worker * sp.rows, last = min(a.rows - first, sp.rows) + first;
     const uint32_t col = 8 * (threadIdx.x + 256 * (block_index() % strips));
-    const int count = count_at<EIGHTS>(a.cols, col);
+    const int count = count_at(a.cols, col);
     Columns c;
     c.apart = 256;
     c.before = own + threadIdx.x;
@@ -583,16 +618,17 @@ __global__ __launch_bounds__(256) void norm_grad_long(NormGradArgs a, Split sp, 
             v.load(a, row, now(col), count);
             take_row(a, v, sp.rows_of[row], row, now(col), count, c);
         }
-        if constexpr (BLOCK) end_gate<EIGHTS>(a, sp, worker, first, last, end, now(col), count, c);
+        if constexpr (BLOCK) end_gate<EIGHTS>(a, sp, worker, first, last, end, now(col), count, 0, c);
     }
     end_worker(a, sp, worker, col, count, c);
 }
 
 // The workers' sums, in order: y = 0 and 1 dbefore and dafter, from 2 on the gates whose rows are more
 // than one worker's: of a few gates gate y - 2, else the one that goes from worker y - 2 into the next.
-__global__ __launch_bounds__(kJoinCols * kJoinRows) void join(NormGradArgs a, Split sp, bool few_gates) {
-    __shared__ float lds[kJoinRows][kJoinCols];
-    const int x = threadIdx.x % kJoinCols, y = threadIdx.x / kJoinCols;
+template <int ROWS>
+__global__ __launch_bounds__(kJoinCols * ROWS) void join(NormGradArgs a, Split sp, bool few_gates) {
+    __shared__ float lds[ROWS][kJoinCols];
+    const int x = threadIdx.x, y = threadIdx.y;
     const uint64_t col = static_cast<uint64_t>(blockIdx.x) * kJoinCols + x;
     void *out = blockIdx.y == 0 ? a.dbefore : blockIdx.y == 1 ? a.dafter : a.dgate;
     if (out == nullptr) return;
@@ -618,14 +654,14 @@ __global__ __launch_bounds__(kJoinCols * kJoinRows) void join(NormGradArgs a, Sp
     }
     if (col < a.cols) {
 #pragma unroll 8
-        for (uint32_t w = from + y; w < to; w += kJoinRows) v += p[w * pitch + col];
+        for (uint32_t w = from + y; w < to; w += ROWS) v += p[w * pitch + col];
     }
     lds[y][x] = v;
     __syncthreads();
     if (y != 0 || col >= a.cols) return;
     v = 0.0f;
 #pragma unroll
-    for (int i = 0; i < kJoinRows; ++i) v += lds[i][x];
+    for (int i = 0; i < ROWS; ++i) v += lds[i][x];
     if (a.accumulate) v += a.out_bf16 ? load1<PS_BF16>(out, at) : load1<PS_F32>(out, at);
     if (a.out_bf16) store1<PS_BF16>(out, at, v);
     else store1<PS_F32>(out, at, v);
@@ -650,7 +686,7 @@ hipError_t launch(const NormArgs &a, hipStream_t s) {
     const uint32_t threads = threads_of(a.cols);
     const uint32_t together = threads == 64 ? 4 : 1;   // workers of a workgroup
     dim3 grid;
-    if (a.cols > 2 * kRowCols) {
+    if (a.cols < 8 || a.cols > 2 * kRowCols) {
         if (!grid_of(a.rows, threads, &grid)) return hipErrorInvalidConfiguration;
         norm_long<X, Y, BLOCK><<<grid, threads, 0, s>>>(a);
         return hipGetLastError();
@@ -663,10 +699,10 @@ hipError_t launch(const NormArgs &a, hipStream_t s) {
     if (!grid_of((a.rows + each - 1ull) / each / together + 1, threads * together, &grid))
         return hipErrorInvalidConfiguration;
     const dim3 block(threads, together);
-    const bool eights = a.cols % 8 == 0;
-    if (a.cols > kRowCols && eights) norm<X, Y, 2, BLOCK, true><<<grid, block, 0, s>>>(a, each);
+    const bool odd = a.cols % 8 != 0;
+    if (a.cols > kRowCols && odd) norm<X, Y, 2, BLOCK, true><<<grid, block, 0, s>>>(a, each);
     else if (a.cols > kRowCols) norm<X, Y, 2, BLOCK, false><<<grid, block, 0, s>>>(a, each);
-    else if (eights) norm<X, Y, 1, BLOCK, true><<<grid, block, 0, s>>>(a, each);
+    else if (odd) norm<X, Y, 1, BLOCK, true><<<grid, block, 0, s>>>(a, each);
     else norm<X, Y, 1, BLOCK, false><<<grid, block, 0, s>>>(a, each);
     return hipGetLastError();
 }
@@ -678,6 +714,9 @@ hipError_t launch(const NormArgs &a, int y_dtype, hipStream_t s) {
     return y_dtype == PS_F32 ? launch<X, PS_F32, true>(a, s) : launch<X, PS_BF16, true>(a, s);
 }
 
+// Backward: whether workers hold whole rows.
+bool in_registers(uint64_t cols) { return cols >= 8 && cols <= kRowCols; }
+
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
 Split split(uint64_t rows, uint64_t cols) {
@@ -686,7 +725,8 @@ Split split(uint64_t rows, uint64_t cols) {
     if (rows == 0) return sp;
     // In us with 256, 512, 1024 and 2048 workers, their sums' joining included: 16384 x 4096 bf16 166, 175,
     // 187 and 198; 32768 x 1024 165, 122, 95 and 110; 100000 x 512 392, 209, 137 and 148
-    const uint64_t most = cols > kRowCols ? 64 : std::clamp<uint64_t>(2048 * 64 / threads_of(cols), 256, 1024);
+    const uint64_t most = in_registers(cols) ? std::clamp<uint64_t>(2048 * 64 / threads_of(cols), 256, 1024)
+                                             : std::clamp<uint64_t>(1024 * 2048 / cols, 64, 1024);
     sp.rows = static_cast<uint32_t>((rows + most - 1) / most);
     sp.workers = static_cast<uint32_t>((rows + sp.rows - 1) / sp.rows);
     return sp;
@@ -709,16 +749,16 @@ hipError_t launch(const NormGradArgs &a, hipStream_t s) {
             if (!grid_of((a.gates * a.cols + 255) / 256, 256, &grid)) return hipErrorInvalidConfiguration;
             no_rows<<<grid, 256, 0, s>>>(a);
         }
-    } else if (a.cols <= kRowCols) {
+    } else if (in_registers(a.cols)) {
         const uint32_t together = threads == 64 ? 4 : 1;
         grid = dim3((sp.workers + together - 1) / together);
         const dim3 block(threads, together);
         const uint32_t own = 4 * sizeof(f32x4) * threads * together;
-        if (a.cols % 8 == 0) norm_grad<X, Y, BLOCK, true><<<grid, block, own, s>>>(a, sp);
+        if (a.cols % 8 != 0) norm_grad<X, Y, BLOCK, true><<<grid, block, own, s>>>(a, sp);
         else norm_grad<X, Y, BLOCK, false><<<grid, block, own, s>>>(a, sp);
     } else {
-        if (!grid_of(a.rows, 1024, &grid)) return hipErrorInvalidConfiguration;
-        row_sums<X, Y, BLOCK><<<grid, 1024, 0, s>>>(a, sp);
+        if (!grid_of(a.rows, threads, &grid)) return hipErrorInvalidConfiguration;
+        row_sums<X, Y, BLOCK><<<grid, threads, 0, s>>>(a, sp);
         const uint64_t strips = (a.cols + 2047) / 2048;
         if (!grid_of(strips * sp.workers, 256, &grid)) return hipErrorInvalidConfiguration;
         norm_grad_long<X, Y, BLOCK><<<grid, 256, 0, s>>>(a, sp, static_cast<uint32_t>(strips));
@@ -729,7 +769,8 @@ hipError_t launch(const NormGradArgs &a, hipStream_t s) {
     const bool few_gates = a.gates < sp.workers;
     grid = dim3(static_cast<uint32_t>((a.cols + kJoinCols - 1) / kJoinCols),
                 gates ? 2 + (few_gates ? a.gates : sp.workers - 1) : 2);
-    join<<<grid, kJoinCols * kJoinRows, 0, s>>>(a, sp, few_gates);
+    if (sp.workers > 64) join<32><<<grid, dim3(kJoinCols, 32), 0, s>>>(a, sp, few_gates);
+    else join<4><<<grid, dim3(kJoinCols, 4), 0, s>>>(a, sp, few_gates);
     return hipGetLastError();
 }
 
@@ -749,7 +790,7 @@ hipError_t launch_norm(const NormArgs &a, int x_dtype, int y_dtype, hipStream_t 
 size_t norm_grad_workspace(int64_t rows, int64_t cols) {
     const Split sp = split(rows, cols);
     return 4 * align256(sizeof(float) * sp.workers * sp.pitch) +
-           (static_cast<uint64_t>(cols) > kRowCols ? sizeof(f32x4) * static_cast<size_t>(rows) : 0);
+           (!in_registers(static_cast<uint64_t>(cols)) ? sizeof(f32x4) * static_cast<size_t>(rows) : 0);
 }
 
 hipError_t launch_norm_grad(const NormGradArgs &a, int x_dtype, int y_dtype, hipStream_t s) {
