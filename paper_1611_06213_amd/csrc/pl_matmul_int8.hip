@@ -583,7 +583,9 @@ struct Choice {
 };
 
 // What a product takes, in us, by rounds of tiles: a compute unit has one large tile at a time, or two
-// small ones, which cover each other's first loads and last stores.
+// small ones, which cover each other's first loads and last stores. Of 8000 products of random sizes, from 33 x
+// 64 x 64 to 1.1 TFLOP, the choice takes 0.7% longer than the best of ten to sixteen tried (9% or more in one of
+// twenty).
 double tiles_take(uint64_t m, uint64_t n, uint64_t blocks, bool large, uint64_t parts) {
     const uint64_t b = large ? 256 : 128, at_once = large ? kCus : 2 * kCus;
     const uint64_t units = (m + b - 1) / b * ((n + b - 1) / b) * parts;
