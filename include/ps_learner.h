@@ -185,7 +185,8 @@ int pl_norm_grad(const void *h, int x_dtype, int64_t h_ld, const void *y, int y_
 size_t pl_norm_grad_workspace(int64_t rows, int64_t cols);
 
 /* ---- A matrix in 8-bit integers with a scale for each row (a token's activations, or a
- * channel's weights): element (r, c) = values[r * pl_int8_ld(cols) + c] * scales[r]. The scale is
+ * channel's weights): element (r, c) = values[r * pl_int8_ld(cols) + c] * scales[r], values from -127
+ * to 127. The scale is
  * most / 127, most the largest magnitude of the row or 2^-100 if that is larger; elements times
  * 127 (1 / most), each step in fp32, are rounded to nearest even. A row with a NaN or an infinity has the scale NaN. The
  * values' rows are padded with zeros to multiples of 128. Both arrays lie on 16-byte boundaries. */

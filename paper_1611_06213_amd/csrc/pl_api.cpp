@@ -8,7 +8,6 @@
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
-#include <new>
 #include <vector>
 
 #include "pl_kernels.h"
@@ -847,7 +846,7 @@ int pl_adamw_plan(const pl_adamw_tensor *tensors, int64_t n, int weight_dtype, i
             if (count != 0) grads.push_back(s);
         }
         if (int rc = push ? adamw_apart(grads, weights) : adamw_apart(weights, grads)) return rc;
-    } catch (const std::bad_alloc &) {
+    } catch (...) {
         return fail(PS_ENOMEM, "no memory for the check of %lld tensors", static_cast<long long>(n));
     }
     const int64_t most = adamw_part();

@@ -696,8 +696,8 @@ hipError_t launch(const NormArgs &a, hipStream_t s) {
     // of a wave, 200000 x 512, 139, 168 and 170.
     const uint64_t most = threads == 64 ? ~uint64_t(0) >> 1 : 4096;
     const uint32_t each = static_cast<uint32_t>((a.rows + most - 1) / most);
-    if (!grid_of((a.rows + each - 1ull) / each / together + 1, threads * together, &grid))
-        return hipErrorInvalidConfiguration;
+    const uint64_t workers = (a.rows + each - 1ull) / each;
+    if (!grid_of((workers + together - 1) / together, threads * together, &grid)) return hipErrorInvalidConfiguration;
     const dim3 block(threads, together);
     const bool odd = a.cols % 8 != 0;
     if (a.cols > kRowCols && odd) norm<X, Y, 2, BLOCK, true><<<grid, block, 0, s>>>(a, each);

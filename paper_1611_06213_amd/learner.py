@@ -560,9 +560,9 @@ def rms_norm(x, weight=None, eps: float = 1e-6, dtype=None, out=None):
     src, code, ld = _matrix("x", x)
     rows, cols = x.shape
     w, w_code = _vector("weight", weight, cols)
-    if out is not None and dtype is not None and out.dtype != dtype:
-        raise TypeError(f"out is {out.dtype}, not {dtype}")
-    out = _like("out", out, rows, cols, x.dtype if dtype is None and out is None else dtype or out.dtype, x.device)
+    if out is not None:
+        _on_device("out", out)
+    out = _like("out", out, rows, cols, dtype or (x if out is None else out).dtype, x.device)
     dst, dst_code, dst_ld = _matrix("out", out)
     _check(load_library().pl_norm(src, code, ld, None, dst_code, 0, rows, cols, None, PS_F32, 0, 0, None, w,
                                   _one_type("weights", w_code), 1.0, eps, None, 0, _there(dst), dst_ld,
@@ -810,12 +810,13 @@ class AdamW:
     (`m_scales`, `v_scales`) hold tensor after tensor, each from a multiple of 128 elements on.
 
     Steps are made one after another, on torch's current stream. A step can be captured in a graph; replayed it goes
-    on counting. Autograd does not see that weights change."""
+    on counting. The memory that the tensors have when the optimizer is made is what it reads and writes. Autograd
+    does not see that weights change."""
 
     def __init__(self, weights: Sequence[torch.Tensor], grads: Sequence[torch.Tensor],
                  decay: Union[float, Sequence[float]] = 0.01, betas: Tuple[float, float] = (0.9, 0.999),
                  eps: float = 1e-8, bits: int = 32, push: bool = False, seed: int = 0):
-        self.weights, self.grads = list(weights), list(grads)
+        self.weights, self.grads = tuple(weights), tuple(grads)
         count = len(self.weights)
         if count == 0 or len(self.grads) != count:
             raise ValueError(f"{count} weights and {len(self.grads)} gradients")
@@ -826,14 +827,18 @@ class AdamW:
         decays = [float(decay)] * count if isinstance(decay, (int, float)) else [float(d) for d in decay]
         if len(decays) != count:
             raise ValueError(f"{len(decays)} decays for {count} weights")
+        here = torch.cuda.current_device() if torch.cuda.is_available() else None
         for name, ts in (("weights", self.weights), ("grads", self.grads)):
             for i, t in enumerate(ts):
-                _on_device(f"{name}[{i}]", t)
+                if not isinstance(t, torch.Tensor) or not t.is_cuda or t.device.index != here:
+                    _on_device(f"{name}[{i}]", t)   # raises
                 if t.dtype != ts[0].dtype:
                     raise TypeError(f"{name}: {ts[0].dtype} and {t.dtype}")
                 if not t.is_contiguous() or t.numel() != self.weights[i].numel():
                     raise ValueError(f"{name}[{i}]: {self.weights[i].numel()} contiguous elements expected, not "
                                      f"{tuple(t.shape)}, {t.stride()} elements apart")
+        # the plan names their memory, which so lives as long as the optimizer, whatever becomes of the tensors
+        self._memory = [t.untyped_storage() for t in (*self.weights, *self.grads)]
         self.bits, self.push, self.seed = bits, bool(push), seed
         self.betas, self.eps = (float(betas[0]), float(betas[1])), float(eps)
         self._codes = _code(self.weights[0].dtype), _code(self.grads[0].dtype)

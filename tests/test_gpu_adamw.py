@@ -123,6 +123,41 @@ def test_large_parts(torch, learner):  # noqa: F811
                 assert bool(((v[i] > 0) == (b[:n] > 0)).all())
 
 
+def test_offsets_past_32_bits(torch, learner):  # noqa: F811
+    """More than 2^32 elements: a tensor at the end as in a list of its own but for its random numbers, which go by
+    its place."""
+    if learner._native is False:
+        pytest.skip("the same library calls")
+    big, n = (1 << 32) + 5, 2900
+    flat_w = torch.zeros(big + n, device="cuda", dtype=torch.bfloat16)
+    flat_g = torch.zeros(big + n, device="cuda", dtype=torch.bfloat16)
+    flat_w[big:] = randn(torch, gen(torch, 1), n)
+    flat_g[big:] = randn(torch, gen(torch, 2), n)
+    w, g = flat_w[big:].clone(), flat_g[big:].clone()
+    opt = learner.AdamW([flat_w[:big], flat_w[big:]], [flat_g[:big], flat_g[big:]], 0.01, bits=8, push=True, seed=3)
+    one = learner.AdamW([w], [g], 0.01, bits=8, push=True, seed=3)
+    opt.step(0.01)
+    one.step(0.01)
+    assert torch.equal(flat_g[big:], g) and bool((flat_g[:1000] == 0).all()) and opt.steps == 1
+    at = -(-big // 128) * 128
+    assert torch.equal(opt.m_scales[at // 128:], one.m_scales)
+    assert [adamw_word(j, 1, 3) for j in range(8)] == adamw_ref.random_words(8, 1, 3).tolist()
+    padded = np.zeros(2944, np.float32)
+    padded[:n] = np.float32(1 - 0.9) * ref.f64(randn(torch, gen(torch, 2), n).bfloat16()).astype(np.float32)
+    codes, scales = adamw_ref.encode(padded, np.array([adamw_word(at + j, 1, 3) & 0xFFFF for j in range(2944)]), True)
+    assert np.array_equal(opt.m[at:].cpu().numpy(), codes) and np.array_equal(one.m_scales.cpu().numpy(), scales)
+
+
+def adamw_word(j, t, seed):
+    """Word j & 3 of Philox4x32-7 of (j >> 2, t) and the seed, in Python's whole numbers."""
+    c, k = [j >> 2 & 0xFFFFFFFF, j >> 34, t & 0xFFFFFFFF, t >> 32], [seed & 0xFFFFFFFF, seed >> 32]
+    for _ in range(7):
+        p0, p1 = c[0] * 0xD2511F53, c[2] * 0xCD9E8D57
+        c = [p1 >> 32 ^ c[1] ^ k[0], p1 & 0xFFFFFFFF, p0 >> 32 ^ c[3] ^ k[1], p0 & 0xFFFFFFFF]
+        k = [(k[0] + 0x9E3779B9) & 0xFFFFFFFF, (k[1] + 0xBB67AE85) & 0xFFFFFFFF]
+    return c[j & 3]
+
+
 def test_rounding_is_right_on_average(torch, learner):  # noqa: F811
     """m of a constant gradient after one step is 0.1 g; the mean of many roundings differs from it by five standard
     errors at most: a rounding's variance is at most a quarter of the spacing squared, the spacing 2^-3 of the value

@@ -130,6 +130,17 @@ def test_large_tiles(torch, learner):  # noqa: F811
         close(y[m - 2:], want, tol)
 
 
+def test_offsets_past_32_bits(torch, learner):  # noqa: F811
+    """Integers and results of more than 2^32 elements: the last rows as by themselves."""
+    k, m = 640, (1 << 32) // 640 + 300
+    x = torch.zeros(m, k, device="cuda", dtype=torch.bfloat16)
+    x[-256:] = randn(torch, gen(torch, 1), 256, k)
+    w = learner.quantize_int8(randn(torch, gen(torch, 2), 650, k))
+    y = learner.linear_int8(x, w)
+    assert y.numel() > 1 << 32 and bool((y[:300] == 0).all())
+    assert torch.equal(y[-256:], learner.linear_int8(x[-256:], w))
+
+
 def test_largest_sums(torch, learner):  # noqa: F811
     """2^17 products of 127^2 are the largest sum; one more column is refused."""
     k = 1 << 17

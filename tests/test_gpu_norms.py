@@ -310,6 +310,43 @@ def test_many_rows_of_few_columns(torch, learner):  # noqa: F811
         assert torch.equal(got.y, dh * gate.repeat_interleave(rows // gates, 0)) and torch.equal(got.x, dh)
 
 
+def test_types_of_gate_and_gradients(torch, learner):  # noqa: F811
+    """A gate of another type than the norms' weights, gradients of another than either."""
+    for gate_type, weight_type, out_type in (("bf16", "f32", "f32"), ("f32", "bf16", "bf16"), ("bf16", "f32", "bf16")):
+        c = Case(torch, 30, 77, 6, True, True, "bf16", "bf16", weight_type)
+        c.gate = c.gate.to(dt(torch, gate_type))
+        h, z = learner.residual_norm(c.x, c.y, c.gate, c.after, c.before, 1.0, EPS)
+        wh, wz, th, tz = forward(*(c.ref(k) for k in ("x", "y", "gate", "after", "before")), 1.0)
+        close(h, wh, th, B16)
+        close(z, wz, tz, B16)
+        got = learner.residual_norm_grad(c.h, c.y, c.dh, c.dz, c.gate, c.after, c.before, 1.0, EPS,
+                                         weight_dtype=dt(torch, out_type))
+        want = backward(c.ref("h"), c.ref("y"), c.ref("dh"), c.ref("dz"), c.ref("gate"), c.ref("after"),
+                        c.ref("before"), 1.0)
+        for name, t in got._asdict().items():
+            close(t, *want[name], rounding(t))
+
+
+def test_offsets_past_32_bits(torch, learner):  # noqa: F811
+    """Matrices of more than 2^32 elements: the last rows as by themselves, sums over all rows of whole numbers
+    exactly."""
+    cols = 8192
+    rows = (1 << 32) // cols + 1029
+    x = torch.zeros(rows, cols, device="cuda", dtype=torch.bfloat16)
+    y = torch.zeros_like(x)
+    last = slice(rows - 1024, rows)
+    g = gen(torch, 1)
+    x[last], y[last] = randn(torch, g, 1024, cols), randn(torch, g, 1024, cols)
+    w = torch.ones(cols, device="cuda")
+    h, z = learner.residual_norm(x, y, after=w, before=w)
+    h1, z1 = learner.residual_norm(x[last], y[last], after=w, before=w)
+    assert torch.equal(h[last], h1) and torch.equal(z[last], z1) and bool((h[:5] == 0).all())
+    del h, z
+    y.fill_(1.0)
+    got = learner.residual_norm_grad(x, y, y, None, w)
+    assert bool((got.gate == rows).all()) and bool((got.y[last] == 1).all()) and bool((got.x[last] == 1).all())
+
+
 def test_streams_and_graphs(torch, learner):  # noqa: F811
     """Captured once, replayed on new inputs, with eager work between; two graphs that run at once share nothing."""
     c = Case(torch, 130, 700, 13, True, True, "bf16", "bf16", "f32")
