@@ -145,12 +145,12 @@ struct Four {
 // A workgroup makes the step of one part, whose loads are all under way while one wave computes the
 // factors that depend on the number of the step. FULL: the part has all its elements.
 template <int W, int G, int BITS, bool PUSH, bool FULL>
-__device__ __forceinline__ void step_part(const AdamwArgs &a, AdamwPart *part, Factors &shared) {
+__device__ __forceinline__ void step_part(const AdamwArgs &a, AdamwPart *part, const AdamwPart &p, Factors &shared) {
 #pragma clang fp contract(off)
-    void *const w = part->weight, *const g = part->grad;
-    const int64_t first = part->at;   // of the states
-    const int count = FULL ? kPart : static_cast<int>(part->count);
-    const float decay = part->decay;
+    void *const w = p.weight, *const g = p.grad;
+    const int64_t first = p.at;   // of the states
+    const int count = FULL ? kPart : static_cast<int>(p.count);
+    const float decay = p.decay;
     const int room = (count + 127) & ~127;
     Four x[kFours];
 #pragma unroll
@@ -173,7 +173,7 @@ __device__ __forceinline__ void step_part(const AdamwArgs &a, AdamwPart *part, F
     if (threadIdx.x < 2) {
         // Each part counts the steps for itself: the count of a captured step goes on when it is
         // replayed, and no part waits for another.
-        const int64_t t = part->steps + 1;
+        const int64_t t = p.steps + 1;
         const double rest = 1.0 - exp2(static_cast<double>(t) * (threadIdx.x == 0 ? a.log2_beta1 : a.log2_beta2));
         if (threadIdx.x == 0) {
             part->steps = t;
@@ -265,8 +265,9 @@ __global__ __launch_bounds__(kThreads) void adamw(AdamwArgs a) {
     const uint64_t index = block_index();
     if (index >= a.parts) return;
     AdamwPart *const part = a.plan + index;
-    if (part->count == kPart) step_part<W, G, BITS, PUSH, true>(a, part, shared);
-    else step_part<W, G, BITS, PUSH, false>(a, part, shared);
+    const AdamwPart p = *part;   // with the number of steps: a load of it behind the others would wait for them
+    if (p.count == kPart) step_part<W, G, BITS, PUSH, true>(a, part, p, shared);
+    else step_part<W, G, BITS, PUSH, false>(a, part, p, shared);
 }
 
 // The values of states in 8 bits, sixteen lanes a block.
