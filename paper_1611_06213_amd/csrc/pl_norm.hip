@@ -369,7 +369,8 @@ struct RowBits {
     Bits8<X> h, dh;
     Bits8<Y> y, dz;
     __device__ __forceinline__ void load(const NormGradArgs &a, uint32_t row, uint32_t col, int count) {
-        h = bits8<X, EIGHTS>(row_of<X>(a.h, row, a.h_ld), col, count);
+        // without dz nothing depends on h, an infinite one's products with zeros neither
+        h = a.dz != nullptr ? bits8<X, EIGHTS>(row_of<X>(a.h, row, a.h_ld), col, count) : Bits8<X>{};
         if constexpr (BLOCK) y = bits8<Y, EIGHTS>(row_of<Y>(a.y, row, a.y_ld), col, count);
         dh = a.dh != nullptr ? bits8<X, EIGHTS>(row_of<X>(a.dh, row, a.dh_ld), col, count) : Bits8<X>{};
         dz = a.dz != nullptr ? bits8<Y, EIGHTS>(row_of<Y>(a.dz, row, a.dz_ld), col, count) : Bits8<Y>{};
@@ -447,7 +448,11 @@ __device__ __forceinline__ void take_row(const NormGradArgs &a, const RowBits<X,
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             c.d_branch[e] += d[e] * (y[e] * r[2]);
-            d[e] = r[2] * (d[e] * c.branch[e] - y[e] * r[3]);
+            d[e] *= c.branch[e];
+        }
+        if (a.after != nullptr) {   // else y has no part in it, and may be infinite
+#pragma unroll
+            for (int e = 0; e < 8; ++e) d[e] = r[2] * (d[e] - y[e] * r[3]);
         }
         put_row8<Y, EIGHTS>(row_of<Y>(a.dy, row, a.dy_ld), col, d, count);
     }

@@ -278,6 +278,27 @@ def test_rows_of_zeros_and_not_finite(torch, learner):  # noqa: F811
     assert bool(g.x.isfinite().all()) and torch.equal(g.y[4:], alone.y)
 
 
+@pytest.mark.parametrize("cols", [5, 300, 301, 9000])
+def test_infinities_that_no_gradient_depends_on(torch, learner, cols):  # noqa: F811
+    """Without a norm before the next block the stream's gradient does not depend on the stream, without one after
+    this block its output's not on the output."""
+    g = gen(torch, cols)
+    h, y, dh, dz = (randn(torch, g, 7, cols) for _ in range(4))
+    gate, w = randn(torch, g, cols), randn(torch, g, cols)
+    h[1, 2] = h[2, 0] = float("inf")
+    h[3, cols - 1] = float("nan")
+    got = learner.residual_norm_grad(h, y, dh, gate=gate, after=w)
+    clean = learner.residual_norm_grad(torch.zeros_like(h), y, dh, gate=gate, after=w)
+    assert torch.equal(got.x, dh)
+    assert all(torch.equal(a, b) for a, b in zip(got[1:4], clean[1:4]))
+    y[1, 1], y[4, 3] = float("nan"), float("-inf")
+    for next_norm in ({}, {"normed_grad": dz, "before": w}):
+        finite = torch.ones_like(h)
+        got = learner.residual_norm_grad(finite, y, dh, gate=gate, **next_norm)
+        clean = learner.residual_norm_grad(finite, torch.zeros_like(y), dh, gate=gate, **next_norm)
+        assert torch.equal(got.x, clean.x) and torch.equal(got.y, clean.y)
+
+
 def test_no_rows_and_no_columns(torch, learner):  # noqa: F811
     for dtype in (torch.float32, torch.bfloat16):
         x = torch.ones(0, 40, device="cuda", dtype=dtype)
