@@ -163,7 +163,7 @@ size_t pl_linear_fp8_grad_workspace(int64_t m, int64_t n, int64_t k, int out_dty
  * neighbouring rows (one sequence's, say; 1: for all; rows: one each); rows is a multiple of it.
  * Either output may be NULL, out only without a block. normed is that of the sums before they
  * are rounded to out's type. eps > 0. Squares are summed in fp32: a row whose sum of squares
- * passes 3.4e38 is normed to zeros. rows < 2^31, cols <= 2^31. */
+ * passes 3.4e38 is normed to zeros. rows < 2^31, cols <= 2^29. */
 int pl_norm(const void *x, int x_dtype, int64_t x_ld, const void *y, int y_dtype, int64_t y_ld,
             int64_t rows, int64_t cols, const void *gate, int gate_dtype, int64_t gates,
             int64_t gate_ld, const void *after, const void *before, int weight_dtype, float scale,
@@ -228,8 +228,8 @@ size_t pl_linear_int8_workspace(int64_t m, int64_t n, int64_t k);
  * it to a server with lr 1 and momentum 0, which makes the step when it applies it.
  *
  * The states m and v are vectors of pl_adamw_room() elements that hold tensor after tensor, each
- * from a multiple of 128 elements on; what lies between is zeros and stays so. New ones are
- * zeros. Weights are fp32 (with push also bf16), gradients fp32 or bf16, all of a type.
+ * from a multiple of 128 elements on; what lies between is zeros and, with finite factors, stays
+ * so. New ones are zeros. beta1 and beta2 are 0 to 1 - 2^-28. Weights are fp32 (with push also bf16), gradients fp32 or bf16, all of a type.
  *
  * bits = 32: the states are fp32. bits = 8: a byte an element, and for each 128 elements a byte s
  * in m_scales and v_scales, the exponent field of the block's largest magnitude as an fp32 number,

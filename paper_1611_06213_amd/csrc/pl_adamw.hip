@@ -27,7 +27,6 @@ constexpr int kThreads = 256;
 constexpr int kFour = 4;    // neighbouring elements a lane
 constexpr int kFours = 2;   // of them: 138M elements in 8 bits 389 us with one, 371 with two, 378 with four
 constexpr int kPart = kThreads * kFour * kFours;
-constexpr float kPlainEps = 0x1p-30f;
 
 typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
 typedef u16x4 u16x4_any __attribute__((aligned(2)));
@@ -214,9 +213,9 @@ __device__ __forceinline__ void step_part(const AdamwArgs &a, AdamwPart *part, c
             m[e] = a.beta1 * m[e] + a.rest1 * ge;
             v[e] = a.beta2 * v[e] + a.rest2 * (ge * ge);
         }
-        // The instructions' root and reciprocal err by one unit and take numbers below 2^-126 for zeros:
-        // next to an eps of kPlainEps their roots, below 2^-63 and times 2^9 at most, round away.
-        if (a.eps >= kPlainEps) {
+        // The instructions' root and reciprocal err by one unit and take numbers below 2^-126 for zeros, whose
+        // roots are below 2^-63: times 2^9, as `root` is at most, they round away next to an eps of 2^-30.
+        if (a.plain) {
 #pragma unroll
             for (int e = 0; e < kFour; ++e)
                 y[e] = m[e] * f.up * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(v[e]) * f.root + a.eps);

@@ -472,12 +472,14 @@ int pl_linear_fp8_grad(const void *x, int x_dtype, int64_t x_ld, const void *gra
 
 namespace {
 
+constexpr int64_t kMostNormed = int64_t(1) << 29;   // columns: four threads each are one launch
+
 // What the norms and their gradients have in common, checked; *in: spans of gate, after and before.
 int norm_vectors(int64_t rows, int64_t cols, bool block, const void *gate, int gate_dtype, int64_t gates,
                  int64_t gate_ld, const void *after, const void *before, int weight_dtype, float scale, float eps,
                  Span *in) {
     if (int rc = size_in("rows", rows, kMax / 2 - 1)) return rc;
-    if (int rc = size_in("cols", cols, kMax / 2)) return rc;
+    if (int rc = size_in("cols", cols, kMostNormed)) return rc;
     if (!(eps > 0.0f) || std::isinf(eps)) return fail(PS_EINVAL, "eps %g", static_cast<double>(eps));
     if (!block && (gate != nullptr || after != nullptr)) return fail(PS_EINVAL, "a gate or after without y");
     if (!block && scale != 1.0f) return fail(PS_EINVAL, "a scale without y");
@@ -551,7 +553,7 @@ int pl_norm(const void *x, int x_dtype, int64_t x_ld, const void *y, int y_dtype
 }
 
 size_t pl_norm_grad_workspace(int64_t rows, int64_t cols) {
-    if (rows <= 0 || rows >= kMax / 2 || cols <= 0 || cols > kMax / 2) return 0;
+    if (rows <= 0 || rows >= kMax / 2 || cols <= 0 || cols > kMostNormed) return 0;
     return norm_grad_workspace(rows, cols);
 }
 
@@ -887,7 +889,7 @@ int pl_adamw_step(void *plan, int64_t parts, int weight_dtype, int grad_dtype, i
     if (!is_dtype(grad_dtype)) return fail(PS_EINVAL, "grad: dtype %d", grad_dtype);
     if (bits != 8 && bits != 32) return fail(PS_EINVAL, "states of %d bits", bits);
     for (const double b : {beta1, beta2})
-        if (!(b >= 0.0 && b < 1.0)) return fail(PS_EINVAL, "beta %g outside [0, 1)", b);
+        if (!(b >= 0.0 && b <= 1.0 - 0x1p-28)) return fail(PS_EINVAL, "beta %.10g outside [0, 1 - 2^-28]", b);
     if (!(eps >= 0.0f) || std::isinf(eps)) return fail(PS_EINVAL, "eps %g", static_cast<double>(eps));
     Span s[7] = {};
     const uint64_t n = static_cast<uint64_t>(room);
@@ -924,6 +926,7 @@ int pl_adamw_step(void *plan, int64_t parts, int weight_dtype, int grad_dtype, i
     a.lr_at = lr_at;
     a.factor_at = factor_at;
     a.seed = seed;
+    a.plain = eps >= 0x1p-30f && 1.0 - beta2 >= 0x1p-18;
     return launched(launch_adamw(a, weight_dtype, grad_dtype, bits, push != 0, static_cast<hipStream_t>(stream)),
                     "pl_adamw_step");
 }

@@ -216,6 +216,25 @@ def test_zero_gradients_and_small_numbers(torch, learner):  # noqa: F811
         assert bool(w.isfinite().all()) and float(w.abs().max()) < 60 and float(w[5]) == 0 and bool((w[200:] == 0).all())
 
 
+@pytest.mark.parametrize("eps", [2.0 ** -30, 2.0 ** -31])
+@pytest.mark.parametrize("beta2", [1 - 2.0 ** -18, 1 - 2.0 ** -28])
+def test_second_moments_below_normal_numbers(torch, learner, beta2, eps):  # noqa: F811
+    """v of 2^-127 to 2^-126 and less, multiplied by 2^18 and 2^28 in the first step: of a denominator with this eps
+    more than a step's tolerance where the factor is large."""
+    size = 1.9 * 2.0 ** -(50 if beta2 > 1 - 2.0 ** -20 else 55)
+    g = size * torch.cat([torch.ones(64), 0.7 * torch.ones(64), 1e-3 * torch.ones(64)]).cuda()
+    w = torch.zeros(192, device="cuda")
+    opt = learner.AdamW([w], [g], 0.0, (0.0, beta2), eps)
+    want = adamw_ref.Reference([192], [0.0], (0.0, beta2), eps, 32, 0)
+    for _ in range(2):
+        before = ref.f64(w)
+        opt.step(1.0)
+        (step, tol), = want.step([before], [ref.f64(g)], 1.0)
+        same_states(opt, want)
+        value = before - step
+        assert (abs(ref.f64(w) - value) <= tol + U * (abs(value) + tol)).all()
+
+
 def test_numbers_on_the_device_and_graphs(torch, learner):  # noqa: F811
     """lr and factor from device memory; a captured step counts on when it is replayed; two optimizers' graphs at
     once; a saved state goes on."""

@@ -22,6 +22,9 @@ def test_norm_refuses(lib):  # noqa: F811
     refused(lib, call(rows=1 << 31), "rows")
     refused(lib, call(rows=-1), "rows")
     refused(lib, call(cols=(1 << 31) + 1), "cols")
+    # more columns than one launch joins the gradients' sums of
+    refused(lib, call(cols=(1 << 29) + 1, xld=1 << 30, yld=1 << 30, old=1 << 30, nld=1 << 30), "cols")
+    assert lib.pl_norm_grad_workspace(1, 1 << 29) > 0 and lib.pl_norm_grad_workspace(1, (1 << 29) + 1) == 0
     for eps in (0.0, -1.0, float("nan"), float("inf")):
         refused(lib, call(eps=eps), "eps")
     refused(lib, call(x=None), "x: null")
@@ -229,7 +232,7 @@ def test_adamw_step_refuses(lib):  # noqa: F811
     refused(lib, call(wdt=1), "weight")
     refused(lib, call(gdt=7), "grad")
     refused(lib, call(bits=16), "16 bits")
-    for b in (1.0, -0.5, float("nan")):
+    for b in (1.0, -0.5, float("nan"), 1 - 2.0 ** -29):
         refused(lib, call(b1=b), "beta")
         refused(lib, call(b2=b), "beta")
     refused(lib, call(eps=-1.0), "eps")
