@@ -75,9 +75,10 @@ __device__ __forceinline__ uint32_t most_of_wave(uint32_t m) {
 }
 
 // A row a wave (threadIdx.y) or a row a workgroup.
-template <int X>
-__global__ __launch_bounds__(256) void quantize(Int8QuantArgs a) {
-    __shared__ uint32_t lds[4];
+template <int X, int THREADS>
+__global__ __launch_bounds__(THREADS) void quantize(Int8QuantArgs a) {
+    constexpr int kWaves = THREADS / 64;
+    __shared__ uint32_t lds[kWaves];
     const int64_t row = static_cast<int64_t>(block_index()) * blockDim.y + threadIdx.y;
     if (row >= a.rows) return;   // a whole wave, or a whole workgroup
     const int64_t ld = (a.cols + 127) / 128 * 128, step = 8 * blockDim.x, first = 8 * threadIdx.x;
@@ -98,7 +99,8 @@ __global__ __launch_bounds__(256) void quantize(Int8QuantArgs a) {
     if (blockDim.x > 64) {
         if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = m;
         __syncthreads();
-        m = max(max(lds[0], lds[1]), max(lds[2], lds[3]));
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) m = max(m, lds[w]);
     }
     const RowScale s(m);
     if (threadIdx.x == 0) a.scales[row] = s.scale;
@@ -648,10 +650,11 @@ bool is_slim(uint64_t m, uint64_t n, uint64_t k) {
 }
 
 // Whether slim converts x itself: a row's bytes in LDS and the padding. Every workgroup converts all of x: in
-// us, so and in two launches, 16 x 1000 x 900 6.2 and 8.6, 4 x 4096 x 9216 12.3 and 13.3, 24 x 1000 x 900 8.7
-// and 8.1, 1 x 25088 x 4096 24.9 and 24.0.
+// us, so and in two launches, 16 x 1000 x 900 6.0 and 6.9, 4 x 4096 x 9216 12.2 and 13.0, 1 x 4096 x 25088 23.1
+// and 25.8, 1 x 4096 x 40000 35 and 37, 12 x 4096 x 4096 11.2 and 9.5, 3 x 4096 x 16384 20.4 and 18.8, 24 x 1000
+// x 900 8.7 and 8.1.
 bool few_bytes(uint64_t m, uint64_t n, uint64_t blocks) {
-    return m <= 16 && n <= 8192 && m * (blocks * 128 + 16) <= 51200;
+    return m <= 16 && n <= 8192 && m * (blocks * 128 + 16) <= 45056;
 }
 
 // Of slim: where few columns of out leave compute units idle, a long k is split, to a block a wave at
@@ -726,16 +729,29 @@ hipError_t launch(const Int8Args &g, hipStream_t s) {
     return e != hipSuccess || sp.parts == 1 ? e : launch_join<OUT>(g, sp.parts, s);
 }
 
+template <int X, int THREADS>
+hipError_t launch_quantize(const Int8QuantArgs &a, dim3 threads, hipStream_t s) {
+    dim3 grid;
+    if (!grid_of((a.rows + threads.y - 1) / threads.y, THREADS, &grid)) return hipErrorInvalidConfiguration;
+    quantize<X, THREADS><<<grid, threads, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+// As many threads as keep a row, if they are not too many to come and go: in us with 256, 512 and 1024, bf16, 8192 x
+// 8192 32, 39 and 99, 4096 x 16384 42, 32 and 49, 4096 x 25088 78, 60 and 61, 128 x 25088 7.7, 5.0 and 4.4, 2048 x
+// 100000 201, 165 and 150.
+template <int X>
+hipError_t launch_quantize(const Int8QuantArgs &a, hipStream_t s) {
+    return a.cols <= 512     ? launch_quantize<X, 256>(a, dim3(64, 4), s)
+           : a.cols <= 8192  ? launch_quantize<X, 256>(a, dim3(256), s)
+           : a.cols <= 32768 ? launch_quantize<X, 512>(a, dim3(512), s)
+                             : launch_quantize<X, 1024>(a, dim3(1024), s);
+}
+
 }  // namespace
 
 hipError_t launch_quantize_int8(const Int8QuantArgs &a, int dtype, hipStream_t s) {
-    const bool waves = a.cols <= 512;   // a row a wave
-    dim3 grid;
-    if (!grid_of(waves ? (a.rows + 3) / 4 : a.rows, 256, &grid)) return hipErrorInvalidConfiguration;
-    const dim3 threads = waves ? dim3(64, 4) : dim3(256);
-    if (dtype == PS_F32) quantize<PS_F32><<<grid, threads, 0, s>>>(a);
-    else quantize<PS_BF16><<<grid, threads, 0, s>>>(a);
-    return hipGetLastError();
+    return dtype == PS_F32 ? launch_quantize<PS_F32>(a, s) : launch_quantize<PS_BF16>(a, s);
 }
 
 size_t int8_workspace(int64_t m, int64_t n, int64_t k) {

@@ -44,7 +44,7 @@ def close(t, want, tol):
 
 
 @pytest.mark.parametrize("rows,cols", [(1, 1), (3, 127), (4, 128), (5, 129), (9, 512), (7, 513), (2, 2048), (3, 2055),
-                                       (6, 8192), (2, 8200), (1, 30001), (300, 40)])
+                                       (6, 8192), (2, 8200), (3, 16391), (1, 30001), (2, 32777), (300, 40)])
 @pytest.mark.parametrize("x", ["f32", "bf16"])
 def test_quantize(torch, learner, rows, cols, x):  # noqa: F811
     g = gen(torch, rows + cols)
