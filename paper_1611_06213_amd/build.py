@@ -124,7 +124,7 @@ def build_binding(verbose: bool = False) -> str:
             (LEARNER_BINDING, _binding_cmd(
                 LEARNER_BINDING_SRC, LEARNER_BINDING,
                 ["-D__HIP_PLATFORM_AMD__", "-DUSE_ROCM", "-isystem", os.path.join(ROCM, "include")],
-                ["-lc10_hip", "-L", HERE, "-lgadeilearner", "-Wl,-rpath,$ORIGIN"]))]
+                ["-lc10_hip", "-ltorch_hip", "-L", HERE, "-lgadeilearner", "-Wl,-rpath,$ORIGIN"]))]
     running = []
     for out, cmd in cmds:
         if verbose:
