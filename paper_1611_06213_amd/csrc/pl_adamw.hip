@@ -17,7 +17,9 @@
 // b2) of itself a step, 2^-10, would never leave a number of 3 fraction bits if rounded to nearest.
 // A positive v is never rounded to 0, below which m / sqrt(v) has no bound.
 //
-// Bound by memory in 32 bits, by memory and vector instructions in 8.
+// Bound by memory in 32 bits, by memory and vector instructions in 8: 61M elements in 32 bits 298 us (1.71 GB, 5.7
+// TB/s; a copy reaches 5.1), 138M in 8 bits with bf16 gradients 319 us (1.94 GB, 6.1 TB/s; vector instructions
+// three quarters of the time).
 #include "pl_device.h"
 
 namespace gadei::learner {
@@ -25,7 +27,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kFour = 4;    // neighbouring elements a lane
-constexpr int kFours = 2;   // of them: 138M elements in 8 bits 389 us with one, 371 with two, 378 with four
+constexpr int kFours = 2;   // of them: 138M elements in 8 bits 333 us with one, 316 with two, 330 with four
 constexpr int kPart = kThreads * kFour * kFours;
 
 typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
@@ -55,15 +57,41 @@ __device__ __forceinline__ u32x4 random4(uint64_t j, uint64_t t, uint64_t seed) 
     return u32x4{c0, c1, c2, c3};
 }
 
+// Loads and stores, PAST: past the caches. So go gradients and states, which nothing reads before the next step,
+// and weights (with push the steps) where they do not fit in the last level: in us, none past them, gradients and
+// states, and all: 25M in 32 bits 141, 127 and 128 (again on the same tensors 141, 106 and 128), 61M 340, 320 and
+// 317 (340, 252 and 312), 138M 775, 737 and 723; 138M in 8 bits with bf16 gradients 370, 343 and 331.
+constexpr uint64_t kLastLevel = 256ull << 20;
+template <bool PAST>
+__device__ __forceinline__ f32x4 get(const f32x4_any *p) {
+    if constexpr (PAST) return __builtin_nontemporal_load(p);
+    else return *p;
+}
+template <bool PAST>
+__device__ __forceinline__ u32x2 get(const u32x2_any *p) {
+    if constexpr (PAST) return __builtin_nontemporal_load(p);
+    else return *p;
+}
+template <bool PAST>
+__device__ __forceinline__ void put(f32x4_any *p, f32x4 x) {
+    if constexpr (PAST) __builtin_nontemporal_store(x, p);
+    else *p = x;
+}
+template <bool PAST>
+__device__ __forceinline__ void put(u32x2_any *p, u32x2 x) {
+    if constexpr (PAST) __builtin_nontemporal_store(x, p);
+    else *p = x;
+}
+
 // Four elements as loaded; those past `count` are 0.
-template <int DT>
+template <int DT, bool PAST>
 __device__ __forceinline__ f32x4 load4(const void *p, int64_t i, int count) {
     f32x4 x = {0, 0, 0, 0};
     if (count >= kFour) {
         if constexpr (DT == PS_F32) {
-            x = *reinterpret_cast<const f32x4_any *>(static_cast<const float *>(p) + i);
+            x = get<PAST>(reinterpret_cast<const f32x4_any *>(static_cast<const float *>(p) + i));
         } else {
-            const u32x2 w = *reinterpret_cast<const u32x2_any *>(static_cast<const uint16_t *>(p) + i);
+            const u32x2 w = get<PAST>(reinterpret_cast<const u32x2_any *>(static_cast<const uint16_t *>(p) + i));
             x = f32x4{lo_bf16(w[0]), hi_bf16(w[0]), lo_bf16(w[1]), hi_bf16(w[1])};
         }
     } else {
@@ -74,14 +102,14 @@ __device__ __forceinline__ f32x4 load4(const void *p, int64_t i, int count) {
     return x;
 }
 
-template <int DT>
+template <int DT, bool PAST>
 __device__ __forceinline__ void store4(void *p, int64_t i, f32x4 x, int count) {
     if (count >= kFour) {
         if constexpr (DT == PS_F32)
-            *reinterpret_cast<f32x4_any *>(static_cast<float *>(p) + i) = x;
+            put<PAST>(reinterpret_cast<f32x4_any *>(static_cast<float *>(p) + i), x);
         else
-            *reinterpret_cast<u32x2_any *>(static_cast<uint16_t *>(p) + i) =
-                u32x2{bf16x2_rne(x[0], x[1]), bf16x2_rne(x[2], x[3])};
+            put<PAST>(reinterpret_cast<u32x2_any *>(static_cast<uint16_t *>(p) + i),
+                      u32x2{bf16x2_rne(x[0], x[1]), bf16x2_rne(x[2], x[3])});
     } else {
 #pragma unroll
         for (int e = 0; e < kFour; ++e)
@@ -143,7 +171,7 @@ struct Four {
 
 // A workgroup makes the step of one part, whose loads are all under way while one wave computes the
 // factors that depend on the number of the step. FULL: the part has all its elements.
-template <int W, int G, int BITS, bool PUSH, bool FULL>
+template <int W, int G, int BITS, bool PUSH, bool WEIGHTS_PAST, bool FULL>
 __device__ __forceinline__ void step_part(const AdamwArgs &a, AdamwPart *part, const AdamwPart &p, Factors &shared) {
 #pragma clang fp contract(off)
     void *const w = p.weight, *const g = p.grad;
@@ -156,14 +184,14 @@ __device__ __forceinline__ void step_part(const AdamwArgs &a, AdamwPart *part, c
     for (int j = 0; j < kFours; ++j) {
         const int i = (threadIdx.x + j * kThreads) * kFour, left = FULL ? kFour : count - i;
         if (!FULL && i >= room) continue;
-        x[j].w = load4<W>(w, i, left);
-        x[j].g = load4<G>(g, i, left);
+        x[j].w = load4<W, WEIGHTS_PAST>(w, i, left);
+        x[j].g = load4<G, true>(g, i, left);
         if constexpr (BITS == 32) {
-            x[j].m = *reinterpret_cast<const f32x4 *>(static_cast<const float *>(a.m) + first + i);
-            x[j].v = *reinterpret_cast<const f32x4 *>(static_cast<const float *>(a.v) + first + i);
+            x[j].m = get<true>(reinterpret_cast<const f32x4_any *>(static_cast<const float *>(a.m) + first + i));
+            x[j].v = get<true>(reinterpret_cast<const f32x4_any *>(static_cast<const float *>(a.v) + first + i));
         } else {
-            x[j].cm = *reinterpret_cast<const uint32_t *>(static_cast<const uint8_t *>(a.m) + first + i);
-            x[j].cv = *reinterpret_cast<const uint32_t *>(static_cast<const uint8_t *>(a.v) + first + i);
+            x[j].cm = __builtin_nontemporal_load(reinterpret_cast<const uint32_t *>(static_cast<const uint8_t *>(a.m) + first + i));
+            x[j].cv = __builtin_nontemporal_load(reinterpret_cast<const uint32_t *>(static_cast<const uint8_t *>(a.v) + first + i));
             x[j].bm = a.m_scales[(first + i) >> 7];
             x[j].bv = a.v_scales[(first + i) >> 7];
         }
@@ -228,11 +256,11 @@ __device__ __forceinline__ void step_part(const AdamwArgs &a, AdamwPart *part, c
             y[e] = f.lr * (y[e] + decay * x[j].w[e]);
             if (!PUSH) y[e] = x[j].w[e] - y[e];
         }
-        if constexpr (PUSH) store4<G>(g, i, y, left);
-        else store4<W>(w, i, y, left);
+        if constexpr (PUSH) store4<G, WEIGHTS_PAST>(g, i, y, left);
+        else store4<W, WEIGHTS_PAST>(w, i, y, left);
         if constexpr (BITS == 32) {
-            *reinterpret_cast<f32x4 *>(static_cast<float *>(a.m) + at) = m;
-            *reinterpret_cast<f32x4 *>(static_cast<float *>(a.v) + at) = v;
+            put<true>(reinterpret_cast<f32x4_any *>(static_cast<float *>(a.m) + at), m);
+            put<true>(reinterpret_cast<f32x4_any *>(static_cast<float *>(a.v) + at), v);
         } else {
             uint32_t mm = 0, mv = 0;
 #pragma unroll
@@ -248,8 +276,8 @@ __device__ __forceinline__ void step_part(const AdamwArgs &a, AdamwPart *part, c
                 cm[e] = encode<true>(m[e], bm, r[e] & 0xffffu);
                 cv[e] = encode<false>(v[e], bv, r[e] >> 16);
             }
-            *reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(a.m) + at) = upper_bytes(cm);
-            *reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(a.v) + at) = upper_bytes(cv);
+            __builtin_nontemporal_store(upper_bytes(cm), reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(a.m) + at));
+            __builtin_nontemporal_store(upper_bytes(cv), reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(a.v) + at));
             if ((threadIdx.x & 31) == 0) {
                 a.m_scales[at >> 7] = static_cast<uint8_t>(bm);
                 a.v_scales[at >> 7] = static_cast<uint8_t>(bv);
@@ -258,21 +286,21 @@ __device__ __forceinline__ void step_part(const AdamwArgs &a, AdamwPart *part, c
     }
 }
 
-template <int W, int G, int BITS, bool PUSH>
+template <int W, int G, int BITS, bool PUSH, bool WEIGHTS_PAST>
 __global__ __launch_bounds__(kThreads) void adamw(AdamwArgs a) {
     __shared__ Factors shared;
     const uint64_t index = block_index();
     if (index >= a.parts) return;
     AdamwPart *const part = a.plan + index;
     const AdamwPart p = *part;   // with the number of steps: a load of it behind the others would wait for them
-    if (p.count == kPart) step_part<W, G, BITS, PUSH, true>(a, part, p, shared);
-    else step_part<W, G, BITS, PUSH, false>(a, part, p, shared);
+    if (p.count == kPart) step_part<W, G, BITS, PUSH, WEIGHTS_PAST, true>(a, part, p, shared);
+    else step_part<W, G, BITS, PUSH, WEIGHTS_PAST, false>(a, part, p, shared);
 }
 
 // The values of states in 8 bits, sixteen lanes a block.
-template <bool SIGNED, int OUT>
+template <bool SIGNED, int OUT, bool PAST>
 __device__ __forceinline__ void values(const uint8_t *codes, const uint8_t *scales, void *out, uint64_t at) {
-    const u32x2 c = *reinterpret_cast<const u32x2 *>(codes + at);
+    const u32x2 c = get<PAST>(reinterpret_cast<const u32x2_any *>(codes + at));
     const int byte = scales[at >> 7];
     float x[8];
 #pragma unroll
@@ -280,22 +308,23 @@ __device__ __forceinline__ void values(const uint8_t *codes, const uint8_t *scal
         x[e] = decode<SIGNED>(c[e >> 2], e & 3, byte);
         if (byte == kBad) x[e] = __builtin_nanf("");
     }
-    store8<OUT>(out, static_cast<int64_t>(at), x);
+    store8<OUT, PAST>(out, static_cast<int64_t>(at), x);
 }
 
-template <int OUT>
+template <int OUT, bool PAST>
 __global__ __launch_bounds__(kThreads) void moments(MomentsArgs a) {
     const uint64_t at = (static_cast<uint64_t>(block_index()) * kThreads + threadIdx.x) * 8;
     if (at >= a.room) return;
-    values<true, OUT>(a.m, a.m_scales, a.m_out, at);
-    values<false, OUT>(a.v, a.v_scales, a.v_out, at);
+    values<true, OUT, PAST>(a.m, a.m_scales, a.m_out, at);
+    values<false, OUT, PAST>(a.v, a.v_scales, a.v_out, at);
 }
 
 template <int W, int G, int BITS, bool PUSH>
 hipError_t launch(const AdamwArgs &a, hipStream_t s) {
     dim3 grid;
     if (!grid_of(a.parts, kThreads, &grid)) return hipErrorInvalidConfiguration;
-    adamw<W, G, BITS, PUSH><<<grid, kThreads, 0, s>>>(a);
+    if (a.parts * kPart * kBytes<W> > kLastLevel) adamw<W, G, BITS, PUSH, true><<<grid, kThreads, 0, s>>>(a);
+    else adamw<W, G, BITS, PUSH, false><<<grid, kThreads, 0, s>>>(a);
     return hipGetLastError();
 }
 
@@ -322,8 +351,13 @@ hipError_t launch_adamw(const AdamwArgs &a, int weight_dtype, int grad_dtype, in
 hipError_t launch_moments(const MomentsArgs &a, int dtype, hipStream_t s) {
     dim3 grid;
     if (!grid_of((a.room / 8 + kThreads - 1) / kThreads, kThreads, &grid)) return hipErrorInvalidConfiguration;
-    if (dtype == PS_F32) moments<PS_F32><<<grid, kThreads, 0, s>>>(a);
-    else moments<PS_BF16><<<grid, kThreads, 0, s>>>(a);
+    // Results of which more than half of the last level's size is written, past the caches: in us in fp32 and bf16,
+    // 138M 299 and 140, not so 347 and 146, 61M 133 and 63, 153 and 66; but 12M 28 and 14.6, 27 and 12.9.
+    const bool past = 2 * a.room * (dtype == PS_F32 ? 4 : 2) > kLastLevel / 2;
+    if (dtype == PS_F32 && past) moments<PS_F32, true><<<grid, kThreads, 0, s>>>(a);
+    else if (dtype == PS_F32) moments<PS_F32, false><<<grid, kThreads, 0, s>>>(a);
+    else if (past) moments<PS_BF16, true><<<grid, kThreads, 0, s>>>(a);
+    else moments<PS_BF16, false><<<grid, kThreads, 0, s>>>(a);
     return hipGetLastError();
 }
 
