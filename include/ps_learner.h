@@ -186,10 +186,10 @@ size_t pl_norm_grad_workspace(int64_t rows, int64_t cols);
 
 /* ---- A matrix in 8-bit integers with a scale for each row (a token's activations, or a
  * channel's weights): element (r, c) = values[r * pl_int8_ld(cols) + c] * scales[r], values from -127
- * to 127. The scale is
- * most / 127, most the largest magnitude of the row or 2^-100 if that is larger; elements times
- * 127 (1 / most), each step in fp32, are rounded to nearest even. A row with a NaN or an infinity has the scale NaN. The
- * values' rows are padded with zeros to multiples of 128. Both arrays lie on 16-byte boundaries. */
+ * to 127. The scale is most / 127, most the largest magnitude of the row or 2^-100 if that is larger;
+ * elements times 127 (1 / most), each step in fp32, are rounded to nearest even. A row with a NaN or an
+ * infinity has the scale NaN. The values' rows are padded with zeros to multiples of 128. Both arrays
+ * lie on 16-byte boundaries. */
 typedef struct pl_int8 {
     int8_t *values;   /* pl_int8_values_bytes(rows, cols) bytes */
     float *scales;    /* rows */
@@ -204,8 +204,8 @@ int pl_quantize_int8(const void *x, int dtype, int64_t rows, int64_t cols, int64
 /* out = a b^T (+ bias) (then max(., 0) with relu; a NaN stays) for a (m x k) and b (n x k), out
  * m x n. Sums of products of integers are exact, so an element depends on its rows of a and b
  * alone, not on how many others there are; then it is the sum times a's scale, times b's, plus
- * the bias, each step in fp32 (whose range the first may pass before the second). bias: n values or NULL. m, n, k may be 0;
- * m, n <= 2^28, k <= 2^17. */
+ * the bias, each step in fp32 (whose range the first may pass before the second). bias: n values
+ * or NULL. m, n, k may be 0; m, n <= 2^28, k <= 2^17. */
 int pl_matmul_int8(int64_t m, int64_t n, int64_t k, const pl_int8 *a, const pl_int8 *b,
                    const void *bias, int bias_dtype, int relu, void *out, int out_dtype,
                    int64_t out_ld, void *workspace, size_t workspace_bytes, void *stream);
@@ -229,7 +229,8 @@ size_t pl_linear_int8_workspace(int64_t m, int64_t n, int64_t k);
  *
  * The states m and v are vectors of pl_adamw_room() elements that hold tensor after tensor, each
  * from a multiple of 128 elements on; what lies between is zeros and, with finite factors, stays
- * so. New ones are zeros. beta1 and beta2 are 0 to 1 - 2^-28. Weights are fp32 (with push also bf16), gradients fp32 or bf16, all of a type.
+ * so. New ones are zeros. beta1 and beta2 are 0 to 1 - 2^-28. Weights are fp32 (with push also
+ * bf16), gradients fp32 or bf16, all of a type.
  *
  * bits = 32: the states are fp32. bits = 8: a byte an element, and for each 128 elements a byte s
  * in m_scales and v_scales, the exponent field of the block's largest magnitude as an fp32 number,

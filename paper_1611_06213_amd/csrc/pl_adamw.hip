@@ -18,8 +18,8 @@
 // A positive v is never rounded to 0, below which m / sqrt(v) has no bound.
 //
 // Bound by memory in 32 bits, by memory and vector instructions in 8: 61M elements in 32 bits 298 us (1.71 GB, 5.7
-// TB/s; a copy reaches 5.1), 138M in 8 bits with bf16 gradients 319 us (1.94 GB, 6.1 TB/s; vector instructions
-// three quarters of the time).
+// TB/s; a copy reaches 5.1), 138M in 8 bits with bf16 gradients 317 us (1.94 GB, 6.1 TB/s; vector instructions
+// five sixths of the time).
 #include "pl_device.h"
 
 namespace gadei::learner {
@@ -119,7 +119,9 @@ __device__ __forceinline__ void store4(void *p, int64_t i, f32x4 x, int count) {
 
 // The byte of a block whose largest magnitude has these bits (of NaN, with any sign): the exponent field, one
 // more above 1.875 times its power of two, which is the largest code. 255: not finite, or above 1.875 * 2^127.
-__device__ __forceinline__ int block_byte(uint32_t bits) { return static_cast<int>(min((bits + 0xfffffu) >> 23, 255u)); }
+__device__ __forceinline__ int block_byte(uint32_t bits) {
+    return static_cast<int>(min((bits + 0xfffffu) >> 23, 255u));
+}
 constexpr int kBad = 255;
 
 // Element e of four codes. A code is the upper bits of a small fp32 number, m's below its sign.
@@ -143,7 +145,8 @@ __device__ __forceinline__ uint32_t encode(float x, int byte, uint32_t r) {
 
 // The upper bytes of four words.
 __device__ __forceinline__ uint32_t upper_bytes(const uint32_t (&x)[kFour]) {
-    const uint32_t lo = __builtin_amdgcn_perm(x[1], x[0], 0x0c0c0703), hi = __builtin_amdgcn_perm(x[3], x[2], 0x07030c0c);
+    const uint32_t lo = __builtin_amdgcn_perm(x[1], x[0], 0x0c0c0703);
+    const uint32_t hi = __builtin_amdgcn_perm(x[3], x[2], 0x07030c0c);
     return lo | hi;
 }
 
@@ -190,8 +193,10 @@ __device__ __forceinline__ void step_part(const AdamwArgs &a, AdamwPart *part, c
             x[j].m = get<true>(reinterpret_cast<const f32x4_any *>(static_cast<const float *>(a.m) + first + i));
             x[j].v = get<true>(reinterpret_cast<const f32x4_any *>(static_cast<const float *>(a.v) + first + i));
         } else {
-            x[j].cm = __builtin_nontemporal_load(reinterpret_cast<const uint32_t *>(static_cast<const uint8_t *>(a.m) + first + i));
-            x[j].cv = __builtin_nontemporal_load(reinterpret_cast<const uint32_t *>(static_cast<const uint8_t *>(a.v) + first + i));
+            const auto *const m = static_cast<const uint8_t *>(a.m) + first + i;
+            const auto *const v = static_cast<const uint8_t *>(a.v) + first + i;
+            x[j].cm = __builtin_nontemporal_load(reinterpret_cast<const uint32_t *>(m));
+            x[j].cv = __builtin_nontemporal_load(reinterpret_cast<const uint32_t *>(v));
             x[j].bm = a.m_scales[(first + i) >> 7];
             x[j].bv = a.v_scales[(first + i) >> 7];
         }
@@ -276,8 +281,9 @@ __device__ __forceinline__ void step_part(const AdamwArgs &a, AdamwPart *part, c
                 cm[e] = encode<true>(m[e], bm, r[e] & 0xffffu);
                 cv[e] = encode<false>(v[e], bv, r[e] >> 16);
             }
-            __builtin_nontemporal_store(upper_bytes(cm), reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(a.m) + at));
-            __builtin_nontemporal_store(upper_bytes(cv), reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(a.v) + at));
+            auto *const to_m = static_cast<uint8_t *>(a.m) + at, *const to_v = static_cast<uint8_t *>(a.v) + at;
+            __builtin_nontemporal_store(upper_bytes(cm), reinterpret_cast<uint32_t *>(to_m));
+            __builtin_nontemporal_store(upper_bytes(cv), reinterpret_cast<uint32_t *>(to_v));
             if ((threadIdx.x & 31) == 0) {
                 a.m_scales[at >> 7] = static_cast<uint8_t>(bm);
                 a.v_scales[at >> 7] = static_cast<uint8_t>(bv);

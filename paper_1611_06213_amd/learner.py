@@ -882,7 +882,8 @@ class AdamW:
             t = getattr(self, name)
             _on_device(name, t)
             if t.dtype != kind or t.numel() != n or not t.is_contiguous():
-                raise ValueError(f"{name}: {n} contiguous elements of {kind} expected, not {t.dtype} of {tuple(t.shape)}")
+                raise ValueError(f"{name}: {n} contiguous elements of {kind} expected, not {t.dtype} of "
+                                 f"{tuple(t.shape)}")
             out.append(t.data_ptr())
         return out if self.bits == 8 else out + [None, None]
 
