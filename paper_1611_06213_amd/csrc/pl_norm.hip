@@ -17,9 +17,9 @@
 // Bound by memory. A row stays in registers, eight neighbouring columns a thread (`N` times), so each
 // matrix is read and written once; longer rows are read again. Sums over rows stay in registers over
 // a worker's rows, go to the workspace and are joined in order. Forward 16384 x 8192 bf16 takes 200 us
-// (1.07 GB, 5.4 TB/s), 4096 x 4096 with an fp32 stream 40 us (0.20 GB, 5.0), backward 16384 x 4096 bf16
-// with 32 gates 175 us and 7 for joining (0.81 GB, 4.6; vector instructions 60% of the time); a copy
-// reaches 5.1. The loads of two or three rows ahead instead of one, or twice the workers, take as long.
+// (1.07 GB, 5.4 TB/s; a kernel that only adds takes 198), 4096 x 4096 with an fp32 stream 40 us (0.20 GB,
+// 5.0), backward 16384 x 4096 bf16 with 32 gates 166 us and 7 for joining (0.81 GB, 4.9; vector
+// instructions 60% of the time; a kernel that only adds takes 154). The loads of two or three rows ahead instead of one, or twice the workers, take as long.
 #include <algorithm>
 #include <type_traits>
 
