@@ -362,3 +362,37 @@ def test_refusals(torch, learner):  # noqa: F811
     empty = A([w[:0]], [g[:0]])
     empty.step(0.1)
     assert empty.steps == 0 and empty.moments()[0].numel() == 0
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+@pytest.mark.parametrize("grads,push", [("f32", False), ("bf16", False), ("f32", True)])
+def test_weights_past_the_caches(torch, learner, bits, grads, push):  # noqa: F811
+    """Weights in 32 bits that do not fit in the last level (256 MB): the list's first elements as in a shorter list,
+    whose weights do, states and codes to the bit over several steps, as random numbers go by an element's place; its
+    last ones, of which the random numbers of 8 bits differ, for one step."""
+    if learner._native is False:
+        pytest.skip("the same library calls")
+    big, first, last = 70_000_001, 128 * 20_003, 5003
+    w = torch.randn(big + 129, generator=gen(torch, 1), device="cuda") * 0.1
+    g = (torch.randn(big + 129, generator=gen(torch, 2), device="cuda") * 1e-2).to(dt(torch, grads))
+    parts = [(slice(0, big), slice(big, big + 129)), (slice(0, first),),
+             (slice(big - last, big), slice(big, big + 129))]
+    flats = [(w.clone(), g.clone()) for _ in parts]
+    opts = [learner.AdamW([a[s] for s in where], [b[s] for s in where], 0.05, bits=bits, push=push, seed=7)
+            for (a, b), where in zip(flats, parts)]
+    for k in range(3):
+        if push:
+            for _, b in flats:
+                b.copy_(g).mul_(0.5 ** k)
+        for opt in opts:
+            opt.step(0.01, 0.5)
+        (a, b), (a1, b1), (a2, b2) = flats
+        out, out1, out2 = (b, b1, b2) if push else (a, a1, a2)
+        assert torch.equal(out[:first], out1[:first]) and not torch.equal(out[:first], (g if push else w)[:first])
+        if k == 0 or bits == 32:
+            assert torch.equal(out[big - last:], out2[big - last:])
+        room = first // 128
+        for name, n in (("m", first), ("v", first), ("m_scales", room), ("v_scales", room))[:4 if bits == 8 else 2]:
+            assert torch.equal(getattr(opts[0], name)[:n], getattr(opts[1], name)[:n]), name
+        # what is only read
+        assert torch.equal(a, w) if push else torch.equal(b, g)
