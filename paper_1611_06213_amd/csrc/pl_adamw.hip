@@ -117,10 +117,11 @@ __device__ __forceinline__ void store4(void *p, int64_t i, f32x4 x, int count) {
     }
 }
 
-// The byte of a block whose largest magnitude has these bits (of NaN, with any sign): the exponent field, one
-// more above 1.875 times its power of two, which is the largest code. 255: not finite, or above 1.875 * 2^127.
+// The byte of a block whose largest magnitude has these bits (of NaN, with any sign and payload: without the sign
+// the sum does not pass 32 bits): the exponent field, one more above 1.875 times its power of two, which is the
+// largest code. 255: not finite, or above 1.875 * 2^127.
 __device__ __forceinline__ int block_byte(uint32_t bits) {
-    return static_cast<int>(min((bits + 0xfffffu) >> 23, 255u));
+    return static_cast<int>(min(((bits & 0x7fffffffu) + 0xfffffu) >> 23, 255u));
 }
 constexpr int kBad = 255;
 
@@ -271,7 +272,7 @@ __device__ __forceinline__ void step_part(const AdamwArgs &a, AdamwPart *part, c
 #pragma unroll
             for (int e = 0; e < kFour; ++e) {
                 mm = max(mm, __float_as_uint(m[e]) & 0x7fffffffu);
-                mv = max(mv, __float_as_uint(v[e]));   // not negative, or NaN
+                mv = max(mv, __float_as_uint(v[e]));   // not negative, or a NaN, of which one with a sign is largest
             }
             const int bm = block_byte(most_of_32(mm)), bv = block_byte(most_of_32(mv));
             const u32x4 r = random4(static_cast<uint64_t>(at) >> 2, f.t, a.seed);

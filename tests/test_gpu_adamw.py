@@ -365,6 +365,41 @@ def test_refusals(torch, learner):  # noqa: F811
 
 
 @pytest.mark.parametrize("bits", [8, 32])
+@pytest.mark.parametrize("grads,patterns", [
+    ("f32", (0xFFFFFFFF, 0xFFF00001, 0xFFC00000, 0x7FFFFFFF, 0x7FC00000, 0xFF800000)),
+    ("bf16", (0xFFFF, 0xFFF1, 0xFFC0, 0x7FFF, 0xFF80))])
+@pytest.mark.parametrize("push", [False, True])
+def test_not_finite_of_any_bits(torch, learner, bits, grads, patterns, push):  # noqa: F811
+    """A NaN of any sign and payload, of memory filled with ones, say, and the lower infinity: products and sums keep
+    a NaN's bits, so that they come to where a block's largest is found. The block of 8 bits is NaN, no other is."""
+    kind = torch.int32 if grads == "f32" else torch.int16
+    half = 1 << (31 if grads == "f32" else 15)
+    for pattern in patterns:
+        bad = pattern - 2 * half if pattern >= half else pattern
+        for where in (slice(130, 131), slice(128, 256)):
+            w, g = torch.ones(500, device="cuda"), torch.full((500,), 0.01, device="cuda", dtype=dt(torch, grads))
+            g.view(kind)[where] = bad
+            want = adamw_ref.Reference([500], [0.0], (0.9, 0.999), 1e-8, bits, 0)
+            opt = learner.AdamW([w], [g], 0.0, bits=bits, push=push)
+            before = ref.f64(g)
+            opt.step(0.1)
+            want.step([np.ones(500)], [before], 0.1)
+            got = g if push else w
+            assert bool(got[where].isnan().all()) and int(got.isnan().sum()) == where.stop - where.start, hex(pattern)
+            m, v = opt.moments()
+            if bits == 8:
+                assert opt.v_scales.tolist()[1] == 255 and opt.m_scales.tolist()[1] == 255, hex(pattern)
+                for x in (m, v):
+                    assert bool(x[128:256].isnan().all()) and int(x.isnan().sum()) == 128, hex(pattern)
+            same_states(opt, want)
+            if push:
+                g.fill_(0.01)
+                opt.step(0.1)
+                want.step([np.ones(500)], [ref.f64(torch.full_like(g, 0.01))], 0.1)
+                same_states(opt, want)
+
+
+@pytest.mark.parametrize("bits", [8, 32])
 @pytest.mark.parametrize("grads,push", [("f32", False), ("bf16", False), ("f32", True)])
 def test_weights_past_the_caches(torch, learner, bits, grads, push):  # noqa: F811
     """Weights in 32 bits that do not fit in the last level (256 MB): the list's first elements as in a shorter list,
