@@ -361,7 +361,9 @@ struct Gate {
 bool gate(PyObject *o, int64_t cols, Gate *g) {
     if (o == Py_None) return true;
     Matrix m;
-    if (!device_tensor(o, &g->t) || !as_matrix(g->t.dim() == 1 ? g->t.unsqueeze(0) : g->t, &m) || m.cols != cols)
+    // without rows it has no address, which stands for no gate
+    if (!device_tensor(o, &g->t) || !as_matrix(g->t.dim() == 1 ? g->t.unsqueeze(0) : g->t, &m) || m.cols != cols ||
+        m.rows == 0)
         return false;
     g->p = m.p;
     g->dtype = m.dtype;

@@ -525,13 +525,15 @@ def _one_type(what: str, *codes) -> int:
     return there.pop() if there else PS_F32
 
 
-def _gate(name: str, gate, cols: int):
-    """(pointer, dtype code, rows, row stride) of a gate: `cols` values for all rows, or a matrix."""
+def _gate(name: str, gate, rows: int, cols: int):
+    """(pointer, dtype code, rows, row stride) of a gate: `cols` values for all rows, or a matrix. The library refuses
+    one of no rows that has an address; of a stream of no rows either it may be none at all."""
     if gate is None:
         return None, PS_F32, 0, 0
     _on_device(name, gate)
-    rows = gate[None] if gate.dim() == 1 else gate
-    return (*_matrix(name, rows, cols=cols)[:2], rows.shape[0], rows.stride(0))
+    m = gate[None] if gate.dim() == 1 else gate
+    ptr, code, ld = _matrix(name, m, cols=cols)
+    return _there(ptr) if rows or m.shape[0] else None, code, m.shape[0], ld
 
 
 def _like(name: str, out, rows: int, cols: int, dtype, device):
@@ -587,7 +589,7 @@ def residual_norm(x, y, gate=None, after=None, before=None, scale: float = 1.0, 
     src, code, ld = _matrix("x", x)
     rows, cols = x.shape
     blk, blk_code, blk_ld = _matrix("y", y, rows, cols)
-    gt, gt_code, gates, gt_ld = _gate("gate", gate, cols)
+    gt, gt_code, gates, gt_ld = _gate("gate", gate, rows, cols)
     (aft, aft_code), (bef, bef_code) = _vector("after", after, cols), _vector("before", before, cols)
     if before is None and normed_out is not None:
         raise ValueError("normed_out without before")
@@ -649,7 +651,7 @@ def _norm_grad(h, y, grad, normed_grad, gate, after, before, scale, eps, weight_
         if blk_code is not None and nrm_code != blk_code:
             raise TypeError(f"normed_grad is {normed_grad.dtype}, y {y.dtype}")
         blk_code = nrm_code
-    gt, gt_code, gates, gt_ld = _gate("gate", gate, cols)
+    gt, gt_code, gates, gt_ld = _gate("gate", gate, rows, cols)
     (aft, aft_code), (bef, bef_code) = _vector("after", after, cols), _vector("before", before, cols)
     if before is not None and normed_grad is None:
         raise ValueError("before without normed_grad")

@@ -456,3 +456,25 @@ def test_refusals(torch, learner):  # noqa: F811
 def ps_error():
     from paper_1611_06213_amd import ps
     return ps.PSError
+
+
+def test_gates_without_rows_or_columns(torch, learner):  # noqa: F811
+    """A gate of no rows is none at all only where the stream has none either; one of no columns has nothing to say."""
+    x, y = torch.ones(6, 20, device="cuda"), torch.ones(6, 20, device="cuda")
+    none = torch.ones(0, 20, device="cuda")
+    for call in (lambda: learner.residual_norm(x, y, none),
+                 lambda: learner.residual_norm(x, y, none, before=torch.ones(20, device="cuda")),
+                 lambda: learner.residual_norm_grad(x, y, x, gate=none),
+                 lambda: learner.residual_norm_grad(x, y, x, gate=none, gate_out=none.clone())):
+        with pytest.raises(ps_error(), match="0 rows"):
+            call()
+    for dtype in (torch.float32, torch.bfloat16):
+        e = torch.ones(0, 20, device="cuda", dtype=dtype)
+        h, z = learner.residual_norm(e, e, none)
+        assert h.shape == (0, 20) and z is None
+        assert learner.residual_norm_grad(e, e, e, gate=none).gate.shape == (0, 20)
+        e = torch.ones(6, 0, device="cuda", dtype=dtype)
+        for gate in (torch.ones(0, device="cuda"), torch.ones(3, 0, device="cuda")):
+            h, z = learner.residual_norm(e, e, gate)
+            assert h.shape == (6, 0) and z is None
+            assert learner.residual_norm_grad(e, e, e, gate=gate).gate.shape == gate.shape
