@@ -314,3 +314,77 @@ def test_waits_for_copies(tmp_path):
         assert copies == 8 * n, name
         checked += 1
     assert checked == 6
+
+
+REGS = re.compile(r"\b([av])(?:(\d+)|\[(\d+):(\d+)\])")
+
+
+def registers(text):
+    return {f"{kind}{i}" for kind, one, first, last in REGS.findall(text)
+            for i in (range(int(first), int(last) + 1) if first else (int(one),))}
+
+
+def too_near(lines):
+    """Where a matrix instruction comes fewer than two wait states after a vector instruction that writes what it reads,
+    or another instruction than these fewer than 19 after one whose sums it names (16 passes, the longest, and 3)."""
+    time, wrote, product, found = 0, {}, {}, []
+    for line in lines:
+        op, _, rest = line.partition(" ")
+        if op == "s_nop":
+            time += int(rest) + 1
+            continue
+        if op.startswith("v_mfma"):
+            out = registers(rest.split(",")[0])
+            found += [line for r in registers(rest) if time - wrote.get(r, -99) <= 2]
+            product.update((r, time) for r in out)
+        elif re.match(r"(v|ds|buffer|global|flat|scratch)_", op):
+            found += [line for r in registers(rest) if time - product.get(r, -99) <= 19]
+            if op.startswith("v_"):
+                named = rest.split(",")
+                wrote.update((r, time) for r in registers(",".join(named[:2] if "swap" in op else named[:1])))
+        time += 1
+    return found
+
+
+@pytest.mark.parametrize("between,near", [
+    (["s_nop 0"], True), (["s_nop 1"], False), (["s_nop 0", "s_mov_b32 s0, 0"], False),
+    (["v_mov_b32_e32 v9, 0", "v_mov_b32_e32 v3, 0", "s_nop 0"], True)])
+def test_too_near(between, near):
+    product = "v_mfma_i32_16x16x64_i8 a[0:3], v[0:3], v[4:7], a[0:3]"
+    assert (too_near(["v_accvgpr_write_b32 a3, v8", *between, product]) != []) == near
+    for waits, early in ((["s_nop 15", "s_nop 1"], True), (["s_nop 15", "s_nop 2"], False)):
+        for use in ("v_accvgpr_read_b32 v8, a2", "global_store_dwordx4 v[8:9], a[0:3], off", "v_accvgpr_mov_b32 a0, a9"):
+            assert (too_near([product, *waits, use]) != []) == early
+    assert too_near([product, product, "v_mov_b32_e32 v8, 0"]) == []
+
+
+def test_products_wait_for_what_they_read(tmp_path):
+    """The tiled products' matrix instructions are inline assembly, of whose time the compiler knows nothing: as
+    compiled, no operand is written right before one, and no sum is read or written before it is there. Each loop
+    follows itself, too."""
+    src = os.path.join(B.CSRC, "pl_matmul_int8.hip")
+    out = str(tmp_path / "int8.s")
+    flags = [f for f in B.LEARNER_FLAGS if f != "-fPIC"]
+    subprocess.run([B.HIPCC, *flags, "--cuda-device-only", "-S", src, "-o", out], check=True,
+                   stderr=subprocess.DEVNULL)
+    text, checked = open(out).read(), 0
+    for name in re.findall(r"^(\S*tilesILi\S*):", text, re.M):
+        body = text[text.index("\n" + name + ":") + 1:]
+        lines = [line.split(";")[0].strip() for line in body[:body.index(".Lfunc_end")].splitlines()[1:]]
+        lines = [line for line in lines if line and (not line.startswith(".") or line.endswith(":"))]
+        labels = {line[:-1]: i for i, line in enumerate(lines) if line.endswith(":")}
+        products = [i for i, line in enumerate(lines) if line.startswith("v_mfma")]
+        # four blocks of k's halves, each with 4 F F products
+        tile = int(re.search(r"tilesILi(\d)E", name).group(1))
+        assert len(products) == 4 * 4 * tile * tile, name
+        assert not any(line.startswith("v_cmpx") for line in lines[products[0] - 8:products[-1]])
+        assert too_near(lines) == [], name
+        loops = 0
+        for i, line in enumerate(lines):
+            target = labels.get(line.split()[-1], i) if line.startswith(("s_cbranch", "s_branch")) else i
+            if target < i and any(target < p < i for p in products):
+                loops += 1
+                assert too_near(lines[target:i] + lines[target:i]) == [], name
+        assert loops >= 1, name
+        checked += 1
+    assert checked == 6
