@@ -419,17 +419,18 @@ __device__ __forceinline__ void add_sums(float (&s)[kSums], const RowBits<X, Y, 
     }
 }
 
-// rh, k1 = rh^2 mean(u h), ry, k2 = ry^2 mean(v y). Without a norm before or after: 0, 0 and 1, 0.
+// rh, k1 = rh^2 mean(u h), ry, k2 = ry^2 mean(v y). Without a norm before or after: 0, 0 and 1, 0. A factor's square
+// by itself passes fp32's range in a row of zeros where eps is below 2^-128.
 __device__ __forceinline__ f32x4 row_factors(const NormGradArgs &a, const float (&s)[kSums]) {
     const float n = static_cast<float>(a.cols);
     f32x4 r = {0.0f, 0.0f, 1.0f, 0.0f};
     if (a.dz != nullptr) {
         r[0] = inverse_root(s[0], a.cols, a.eps);
-        r[1] = r[0] * r[0] * (s[1] / n);
+        r[1] = r[0] * (r[0] * (s[1] / n));
     }
     if (a.after != nullptr) {
         r[2] = inverse_root(s[2], a.cols, a.eps);
-        r[3] = r[2] * r[2] * ((s[3] + r[0] * (s[4] - r[1] * s[5])) / n);
+        r[3] = r[2] * (r[2] * ((s[3] + r[0] * (s[4] - r[1] * s[5])) / n));
     }
     return r;
 }

@@ -478,3 +478,20 @@ def test_gates_without_rows_or_columns(torch, learner):  # noqa: F811
             h, z = learner.residual_norm(e, e, gate)
             assert h.shape == (6, 0) and z is None
             assert learner.residual_norm_grad(e, e, e, gate=gate).gate.shape == gate.shape
+
+
+@pytest.mark.parametrize("cols", [5, 300, 301, 9000])
+@pytest.mark.parametrize("eps", [2.0 ** -126, 1e-40, 2.0 ** -149])
+def test_rows_of_zeros_with_a_small_eps(torch, learner, monkeypatch, cols, eps):  # noqa: F811
+    """Whose norm's factor is up to 2^74.5, and its square past fp32's range."""
+    eps = float(np.float32(eps))
+    monkeypatch.setitem(globals(), "EPS", eps)
+    c = Case(torch, 6, cols, 3, True, True, "f32", "f32", "f32", 1.25)
+    c.h[0], c.h[3], c.y[1], c.y[5] = 0, 0, 0, 0
+    want = backward(c.ref("h"), c.ref("y"), c.ref("dh"), c.ref("dz"), c.ref("gate"), c.ref("after"), c.ref("before"),
+                    c.scale)
+    got = learner.residual_norm_grad(c.h, c.y, c.dh, c.dz, c.gate, c.after, c.before, c.scale, eps)
+    for name, t in got._asdict().items():
+        close(t, *want[name], rounding(t))
+    z = learner.rms_norm(c.h, c.before, eps)
+    assert bool((z[0] == 0).all()) and bool(z.isfinite().all())
