@@ -248,7 +248,8 @@ __device__ __forceinline__ void step_part(const AdamwArgs &a, AdamwPart *part, c
             v[e] = a.beta2 * v[e] + a.rest2 * (ge * ge);
         }
         // The instructions' root and reciprocal err by one unit and take numbers below 2^-126 for zeros, whose
-        // roots are below 2^-63: times 2^9, as `root` is at most, they round away next to an eps of 2^-30.
+        // roots are below 2^-63: times 2^9, as `root` is at most, they round away next to an eps of 2^-30. Of a
+        // denominator up to 2^100 and 2^73 the reciprocal is no such number.
         if (a.plain) {
 #pragma unroll
             for (int e = 0; e < kFour; ++e)

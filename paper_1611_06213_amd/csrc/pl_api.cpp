@@ -926,7 +926,7 @@ int pl_adamw_step(void *plan, int64_t parts, int weight_dtype, int grad_dtype, i
     a.lr_at = lr_at;
     a.factor_at = factor_at;
     a.seed = seed;
-    a.plain = eps >= 0x1p-30f && 1.0 - beta2 >= 0x1p-18;
+    a.plain = eps >= 0x1p-30f && eps <= 0x1p100f && 1.0 - beta2 >= 0x1p-18;
     return launched(launch_adamw(a, weight_dtype, grad_dtype, bits, push != 0, static_cast<hipStream_t>(stream)),
                     "pl_adamw_step");
 }

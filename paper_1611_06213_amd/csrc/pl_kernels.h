@@ -107,7 +107,7 @@ struct AdamwArgs {
     float beta1, beta2, rest1, rest2, eps, lr, factor;   // rest = 1 - beta
     const float *lr_at, *factor_at;  // on the device, or null
     uint64_t seed;
-    bool plain;                      // eps >= 2^-30, rest2 >= 2^-18
+    bool plain;                      // 2^-30 <= eps <= 2^100, rest2 >= 2^-18
 };
 uint32_t adamw_part();   // elements of a part, at most, a multiple of 128
 hipError_t launch_adamw(const AdamwArgs &a, int weight_dtype, int grad_dtype, int bits, bool push, hipStream_t s);

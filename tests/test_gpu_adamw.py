@@ -431,3 +431,22 @@ def test_weights_past_the_caches(torch, learner, bits, grads, push):  # noqa: F8
             assert torch.equal(getattr(opts[0], name)[:n], getattr(opts[1], name)[:n]), name
         # what is only read
         assert torch.equal(a, w) if push else torch.equal(b, g)
+
+
+@pytest.mark.parametrize("eps", [2.0 ** 100, 2.0 ** 101, 2.0 ** 126, 1e38, 3e38])
+@pytest.mark.parametrize("bits", [8, 32])
+def test_large_eps(torch, learner, eps, bits):  # noqa: F811
+    """Denominators whose reciprocals are below 2^-126."""
+    eps = float(np.float32(eps))
+    g = randn(torch, gen(torch, 3), 300, std=1e17)
+    w = torch.zeros(300, device="cuda")
+    opt = learner.AdamW([w], [g], 0.0, (0.9, 0.99), eps, bits)
+    want = adamw_ref.Reference([300], [0.0], (0.9, 0.99), eps, bits, 0)
+    for _ in range(2):
+        before = ref.f64(w)
+        opt.step(1.0)
+        (step, tol), = want.step([before], [ref.f64(g)], 1.0)
+        same_states(opt, want)
+        value, got = before - step, ref.f64(w)
+        ok = abs(got - value) <= tol + U * (abs(value) + tol) + 1e-45
+        assert ok.all(), (got[~ok][:3], value[~ok][:3])
