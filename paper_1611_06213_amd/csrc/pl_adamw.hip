@@ -58,9 +58,10 @@ __device__ __forceinline__ u32x4 random4(uint64_t j, uint64_t t, uint64_t seed) 
 }
 
 // Loads and stores, PAST: past the caches. So go gradients and states, which nothing reads before the next step,
-// and weights (with push the steps) where they do not fit in the last level: in us, none past them, gradients and
-// states, and all: 25M in 32 bits 141, 127 and 128 (again on the same tensors 141, 106 and 128), 61M 340, 320 and
-// 317 (340, 252 and 312), 138M 775, 737 and 723; 138M in 8 bits with bf16 gradients 370, 343 and 331.
+// and weights (with push the steps) where they do not fit in the last level, counted as whole parts of weights:
+// in us, none past them, gradients and states, and all: 25M in 32 bits 141, 127 and 128 (again on the same tensors
+// 141, 106 and 128), 61M 340, 320 and 317 (340, 252 and 312), 138M 775, 737 and 723; 138M in 8 bits with bf16
+// gradients 370, 343 and 331.
 constexpr uint64_t kLastLevel = 256ull << 20;
 template <bool PAST>
 __device__ __forceinline__ f32x4 get(const f32x4_any *p) {

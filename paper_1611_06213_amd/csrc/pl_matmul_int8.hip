@@ -14,10 +14,11 @@
 // 64 rows of a, reads b straight into registers. Where there are too few tiles to fill the card, k is
 // split over workgroups; the parts' sums go to the workspace and `join` adds them up.
 //
-// 8192 x 8192 x 8192 to bf16 takes 417 us (2.6 POP/s; bound by matrix pipes and the clock that power
-// allows: 505 us when the card is warm from calls like it), 1 x 4096 x 25088 21 us (103 MB, 4.9 TB/s; bound
-// by reading b), 128 x 4096 x 9216 15 and 4 for the join (bound by the latency of its first loads and last
-// stores, as a workgroup has 12 blocks of k).
+// 8192 x 8192 x 8192 to bf16 takes 466 us (2.4 POP/s; bound by matrix pipes and the clock that power
+// allows: 430 in the first call, to 600 where calls follow one another; the library's product, into 32-bit sums,
+// 451, 445 and to 580 in turn with it), 1 x 4096 x 25088 21 us (103 MB, 4.9 TB/s; bound by reading b), 128 x 4096
+// x 9216 15 and 4 for the join (bound by the latency of its first loads and last stores, as a workgroup has 12
+// blocks of k).
 #include <algorithm>
 
 #include "pl_fp8.h"
@@ -594,9 +595,10 @@ struct Choice {
 };
 
 // What a product takes, in us, by rounds of tiles: a compute unit has one large tile at a time, or two
-// small ones, which cover each other's first loads and last stores. Of 8000 products of random sizes, from 33 x
-// 64 x 64 to 1.1 TFLOP, the choice takes 0.7% longer than the best of ten to sixteen tried (9% or more in one of
-// twenty).
+// small ones, which cover each other's first loads and last stores. Of 24600 products of random sizes, from 33 x
+// 64 x 64 to 1.1 TFLOP, the choice takes about 1% longer than the best of ten to sixteen tried (9% or more in one
+// of twenty). It is worst where it takes large tiles for 4 to 12 blocks of k, of which it expects too little: 8%
+// longer on average, 12267 x 808 x 956 30 us instead of 21.
 double tiles_take(uint64_t m, uint64_t n, uint64_t blocks, bool large, uint64_t parts) {
     const uint64_t b = large ? 256 : 128, at_once = large ? kCus : 2 * kCus;
     const uint64_t units = (m + b - 1) / b * ((n + b - 1) / b) * parts;

@@ -19,7 +19,13 @@
 // a worker's rows, go to the workspace and are joined in order. Forward 16384 x 8192 bf16 takes 200 us
 // (1.07 GB, 5.4 TB/s; a kernel that only adds takes 198), 4096 x 4096 with an fp32 stream 40 us (0.20 GB,
 // 5.0), backward 16384 x 4096 bf16 with 32 gates 166 us and 7 for joining (0.81 GB, 4.9; vector
-// instructions 60% of the time; a kernel that only adds takes 154). The loads of two or three rows ahead instead of one, or twice the workers, take as long.
+// instructions 60% of the time; a kernel that only adds takes 154). The loads of two or three rows ahead instead
+// of one, or twice the workers, take as long.
+//
+// Rows that no thread's eights hold are read again for each sum: 4096 x 25088 bf16 245 us forward (0.82 GB, 3.4
+// TB/s), 448 backward (1.23 GB, 2.8). Narrow ones leave lanes idle, as a wave or a workgroup has one row: 2^20 x 5
+// fp32 857 and 2746 us (0.1 and 0.05 TB/s), 32768 x 100 bf16 19 and 58, 100000 x 188 51 and 145, as long as 100000 x 512
+// (71 and 143).
 #include <algorithm>
 #include <type_traits>
 

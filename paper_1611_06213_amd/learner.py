@@ -8,6 +8,9 @@ layers in 8-bit integers, with which a replica answers. Weights are
 read where they lie in a replica (any view with unit column stride), weight
 gradients are written where they belong in a gradient row.
 
+Native calls make their results past torch's dispatcher: its modes, and the deterministic fill of new
+memory, do not see them.
+
 No call records anything for autograd: a result does not require a gradient, whatever its
 arguments do. The backward pass is a call of its own (`embedding_grad`, `linear_fp8_grad`,
 `residual_norm_grad`, `dropout` again).
@@ -580,7 +583,8 @@ def residual_norm(x, y, gate=None, after=None, before=None, scale: float = 1.0, 
 
     over rows; without `after` the block's output is not normed, without `gate` not gated. Returns (h, z), or
     (h, None) without `before`. h is of x's type, z, of the h that is not yet rounded, of y's. `gate` has a value
-    for each column, or is a matrix whose rows are each for as many neighbouring rows of x."""
+    for each column, or is a matrix whose rows (one at least, if x has any) are each for as many neighbouring rows of
+    x."""
     native = _native or _native_calls()
     if native:
         done = native.norm(x, y, gate, after, before, scale, eps, None, out, normed_out)
