@@ -24,8 +24,8 @@
 //
 // Rows that no thread's eights hold are read again for each sum: 4096 x 25088 bf16 245 us forward (0.82 GB, 3.4
 // TB/s), 448 backward (1.23 GB, 2.8). Narrow ones leave lanes idle, as a wave or a workgroup has one row: 2^20 x 5
-// fp32 857 and 2746 us (0.1 and 0.05 TB/s), 32768 x 100 bf16 19 and 58, 100000 x 188 51 and 145, as long as 100000 x 512
-// (71 and 143).
+// fp32 857 and 2746 us (0.1 and 0.05 TB/s), 32768 x 100 bf16 19 and 58, 100000 x 188 51 and 145, backward as long as
+// 100000 x 512 (71 and 143).
 #include <algorithm>
 #include <type_traits>
 
